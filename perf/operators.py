@@ -128,7 +128,7 @@ def work(case):
     if c["kind"] == "distill":
         return {"bytes": c["N"] * (2 * c["V"] * e + 12 * c["K"] + 12), "flops": 7 * c["N"] * c["V"]}
     if c["kind"] == "distill_apart":
-        return {"bytes": c["N"] * (3 * c["V"] * e + 24 * c["K"] + 20), "flops": 7 * c["N"] * c["V"]}
+        return {"bytes": c["N"] * (3 * c["V"] * e + 24 * c["K"] + 24), "flops": 7 * c["N"] * c["V"]}
     M, N, K = c["M"], c["N"], c["K"]
     return {"bytes": M * K * e + N * K + 4 * N * (2 if c["bias"] else 1) + M * N * e, "flops": 2 * M * N * K}
 
@@ -416,9 +416,9 @@ def _own(st):
     if c["kind"] == "distill":
         mg.distill_topk(cfg, st["logits"], st["ids"], st["teacher"], st["weight"], loss, None, grad, ws)
     else:
-        lse = _kept(st, "lse", lambda: new(N))
-        mg.distill_topk(cfg, st["logits"], st["ids"], st["teacher"], None, loss, lse, None, ws)
-        mg.distill_topk_backward(cfg, st["logits"], st["ids"], st["teacher"], lse, st["weight"], grad)
+        stats = _kept(st, "stats", lambda: new(N, 2))
+        mg.distill_topk(cfg, st["logits"], st["ids"], st["teacher"], None, loss, stats, None, ws)
+        mg.distill_topk_backward(cfg, st["logits"], st["ids"], st["teacher"], stats, st["weight"], grad)
     return {"loss": loss, "dlogits": grad}
 
 
