@@ -1,0 +1,88 @@
+// Internal declarations of the operators around a gated linear recurrent layer (include/mgrit_ops.h).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "../../include/mgrit_ops.h"
+
+namespace mg {
+
+// ---- gated linear recurrence (kernels_glr.hip)
+// A workgroup of GLR_WAVES waves covers one row of the batch, 2 * lanes channels (two per lane) and
+// GLR_WAVES * (64 / lanes) * GLR_STEPS steps: a wave's lanes hold 64 / lanes runs of GLR_STEPS steps.
+constexpr int GLR_WAVES = 8, GLR_STEPS = 16;
+struct GlrShape {
+  int lanes;                // lanes across the channels: 16, 32 or 64
+  int steps;                // of a tile
+  int chunks;               // tiles along the sequence
+  int cols;                 // tiles along the channels
+  long long words;          // tiles' words in the workspace (none where a sequence is one tile)
+};
+inline GlrShape glr_shape(const glr_cfg& c) {
+  GlrShape s;
+  s.lanes = c.H > 64 ? 64 : c.H > 32 ? 32 : 16;
+  s.steps = GLR_WAVES * (64 / s.lanes) * GLR_STEPS;
+  s.chunks = (c.T + s.steps - 1) / s.steps;
+  s.cols = (c.H + 2 * s.lanes - 1) / (2 * s.lanes);
+  s.words = s.chunks > 1 ? (long long)s.chunks * c.B * s.cols * 2 * s.lanes : 0;
+  return s;
+}
+struct GlrArgs {
+  glr_cfg c;
+  GlrShape s;
+  glr_seq gate, value, h, dh, dgate, dvalue;
+  const float* h0;
+  const uint8_t* reset;
+  float* h_last;
+  float* saved;             // [chunks,B,H]: state before a tile's first step
+  const float* dh_last;
+  float* dh0;
+  unsigned long long* words;
+  int* ticket;
+};
+hipError_t launch_glr_forward(const GlrArgs& a, hipStream_t s);
+hipError_t launch_glr_backward(const GlrArgs& a, hipStream_t s);
+
+struct GlrStepArgs {
+  glr_cfg c;
+  glr_seq gate, value, h;
+  const int32_t* slots;
+  int n_slots;
+  const uint8_t* reset;
+  const float* state_in;
+  float* state_out;
+};
+hipError_t launch_glr_step(const GlrStepArgs& a, hipStream_t s);
+
+// ---- rows of logits (kernels_logits.hip)
+struct LogitsArgs {
+  logits_cfg c;
+  const void* logits;
+  const int64_t* ids;       // tokens[N] / the teacher's ids[N,K]
+  float *logp, *entropy, *top_logp;
+  int64_t* top_ids;
+  const float *teacher, *weight;
+  float* loss;
+  float* stats;             // [N,2]
+  const float* stats_in;
+  void* dlogits;
+  char* workspace;
+};
+size_t logits_workspace(const logits_cfg& c);
+hipError_t launch_token_logprobs(const LogitsArgs& a, hipStream_t s);
+hipError_t launch_distill(const LogitsArgs& a, hipStream_t s);
+hipError_t launch_distill_grad(const LogitsArgs& a, hipStream_t s);
+
+// ---- product in 8-bit integers (kernels_q8.hip)
+struct Q8Args {
+  q8_cfg c;
+  const void* x;
+  const int8_t* w;
+  const float *w_scale, *bias;
+  void* y;
+  int8_t* q;                // [M, q8_row_bytes(K)]
+  float* scale;             // [M]
+};
+hipError_t launch_q8_quantize(const Q8Args& a, hipStream_t s);
+hipError_t launch_q8_linear(const Q8Args& a, hipStream_t s);
+
+}  // namespace mg
