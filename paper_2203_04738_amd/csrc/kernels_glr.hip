@@ -15,6 +15,8 @@
 //
 // Tiles are taken by a ticket, first tiles first (the adjoint: last tiles first), so that those a workgroup waits for
 // have been started, wait for none behind it, and every wait ends.
+#include <type_traits>
+
 #include "elem.h"
 #include "ops.h"
 
@@ -23,6 +25,7 @@ namespace mg {
 constexpr int GLR_THREADS = GLR_WAVES * 64;
 constexpr int GLR_RUNS_X_CH = GLR_WAVES * 128;      // runs of a tile x its channels
 constexpr int GLR_WINDOW = 32;                      // tiles looked at at a time
+constexpr float LOG2E = 1.44269504088896341f;
 constexpr unsigned GLR_NONE = 0xffffffffu, GLR_FREE = 0x80000000u;
 
 struct Pair {
@@ -33,6 +36,15 @@ struct Pair {
 template <typename E>
 struct RawPair {
   unsigned w[sizeof(E) / 2];
+  __device__ inline void anew() {
+#pragma unroll
+    for (unsigned& x : w) asm volatile("" : "+v"(x));
+  }
+  __device__ inline void set(float x) {
+    const E e = elem_of<E>(x);
+    if constexpr (sizeof(E) == 4) w[0] = w[1] = __float_as_uint(e);
+    else w[0] = (unsigned)e.bits * 0x10001u;
+  }
   __device__ inline float at(int i) const {
     if constexpr (sizeof(E) == 4) return __uint_as_float(w[i]);
     else return word_elem<E>(w[0], i);
@@ -73,21 +85,44 @@ __device__ inline void store_pair(E* p, float a, float b, bool second) {
   }
 }
 
-// a and, for GLR_MIX, 1 - a of a gate.  sigmoid: with e = exp(-|g|), the smaller of the two is e / (1 + e), to
-// full precision at any g, and the larger one minus that.
+// a and, for GLR_MIX, 1 - a of a gate, both to full precision: with e = exp(-|g|), the smaller of the two is
+// e / (1 + e) at any g, and the larger one 1 minus that.
 template <int FORM>
 struct Gate {
   float a, na;
   __device__ inline explicit Gate(float g) {
     if constexpr (FORM == GLR_MIX) {
-      const float e = __builtin_amdgcn_exp2f(-1.44269504088896341f * fabsf(g));
+      const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(g));
       const float s = e * __builtin_amdgcn_rcpf(1.0f + e), l = 1.0f - s;
       a = g < 0.0f ? s : l;
       na = g < 0.0f ? l : s;
     } else {
-      a = __builtin_amdgcn_exp2f(1.44269504088896341f * g);
+      a = __builtin_amdgcn_exp2f(LOG2E * g);
       na = 1.0f;
     }
+  }
+};
+// The same in one float that the adjoint keeps between its sweeps: the smaller of a and 1 - a under the sign of g, which
+// says which of the two it is.
+template <int FORM>
+struct KeptGate {
+  float v;
+  __device__ inline void set(float g) {
+    if constexpr (FORM == GLR_MIX) {
+      const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(g));
+      v = copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), g);
+    } else {
+      v = __builtin_amdgcn_exp2f(LOG2E * g);
+    }
+  }
+  // What was computed from it is computed again from here on rather than kept: registers are what the adjoint lacks.
+  __device__ inline void anew() { asm volatile("" : "+v"(v)); }
+  __device__ inline bool small_a() const { return (int)__float_as_uint(v) < 0; }
+  __device__ inline float a() const {
+    return FORM == GLR_DECAY ? v : small_a() ? fabsf(v) : 1.0f - fabsf(v);
+  }
+  __device__ inline float na() const {
+    return FORM == GLR_DECAY ? 1.0f : small_a() ? 1.0f - fabsf(v) : fabsf(v);
   }
 };
 
@@ -117,50 +152,103 @@ __global__ __launch_bounds__(256) void glr_clear_kernel(unsigned long long* word
   if (i == 0) *ticket = 0;
 }
 
-// Where a thread stands.
+// Where a thread stands.  WIDE: 64 lanes across the channels; a run is a wave then, and all but the lane's own channel is the
+// same in the whole wave (and in scalar registers, addresses and the ends of the sequence too).
+template <bool WIDE>
 struct GlrPlace {
-  int lane_c, run, chunk, b, ch;       // lane across the channels, run of the tile, tile, batch row, channel
+  int lanes, lane_c, run, chunk, b;    // lanes across the channels, this one's place; run of the tile, tile, batch row
+  int ch0, ch;                         // first channel of the tile, of the lane
   int t0;                              // first step of the run
   bool has, second;                    // whether channels ch and ch + 1 exist
   __device__ inline GlrPlace(const GlrArgs& a, int tile, bool backward) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int per_wave = 64 / a.s.lanes;
-    lane_c = lane & (a.s.lanes - 1);
-    run = wave * per_wave + lane / a.s.lanes;
+    lanes = WIDE ? 64 : a.s.lanes;
+    lane_c = lane & (lanes - 1);
+    run = WIDE ? __builtin_amdgcn_readfirstlane(wave) : wave * (64 / lanes) + lane / lanes;
+    tile = __builtin_amdgcn_readfirstlane(tile);
     const int across = a.s.cols * a.c.B;
     const int k = tile / across, rest = tile - k * across;
     chunk = backward ? a.s.chunks - 1 - k : k;
     b = rest / a.s.cols;
-    ch = (rest - b * a.s.cols) * 2 * a.s.lanes + 2 * lane_c;
+    ch0 = (rest - b * a.s.cols) * 2 * lanes;
+    ch = ch0 + 2 * lane_c;
     t0 = chunk * a.s.steps + run * GLR_STEPS;
     has = ch < a.c.H;
     second = ch + 1 < a.c.H;
   }
+  __device__ inline int runs() const { return GLR_THREADS / lanes; }
 };
 
 // Bits of the steps of the thread's run that reset (lanes >= 16 across the channels: each of the first 16
 // lanes of a run looks at one step).
-__device__ inline unsigned reset_bits(const GlrArgs& a, const GlrPlace& p) {
+template <bool WIDE>
+__device__ inline unsigned reset_bits(const GlrArgs& a, const GlrPlace<WIDE>& p) {
+  if (!a.reset) return 0;
   const int t = p.t0 + p.lane_c;
   bool r = false;
   if (p.lane_c < GLR_STEPS && t < a.c.T) r = a.reset[(long long)t * a.c.B + p.b] != 0;
   const unsigned long long all = __ballot(r);
-  return (unsigned)(all >> ((threadIdx.x & 63) / a.s.lanes * a.s.lanes)) & ((1u << GLR_STEPS) - 1);
+  return (unsigned)(WIDE ? all : all >> ((threadIdx.x & 63) / p.lanes * p.lanes)) & ((1u << GLR_STEPS) - 1);
+}
+// Whether no step of the wave's runs resets or lies behind the sequence's end: the same answer in all lanes of the wave,
+// whose sweeps then look at neither.
+template <bool WIDE>
+__device__ inline bool glr_whole(const GlrArgs& a, const GlrPlace<WIDE>& p, unsigned resets) {
+  const bool odd = resets != 0 || p.t0 + GLR_STEPS > a.c.T;
+  return WIDE ? !odd : !__any(odd);
 }
 
-// The 16 steps of a run of an input array; steps and channels that do not exist are read at the last one that does.
-template <typename E, bool ALIGNED>
-__device__ inline void load_run(const glr_seq& q, const GlrArgs& a, const GlrPlace& p,
+// The steps of a thread's run in an array.  WIDE: a base that is the same in the whole wave and 32-bit offsets (the
+// host has looked at the strides).
+template <typename E, bool WIDE>
+struct RunOf {
+  char* base;
+  long long far;                        // WIDE: not used
+  unsigned off, step;                   // bytes; step: WIDE only
+  long long stride;
+  __device__ inline RunOf(const glr_seq& q, const GlrPlace<WIDE>& p, int t0, unsigned lane_c) {
+    E* at = (E*)q.data + p.b * q.stride_b + p.ch0;
+    off = 2 * lane_c * sizeof(E);
+    stride = q.stride_t * (long long)sizeof(E);
+    step = (unsigned)stride;
+    base = (char*)(at + t0 * q.stride_t);
+    far = 0;
+  }
+  __device__ inline E* at() const { return (E*)(WIDE ? base + off : base + far + off); }
+  __device__ inline void next(bool on = true) {
+    if (WIDE) off += on ? step : 0;
+    else far += on ? stride : 0;
+  }
+};
+
+// The 16 steps of a run of an input array; steps and channels that do not exist are read at one that does.
+template <typename E, bool ALIGNED, bool WIDE>
+__device__ inline void load_run(const glr_seq& q, const GlrArgs& a, const GlrPlace<WIDE>& p,
                                 RawPair<E> (&v)[GLR_STEPS]) {
-  const int ch = p.has ? p.ch : 0;
-  const E* base = (const E*)q.data + p.b * q.stride_b + ch;
-  const bool second = ch + 1 < a.c.H;
+  const unsigned lane_c = p.has ? p.lane_c : 0;
+  const bool second = p.ch0 + 2 * (int)lane_c + 1 < a.c.H;
+  RunOf<E, WIDE> run(q, p, min(p.t0, a.c.T - 1), lane_c);
 #pragma unroll
   for (int r = 0; r < GLR_STEPS; ++r) {
-    const int t = min(p.t0 + r, a.c.T - 1);
-    v[r] = load_pair<E, ALIGNED>(base + t * q.stride_t, second);
+    v[r] = load_pair<E, ALIGNED>(run.at(), second);
+    run.next(p.t0 + r + 1 < a.c.T);
   }
 }
+
+// Steps behind the sequence's end change nothing: a = 1, b = 0.
+template <int FORM, typename E, bool WIDE>
+__device__ inline void clear_tail(const GlrArgs& a, const GlrPlace<WIDE>& p, RawPair<E> (&g)[GLR_STEPS],
+                                  RawPair<E> (&v)[GLR_STEPS]) {
+#pragma unroll
+  for (int r = 0; r < GLR_STEPS; ++r)
+    if (p.t0 + r >= a.c.T) {
+      g[r].set(FORM == GLR_MIX ? __builtin_inff() : 0.f);
+      v[r].set(0.f);
+    }
+}
+
+// x, or 0 (whatever x is) at a step that resets
+__device__ inline float unless(unsigned resets, int r, float x) { return resets >> r & 1 ? 0.f : x; }
 
 struct GlrShared {
   float2 run[GLR_RUNS_X_CH];                        // (A, S) of every run and channel
@@ -169,14 +257,43 @@ struct GlrShared {
   int tile;
 };
 
-// The state before tile `chunk` of the thread's two channels (in sh.carry, for the lanes of run 0), from the words of
+// The state before a tile from the n words of the tiles before it that the window holds for a channel (word 0 the
+// nearest): false where a word that is needed is not there yet.  The words are read eight at a time.
+__device__ inline bool window_state(const unsigned long long* w, int n, int stride, float& h) {
+  int at = -1;
+  bool stop = false;
+  for (int i0 = 0; i0 < n && !stop; i0 += 8) {
+    unsigned A[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) A[k] = (unsigned)w[min(i0 + k, n - 1) * stride];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (stop || i0 + k >= n) continue;
+      stop = A[k] == GLR_NONE || A[k] == GLR_FREE;
+      if (A[k] == GLR_FREE) at = i0 + k;
+    }
+  }
+  if (at < 0) return false;
+  h = __uint_as_float((unsigned)(w[at * stride] >> 32));
+  for (int i0 = (at - 1) & ~7; i0 >= 0; i0 -= 8) {
+    unsigned long long v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = w[min(i0 + k, at) * stride];
+#pragma unroll
+    for (int k = 7; k >= 0; --k)
+      if (i0 + k < at) h = fmaf(__uint_as_float((unsigned)v[k]), h, __uint_as_float((unsigned)(v[k] >> 32)));
+  }
+  return true;
+}
+
+// The state before tile `chunk` of the thread's two channels, in sh.carry, from the words of
 // the tiles before it (backward: behind it), whose distance is 1, 2, ...  All threads of the workgroup call it.
-__device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace& p, bool backward, GlrShared& sh) {
+template <bool WIDE>
+__device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace<WIDE>& p, bool backward, GlrShared& sh) {
   const int before = backward ? a.s.chunks - 1 - p.chunk : p.chunk;
-  const int n = min(before, GLR_WINDOW), runs = GLR_THREADS / a.s.lanes, chans = 2 * a.s.lanes;
+  const int n = min(before, GLR_WINDOW), runs = p.runs(), chans = 2 * p.lanes;
   const long long per_tile = (long long)a.c.B * a.s.cols * chans;
-  const int col = p.ch / chans;
-  const long long at = ((long long)p.b * a.s.cols + col) * chans + 2 * p.lane_c;
+  const long long at = (long long)p.b * a.s.cols * chans + p.ch;
   for (;;) {
     for (int i = p.run; i < n; i += runs) {
       const int other = backward ? p.chunk + 1 + i : p.chunk - 1 - i;
@@ -186,29 +303,10 @@ __device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace& p, bool b
     }
     __syncthreads();
     int ok = 1;
-    if (p.run == 0) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        int i = 0;
-        bool found = false;
-        for (; i < n; ++i) {
-          const unsigned A = (unsigned)sh.window[i * chans + 2 * p.lane_c + k];
-          if (A == GLR_NONE) break;
-          if (A == GLR_FREE) {
-            found = true;
-            break;
-          }
-        }
-        if (found) {
-          float h = __uint_as_float((unsigned)(sh.window[i * chans + 2 * p.lane_c + k] >> 32));
-          while (--i >= 0) {
-            const unsigned long long w = sh.window[i * chans + 2 * p.lane_c + k];
-            h = fmaf(__uint_as_float((unsigned)w), h, __uint_as_float((unsigned)(w >> 32)));
-          }
-          sh.carry[2 * p.lane_c + k] = h;
-        }
-        ok &= found;
-      }
+    if (p.run < 2) {                                  // run 0: channel ch, run 1: ch + 1
+      float h = 0.f;
+      ok = window_state(&sh.window[2 * p.lane_c + p.run], n, chans, h);
+      sh.carry[2 * p.lane_c + p.run] = h;
     }
     if (__syncthreads_and(ok)) return;
     __builtin_amdgcn_s_sleep(1);
@@ -216,57 +314,50 @@ __device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace& p, bool b
 }
 
 // What both directions do between their sweeps: from (A, S) of the thread's run, per channel, the state before
-// the run.  first: the state before the sequence's first tile (backward: behind its last one).  Returns in
-// `out` (run 0's threads) the state behind the tile.
-template <bool BACKWARD>
-__device__ inline Pair glr_join(const GlrArgs& a, const GlrPlace& p, Pair A, Pair S, Pair first, Pair& out,
+// the run.  first: the state before the sequence's first tile (backward: behind its last one).  The threads of the
+// tile's last run (backward: its first) get in `out` the state behind the tile.
+template <bool BACKWARD, bool WIDE>
+__device__ inline Pair glr_join(const GlrArgs& a, const GlrPlace<WIDE>& p, Pair A, Pair S, Pair first, Pair& out,
                                 GlrShared& sh) {
-  const int chans = 2 * a.s.lanes, runs = GLR_THREADS / a.s.lanes, c = 2 * p.lane_c;
+  const int chans = 2 * p.lanes, runs = p.runs(), c = 2 * p.lane_c;
   sh.run[p.run * chans + c] = make_float2(A.x, S.x);
   sh.run[p.run * chans + c + 1] = make_float2(A.y, S.y);
-  __syncthreads();
   const bool at_start = BACKWARD ? p.chunk == a.s.chunks - 1 : p.chunk == 0;
   const bool chain = a.s.chunks > 1;
+  const int place = BACKWARD ? runs - 1 - p.run : p.run;      // runs of the tile before this one
+  if (at_start && place == 0) {
+    sh.carry[c] = first.x;
+    sh.carry[c + 1] = first.y;
+  }
+  __syncthreads();
+  // the runs before it, as one
+  Pair pA = {1.f, 1.f}, pS = {0.f, 0.f};
+  for (int i = 0; i < place; ++i) {
+    const int r = BACKWARD ? runs - 1 - i : i;
+    const float2 x = sh.run[r * chans + c], y = sh.run[r * chans + c + 1];
+    pS.x = behind(x.x, x.y, pS.x);
+    pS.y = behind(y.x, y.y, pS.y);
+    pA.x = both(x.x, pA.x);
+    pA.y = both(y.x, pA.y);
+  }
   unsigned long long* word =
       a.words + (((long long)p.chunk * a.c.B + p.b) * a.s.cols) * chans + p.ch;
-  Pair tA = {1.f, 1.f}, tS = {0.f, 0.f};            // of the whole tile
-  if (p.run == 0) {
-    for (int i = 0; i < runs; ++i) {
-      const int r = BACKWARD ? runs - 1 - i : i;
-      const float2 x = sh.run[r * chans + c], y = sh.run[r * chans + c + 1];
-      tS.x = behind(x.x, x.y, tS.x);
-      tS.y = behind(y.x, y.y, tS.y);
-      tA.x = both(x.x, tA.x);
-      tA.y = both(y.x, tA.y);
-    }
-    if (chain && !at_start) {
-      store_word(word, make_word(tA.x, tS.x));
-      store_word(word + 1, make_word(tA.y, tS.y));
-    }
+  const bool last = place == runs - 1;
+  if (last && chain && !at_start) {
+    store_word(word, make_word(both(A.x, pA.x), behind(A.x, S.x, pS.x)));
+    store_word(word + 1, make_word(both(A.y, pA.y), behind(A.y, S.y, pS.y)));
   }
-  if (at_start) {
-    if (p.run == 0) {
-      sh.carry[c] = first.x;
-      sh.carry[c + 1] = first.y;
-    }
-    __syncthreads();
-  } else {
-    glr_look_back(a, p, BACKWARD, sh);
-  }
+  if (!at_start) glr_look_back(a, p, BACKWARD, sh);
   Pair h = {sh.carry[c], sh.carry[c + 1]};
-  if (p.run == 0) {
-    out.x = behind(tA.x, tS.x, h.x);
-    out.y = behind(tA.y, tS.y, h.y);
+  h.x = behind(pA.x, pS.x, h.x);
+  h.y = behind(pA.y, pS.y, h.y);
+  if (last) {
+    out.x = behind(A.x, S.x, h.x);
+    out.y = behind(A.y, S.y, h.y);
     if (chain) {
       store_word(word, make_word(-0.0f, out.x));
       store_word(word + 1, make_word(-0.0f, out.y));
     }
-  }
-  for (int i = 0; i < (BACKWARD ? runs - 1 - p.run : p.run); ++i) {
-    const int r = BACKWARD ? runs - 1 - i : i;
-    const float2 x = sh.run[r * chans + c], y = sh.run[r * chans + c + 1];
-    h.x = behind(x.x, x.y, h.x);
-    h.y = behind(y.x, y.y, h.y);
   }
   return h;
 }
@@ -278,84 +369,89 @@ __device__ inline int glr_tile(const GlrArgs& a, GlrShared& sh) {
   return sh.tile;
 }
 
-template <typename E, bool ALIGNED, int FORM, bool RESET>
-__global__ __launch_bounds__(GLR_THREADS) void glr_forward_kernel(GlrArgs a) {
+template <typename E, bool ALIGNED, int FORM, bool WIDE>
+__global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) {
   __shared__ GlrShared sh;
-  const GlrPlace p(a, glr_tile(a, sh), false);
+  const GlrPlace<WIDE> p(a, glr_tile(a, sh), false);
   RawPair<E> g[GLR_STEPS], v[GLR_STEPS];
-  load_run<E, ALIGNED>(a.gate, a, p, g);
-  load_run<E, ALIGNED>(a.value, a, p, v);
-  const unsigned resets = RESET ? reset_bits(a, p) : 0u;
+  load_run<E, ALIGNED, WIDE>(a.gate, a, p, g);
+  load_run<E, ALIGNED, WIDE>(a.value, a, p, v);
+  const unsigned resets = reset_bits(a, p);
+  const int runs = p.runs();
   Pair first = {0.f, 0.f};
   if (p.chunk == 0 && a.h0 && p.run == 0) {
     const long long at = (long long)p.b * a.c.H + p.ch;
     if (p.has) first.x = a.h0[at];
     if (p.second) first.y = a.h0[at + 1];
   }
+  const bool whole = glr_whole(a, p, resets);
   // from a zero state: S[r], and A[r] of the steps up to r
   float A[GLR_STEPS][2], S[GLR_STEPS][2];
+  auto sweep = [&](auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
+    float pa[2] = {1.f, 1.f}, ps[2] = {0.f, 0.f};
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    float pa = 1.f, ps = 0.f;
+    for (int r = 0; r < GLR_STEPS; ++r)
 #pragma unroll
-    for (int r = 0; r < GLR_STEPS; ++r) {
-      const Gate<FORM> gt(g[r].at(k));
-      const float b = FORM == GLR_MIX ? gt.na * v[r].at(k) : v[r].at(k);
-      if (p.t0 + r < a.c.T) {
-        if (RESET && (resets >> r & 1)) {
-          pa = -0.0f;
-          ps = b;
-        } else {
-          pa = RESET && is_free(pa) ? pa : pa * gt.a;
-          ps = fmaf(gt.a, ps, b);
-        }
+      for (int k = 0; k < 2; ++k) {
+        const Gate<FORM> gt(g[r].at(k));
+        const float b = FORM == GLR_MIX ? gt.na * v[r].at(k) : v[r].at(k);
+        pa[k] *= gt.a;
+        ps[k] = MASKED && (resets >> r & 1) ? b : fmaf(gt.a, ps[k], b);
+        A[r][k] = MASKED && (resets & ((2u << r) - 1)) ? -0.0f : pa[k];
+        S[r][k] = ps[k];
       }
-      A[r][k] = pa;
-      S[r][k] = ps;
-    }
+  };
+  if (whole) {
+    sweep(std::false_type{});
+  } else {
+    clear_tail<FORM>(a, p, g, v);
+    sweep(std::true_type{});
   }
   constexpr int L = GLR_STEPS - 1;
-  Pair end;
-  const Pair h = glr_join<false>(a, p, {A[L][0], A[L][1]}, {S[L][0], S[L][1]}, first, end, sh);
-  if (p.run == 0) {
-    const long long at = (long long)p.b * a.c.H + p.ch;
-    if (a.saved) {
-      float* s = a.saved + (long long)p.chunk * a.c.B * a.c.H + at;
-      if (p.has) s[0] = h.x;
-      if (p.second) s[1] = h.y;
-    }
-    if (a.h_last && p.chunk == a.s.chunks - 1) {
-      if (p.has) a.h_last[at] = end.x;
-      if (p.second) a.h_last[at + 1] = end.y;
-    }
+  Pair end = {0.f, 0.f};
+  const Pair h = glr_join<false, WIDE>(a, p, {A[L][0], A[L][1]}, {S[L][0], S[L][1]}, first, end, sh);
+  const long long at = (long long)p.b * a.c.H + p.ch;
+  if (p.run == 0 && a.saved) {
+    float* s = a.saved + (long long)p.chunk * a.c.B * a.c.H + at;
+    if (p.has) s[0] = h.x;
+    if (p.second) s[1] = h.y;
+  }
+  if (p.run == runs - 1 && a.h_last && p.chunk == a.s.chunks - 1) {
+    if (p.has) a.h_last[at] = end.x;
+    if (p.second) a.h_last[at + 1] = end.y;
   }
   if (!p.has) return;
-  E* out = (E*)a.h.data + p.b * a.h.stride_b + p.ch;
+  RunOf<E, WIDE> out(a.h, p, p.t0, p.lane_c);
+  auto write = [&](auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
 #pragma unroll
-  for (int r = 0; r < GLR_STEPS; ++r) {
-    const int t = p.t0 + r;
-    if (t >= a.c.T) break;
-    const float x = RESET ? behind(A[r][0], S[r][0], h.x) : fmaf(A[r][0], h.x, S[r][0]);
-    const float y = RESET ? behind(A[r][1], S[r][1], h.y) : fmaf(A[r][1], h.y, S[r][1]);
-    store_pair<E, ALIGNED>(out + t * a.h.stride_t, x, y, p.second);
-  }
+    for (int r = 0; r < GLR_STEPS; ++r, out.next()) {
+      const float x = MASKED ? behind(A[r][0], S[r][0], h.x) : fmaf(A[r][0], h.x, S[r][0]);
+      const float y = MASKED ? behind(A[r][1], S[r][1], h.y) : fmaf(A[r][1], h.y, S[r][1]);
+      if (!MASKED || p.t0 + r < a.c.T) store_pair<E, ALIGNED>(out.at(), x, y, p.second);
+    }
+  };
+  if (whole) write(std::false_type{});
+  else write(std::true_type{});
 }
 
 // mu_t = a_t l_t is what step t hands on to step t - 1: mu -> a (dh + mu), the same composition from the other end.
-template <typename E, bool ALIGNED, int FORM, bool RESET>
-__global__ __launch_bounds__(GLR_THREADS) void glr_backward_kernel(GlrArgs a) {
+template <typename E, bool ALIGNED, int FORM, bool WIDE>
+__global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a) {
   __shared__ GlrShared sh;
   __shared__ float2 fwd[GLR_RUNS_X_CH];             // (A, S) of every run forward
-  const GlrPlace p(a, glr_tile(a, sh), true);
-  const int chans = 2 * a.s.lanes, c = 2 * p.lane_c;
+  const GlrPlace<WIDE> p(a, glr_tile(a, sh), true);
+  const int chans = 2 * p.lanes, c = 2 * p.lane_c;
   RawPair<E> g[GLR_STEPS], v[GLR_STEPS], d[GLR_STEPS];
-  load_run<E, ALIGNED>(a.gate, a, p, g);
-  load_run<E, ALIGNED>(a.value, a, p, v);
-  load_run<E, ALIGNED>(a.dh, a, p, d);
-  const unsigned resets = RESET ? reset_bits(a, p) : 0u;
+  load_run<E, ALIGNED, WIDE>(a.gate, a, p, g);
+  load_run<E, ALIGNED, WIDE>(a.value, a, p, v);
+  load_run<E, ALIGNED, WIDE>(a.dh, a, p, d);
+  const unsigned resets = reset_bits(a, p);
   const long long at = (long long)p.b * a.c.H + p.ch;
+  const int runs = p.runs();
   Pair first = {0.f, 0.f}, h = {0.f, 0.f};
-  if (p.chunk == a.s.chunks - 1 && a.dh_last && p.run == 0) {
+  if (p.chunk == a.s.chunks - 1 && a.dh_last && p.run == runs - 1) {
     if (p.has) first.x = a.dh_last[at];
     if (p.second) first.y = a.dh_last[at + 1];
   }
@@ -364,37 +460,55 @@ __global__ __launch_bounds__(GLR_THREADS) void glr_backward_kernel(GlrArgs a) {
     if (p.has) h.x = s[0];
     if (p.second) h.y = s[1];
   }
-  float pA[2], pS[2], qS[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    pA[k] = 1.f;
-    pS[k] = qS[k] = 0.f;
-    float as[GLR_STEPS];
+  const bool whole = glr_whole(a, p, resets);
+  KeptGate<FORM> gk[GLR_STEPS][2];
+  auto anew = [&]() {
 #pragma unroll
     for (int r = 0; r < GLR_STEPS; ++r) {
-      const Gate<FORM> gt(g[r].at(k));
-      as[r] = gt.a;
-      if (p.t0 + r < a.c.T) {
-        const float b = FORM == GLR_MIX ? gt.na * v[r].at(k) : v[r].at(k);
-        if (RESET && (resets >> r & 1)) {
-          pA[k] = -0.0f;
-          pS[k] = b;
-        } else {
-          pA[k] = RESET && is_free(pA[k]) ? pA[k] : pA[k] * gt.a;
-          pS[k] = fmaf(gt.a, pS[k], b);
-        }
-      }
+      gk[r][0].anew();
+      gk[r][1].anew();
+      v[r].anew();
     }
+  };
+  float pA[2], pS[2], qS[2];
+  auto sums = [&](auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
+    pA[0] = pA[1] = 1.f;
+    pS[0] = pS[1] = qS[0] = qS[1] = 0.f;
 #pragma unroll
-    for (int r = GLR_STEPS - 1; r >= 0; --r) {
-      if (p.t0 + r >= a.c.T) continue;
-      qS[k] = RESET && (resets >> r & 1) ? 0.f : as[r] * (d[r].at(k) + qS[k]);
-    }
+    for (int r = 0; r < GLR_STEPS; ++r)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        gk[r][k].set(g[r].at(k));
+        const float ga = gk[r][k].a();
+        const float b = FORM == GLR_MIX ? gk[r][k].na() * v[r].at(k) : v[r].at(k);
+        pA[k] *= ga;
+        pS[k] = MASKED && (resets >> r & 1) ? b : fmaf(ga, pS[k], b);
+      }
+    anew();
+#pragma unroll
+    for (int r = GLR_STEPS - 1; r >= 0; --r)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        qS[k] = gk[r][k].a() * (d[r].at(k) + qS[k]);
+        if (MASKED) qS[k] = unless(resets, r, qS[k]);
+      }
+    if (MASKED && resets) pA[0] = pA[1] = -0.0f;
+  };
+  if (whole) {
+    sums(std::false_type{});
+  } else {
+    clear_tail<FORM>(a, p, g, v);
+#pragma unroll
+    for (int r = 0; r < GLR_STEPS; ++r)
+      if (p.t0 + r >= a.c.T) d[r].set(0.f);
+    sums(std::true_type{});
   }
+  anew();
   fwd[p.run * chans + c] = make_float2(pA[0], pS[0]);
   fwd[p.run * chans + c + 1] = make_float2(pA[1], pS[1]);
-  Pair end;
-  const Pair mu = glr_join<true>(a, p, {pA[0], pA[1]}, {qS[0], qS[1]}, first, end, sh);
+  Pair end = {0.f, 0.f};
+  const Pair mu = glr_join<true, WIDE>(a, p, {pA[0], pA[1]}, {qS[0], qS[1]}, first, end, sh);
   if (p.run == 0 && p.chunk == 0 && a.dh0) {
     if (p.has) a.dh0[at] = end.x;
     if (p.second) a.dh0[at + 1] = end.y;
@@ -405,47 +519,49 @@ __global__ __launch_bounds__(GLR_THREADS) void glr_backward_kernel(GlrArgs a) {
     h.x = behind(x.x, x.y, h.x);
     h.y = behind(y.x, y.y, h.y);
   }
-  float l[GLR_STEPS][2];
+  RunOf<E, WIDE> dg(a.dgate, p, p.t0, p.lane_c), dv(a.dvalue, p, p.t0, p.lane_c);
+  auto write = [&](auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
+    float l[GLR_STEPS][2], m[2] = {mu.x, mu.y};
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    float m = k ? mu.y : mu.x;
+    for (int r = GLR_STEPS - 1; r >= 0; --r)
 #pragma unroll
-    for (int r = GLR_STEPS - 1; r >= 0; --r) {
-      l[r][k] = 0.f;
-      if (p.t0 + r >= a.c.T) continue;
-      l[r][k] = d[r].at(k) + m;
-      m = RESET && (resets >> r & 1) ? 0.f : Gate<FORM>(g[r].at(k)).a * l[r][k];
-    }
-  }
-  E* dg = (E*)a.dgate.data + p.b * a.dgate.stride_b + p.ch;
-  E* dv = (E*)a.dvalue.data + p.b * a.dvalue.stride_b + p.ch;
-#pragma unroll
-  for (int r = 0; r < GLR_STEPS; ++r) {
-    const int t = p.t0 + r;
-    if (t >= a.c.T) break;
-    float og[2], ov[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const Gate<FORM> gt(g[r].at(k));
-      const float val = v[r].at(k), cur = k ? h.y : h.x;
-      const bool cut = RESET && (resets >> r & 1);
-      const float past = cut ? 0.f : cur;
-      float next;
-      if constexpr (FORM == GLR_MIX) {
-        ov[k] = l[r][k] * gt.na;
-        og[k] = ov[k] * gt.a * (past - val);
-        next = gt.na * val;
-      } else {
-        ov[k] = l[r][k];
-        og[k] = cut ? 0.f : l[r][k] * gt.a * past;
-        next = val;
+      for (int k = 0; k < 2; ++k) {
+        l[r][k] = d[r].at(k) + m[k];
+        m[k] = gk[r][k].a() * l[r][k];
+        if (MASKED) m[k] = unless(resets, r, m[k]);
       }
-      next = cut ? next : fmaf(gt.a, past, next);
-      (k ? h.y : h.x) = next;
+    anew();
+#pragma unroll
+    for (int r = 0; r < GLR_STEPS; ++r) {
+      float og[2], ov[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float ga = gk[r][k].a(), val = v[r].at(k);
+        float past = k ? h.y : h.x, in = val;
+        if (MASKED) past = unless(resets, r, past);
+        if constexpr (FORM == GLR_MIX) {
+          const float na = gk[r][k].na();
+          ov[k] = l[r][k] * na;
+          og[k] = ov[k] * ga * (past - val);
+          in = na * val;
+        } else {
+          ov[k] = l[r][k];
+          og[k] = l[r][k] * ga * past;
+          if (MASKED) og[k] = unless(resets, r, og[k]);
+        }
+        (k ? h.y : h.x) = MASKED && (resets >> r & 1) ? in : fmaf(ga, past, in);
+      }
+      if (!MASKED || p.t0 + r < a.c.T) {
+        store_pair<E, ALIGNED>(dg.at(), og[0], og[1], p.second);
+        store_pair<E, ALIGNED>(dv.at(), ov[0], ov[1], p.second);
+      }
+      dg.next();
+      dv.next();
     }
-    store_pair<E, ALIGNED>(dg + t * a.dgate.stride_t, og[0], og[1], p.second);
-    store_pair<E, ALIGNED>(dv + t * a.dvalue.stride_t, ov[0], ov[1], p.second);
-  }
+  };
+  if (whole) write(std::false_type{});
+  else write(std::true_type{});
 }
 
 // Whether two channels of every step of the array are one aligned word.
@@ -454,27 +570,32 @@ static bool pairs(const glr_seq& q, int H) {
   return H % 2 == 0 && q.stride_t % 2 == 0 && q.stride_b % 2 == 0 && (uintptr_t)q.data % (2 * sizeof(E)) == 0;
 }
 
-template <typename E, int FORM, bool RESET>
+template <typename E, int FORM, bool WIDE>
 static void glr_start(const GlrArgs& a, bool backward, unsigned grid, hipStream_t s) {
   const int H = a.c.H;
   bool al = pairs<E>(a.gate, H) && pairs<E>(a.value, H);
   al = al && (backward ? pairs<E>(a.dh, H) && pairs<E>(a.dgate, H) && pairs<E>(a.dvalue, H) : pairs<E>(a.h, H));
   const dim3 g(grid), t(GLR_THREADS);
   if (backward) {
-    if (al) hipLaunchKernelGGL((glr_backward_kernel<E, true, FORM, RESET>), g, t, 0, s, a);
-    else hipLaunchKernelGGL((glr_backward_kernel<E, false, FORM, RESET>), g, t, 0, s, a);
+    if (al) hipLaunchKernelGGL((glr_backward_kernel<E, true, FORM, WIDE>), g, t, 0, s, a);
+    else hipLaunchKernelGGL((glr_backward_kernel<E, false, FORM, WIDE>), g, t, 0, s, a);
   } else {
-    if (al) hipLaunchKernelGGL((glr_forward_kernel<E, true, FORM, RESET>), g, t, 0, s, a);
-    else hipLaunchKernelGGL((glr_forward_kernel<E, false, FORM, RESET>), g, t, 0, s, a);
+    if (al) hipLaunchKernelGGL((glr_forward_kernel<E, true, FORM, WIDE>), g, t, 0, s, a);
+    else hipLaunchKernelGGL((glr_forward_kernel<E, false, FORM, WIDE>), g, t, 0, s, a);
   }
 }
+// Whether the 16 steps of a run lie within 32-bit offsets.
+static bool near(const glr_seq& q, int size) { return !q.data || q.stride_t * size < (1LL << 27); }
 template <typename E>
 static void glr_form(const GlrArgs& a, bool backward, unsigned grid, hipStream_t s) {
+  const int e = sizeof(E);
+  const bool wide = a.s.lanes == 64 && near(a.gate, e) && near(a.value, e) && near(a.h, e) && near(a.dh, e) &&
+                    near(a.dgate, e) && near(a.dvalue, e);
   if (a.c.form == GLR_MIX) {
-    if (a.reset) glr_start<E, GLR_MIX, true>(a, backward, grid, s);
+    if (wide) glr_start<E, GLR_MIX, true>(a, backward, grid, s);
     else glr_start<E, GLR_MIX, false>(a, backward, grid, s);
   } else {
-    if (a.reset) glr_start<E, GLR_DECAY, true>(a, backward, grid, s);
+    if (wide) glr_start<E, GLR_DECAY, true>(a, backward, grid, s);
     else glr_start<E, GLR_DECAY, false>(a, backward, grid, s);
   }
 }

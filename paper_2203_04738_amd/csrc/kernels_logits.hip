@@ -11,6 +11,8 @@
 // are ranked by counting how many beat each.  Keys with indices are all different, so the result does not
 // depend on the order in which candidates arrive.  Where there are more candidates than LDS takes (rows of
 // equal values), the alternatives are found one after the other, each the largest below the last.
+#include <type_traits>
+
 #include "elem.h"
 #include "ops.h"
 
@@ -118,15 +120,33 @@ struct Stats {
 };
 __device__ inline float finite_max(float m) { return m == -__builtin_inff() ? 0.f : m; }
 
+// How an exponent c (x - m) is computed for every x of a row: as one multiply-add fma(x, c, -r) with r = c m rounded,
+// whose rounding d = c m - r is the same for the whole row, or, where r is not finite (rows whose largest
+// value is the type's lowest), as it is written.
+struct Exponent {
+  float c, m, r;
+  bool one;
+  __device__ inline Exponent(float c_, float max) : c(c_), m(finite_max(max)), r(m * c_), one(fabsf(r) < __builtin_inff()) {}
+  // 2^-d, what a sum of 2^fma(x, c, -r) is to be multiplied by
+  __device__ inline float scale() const { return one ? __builtin_amdgcn_exp2f(-rest()) : 1.f; }
+  __device__ inline float rest() const { return one ? fmaf(m, c, -r) : 0.f; }
+};
+template <bool ONE>
+__device__ inline float exponent(const Exponent& x, float v) {
+  return ONE ? fmaf(v, x.c, -x.r) : (v - x.m) * x.c;
+}
+
+// (largest: the thread's own largest value)
 template <typename E, int NW, bool ENTROPY>
-__device__ inline Stats team_stats(const Held<E, NW>& x, float c, int tid, float (*part)[2]) {
+__device__ inline Stats team_stats(const Held<E, NW>& x, float c, int tid, float (*part)[2], float* largest = nullptr) {
   using T = TeamOf<E, NW>;
-  Stats r;
+  Stats st;
   float m = -__builtin_inff();
 #pragma unroll
   for (int j = 0; j < T::loads; ++j)
 #pragma unroll
     for (int k = 0; k < T::per_load; ++k) m = fmaxf(m, x.at(j, k));
+  if (largest) *largest = m;
   m = wave_max(m);
   if constexpr (NW > 1) {
     if ((tid & 63) == 0) part[tid >> 6][0] = m;
@@ -136,18 +156,21 @@ __device__ inline Stats team_stats(const Held<E, NW>& x, float c, int tid, float
     for (int o = 1; o < NW; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
     __syncthreads();
   }
-  r.m = m;
-  const float m0 = finite_max(m);
+  const Exponent ex(c, m);
   float s = 0.f, u = 0.f;
+  auto sum = [&](auto one) {
 #pragma unroll
-  for (int j = 0; j < T::loads; ++j)
+    for (int j = 0; j < T::loads; ++j)
 #pragma unroll
-    for (int k = 0; k < T::per_load; ++k) {
-      const float z = (x.at(j, k) - m0) * c;
-      const float e = __builtin_amdgcn_exp2f(z);
-      s += e;
-      if (ENTROPY) u = fmaf(e, fmaxf(z, -1e30f), u);         // (0 times -inf is 0 here)
-    }
+      for (int k = 0; k < T::per_load; ++k) {
+        const float z = exponent<decltype(one)::value>(ex, x.at(j, k));
+        const float e = __builtin_amdgcn_exp2f(z);
+        s += e;
+        if (ENTROPY) u = fmaf(e, fmaxf(z, -1e30f), u);       // (0 times -inf is 0 here)
+      }
+  };
+  if (ex.one) sum(std::true_type{});
+  else sum(std::false_type{});
   s = wave_sum(s);
   if (ENTROPY) u = wave_sum(u);
   if constexpr (NW > 1) {
@@ -157,16 +180,18 @@ __device__ inline Stats team_stats(const Held<E, NW>& x, float c, int tid, float
     }
     __syncthreads();
     s = part[tid & (NW - 1)][0];
-    u = part[tid & (NW - 1)][1];
+    if (ENTROPY) u = part[tid & (NW - 1)][1];
 #pragma unroll
     for (int o = 1; o < NW; o <<= 1) {
       s += __shfl_xor(s, o, 64);
-      u += __shfl_xor(u, o, 64);
+      if (ENTROPY) u += __shfl_xor(u, o, 64);
     }
   }
-  r.s = s;
-  r.u = u;
-  return r;
+  const float f = ex.scale();
+  st.m = m;
+  st.s = s * f;
+  st.u = (u - ex.rest() * s) * f;
+  return st;
 }
 
 // log p of a logit, from the statistics of its row
@@ -176,13 +201,13 @@ __device__ inline float log_prob(float x, const Stats& r, float inv_t) {
 }
 __device__ inline float entropy_of(const Stats& r) { return r.s == 0.f ? 0.f : logf(r.s) - r.u * LN2 / r.s; }
 
-// K-th largest of the 64 * PER keys that the lanes of a wave hold (0: no key), or a little less: its top
-// BITS bits.  0 if there are fewer than K.
+// K-th largest of the 64 * PER keys that the lanes of a wave hold (0: no key), or a little less: its top 16
+// bits (all that a 16-bit type has).  0 if there are fewer than K.
 template <int PER>
 __device__ inline unsigned kth_key(const unsigned (&key)[PER], int K) {
   unsigned t = 0;
 #pragma unroll 1
-  for (int bit = 31; bit >= 12; --bit) {
+  for (int bit = 31; bit >= 16; --bit) {
     const unsigned u = t | (1u << bit);
     int n = 0;
 #pragma unroll
@@ -201,20 +226,15 @@ struct TopShared {
   int n;
 };
 
-// The K largest of what the team holds, in falling order: put(rank, full key).
+// The K largest of the entries lo .. hi-1 of a row that the team holds, in falling order: put(rank, full key).  largest:
+// the thread's own largest value; ordinary: no NaN and no +inf.  (What few rows need reads the row from the caches, in loops:
+// it would cost the others registers.)
 template <typename E, int NW, typename PUT>
-__device__ inline void team_top(const Held<E, NW>& x, int lo, int hi, int K, int tid,
-                                TopShared<NW, TeamOf<E, NW>::cand>& sh, PUT put) {
+__device__ inline void team_top(const Held<E, NW>& x, const E* row, int lo, int hi, int K, int tid, float largest,
+                                bool ordinary, TopShared<NW, TeamOf<E, NW>::cand>& sh, PUT put) {
   using T = TeamOf<E, NW>;
-  unsigned most = 0;
-#pragma unroll
-  for (int j = 0; j < T::loads; ++j)
-#pragma unroll
-    for (int k = 0; k < T::per_load; ++k) {
-      const int i = x.index(j, k);
-      const unsigned key = key_of(x.at(j, k));
-      if (i >= lo && i < hi && key > most) most = key;
-    }
+  // (-inf, all that lies outside the row is, cannot be told from what is in it: no bound then)
+  unsigned most = largest > -__builtin_inff() ? key_of(largest) : 0;
   if (tid == 0) sh.n = 0;
   unsigned threshold;
   if constexpr (NW == 1) {
@@ -240,18 +260,27 @@ __device__ inline void team_top(const Held<E, NW>& x, int lo, int hi, int K, int
     threshold = sh.threshold;
   }
   team_sync<NW>();
-  threshold = max(threshold, 1u);
+  auto take = [&](unsigned key, int i) {
+    const int at = atomicAdd(&sh.n, 1);
+    if (at < T::cand) sh.cand[at] = full_key(key, (unsigned)i);
+  };
+  const bool bounded = ordinary && threshold != 0;
+  if (bounded) {                                             // values compare as their keys do
+    const float bound = value_of(threshold);
+    if (largest >= bound)
 #pragma unroll
-  for (int j = 0; j < T::loads; ++j)
+      for (int j = 0; j < T::loads; ++j)
 #pragma unroll
-    for (int k = 0; k < T::per_load; ++k) {
-      const int i = x.index(j, k);
-      const unsigned key = key_of(x.at(j, k));
-      if (key >= threshold && i >= lo && i < hi) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < T::cand) sh.cand[at] = full_key(key, (unsigned)i);
-      }
+        for (int k = 0; k < T::per_load; ++k) {
+          const float v = x.at(j, k);
+          if (v >= bound) take(key_of(v), x.index(j, k));
+        }
+  } else {                                                   // fewer than K groups above -inf: all that is
+    for (int i = lo + tid; i < hi; i += T::threads) {
+      const float v = elem_f32(row[i]);
+      if (ordinary ? v > -__builtin_inff() : key_of(v) >= threshold) take(key_of(v), i);
     }
+  }
   team_sync<NW>();
   const int n = sh.n;
   if (n <= T::cand) {
@@ -261,20 +290,24 @@ __device__ inline void team_top(const Held<E, NW>& x, int lo, int hi, int K, int
       for (int j = 0; j < n; ++j) rank += sh.cand[j] > mine;
       if (rank < K) put(rank, mine);
     }
+    if (n < K && tid < 64)                                   // -inf at the lowest indices
+      for (int i0 = lo, rank = n; rank < K; i0 += 64) {
+        const bool inf = i0 + tid < hi && elem_f32(row[i0 + tid]) == -__builtin_inff();
+        const u64 mask = __ballot(inf);
+        const int mine = rank + __popcll(mask & ((1ull << tid) - 1));
+        if (inf && mine < K) put(mine, full_key(key_of(-__builtin_inff()), (unsigned)(i0 + tid)));
+        rank += __popcll(mask);
+      }
     return;
   }
   if constexpr (NW > 1) {
     u64 last = ~0ull;
     for (int r = 0; r < K; ++r) {
       u64 best = 0;
-#pragma unroll
-      for (int j = 0; j < T::loads; ++j)
-#pragma unroll
-        for (int k = 0; k < T::per_load; ++k) {
-          const int i = x.index(j, k);
-          const u64 f = full_key(key_of(x.at(j, k)), (unsigned)i);
-          if (i >= lo && i < hi && f < last && f > best) best = f;
-        }
+      for (int i = lo + tid; i < hi; i += T::threads) {
+        const u64 f = full_key(key_of(elem_f32(row[i])), (unsigned)i);
+        if (f < last && f > best) best = f;
+      }
       best = wave_max(best);
       if ((tid & 63) == 0) sh.best[tid >> 6] = best;
       __syncthreads();
@@ -338,7 +371,7 @@ __device__ inline void put_token(const RowArgs& a, long long row, const E* x, co
 }
 
 template <typename E, int NW, bool SEGS>
-__global__ __launch_bounds__((TeamOf<E, NW>::block)) void logprobs_kernel(RowArgs a) {
+__global__ __launch_bounds__((TeamOf<E, NW>::block), NW == 16 ? 8 : 4) void logprobs_kernel(RowArgs a) {
   using T = TeamOf<E, NW>;
   __shared__ float part[NW == 1 ? 1 : NW][2];
   __shared__ TopShared<NW, T::cand> top[T::teams];
@@ -355,7 +388,9 @@ __global__ __launch_bounds__((TeamOf<E, NW>::block)) void logprobs_kernel(RowArg
   Held<E, NW> held;
   held.load(x, lo, hi, lo - begin, tid);
   const float c = a.inv_t * LOG2E;
-  const Stats st = team_stats<E, NW, true>(held, c, tid, part);
+  float largest;
+  const Stats st = team_stats<E, NW, true>(held, c, tid, part, &largest);
+  const bool ordinary = st.s == st.s;                        // (no NaN, no +inf)
   if constexpr (SEGS) {
     if (tid == 0) {
       a.out.m[item] = st.m;
@@ -366,12 +401,13 @@ __global__ __launch_bounds__((TeamOf<E, NW>::block)) void logprobs_kernel(RowArg
       u64* out = a.out.top + item * a.K;
       for (int i = tid; i < a.K; i += T::threads)
         if (i >= hi - lo) out[i] = 0;                        // (a last segment of fewer than K entries)
-      team_top<E, NW>(held, lo, hi, min(a.K, hi - lo), tid, top[team], [&](int r, u64 f) { out[r] = f; });
+      team_top<E, NW>(held, x, lo, hi, min(a.K, hi - lo), tid, largest, ordinary, top[team],
+                     [&](int r, u64 f) { out[r] = f; });
     }
   } else {
     if (tid == 0) put_token(a, row, x, st);
     if (a.K > 0)
-      team_top<E, NW>(held, lo, hi, a.K, tid, top[team], [&](int r, u64 f) {
+      team_top<E, NW>(held, x, lo, hi, a.K, tid, largest, ordinary, top[team], [&](int r, u64 f) {
         a.top_logp[row * a.K + r] = log_prob(value_of((unsigned)(f >> 32)), st, a.inv_t);
         a.top_ids[row * a.K + r] = index_of(f);
       });
@@ -393,7 +429,7 @@ __device__ inline Stats join_stats(const SegOut& o, long long row, int segs, flo
   return {m, wave_sum(s), wave_sum(u)};
 }
 
-constexpr int JOIN_SEGS = 33;                                // of a row at most: 2^20 entries and a piece, 2^15 each
+constexpr int JOIN_SEGS = 33;                                // of a row at most: 2^20 entries and a piece, 2^15 each, or 2^18, 2^13 each
 template <typename E>
 __global__ __launch_bounds__(256) void logprobs_join_kernel(RowArgs a) {
   __shared__ u64 cand[JOIN_SEGS * LOGPROBS_MAX_K];
@@ -525,39 +561,43 @@ template <typename E, int NW>
 __device__ inline void put_gradient(const DistillArgs& a, const Held<E, NW>& x, E* out, int lo, int hi, float m,
                                     float s, float w, const Teacher& t, int tid) {
   using T = TeamOf<E, NW>;
-  const float c = a.inv_t * LOG2E, m0 = finite_max(m);
-  const float f = t.total == 0.f || s == 0.f ? 0.f * s : w * t.total / s;
+  const Exponent ex(a.inv_t * LOG2E, m);
+  const float f = t.total == 0.f || s == 0.f ? 0.f * s : w * t.total / s * ex.scale();
   const bool wide = ((uintptr_t)(out + x.first) & 15) == 0;
+  auto store = [&](auto one) {
 #pragma unroll
-  for (int j = 0; j < T::loads; ++j) {
-    const int i = x.index(j, 0);
-    uintx4 r;
+    for (int j = 0; j < T::loads; ++j) {
+      const int i = x.index(j, 0);
+      uintx4 r;
 #pragma unroll
-    for (int k = 0; k < T::per_load; k += ELEMS_PER_WORD<E>) {
-      float g[2];
+      for (int k = 0; k < T::per_load; k += ELEMS_PER_WORD<E>) {
+        float g[2];
 #pragma unroll
-      for (int e = 0; e < ELEMS_PER_WORD<E>; ++e)
-        g[e] = f * __builtin_amdgcn_exp2f((x.at(j, k + e) - m0) * c);
-      if constexpr (sizeof(E) == 4) r[k] = __float_as_uint(g[0]);
-      else r[k / 2] = pack2<E>(g[0], g[1]);
+        for (int e = 0; e < ELEMS_PER_WORD<E>; ++e)
+          g[e] = f * __builtin_amdgcn_exp2f(exponent<decltype(one)::value>(ex, x.at(j, k + e)));
+        if constexpr (sizeof(E) == 4) r[k] = __float_as_uint(g[0]);
+        else r[k / 2] = pack2<E>(g[0], g[1]);
+      }
+      if (wide && i >= lo && i + T::per_load <= hi) {
+        *reinterpret_cast<uintx4*>(out + i) = r;
+      } else {
+        E e[T::per_load];
+        __builtin_memcpy(e, &r, 16);
+#pragma unroll
+        for (int k = 0; k < T::per_load; ++k)
+          if (i + k >= lo && i + k < hi) out[i + k] = e[k];
+      }
     }
-    if (wide && i >= lo && i + T::per_load <= hi) {
-      *reinterpret_cast<uintx4*>(out + i) = r;
-    } else {
-      E e[T::per_load];
-      __builtin_memcpy(e, &r, 16);
-#pragma unroll
-      for (int k = 0; k < T::per_load; ++k)
-        if (i + k >= lo && i + k < hi) out[i + k] = e[k];
-    }
-  }
+  };
+  if (ex.one) store(std::true_type{});
+  else store(std::false_type{});
   // the entries, over what was stored there before the barrier
   team_sync<NW>();
   if (t.total == 0.f) return;
   for (int k = tid; k < a.K; k += T::threads) {
     const int id = t.id[k];
     if (id < lo || id >= hi) continue;
-    const float p = f * __builtin_amdgcn_exp2f((t.x[k] - m0) * c);
+    const float p = f * __builtin_amdgcn_exp2f(ex.one ? exponent<true>(ex, t.x[k]) : exponent<false>(ex, t.x[k]));
     out[id] = elem_of<E>(p - w * t.total * same_ids(t, a.K, k));
   }
 }
@@ -663,6 +703,7 @@ __global__ __launch_bounds__((TeamOf<E, NW>::block)) void distill_grad_kernel(Di
 }
 
 // ---- launches
+constexpr int CUT_ROWS = 512;
 static int elem_size(int dtype) { return dtype == MGRIT_F32 ? 4 : 2; }
 static bool rows_aligned(const void* p, long long ld, int size) {
   return (uintptr_t)p % 16 == 0 && ld * size % 16 == 0;
@@ -676,19 +717,32 @@ static int team_waves(int V, int size, bool aligned) {
   if (need <= (size == 4 ? TeamOf<float, 16>::elems : TeamOf<Bf16, 16>::elems)) return 16;
   return 0;
 }
-// Segments of a row that no team holds: all as long, of teams of 16 waves.
-static RowShape segments(int V, int size, bool aligned) {
-  const int per = 16 / size, most = size == 4 ? TeamOf<float, 16>::chunks : TeamOf<Bf16, 16>::chunks;
+// Segments of a row, all as long, for teams of `waves` (4 or 16) waves.
+static RowShape segments(int V, int size, bool aligned, int waves = 16) {
+  const int per = 16 / size;
+  const int most = (size == 4 ? TeamOf<float, 16>::chunks : TeamOf<Bf16, 16>::chunks) / 16 * waves;
   const int pieces = (V + (aligned ? 0 : per - 1) + per - 1) / per;
   RowShape s;
   s.segs = (pieces + most - 1) / most;
   s.seg = (pieces + s.segs - 1) / s.segs;
   return s;
 }
+// Waves of the teams that token_logprobs cuts long rows up for (their segments are joined in a second launch), 0 where
+// it leaves rows whole.
+static int logprobs_cut(int N, int V, int size, bool aligned) {
+  const int whole = team_waves(V, size, aligned);
+  if (whole == 1 || whole == 4) return 0;
+  if (whole == 16 && N < CUT_ROWS) return 0;
+  return V <= (1 << 18) ? 4 : 16;
+}
 size_t logits_workspace(const logits_cfg& c) {
   const int size = elem_size(c.dtype);
-  if (team_waves(c.V, size, false)) return 0;
-  const long long n = (long long)c.N * segments(c.V, size, false).segs;
+  // (what is aligned is known with the arrays only: the larger of the two)
+  long long segs = team_waves(c.V, size, false) ? 0 : segments(c.V, size, false).segs;
+  const int cut = logprobs_cut(c.N, c.V, size, false);
+  if (cut) segs = segments(c.V, size, false, cut).segs;
+  if (!segs) return 0;
+  const long long n = c.N * segs;
   return (size_t)((3 * n * 4 + 15) / 16 * 16 + 8 * n * (c.K > LOGPROBS_MAX_K ? 0 : c.K) + 8LL * c.N);
 }
 
@@ -709,6 +763,18 @@ static hipError_t logprobs_start(const LogitsArgs& a, hipStream_t s) {
   const bool aligned = rows_aligned(a.logits, a.c.ld, sizeof(E));
   r.shape = {1, 0};
   const unsigned N = (unsigned)a.c.N;
+  const int cut = logprobs_cut(a.c.N, a.c.V, sizeof(E), aligned);
+  if (cut) {
+    r.shape = segments(a.c.V, sizeof(E), aligned, cut);
+    r.out = seg_out(a.workspace, a.c.N, r.shape.segs);
+    const dim3 grid(N * (unsigned)r.shape.segs);
+    if (cut == 4) hipLaunchKernelGGL((logprobs_kernel<E, 4, true>), grid, dim3(256), 0, s, r);
+    else hipLaunchKernelGGL((logprobs_kernel<E, 16, true>), grid, dim3(1024), 0, s, r);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((logprobs_join_kernel<E>), dim3(N), dim3(256), 0, s, r);
+    return hipGetLastError();
+  }
   switch (team_waves(a.c.V, sizeof(E), aligned)) {
     case 1:
       hipLaunchKernelGGL((logprobs_kernel<E, 1, false>), dim3((N + 3) / 4), dim3(256), 0, s, r);
@@ -716,17 +782,8 @@ static hipError_t logprobs_start(const LogitsArgs& a, hipStream_t s) {
     case 4:
       hipLaunchKernelGGL((logprobs_kernel<E, 4, false>), dim3(N), dim3(256), 0, s, r);
       break;
-    case 16:
+    default:
       hipLaunchKernelGGL((logprobs_kernel<E, 16, false>), dim3(N), dim3(1024), 0, s, r);
-      break;
-    default: {
-      r.shape = segments(a.c.V, sizeof(E), aligned);
-      r.out = seg_out(a.workspace, a.c.N, r.shape.segs);
-      hipLaunchKernelGGL((logprobs_kernel<E, 16, true>), dim3(N * (unsigned)r.shape.segs), dim3(1024), 0, s, r);
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      hipLaunchKernelGGL((logprobs_join_kernel<E>), dim3(N), dim3(256), 0, s, r);
-    }
   }
   return hipGetLastError();
 }

@@ -1,4 +1,9 @@
 // Product in 8-bit integers with a scale for each token and channel (include/mgrit_ops.h).
+//
+// The tokens are quantised into the workspace by a kernel of their own (each row once; the product's tiles would do it once
+// per column of tiles); rows are padded with zeros to 128 bytes, so that the products look at no tail of K.  In the products the
+// channels are the rows of the matrix instruction and the tokens its columns: a lane ends up with four neighbouring
+// channels of one token.
 #include "elem.h"
 #include "ops.h"
 
@@ -6,117 +11,293 @@ namespace mg {
 
 typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef int intx16 __attribute__((ext_vector_type(16)));
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 
-__host__ __device__ inline long long q8_pad(int K) { return ((long long)K + 127) / 128 * 128; }
+__host__ __device__ inline int q8_pad(int K) { return (K + 127) / 128 * 128; }
 
+// ---------------------------------------------------------------------------
+// quantisation
+// ---------------------------------------------------------------------------
 __device__ inline float quant_scale(float amax) { return fmaxf(amax * (1.0f / 127.0f), 0x1p-126f); }
-__device__ inline int quant(float x, float scale) { return (int)rintf(x / scale); }
-
-// One row per workgroup; the second pass reads the row from the caches.  A row that is not finite: scale NaN, zeros.
-template <typename E>
-__global__ __launch_bounds__(256) void q8_quantize_kernel(Q8Args a) {
-  __shared__ float part[4];
-  __shared__ int odd;
-  const long long row = blockIdx.x;
-  const E* x = (const E*)a.x + row * a.c.ldx;
-  const int tid = threadIdx.x, K = a.c.K;
-  if (tid == 0) odd = 0;
-  __syncthreads();
-  float m = 0.f;
-  bool bad = false;
-  for (int k = tid; k < K; k += 256) {
-    const float v = fabsf(elem_f32(x[k]));
-    bad |= !(v < __builtin_inff());
-    m = fmaxf(m, v);
-  }
+__device__ inline unsigned quant(float x, float scale) { return (unsigned)(int)rintf(x / scale) & 255u; }
+__device__ inline float wave_max(float v) {
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  if (__any(bad) && (tid & 63) == 0) odd = 1;
-  if ((tid & 63) == 0) part[tid >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-  const bool finite = odd == 0;
+  for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+
+// A row per team of NW waves, held in registers: LOADS pieces of 16 bytes per thread.  A row that is not finite:
+// scale NaN, zeros.
+template <typename E, int NW, int LOADS>
+__global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void q8_quantize_kernel(Q8Args a) {
+  constexpr int PER = 16 / (int)sizeof(E), THREADS = NW * 64;
+  __shared__ float part[NW];
+  const int tid = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const long long row = NW == 1 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x;
+  if (row >= a.c.M) return;                          // (teams of one wave: whole waves)
+  const E* x = (const E*)a.x + row * a.c.ldx;
+  const int K = a.c.K, pad = q8_pad(K);
+  const bool aligned = ((uintptr_t)x & 15) == 0;
+  uintx4 raw[LOADS];
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j) {
+    const int i = (j * THREADS + tid) * PER;
+    if (aligned && i + PER <= K) {
+      raw[j] = *reinterpret_cast<const uintx4*>(x + i);
+    } else {
+      E e[PER];
+#pragma unroll
+      for (int k = 0; k < PER; ++k) e[k] = i + k < K ? x[i + k] : elem_of<E>(0.f);
+      raw[j] = __builtin_bit_cast(uintx4, e);
+    }
+  }
+  auto at = [&](int j, int k) {
+    return word_elem<E>(raw[j][k / ELEMS_PER_WORD<E>], k % ELEMS_PER_WORD<E>);
+  };
+  // (the larger of a value and NaN is the value: a NaN is made an infinity first)
+  float m = 0.f;
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j)
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const float v = fabsf(at(j, k));
+      m = fmaxf(m, v == v ? v : __builtin_inff());
+    }
+  m = wave_max(m);
+  if constexpr (NW > 1) {
+    if ((tid & 63) == 0) part[tid >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, part[w]);
+  }
+  const bool finite = m < __builtin_inff();
   const float scale = quant_scale(finite ? m : 0.f);
   if (tid == 0) a.scale[row] = finite ? scale : __uint_as_float(0x7fc00000u);
-  const int pad = (int)q8_pad(K);
-  int* out = (int*)(a.q + row * pad);
-  for (int k = 4 * tid; k < pad; k += 1024) {
-    unsigned w = 0;
+  int8_t* out = a.q + row * pad;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (finite && k + i < K) w |= ((unsigned)quant(elem_f32(x[k + i]), scale) & 255u) << (8 * i);
-    out[k / 4] = (int)w;
+  for (int j = 0; j < LOADS; ++j) {
+    const int i = (j * THREADS + tid) * PER;
+    if (i >= pad) continue;
+#pragma unroll
+    for (int k = 0; k < PER; k += 4) {
+      unsigned w = 0;
+      if (finite)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) w |= quant(at(j, k + b), scale) << (8 * b);
+      *reinterpret_cast<unsigned*>(out + i + k) = w;
+    }
   }
 }
 
-// Tile of TM tokens x TN channels, four waves of half of each.  The channels are the rows of the matrix
-// instruction and the tokens its columns: a lane then holds four neighbouring channels of a token.
-// Slices of 128 bytes of K go through LDS; a row's 16-byte pieces are stored in the order piece ^ (row & 7).
+// Rows longer than that, in two passes; the second reads the row from the caches.
+template <typename E>
+__global__ __launch_bounds__(1024) void q8_quantize_long_kernel(Q8Args a) {
+  __shared__ float part[16];
+  const long long row = blockIdx.x;
+  const E* x = (const E*)a.x + row * a.c.ldx;
+  const int tid = threadIdx.x, K = a.c.K, pad = q8_pad(K);
+  float m = 0.f;
+  for (int k = tid; k < K; k += 1024) {
+    const float v = fabsf(elem_f32(x[k]));
+    m = fmaxf(m, v == v ? v : __builtin_inff());
+  }
+  m = wave_max(m);
+  if ((tid & 63) == 0) part[tid >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 16; ++w) m = fmaxf(m, part[w]);
+  const bool finite = m < __builtin_inff();
+  const float scale = quant_scale(finite ? m : 0.f);
+  if (tid == 0) a.scale[row] = finite ? scale : __uint_as_float(0x7fc00000u);
+  unsigned* out = (unsigned*)(a.q + row * pad);
+  for (int k = 4 * tid; k < pad; k += 4096) {
+    unsigned w = 0;
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      if (finite && k + b < K) w |= quant(elem_f32(x[k + b]), scale) << (8 * b);
+    out[k / 4] = w;
+  }
+}
+
+template <typename E>
+static void quantize_start(const Q8Args& a, hipStream_t s) {
+  constexpr int PER = 16 / (int)sizeof(E);
+  const int pad = q8_pad(a.c.K);
+  const unsigned M = (unsigned)a.c.M;
+  if (pad <= 2 * 64 * PER)
+    hipLaunchKernelGGL((q8_quantize_kernel<E, 1, 2>), dim3((M + 3) / 4), dim3(256), 0, s, a);
+  else if (pad <= 8 * 64 * PER && M >= 4096)
+    hipLaunchKernelGGL((q8_quantize_kernel<E, 1, 8>), dim3((M + 3) / 4), dim3(256), 0, s, a);
+  else if (pad <= 4 * 256 * PER)
+    hipLaunchKernelGGL((q8_quantize_kernel<E, 4, 4>), dim3(M), dim3(256), 0, s, a);
+  else if (pad <= 4 * 1024 * PER)
+    hipLaunchKernelGGL((q8_quantize_kernel<E, 16, 4>), dim3(M), dim3(1024), 0, s, a);
+  else
+    hipLaunchKernelGGL(q8_quantize_long_kernel<E>, dim3(M), dim3(1024), 0, s, a);
+}
+hipError_t launch_q8_quantize(const Q8Args& a, hipStream_t s) {
+  if (a.c.dtype == MGRIT_F32) quantize_start<float>(a, s);
+  else if (a.c.dtype == MGRIT_BF16) quantize_start<Bf16>(a, s);
+  else quantize_start<F16>(a, s);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// products
+// ---------------------------------------------------------------------------
+// Four neighbouring channels n .. n+3 of a token, from their sums; wide: one store (the row's place allows it).
+template <typename E>
+__device__ inline void put4(const Q8Args& a, E* y, int n, const intx4& sum, float sm, bool wide) {
+  float v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c = min(n + i, a.c.N - 1);
+    v[i] = (float)sum[i] * sm * a.w_scale[c];
+    if (a.bias) v[i] += a.bias[c];
+  }
+  if (wide && n + 3 < a.c.N) {
+    if constexpr (sizeof(E) == 4)
+      *reinterpret_cast<float4*>(y + n) = make_float4(v[0], v[1], v[2], v[3]);
+    else
+      *reinterpret_cast<uint2*>(y + n) = make_uint2(pack2<E>(v[0], v[1]), pack2<E>(v[2], v[3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < a.c.N) y[n + i] = elem_of<E>(v[i]);
+  }
+}
+template <typename E>
+__device__ inline bool wide_rows(const Q8Args& a) {
+  return ((uintptr_t)a.y | (uintptr_t)(a.c.ldy * sizeof(E))) % (4 * sizeof(E)) == 0;
+}
+
+// Few tokens (up to 16 MB): the weights are read once, straight into the operands of the matrix instruction, and
+// bound it.  A workgroup takes 16 channels; its four waves split K in turns of U slices of 64 bytes (two
+// neighbouring slices are a line of memory) and add their sums up in LDS.
+template <typename E, int MB>
+__global__ __launch_bounds__(256) void q8_few_kernel(Q8Args a) {
+  constexpr int U = MB == 1 ? 8 : 4;
+  __shared__ intx4 sums[4][MB][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int pad = q8_pad(a.c.K), slices = pad / 64, n0 = blockIdx.x * 16;
+  const int8_t* w = a.w + (long long)min(n0 + (lane & 15), a.c.N - 1) * pad + (lane >> 4) * 16;
+  const int8_t* x[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b)
+    x[b] = a.q + (long long)min(16 * b + (lane & 15), a.c.M - 1) * pad + (lane >> 4) * 16;
+  intx4 acc[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) acc[b] = intx4{};
+  for (int s0 = wave * U; s0 < slices; s0 += 4 * U) {
+    intx4 fw[U], fx[U][MB];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = 64 * min(s0 + u, slices - 1);
+      fw[u] = *reinterpret_cast<const intx4*>(w + k);
+#pragma unroll
+      for (int b = 0; b < MB; ++b) fx[u][b] = *reinterpret_cast<const intx4*>(x[b] + k);
+    }
+    __builtin_amdgcn_sched_barrier(0);                 // (all of them in flight)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s0 + u >= slices) break;
+#pragma unroll
+      for (int b = 0; b < MB; ++b)
+        acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u], fx[u][b], acc[b], 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < MB; ++b) sums[wave][b][lane] = acc[b];
+  __syncthreads();
+  const bool wide = wide_rows<E>(a);
+  for (int b = wave; b < MB; b += 4) {
+    const int m = 16 * b + (lane & 15), n = n0 + 4 * (lane >> 4);
+    if (m >= a.c.M || n >= a.c.N) continue;
+    const intx4 sum = sums[0][b][lane] + sums[1][b][lane] + sums[2][b][lane] + sums[3][b][lane];
+    put4<E>(a, (E*)a.y + (long long)m * a.c.ldy, n, sum, a.scale[m], wide);
+  }
+}
+
+// A tile of TM tokens x TN channels: four waves, each half of either.  Slices of 128 bytes of K go through one of two
+// LDS buffers; a row's 16-byte pieces lie in the order piece ^ (row & 7), which spreads a fragment's rows over the banks.
+// While the matrix instructions of slice s run, slice s + 1 goes from registers to the other buffer and slice
+// s + 2 is loaded; the fragments of a quarter of a slice are read during the instructions of the quarter before, the
+// first of the next slice behind the barrier in front of the last quarter.
 template <typename E, int TM, int TN>
-__global__ __launch_bounds__(256) void q8_tile_kernel(Q8Args a) {
+__global__ __launch_bounds__(256) void q8_tile_kernel(Q8Args a, int tiles_m, int tiles_n) {
   constexpr int WM = TM / 64, WN = TN / 64;              // 32 x 32 blocks of a wave
-  __shared__ intx4 sx[TM * 8], sw[TN * 8];
+  constexpr int LX = TM / 32, LW = TN / 32;              // pieces of a slice that a thread moves
+  __shared__ intx4 lds[2][(TM + TN) * 8];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const long long pad = q8_pad(a.c.K);
-  const int tiles_n = (a.c.N + TN - 1) / TN;
-  const int tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
-  const int m0 = tm * TM, n0 = tn * TN;
+  const int pad = q8_pad(a.c.K), slices = pad / 128;
+  // tiles of neighbouring tokens on one XCD (workgroups go to the eight in turn), channels first
+  const int tiles = tiles_m * tiles_n, per = (tiles + 7) / 8;
+  int tile = blockIdx.x;
+  if (tiles % 8 == 0) tile = (tile & 7) * per + (tile >> 3);
+  const int tm = tile / tiles_n, m0 = tm * TM, n0 = (tile - tm * tiles_n) * TN;
   const int wm = (wave & 1) * (TM / 2), wn = (wave >> 1) * (TN / 2);
+  // what the thread moves: piece tid % 8 of rows tid / 8 + 32 i (rows that do not exist: the last one)
+  const int8_t *gx = a.q + (long long)m0 * pad, *gw = a.w + (long long)n0 * pad;
+  unsigned ox[LX], ow[LW];
+#pragma unroll
+  for (int i = 0; i < LX; ++i) ox[i] = min(tid / 8 + 32 * i, a.c.M - 1 - m0) * pad + (tid & 7) * 16;
+#pragma unroll
+  for (int i = 0; i < LW; ++i) ow[i] = min(tid / 8 + 32 * i, a.c.N - 1 - n0) * pad + (tid & 7) * 16;
+  const int to = (tid & ~7) | ((tid & 7) ^ ((tid >> 3) & 7));
+  intx4 rx[LX], rw[LW];
+  auto load = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < LX; ++i) rx[i] = *reinterpret_cast<const intx4*>(gx + s * 128 + ox[i]);
+#pragma unroll
+    for (int i = 0; i < LW; ++i) rw[i] = *reinterpret_cast<const intx4*>(gw + s * 128 + ow[i]);
+  };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < LX; ++i) lds[buf][to + 256 * i] = rx[i];
+#pragma unroll
+    for (int i = 0; i < LW; ++i) lds[buf][TM * 8 + to + 256 * i] = rw[i];
+  };
+  intx4 fx[2][WM], fw[2][WN];
+  auto read = [&](int buf, int kk, int set) {
+    const int piece = (kk * 2 + (lane >> 5)) ^ (lane & 7);
+#pragma unroll
+    for (int j = 0; j < WM; ++j) fx[set][j] = lds[buf][(wm + 32 * j + (lane & 31)) * 8 + piece];
+#pragma unroll
+    for (int i = 0; i < WN; ++i) fw[set][i] = lds[buf][(TM + wn + 32 * i + (lane & 31)) * 8 + piece];
+  };
   intx16 acc[WN][WM];
 #pragma unroll
   for (int i = 0; i < WN; ++i)
 #pragma unroll
     for (int j = 0; j < WM; ++j) acc[i][j] = intx16{};
-  constexpr int LX = TM * 8 / 256, LW = TN * 8 / 256;
-  intx4 rx[LX], rw[LW];
-  auto load = [&](long long k) {
-#pragma unroll
-    for (int i = 0; i < LX; ++i) {
-      const int e = tid + 256 * i, r = min(m0 + (e >> 3), a.c.M - 1);
-      rx[i] = *reinterpret_cast<const intx4*>(a.q + r * pad + k + (e & 7) * 16);
-    }
-#pragma unroll
-    for (int i = 0; i < LW; ++i) {
-      const int e = tid + 256 * i, r = min(n0 + (e >> 3), a.c.N - 1);
-      rw[i] = *reinterpret_cast<const intx4*>(a.w + r * pad + k + (e & 7) * 16);
-    }
-  };
   load(0);
-  for (long long k = 0; k < pad; k += 128) {
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < LX; ++i) {
-      const int e = tid + 256 * i;
-      sx[(e & ~7) | ((e & 7) ^ ((e >> 3) & 7))] = rx[i];
-    }
-#pragma unroll
-    for (int i = 0; i < LW; ++i) {
-      const int e = tid + 256 * i;
-      sw[(e & ~7) | ((e & 7) ^ ((e >> 3) & 7))] = rw[i];
-    }
-    __syncthreads();
-    if (k + 128 < pad) load(k + 128);
+  store(0);
+  if (slices > 1) load(1);
+  __syncthreads();
+  read(0, 0, 0);
+  for (int s = 0; s < slices; ++s) {
+    const int buf = s & 1;
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
-      intx4 fx[WM], fw[WN];
-      const int piece = kk * 2 + (lane >> 5);
-#pragma unroll
-      for (int j = 0; j < WM; ++j) {
-        const int r = wm + 32 * j + (lane & 31);
-        fx[j] = sx[r * 8 + (piece ^ (r & 7))];
+      if (kk == 0 && s + 1 < slices) {
+        store(buf ^ 1);
+        if (s + 2 < slices) load(s + 2);
       }
-#pragma unroll
-      for (int i = 0; i < WN; ++i) {
-        const int r = wn + 32 * i + (lane & 31);
-        fw[i] = sw[r * 8 + (piece ^ (r & 7))];
+      if (kk < 3) {
+        read(buf, kk + 1, (kk + 1) & 1);
+      } else if (s + 1 < slices) {
+        // every wave has read this buffer and written the other one
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        read(buf ^ 1, 0, 0);
       }
 #pragma unroll
       for (int i = 0; i < WN; ++i)
 #pragma unroll
         for (int j = 0; j < WM; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[i], fx[j], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[kk & 1][i], fx[kk & 1][j], acc[i][j], 0, 0, 0);
     }
   }
+  const bool wide = wide_rows<E>(a);
 #pragma unroll
   for (int j = 0; j < WM; ++j) {
     const int m = m0 + wm + 32 * j + (lane & 31);
@@ -126,27 +307,36 @@ __global__ __launch_bounds__(256) void q8_tile_kernel(Q8Args a) {
 #pragma unroll
     for (int i = 0; i < WN; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int n = n0 + wn + 32 * i + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+      for (int e = 0; e < 4; ++e) {
+        const int n = n0 + wn + 32 * i + 8 * e + 4 * (lane >> 5);
         if (n >= a.c.N) continue;
-        const float v = (float)acc[i][j][e] * sm * a.w_scale[n];
-        y[n] = elem_of<E>(a.bias ? v + a.bias[n] : v);
+        const intx4 sum = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+        put4<E>(a, y, n, sum, sm, wide);
       }
   }
 }
 
-hipError_t launch_q8_quantize(const Q8Args& a, hipStream_t s) {
-  const dim3 g((unsigned)a.c.M), t(256);
-  if (a.c.dtype == MGRIT_F32) hipLaunchKernelGGL(q8_quantize_kernel<float>, g, t, 0, s, a);
-  else if (a.c.dtype == MGRIT_BF16) hipLaunchKernelGGL(q8_quantize_kernel<Bf16>, g, t, 0, s, a);
-  else hipLaunchKernelGGL(q8_quantize_kernel<F16>, g, t, 0, s, a);
-  return hipGetLastError();
+template <typename E, int TM, int TN>
+static void tile_start(const Q8Args& a, hipStream_t s) {
+  const int tm = (a.c.M + TM - 1) / TM, tn = (a.c.N + TN - 1) / TN;
+  hipLaunchKernelGGL((q8_tile_kernel<E, TM, TN>), dim3((unsigned)tm * (unsigned)tn), dim3(256), 0, s, a, tm, tn);
 }
-
 template <typename E>
 static void q8_start(const Q8Args& a, hipStream_t s) {
-  const unsigned grid = (unsigned)((a.c.M + 127) / 128) * (unsigned)((a.c.N + 127) / 128);
-  hipLaunchKernelGGL((q8_tile_kernel<E, 128, 128>), dim3(grid), dim3(256), 0, s, a);
+  const unsigned groups = (unsigned)(a.c.N + 15) / 16;
+  if (a.c.M <= 64) {
+    switch ((a.c.M + 15) / 16) {
+      case 1: hipLaunchKernelGGL((q8_few_kernel<E, 1>), dim3(groups), dim3(256), 0, s, a); break;
+      case 2: hipLaunchKernelGGL((q8_few_kernel<E, 2>), dim3(groups), dim3(256), 0, s, a); break;
+      case 3: hipLaunchKernelGGL((q8_few_kernel<E, 3>), dim3(groups), dim3(256), 0, s, a); break;
+      default: hipLaunchKernelGGL((q8_few_kernel<E, 4>), dim3(groups), dim3(256), 0, s, a);
+    }
+    return;
+  }
+  auto tiles = [&](int t) { return (long long)((a.c.M + t - 1) / t) * ((a.c.N + t - 1) / t); };
+  if (tiles(256) >= 192) tile_start<E, 256, 256>(a, s);
+  else if (tiles(128) >= 192) tile_start<E, 128, 128>(a, s);
+  else tile_start<E, 64, 64>(a, s);
 }
 hipError_t launch_q8_linear(const Q8Args& a, hipStream_t s) {
   const hipError_t e = launch_q8_quantize(a, s);

@@ -9,7 +9,7 @@ namespace mg {
 // ---- gated linear recurrence (kernels_glr.hip)
 // A workgroup of GLR_WAVES waves covers one row of the batch, 2 * lanes channels (two per lane) and
 // GLR_WAVES * (64 / lanes) * GLR_STEPS steps: a wave's lanes hold 64 / lanes runs of GLR_STEPS steps.
-constexpr int GLR_WAVES = 8, GLR_STEPS = 16;
+constexpr int GLR_WAVES = 8, GLR_STEPS = 8;
 struct GlrShape {
   int lanes;                // lanes across the channels: 16, 32 or 64
   int steps;                // of a tile

@@ -9,12 +9,12 @@ from __future__ import annotations
 
 import ctypes
 
-from .binding import MGRIT_BF16, MGRIT_F32, _Arg, _check, _marshal, _stream, lib as _base_lib
+from .binding import MGRIT_BF16, MGRIT_F32, _check, lib as _base_lib
 
 MGRIT_F16 = 4                             # dtype of the configurations below, beside MGRIT_F32 and MGRIT_BF16
 GLR_MIX, GLR_DECAY = 0, 1
 LOGPROBS_MAX_K, DISTILL_MAX_K = 64, 256
-_ready = None
+_ready = _torch = _TYPES = None
 
 
 def _fields(c_type, names):
@@ -56,8 +56,11 @@ class Q8Cfg(ctypes.Structure):
 
 
 def _lib() -> ctypes.CDLL:
-    global _ready
+    global _ready, _torch, _TYPES
     if _ready is None:
+        import torch
+        _torch = torch
+        _TYPES = {MGRIT_F32: torch.float32, MGRIT_BF16: torch.bfloat16, MGRIT_F16: torch.float16}
         L, vp, sz, i32 = _base_lib(), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
         szp = ctypes.POINTER(sz)
         for name, cfg, args in (
@@ -80,55 +83,84 @@ def _lib() -> ctypes.CDLL:
     return _ready
 
 
+def _stream() -> int:
+    """The current stream of the current device, as torch.cuda.current_stream().cuda_stream says."""
+    return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device())
+
+
 def _size(name, cfg) -> int:
     n = ctypes.c_size_t(0)
     _check(getattr(_lib(), name)(ctypes.byref(cfg), ctypes.byref(n)), name)
     return int(n.value)
 
 
-def _dtype(cfg):
-    import torch
-    return {MGRIT_F32: torch.float32, MGRIT_BF16: torch.bfloat16, MGRIT_F16: torch.float16}.get(cfg.dtype)
+# An argument is a plain value or (tensor, name, dtype, shape, kind): shape None: any; kind _DENSE:
+# contiguous; _ROWS: the last stride is 1; _SEQ: the same, passed as a pointer to a ``GlrSeq``.
+_DENSE, _ROWS, _SEQ = 0, 1, 2
 
 
-class _Strided(_Arg):
-    """A tensor argument of the configuration's dtype whose last stride is 1."""
+def _unit_rows(t):
+    return t.shape[-1] == 1 or t.stride(-1) == 1
+
+
+def _explain(args):
+    """Raises for the first argument that does not fit: all sizes first, then types, layouts and devices (as
+    binding._marshal does).  Returns where every argument fits."""
+    tensors = [a for a in args if type(a) is tuple and a[0] is not None]
+    for t, name, _, shape, _ in tensors:
+        if not isinstance(t, _torch.Tensor):
+            raise TypeError(f"{name}: expected a CUDA tensor")
+        if shape is not None and tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    for t, name, dtype, _, kind in tensors:
+        if dtype is not None and t.dtype != dtype:
+            raise TypeError(f"{name}: expected dtype {dtype}, got {t.dtype}")
+        if kind == _DENSE and not t.is_contiguous():
+            raise ValueError(f"{name}: tensor must be contiguous")
+        if kind != _DENSE and not _unit_rows(t):
+            raise ValueError(f"{name}: the last dimension must be contiguous")
+        if not t.is_cuda:
+            raise TypeError(f"{name}: expected a CUDA tensor")
+
+
+def _fits(t, dtype, shape, kind):
+    return (isinstance(t, _torch.Tensor) and (shape is None or t.shape == shape) and (dtype is None or t.dtype is dtype)
+            and t.is_cuda and (t.is_contiguous() if kind == _DENSE else _unit_rows(t)))
 
 
 def _call(name, cfg, *args) -> None:
-    """Like binding._call; sequences go as pointers to ``GlrSeq``, matrices as their data pointers."""
-    import torch
-    plain = [a for a in args if isinstance(a, _Arg) and not isinstance(a, _Strided)]
-    strided = [a for a in args if isinstance(a, _Strided) and a.t is not None]
-    for a in strided:
-        if not isinstance(a.t, torch.Tensor):
-            raise TypeError(f"{a.name}: expected a CUDA tensor")
-        if tuple(a.t.shape) != tuple(a.shape):
-            raise ValueError(f"{a.name}: expected shape {tuple(a.shape)}, got {tuple(a.t.shape)}")
-    pointers = dict(zip(map(id, plain), _marshal(plain)))
-    for a in strided:
-        if a.dtype is not None and a.t.dtype != a.dtype:
-            raise TypeError(f"{a.name}: expected dtype {a.dtype}, got {a.t.dtype}")
-        if a.t.shape[-1] > 1 and a.t.stride(-1) != 1:
-            raise ValueError(f"{a.name}: the last dimension must be contiguous")
-        if not a.t.is_cuda:
-            raise TypeError(f"{a.name}: expected a CUDA tensor")
-        if a.t.dim() == 3:
-            pointers[id(a)] = ctypes.byref(GlrSeq(a.t.data_ptr(), a.t.stride(0), a.t.stride(1)))
+    """Checks and marshals the arguments, then calls entry point `name` on the current stream.  (A call of a few
+    microseconds' work is as long as this: one pass over the arguments, the reasons only where one does not fit.)"""
+    L, out = _lib(), []
+    for a in args:
+        if type(a) is not tuple:
+            out.append(a)
+            continue
+        t, _, dtype, shape, kind = a
+        if t is None:
+            out.append(None)
+        elif not _fits(t, dtype, shape, kind):
+            _explain(args)
+            raise AssertionError(a[1])                # (not reached: _explain says what is wrong)
+        elif kind == _SEQ:
+            out.append(ctypes.byref(GlrSeq(t.data_ptr(), t.stride(0), t.stride(1))))
         else:
-            pointers[id(a)] = a.t.data_ptr()
-    out = [pointers.get(id(a)) if isinstance(a, _Arg) else a for a in args]
-    _check(getattr(_lib(), name)(ctypes.byref(cfg), *out, _stream()), name)
+            out.append(t.data_ptr())
+    _check(getattr(L, name)(ctypes.byref(cfg), *out, _stream()), name)
 
 
 def _bytes_of(t, name):
     """A workspace tensor and its size in bytes (the library compares the size with cfg)."""
-    return _Arg(t, name), ctypes.c_size_t(0 if t is None else t.numel() * t.element_size())
+    return (t, name, None, None, _DENSE), 0 if t is None else t.numel() * t.element_size()
+
+
+def _dtype(cfg):
+    _lib()
+    return _TYPES.get(cfg.dtype)
 
 
 def _f32(t, name, *shape):
-    import torch
-    return _Arg(t, name, torch.float32, shape)
+    return t, name, _torch.float32, shape, _DENSE
 
 
 # ---- gated linear recurrence
@@ -141,24 +173,23 @@ def glr_saved_bytes(cfg: GlrCfg) -> int:
 
 
 def _seq(cfg, t, name):
-    return _Strided(t, name, _dtype(cfg), (cfg.T, cfg.B, cfg.H))
+    return t, name, _dtype(cfg), (cfg.T, cfg.B, cfg.H), _SEQ
 
 
-def _reset(cfg, t, *shape):
-    import torch
-    return _Arg(t, "reset", torch.uint8, shape)
+def _reset(t, *shape):
+    return t, "reset", _torch.uint8, shape, _DENSE
 
 
 def glr_forward(cfg, gate, value, h0, reset, h, h_last, saved, workspace) -> None:
     T, B, H = cfg.T, cfg.B, cfg.H
     _call("glr_forward", cfg, _seq(cfg, gate, "gate"), _seq(cfg, value, "value"), _f32(h0, "h0", B, H),
-          _reset(cfg, reset, T, B), _seq(cfg, h, "h"), _f32(h_last, "h_last", B, H), *_bytes_of(saved, "saved"),
+          _reset(reset, T, B), _seq(cfg, h, "h"), _f32(h_last, "h_last", B, H), *_bytes_of(saved, "saved"),
           *_bytes_of(workspace, "workspace"))
 
 
 def glr_backward(cfg, gate, value, reset, saved, dh, dh_last, dgate, dvalue, dh0, workspace) -> None:
     T, B, H = cfg.T, cfg.B, cfg.H
-    _call("glr_backward", cfg, _seq(cfg, gate, "gate"), _seq(cfg, value, "value"), _reset(cfg, reset, T, B),
+    _call("glr_backward", cfg, _seq(cfg, gate, "gate"), _seq(cfg, value, "value"), _reset(reset, T, B),
           *_bytes_of(saved, "saved"), _seq(cfg, dh, "dh"), _f32(dh_last, "dh_last", B, H),
           _seq(cfg, dgate, "dgate"), _seq(cfg, dvalue, "dvalue"), _f32(dh0, "dh0", B, H),
           *_bytes_of(workspace, "workspace"))
@@ -166,16 +197,16 @@ def glr_backward(cfg, gate, value, reset, saved, dh, dh_last, dgate, dvalue, dh0
 
 def glr_step(cfg, gate, value, slots, reset, state_in, state_out, h) -> None:
     """gate, value, h: [B,H]; state_in, state_out: [n_slots,H]."""
-    import torch
+    _lib()
     B, H = cfg.B, cfg.H
     for t, name in ((gate, "gate"), (value, "value"), (h, "h"), (state_in, "state_in"), (state_out, "state_out")):
-        if isinstance(t, torch.Tensor) and t.dim() != 2:
+        if isinstance(t, _torch.Tensor) and t.dim() != 2:
             raise ValueError(f"{name}: expected two dimensions, got shape {tuple(t.shape)}")
-    one = lambda t: t[None] if isinstance(t, torch.Tensor) else t  # noqa: E731
-    n = state_in.shape[0] if isinstance(state_in, torch.Tensor) else 0
+    one = lambda t: t[None] if isinstance(t, _torch.Tensor) else t  # noqa: E731
+    n = state_in.shape[0] if isinstance(state_in, _torch.Tensor) else 0
     _call("glr_step", cfg, _seq(cfg, one(gate), "gate"), _seq(cfg, one(value), "value"),
-          _Arg(slots, "slots", torch.int32, (B,)), ctypes.c_int32(n), _reset(cfg, reset, B),
-          _f32(state_in, "state_in", n, H), _f32(state_out, "state_out", n, H), _seq(cfg, one(h), "h"))
+          (slots, "slots", _torch.int32, (B,), _DENSE), n, _reset(reset, B), _f32(state_in, "state_in", n, H),
+          _f32(state_out, "state_out", n, H), _seq(cfg, one(h), "h"))
 
 
 # ---- rows of logits
@@ -184,56 +215,48 @@ def logits_workspace_bytes(cfg: LogitsCfg) -> int:
 
 
 def _matrix(cfg, t, name, rows, cols):
-    return _Strided(t, name, _dtype(cfg), (rows, cols))
+    return t, name, _dtype(cfg), (rows, cols), _ROWS
 
 
 def _ld(t, cols):
     """Row stride of a matrix (one row: its width, whatever the tensor says)."""
-    import torch
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.shape[0] == 1:
+    _lib()
+    if not isinstance(t, _torch.Tensor) or t.dim() != 2 or t.shape[0] == 1:
         return cols
     return t.stride(0)
 
 
-def _with_strides(cfg, **strides):
-    c = type(cfg).from_buffer_copy(cfg)
-    for k, v in strides.items():
-        setattr(c, k, v)
-    return c
-
-
 def _i64(t, name, *shape):
-    import torch
-    return _Arg(t, name, torch.int64, shape)
+    return t, name, _torch.int64, shape, _DENSE
 
 
 def token_logprobs(cfg, logits, tokens, logp, entropy, top_logp, top_ids, workspace) -> None:
     N, V, K = cfg.N, cfg.V, cfg.K
-    c = _with_strides(cfg, ld=_ld(logits, V))
-    _call("token_logprobs", c, _matrix(cfg, logits, "logits", N, V), _i64(tokens, "tokens", N),
+    cfg.ld = _ld(logits, V)
+    _call("token_logprobs", cfg, _matrix(cfg, logits, "logits", N, V), _i64(tokens, "tokens", N),
           _f32(logp, "logp", N), _f32(entropy, "entropy", N), _f32(top_logp, "top_logp", N, K),
           _i64(top_ids, "top_ids", N, K), *_bytes_of(workspace, "workspace"))
 
 
 def distill_topk(cfg, logits, ids, teacher, weight, loss, stats, dlogits, workspace) -> None:
     N, V, K = cfg.N, cfg.V, cfg.K
-    c = _with_strides(cfg, ld=_ld(logits, V), ld_grad=_ld(dlogits, V))
-    _call("distill_topk", c, _matrix(cfg, logits, "logits", N, V), _i64(ids, "ids", N, K),
+    cfg.ld, cfg.ld_grad = _ld(logits, V), _ld(dlogits, V)
+    _call("distill_topk", cfg, _matrix(cfg, logits, "logits", N, V), _i64(ids, "ids", N, K),
           _f32(teacher, "teacher", N, K), _f32(weight, "weight", N), _f32(loss, "loss", N),
           _f32(stats, "stats", N, 2), _matrix(cfg, dlogits, "dlogits", N, V), *_bytes_of(workspace, "workspace"))
 
 
 def distill_topk_backward(cfg, logits, ids, teacher, stats, dloss, dlogits) -> None:
     N, V, K = cfg.N, cfg.V, cfg.K
-    c = _with_strides(cfg, ld=_ld(logits, V), ld_grad=_ld(dlogits, V))
-    _call("distill_topk_backward", c, _matrix(cfg, logits, "logits", N, V), _i64(ids, "ids", N, K),
+    cfg.ld, cfg.ld_grad = _ld(logits, V), _ld(dlogits, V)
+    _call("distill_topk_backward", cfg, _matrix(cfg, logits, "logits", N, V), _i64(ids, "ids", N, K),
           _f32(teacher, "teacher", N, K), _f32(stats, "stats", N, 2), _f32(dloss, "dloss", N),
           _matrix(cfg, dlogits, "dlogits", N, V))
 
 
 # ---- product in 8-bit integers
 def q8_row_bytes(K: int) -> int:
-    return int(_lib().q8_row_bytes(int(K)))
+    return (int(K) + 127) // 128 * 128
 
 
 def q8_workspace_bytes(cfg: Q8Cfg) -> int:
@@ -242,17 +265,15 @@ def q8_workspace_bytes(cfg: Q8Cfg) -> int:
 
 def q8_quantize(cfg, x, q, scale) -> None:
     """Rows x[M,K] -> q[M, q8_row_bytes(K)] int8, scale[M]."""
-    import torch
     M, K = cfg.M, cfg.K
-    c = _with_strides(cfg, ldx=_ld(x, K))
-    _call("q8_quantize", c, _matrix(cfg, x, "x", M, K), _Arg(q, "q", torch.int8, (M, q8_row_bytes(K))),
+    cfg.ldx = _ld(x, K)
+    _call("q8_quantize", cfg, _matrix(cfg, x, "x", M, K), (q, "q", _torch.int8, (M, q8_row_bytes(K)), _DENSE),
           _f32(scale, "scale", M))
 
 
 def q8_linear(cfg, x, w_q, w_scale, bias, y, workspace) -> None:
-    import torch
     M, N, K = cfg.M, cfg.N, cfg.K
-    c = _with_strides(cfg, ldx=_ld(x, K), ldy=_ld(y, N))
-    _call("q8_linear", c, _matrix(cfg, x, "x", M, K), _Arg(w_q, "w_q", torch.int8, (N, q8_row_bytes(K))),
+    cfg.ldx, cfg.ldy = _ld(x, K), _ld(y, N)
+    _call("q8_linear", cfg, _matrix(cfg, x, "x", M, K), (w_q, "w_q", _torch.int8, (N, q8_row_bytes(K)), _DENSE),
           _f32(w_scale, "w_scale", N), _f32(bias, "bias", N), _matrix(cfg, y, "y", M, N),
           *_bytes_of(workspace, "workspace"))

@@ -66,12 +66,13 @@ def test_recurrence_refusals():
         assert forward(cfg) == code
     assert L.glr_workspace_bytes(None, None) == NULL
     assert L.glr_workspace_bytes(ctypes.byref(big), None) == NULL
-    # one tile: no workspace; several: words for each
-    assert size("glr_workspace_bytes", mg.GlrCfg(128, 2, 130)) == (0, 0)
-    rc, n = size("glr_workspace_bytes", big)
-    assert rc == 0 and n >= 8 * 8 * 2 * 130
+    # one tile: no workspace; several: words for each; a state per tile
+    assert size("glr_workspace_bytes", mg.GlrCfg(16, 2, 130)) == (0, 0)
+    assert size("glr_saved_bytes", mg.GlrCfg(16, 2, 130)) == (0, 4 * 2 * 130)
     rc, saved = size("glr_saved_bytes", big)
-    assert rc == 0 and saved == 4 * 8 * 2 * 130
+    assert rc == 0 and saved % (4 * 2 * 130) == 0 and saved > 4 * 2 * 130
+    rc, n = size("glr_workspace_bytes", big)
+    assert rc == 0 and n >= 2 * saved
     assert forward(big, gate=seq(0, 260, 130)) == NULL
     assert forward(big, gate=seq(P + 2, 260, 130)) == ALIGN
     assert forward(big, gate=seq(P, -260, 130)) == SIZE
