@@ -2,7 +2,7 @@
 //
 // A run of steps is the map h -> A h + S with A = prod a, S its result from a zero state, and two runs behind each
 // other compose to (A2 A1, A2 S1 + S2): that is all a sequence needs to be cut up.  A workgroup reads its
-// tile once, into registers; every lane goes through its run of 16 steps from a zero state; the runs of the tile meet in
+// tile once, into registers; every lane goes through its run of 8 or 16 steps from a zero state; the runs of the tile meet in
 // LDS; the tiles of a sequence meet in the workspace, where each leaves its (A, S) as soon as it has read its
 // tile and, once it knows the state before it, the state behind it.  The bytes are those of the arrays, each read or written once.
 //
@@ -23,8 +23,8 @@
 namespace mg {
 
 constexpr int GLR_THREADS = GLR_WAVES * 64;
-constexpr int GLR_RUNS_X_CH = GLR_WAVES * 128;      // runs of a tile x its channels
-constexpr int GLR_WINDOW = 32;                      // tiles looked at at a time
+constexpr int GLR_CHANNELS = 128;                   // channels of a tile at most
+constexpr int GLR_WORDS = 2048;                     // words looked at at a time: 16 tiles of 128 channels, 32 of 64
 constexpr float LOG2E = 1.44269504088896341f;
 constexpr unsigned GLR_NONE = 0xffffffffu, GLR_FREE = 0x80000000u;
 
@@ -152,19 +152,20 @@ __global__ __launch_bounds__(256) void glr_clear_kernel(unsigned long long* word
   if (i == 0) *ticket = 0;
 }
 
-// Where a thread stands.  WIDE: 64 lanes across the channels; a run is a wave then, and all but the lane's own channel is the
-// same in the whole wave (and in scalar registers, addresses and the ends of the sequence too).
-template <bool WIDE>
+// Where a thread stands.  LANES > 0: that many lanes across the channels, and strides that allow 32-bit offsets
+// within a wave: tile, channels and steps are the wave's (in scalar registers), and a lane has an offset in it.  0: as the
+// shape says, any strides.  STEPS: of a run.
+template <int LANES, int STEPS>
 struct GlrPlace {
   int lanes, lane_c, run, chunk, b;    // lanes across the channels, this one's place; run of the tile, tile, batch row
   int ch0, ch;                         // first channel of the tile, of the lane
-  int t0;                              // first step of the run
+  int t0, wave_t0;                     // first step of the run, of the wave
   bool has, second;                    // whether channels ch and ch + 1 exist
   __device__ inline GlrPlace(const GlrArgs& a, int tile, bool backward) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    lanes = WIDE ? 64 : a.s.lanes;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lanes = LANES ? LANES : a.s.lanes;
     lane_c = lane & (lanes - 1);
-    run = WIDE ? __builtin_amdgcn_readfirstlane(wave) : wave * (64 / lanes) + lane / lanes;
+    run = wave * (64 / lanes) + (LANES == 64 ? 0 : lane / lanes);
     tile = __builtin_amdgcn_readfirstlane(tile);
     const int across = a.s.cols * a.c.B;
     const int k = tile / across, rest = tile - k * across;
@@ -172,75 +173,81 @@ struct GlrPlace {
     b = rest / a.s.cols;
     ch0 = (rest - b * a.s.cols) * 2 * lanes;
     ch = ch0 + 2 * lane_c;
-    t0 = chunk * a.s.steps + run * GLR_STEPS;
+    wave_t0 = chunk * a.s.steps + wave * (64 / lanes) * STEPS;
+    t0 = wave_t0 + (LANES == 64 ? 0 : lane / lanes * STEPS);
     has = ch < a.c.H;
     second = ch + 1 < a.c.H;
   }
   __device__ inline int runs() const { return GLR_THREADS / lanes; }
+  // the wave's steps all lie within the sequence
+  __device__ inline bool inside(const GlrArgs& a) const { return wave_t0 + 64 / lanes * STEPS <= a.c.T; }
 };
 
-// Bits of the steps of the thread's run that reset (lanes >= 16 across the channels: each of the first 16
-// lanes of a run looks at one step).
-template <bool WIDE>
-__device__ inline unsigned reset_bits(const GlrArgs& a, const GlrPlace<WIDE>& p) {
+// Bits of the steps of the thread's run that reset (each of the first lanes of a run looks at one step).
+template <int LANES, int STEPS>
+__device__ inline unsigned reset_bits(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p) {
   if (!a.reset) return 0;
   const int t = p.t0 + p.lane_c;
   bool r = false;
-  if (p.lane_c < GLR_STEPS && t < a.c.T) r = a.reset[(long long)t * a.c.B + p.b] != 0;
+  if (p.lane_c < STEPS && t < a.c.T) r = a.reset[(long long)t * a.c.B + p.b] != 0;
   const unsigned long long all = __ballot(r);
-  return (unsigned)(WIDE ? all : all >> ((threadIdx.x & 63) / p.lanes * p.lanes)) & ((1u << GLR_STEPS) - 1);
+  return (unsigned)(LANES == 64 ? all : all >> ((threadIdx.x & 63) / p.lanes * p.lanes)) & ((1u << STEPS) - 1);
 }
 // Whether no step of the wave's runs resets or lies behind the sequence's end: the same answer in all lanes of the wave,
 // whose sweeps then look at neither.
-template <bool WIDE>
-__device__ inline bool glr_whole(const GlrArgs& a, const GlrPlace<WIDE>& p, unsigned resets) {
-  const bool odd = resets != 0 || p.t0 + GLR_STEPS > a.c.T;
-  return WIDE ? !odd : !__any(odd);
+template <int LANES, int STEPS>
+__device__ inline bool glr_whole(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, unsigned resets) {
+  return p.inside(a) && !__any(resets != 0);
 }
 
-// The steps of a thread's run in an array.  WIDE: a base that is the same in the whole wave and 32-bit offsets (the
-// host has looked at the strides).
-template <typename E, bool WIDE>
+// The steps of a thread's run in an array, from step t on.  LANES > 0: the wave's place and a 32-bit offset (the host has
+// looked at the strides).
+template <typename E, int LANES, int STEPS>
 struct RunOf {
   char* base;
-  long long far;                        // WIDE: not used
-  unsigned off, step;                   // bytes; step: WIDE only
-  long long stride;
-  __device__ inline RunOf(const glr_seq& q, const GlrPlace<WIDE>& p, int t0, unsigned lane_c) {
-    E* at = (E*)q.data + p.b * q.stride_b + p.ch0;
-    off = 2 * lane_c * sizeof(E);
+  long long far, stride;                // bytes; far: LANES == 0
+  unsigned off;
+  __device__ inline RunOf(const glr_seq& q, const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, int t, int lane_c) {
+    const int from = LANES ? min(p.wave_t0, a.c.T - 1) : 0;
     stride = q.stride_t * (long long)sizeof(E);
-    step = (unsigned)stride;
-    base = (char*)(at + t0 * q.stride_t);
+    base = (char*)q.data + (p.b * q.stride_b + p.ch0) * (long long)sizeof(E) + from * stride;
+    off = 2 * lane_c * sizeof(E);
     far = 0;
+    if (LANES) off += (unsigned)(t - from) * (unsigned)stride;
+    else far = t * stride;
   }
-  __device__ inline E* at() const { return (E*)(WIDE ? base + off : base + far + off); }
-  __device__ inline void next(bool on = true) {
-    if (WIDE) off += on ? step : 0;
-    else far += on ? stride : 0;
+  __device__ inline E* at() const { return (E*)(LANES ? base + off : base + far + off); }
+  __device__ inline void next() {
+    if (LANES) off += (unsigned)stride;
+    else far += stride;
   }
 };
 
-// The 16 steps of a run of an input array; steps and channels that do not exist are read at one that does.
-template <typename E, bool ALIGNED, bool WIDE>
-__device__ inline void load_run(const glr_seq& q, const GlrArgs& a, const GlrPlace<WIDE>& p,
-                                RawPair<E> (&v)[GLR_STEPS]) {
-  const unsigned lane_c = p.has ? p.lane_c : 0;
-  const bool second = p.ch0 + 2 * (int)lane_c + 1 < a.c.H;
-  RunOf<E, WIDE> run(q, p, min(p.t0, a.c.T - 1), lane_c);
+// The steps of a run of an input array; steps and channels that do not exist are read at one that does.
+template <typename E, bool ALIGNED, int LANES, int STEPS>
+__device__ inline void load_run(const glr_seq& q, const GlrArgs& a, const GlrPlace<LANES, STEPS>& p,
+                                RawPair<E> (&v)[STEPS]) {
+  const int lane_c = p.has ? p.lane_c : 0;
+  const bool second = p.ch0 + 2 * lane_c + 1 < a.c.H;
+  RunOf<E, LANES, STEPS> run(q, a, p, min(p.t0, a.c.T - 1), lane_c);
+  if (p.inside(a)) {
 #pragma unroll
-  for (int r = 0; r < GLR_STEPS; ++r) {
-    v[r] = load_pair<E, ALIGNED>(run.at(), second);
-    run.next(p.t0 + r + 1 < a.c.T);
+    for (int r = 0; r < STEPS; ++r, run.next()) v[r] = load_pair<E, ALIGNED>(run.at(), second);
+  } else {
+#pragma unroll
+    for (int r = 0; r < STEPS; ++r) {
+      v[r] = load_pair<E, ALIGNED>(run.at(), second);
+      if (p.t0 + r + 1 < a.c.T) run.next();
+    }
   }
 }
 
 // Steps behind the sequence's end change nothing: a = 1, b = 0.
-template <int FORM, typename E, bool WIDE>
-__device__ inline void clear_tail(const GlrArgs& a, const GlrPlace<WIDE>& p, RawPair<E> (&g)[GLR_STEPS],
-                                  RawPair<E> (&v)[GLR_STEPS]) {
+template <int FORM, typename E, int LANES, int STEPS>
+__device__ inline void clear_tail(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, RawPair<E> (&g)[STEPS],
+                                  RawPair<E> (&v)[STEPS]) {
 #pragma unroll
-  for (int r = 0; r < GLR_STEPS; ++r)
+  for (int r = 0; r < STEPS; ++r)
     if (p.t0 + r >= a.c.T) {
       g[r].set(FORM == GLR_MIX ? __builtin_inff() : 0.f);
       v[r].set(0.f);
@@ -251,23 +258,23 @@ __device__ inline void clear_tail(const GlrArgs& a, const GlrPlace<WIDE>& p, Raw
 __device__ inline float unless(unsigned resets, int r, float x) { return resets >> r & 1 ? 0.f : x; }
 
 struct GlrShared {
-  float2 run[GLR_RUNS_X_CH];                        // (A, S) of every run and channel
-  unsigned long long window[GLR_WINDOW * 128];
-  float carry[128];                                 // state before the tile
+  float4 run[GLR_THREADS];                          // (A, S) of runs and channels
+  unsigned long long window[GLR_WORDS];
+  float carry[GLR_CHANNELS];                        // state before the tile
   int tile;
 };
 
 // The state before a tile from the n words of the tiles before it that the window holds for a channel (word 0 the
-// nearest): false where a word that is needed is not there yet.  The words are read eight at a time.
+// nearest): false where a word that is needed is not there yet.  The words are read four at a time.
 __device__ inline bool window_state(const unsigned long long* w, int n, int stride, float& h) {
   int at = -1;
   bool stop = false;
-  for (int i0 = 0; i0 < n && !stop; i0 += 8) {
-    unsigned A[8];
+  for (int i0 = 0; i0 < n && !stop; i0 += 4) {
+    unsigned A[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) A[k] = (unsigned)w[min(i0 + k, n - 1) * stride];
+    for (int k = 0; k < 4; ++k) A[k] = (unsigned)w[min(i0 + k, n - 1) * stride];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < 4; ++k) {
       if (stop || i0 + k >= n) continue;
       stop = A[k] == GLR_NONE || A[k] == GLR_FREE;
       if (A[k] == GLR_FREE) at = i0 + k;
@@ -275,12 +282,12 @@ __device__ inline bool window_state(const unsigned long long* w, int n, int stri
   }
   if (at < 0) return false;
   h = __uint_as_float((unsigned)(w[at * stride] >> 32));
-  for (int i0 = (at - 1) & ~7; i0 >= 0; i0 -= 8) {
-    unsigned long long v[8];
+  for (int i0 = (at - 1) & ~3; i0 >= 0; i0 -= 4) {
+    unsigned long long v[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = w[min(i0 + k, at) * stride];
+    for (int k = 0; k < 4; ++k) v[k] = w[min(i0 + k, at) * stride];
 #pragma unroll
-    for (int k = 7; k >= 0; --k)
+    for (int k = 3; k >= 0; --k)
       if (i0 + k < at) h = fmaf(__uint_as_float((unsigned)v[k]), h, __uint_as_float((unsigned)(v[k] >> 32)));
   }
   return true;
@@ -288,10 +295,10 @@ __device__ inline bool window_state(const unsigned long long* w, int n, int stri
 
 // The state before tile `chunk` of the thread's two channels, in sh.carry, from the words of
 // the tiles before it (backward: behind it), whose distance is 1, 2, ...  All threads of the workgroup call it.
-template <bool WIDE>
-__device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace<WIDE>& p, bool backward, GlrShared& sh) {
+template <int LANES, int STEPS>
+__device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, bool backward, GlrShared& sh) {
   const int before = backward ? a.s.chunks - 1 - p.chunk : p.chunk;
-  const int n = min(before, GLR_WINDOW), runs = p.runs(), chans = 2 * p.lanes;
+  const int runs = p.runs(), chans = 2 * p.lanes, n = min(before, GLR_WORDS / chans);
   const long long per_tile = (long long)a.c.B * a.s.cols * chans;
   const long long at = (long long)p.b * a.s.cols * chans + p.ch;
   for (;;) {
@@ -313,33 +320,70 @@ __device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace<WIDE>& p, 
   }
 }
 
+// (A, S) per channel of the runs before the thread's own in its tile, from the own one, through LDS (`all`).  32
+// lanes: the halves of a wave meet by exchange, the waves in LDS.  before_barrier() is called in front of the barrier.
+template <bool BACKWARD, int LANES, int STEPS, typename FN>
+__device__ inline void runs_before(const GlrPlace<LANES, STEPS>& p, Pair A, Pair S, float4* all, Pair& pA, Pair& pS,
+                                   FN before_barrier) {
+  auto behind_it = [&](const float4& x) {             // one more run: (A, S) of either channel
+    pS.x = behind(x.x, x.y, pS.x);
+    pS.y = behind(x.z, x.w, pS.y);
+    pA.x = both(x.x, pA.x);
+    pA.y = both(x.z, pA.y);
+  };
+  pA = {1.f, 1.f};
+  pS = {0.f, 0.f};
+  if constexpr (LANES > 0) {
+    const int wave = p.run / (64 / LANES);
+    // the other half's run, and whether it lies before the own one
+    const bool later = LANES == 64 || ((threadIdx.x & 32) ? !BACKWARD : BACKWARD);
+    float4 other = {1.f, 0.f, 1.f, 0.f};
+    if constexpr (LANES == 32)
+      other = make_float4(__shfl_xor(A.x, 32, 64), __shfl_xor(S.x, 32, 64), __shfl_xor(A.y, 32, 64),
+                          __shfl_xor(S.y, 32, 64));
+    if (later)
+      all[wave * LANES + p.lane_c] = LANES == 64 ? make_float4(A.x, S.x, A.y, S.y)
+                                                 : make_float4(both(A.x, other.x), behind(A.x, S.x, other.y),
+                                                               both(A.y, other.z), behind(A.y, S.y, other.w));
+    before_barrier();
+    __syncthreads();
+    const int n = BACKWARD ? GLR_WAVES - 1 - wave : wave;
+#pragma unroll
+    for (int i = 0; i < GLR_WAVES - 1; i += 2) {     // (two at a time: the sweeps' results hold the registers)
+      if (i >= n) break;
+      const float4 x = all[(BACKWARD ? GLR_WAVES - 1 - i : i) * LANES + p.lane_c];
+      const float4 y = all[(BACKWARD ? GLR_WAVES - 2 - i : i + 1) * LANES + p.lane_c];
+      behind_it(x);
+      if (i + 1 < n) behind_it(y);
+    }
+    if (LANES == 32 && later) behind_it(other);
+  } else {
+    const int runs = p.runs();
+    all[p.run * p.lanes + p.lane_c] = make_float4(A.x, S.x, A.y, S.y);
+    before_barrier();
+    __syncthreads();
+    for (int i = 0; i < (BACKWARD ? runs - 1 - p.run : p.run); ++i)
+      behind_it(all[(BACKWARD ? runs - 1 - i : i) * p.lanes + p.lane_c]);
+  }
+}
+
 // What both directions do between their sweeps: from (A, S) of the thread's run, per channel, the state before
 // the run.  first: the state before the sequence's first tile (backward: behind its last one).  The threads of the
 // tile's last run (backward: its first) get in `out` the state behind the tile.
-template <bool BACKWARD, bool WIDE>
-__device__ inline Pair glr_join(const GlrArgs& a, const GlrPlace<WIDE>& p, Pair A, Pair S, Pair first, Pair& out,
+template <bool BACKWARD, int LANES, int STEPS>
+__device__ inline Pair glr_join(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, Pair A, Pair S, Pair first, Pair& out,
                                 GlrShared& sh) {
   const int chans = 2 * p.lanes, runs = p.runs(), c = 2 * p.lane_c;
-  sh.run[p.run * chans + c] = make_float2(A.x, S.x);
-  sh.run[p.run * chans + c + 1] = make_float2(A.y, S.y);
   const bool at_start = BACKWARD ? p.chunk == a.s.chunks - 1 : p.chunk == 0;
   const bool chain = a.s.chunks > 1;
   const int place = BACKWARD ? runs - 1 - p.run : p.run;      // runs of the tile before this one
-  if (at_start && place == 0) {
-    sh.carry[c] = first.x;
-    sh.carry[c + 1] = first.y;
-  }
-  __syncthreads();
-  // the runs before it, as one
-  Pair pA = {1.f, 1.f}, pS = {0.f, 0.f};
-  for (int i = 0; i < place; ++i) {
-    const int r = BACKWARD ? runs - 1 - i : i;
-    const float2 x = sh.run[r * chans + c], y = sh.run[r * chans + c + 1];
-    pS.x = behind(x.x, x.y, pS.x);
-    pS.y = behind(y.x, y.y, pS.y);
-    pA.x = both(x.x, pA.x);
-    pA.y = both(y.x, pA.y);
-  }
+  Pair pA, pS;
+  runs_before<BACKWARD, LANES, STEPS>(p, A, S, sh.run, pA, pS, [&]() {
+    if (at_start && place == 0) {
+      sh.carry[c] = first.x;
+      sh.carry[c + 1] = first.y;
+    }
+  });
   unsigned long long* word =
       a.words + (((long long)p.chunk * a.c.B + p.b) * a.s.cols) * chans + p.ch;
   const bool last = place == runs - 1;
@@ -369,13 +413,14 @@ __device__ inline int glr_tile(const GlrArgs& a, GlrShared& sh) {
   return sh.tile;
 }
 
-template <typename E, bool ALIGNED, int FORM, bool WIDE>
+template <typename E, bool ALIGNED, int FORM, int LANES>
 __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) {
+  constexpr int STEPS = GLR_RUN_FWD;
   __shared__ GlrShared sh;
-  const GlrPlace<WIDE> p(a, glr_tile(a, sh), false);
-  RawPair<E> g[GLR_STEPS], v[GLR_STEPS];
-  load_run<E, ALIGNED, WIDE>(a.gate, a, p, g);
-  load_run<E, ALIGNED, WIDE>(a.value, a, p, v);
+  const GlrPlace<LANES, STEPS> p(a, glr_tile(a, sh), false);
+  RawPair<E> g[STEPS], v[STEPS];
+  load_run<E, ALIGNED, LANES, STEPS>(a.gate, a, p, g);
+  load_run<E, ALIGNED, LANES, STEPS>(a.value, a, p, v);
   const unsigned resets = reset_bits(a, p);
   const int runs = p.runs();
   Pair first = {0.f, 0.f};
@@ -384,14 +429,15 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) 
     if (p.has) first.x = a.h0[at];
     if (p.second) first.y = a.h0[at + 1];
   }
-  const bool whole = glr_whole(a, p, resets);
+  // (floats: one form of the sweep for all, which memory bounds; two would take more registers than there are)
+  const bool whole = sizeof(E) == 2 && glr_whole(a, p, resets);
   // from a zero state: S[r], and A[r] of the steps up to r
-  float A[GLR_STEPS][2], S[GLR_STEPS][2];
+  float A[STEPS][2], S[STEPS][2];
   auto sweep = [&](auto masked) {
     constexpr bool MASKED = decltype(masked)::value;
     float pa[2] = {1.f, 1.f}, ps[2] = {0.f, 0.f};
 #pragma unroll
-    for (int r = 0; r < GLR_STEPS; ++r)
+    for (int r = 0; r < STEPS; ++r) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const Gate<FORM> gt(g[r].at(k));
@@ -401,6 +447,7 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) 
         A[r][k] = MASKED && (resets & ((2u << r) - 1)) ? -0.0f : pa[k];
         S[r][k] = ps[k];
       }
+    }
   };
   if (whole) {
     sweep(std::false_type{});
@@ -408,12 +455,12 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) 
     clear_tail<FORM>(a, p, g, v);
     sweep(std::true_type{});
   }
-  constexpr int L = GLR_STEPS - 1;
+  constexpr int L = STEPS - 1;
   Pair end = {0.f, 0.f};
-  const Pair h = glr_join<false, WIDE>(a, p, {A[L][0], A[L][1]}, {S[L][0], S[L][1]}, first, end, sh);
+  const Pair h = glr_join<false, LANES, STEPS>(a, p, {A[L][0], A[L][1]}, {S[L][0], S[L][1]}, first, end, sh);
   const long long at = (long long)p.b * a.c.H + p.ch;
-  if (p.run == 0 && a.saved) {
-    float* s = a.saved + (long long)p.chunk * a.c.B * a.c.H + at;
+  if (a.saved && p.t0 % a.save == 0 && p.t0 < a.c.T) {
+    float* s = a.saved + (long long)(p.t0 / a.save) * a.c.B * a.c.H + at;
     if (p.has) s[0] = h.x;
     if (p.second) s[1] = h.y;
   }
@@ -422,11 +469,11 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) 
     if (p.second) a.h_last[at + 1] = end.y;
   }
   if (!p.has) return;
-  RunOf<E, WIDE> out(a.h, p, p.t0, p.lane_c);
+  RunOf<E, LANES, STEPS> out(a.h, a, p, min(p.t0, a.c.T - 1), p.lane_c);
   auto write = [&](auto masked) {
     constexpr bool MASKED = decltype(masked)::value;
 #pragma unroll
-    for (int r = 0; r < GLR_STEPS; ++r, out.next()) {
+    for (int r = 0; r < STEPS; ++r, out.next()) {
       const float x = MASKED ? behind(A[r][0], S[r][0], h.x) : fmaf(A[r][0], h.x, S[r][0]);
       const float y = MASKED ? behind(A[r][1], S[r][1], h.y) : fmaf(A[r][1], h.y, S[r][1]);
       if (!MASKED || p.t0 + r < a.c.T) store_pair<E, ALIGNED>(out.at(), x, y, p.second);
@@ -437,16 +484,16 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) 
 }
 
 // mu_t = a_t l_t is what step t hands on to step t - 1: mu -> a (dh + mu), the same composition from the other end.
-template <typename E, bool ALIGNED, int FORM, bool WIDE>
+template <typename E, bool ALIGNED, int FORM, int LANES>
 __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a) {
+  constexpr int STEPS = GLR_RUN_BWD;
   __shared__ GlrShared sh;
-  __shared__ float2 fwd[GLR_RUNS_X_CH];             // (A, S) of every run forward
-  const GlrPlace<WIDE> p(a, glr_tile(a, sh), true);
-  const int chans = 2 * p.lanes, c = 2 * p.lane_c;
-  RawPair<E> g[GLR_STEPS], v[GLR_STEPS], d[GLR_STEPS];
-  load_run<E, ALIGNED, WIDE>(a.gate, a, p, g);
-  load_run<E, ALIGNED, WIDE>(a.value, a, p, v);
-  load_run<E, ALIGNED, WIDE>(a.dh, a, p, d);
+  __shared__ float4 fwd[GLR_THREADS];               // (A, S) of runs and channels, forward
+  const GlrPlace<LANES, STEPS> p(a, glr_tile(a, sh), true);
+  RawPair<E> g[STEPS], v[STEPS], d[STEPS];
+  load_run<E, ALIGNED, LANES, STEPS>(a.gate, a, p, g);
+  load_run<E, ALIGNED, LANES, STEPS>(a.value, a, p, v);
+  load_run<E, ALIGNED, LANES, STEPS>(a.dh, a, p, d);
   const unsigned resets = reset_bits(a, p);
   const long long at = (long long)p.b * a.c.H + p.ch;
   const int runs = p.runs();
@@ -461,10 +508,10 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a)
     if (p.second) h.y = s[1];
   }
   const bool whole = glr_whole(a, p, resets);
-  KeptGate<FORM> gk[GLR_STEPS][2];
+  KeptGate<FORM> gk[STEPS][2];
   auto anew = [&]() {
 #pragma unroll
-    for (int r = 0; r < GLR_STEPS; ++r) {
+    for (int r = 0; r < STEPS; ++r) {
       gk[r][0].anew();
       gk[r][1].anew();
       v[r].anew();
@@ -476,7 +523,7 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a)
     pA[0] = pA[1] = 1.f;
     pS[0] = pS[1] = qS[0] = qS[1] = 0.f;
 #pragma unroll
-    for (int r = 0; r < GLR_STEPS; ++r)
+    for (int r = 0; r < STEPS; ++r)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         gk[r][k].set(g[r].at(k));
@@ -487,7 +534,7 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a)
       }
     anew();
 #pragma unroll
-    for (int r = GLR_STEPS - 1; r >= 0; --r)
+    for (int r = STEPS - 1; r >= 0; --r)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         qS[k] = gk[r][k].a() * (d[r].at(k) + qS[k]);
@@ -500,31 +547,28 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a)
   } else {
     clear_tail<FORM>(a, p, g, v);
 #pragma unroll
-    for (int r = 0; r < GLR_STEPS; ++r)
+    for (int r = 0; r < STEPS; ++r)
       if (p.t0 + r >= a.c.T) d[r].set(0.f);
     sums(std::true_type{});
   }
   anew();
-  fwd[p.run * chans + c] = make_float2(pA[0], pS[0]);
-  fwd[p.run * chans + c + 1] = make_float2(pA[1], pS[1]);
+  Pair fA, fS;
+  runs_before<false, LANES, STEPS>(p, {pA[0], pA[1]}, {pS[0], pS[1]}, fwd, fA, fS, []() {});
+  h.x = behind(fA.x, fS.x, h.x);
+  h.y = behind(fA.y, fS.y, h.y);
   Pair end = {0.f, 0.f};
-  const Pair mu = glr_join<true, WIDE>(a, p, {pA[0], pA[1]}, {qS[0], qS[1]}, first, end, sh);
+  const Pair mu = glr_join<true, LANES, STEPS>(a, p, {pA[0], pA[1]}, {qS[0], qS[1]}, first, end, sh);
   if (p.run == 0 && p.chunk == 0 && a.dh0) {
     if (p.has) a.dh0[at] = end.x;
     if (p.second) a.dh0[at + 1] = end.y;
   }
   if (!p.has) return;
-  for (int i = 0; i < p.run; ++i) {
-    const float2 x = fwd[i * chans + c], y = fwd[i * chans + c + 1];
-    h.x = behind(x.x, x.y, h.x);
-    h.y = behind(y.x, y.y, h.y);
-  }
-  RunOf<E, WIDE> dg(a.dgate, p, p.t0, p.lane_c), dv(a.dvalue, p, p.t0, p.lane_c);
+  RunOf<E, LANES, STEPS> dg(a.dgate, a, p, min(p.t0, a.c.T - 1), p.lane_c), dv(a.dvalue, a, p, min(p.t0, a.c.T - 1), p.lane_c);
   auto write = [&](auto masked) {
     constexpr bool MASKED = decltype(masked)::value;
-    float l[GLR_STEPS][2], m[2] = {mu.x, mu.y};
+    float l[STEPS][2], m[2] = {mu.x, mu.y};
 #pragma unroll
-    for (int r = GLR_STEPS - 1; r >= 0; --r)
+    for (int r = STEPS - 1; r >= 0; --r)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         l[r][k] = d[r].at(k) + m[k];
@@ -533,7 +577,7 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a)
       }
     anew();
 #pragma unroll
-    for (int r = 0; r < GLR_STEPS; ++r) {
+    for (int r = 0; r < STEPS; ++r) {
       float og[2], ov[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -570,34 +614,33 @@ static bool pairs(const glr_seq& q, int H) {
   return H % 2 == 0 && q.stride_t % 2 == 0 && q.stride_b % 2 == 0 && (uintptr_t)q.data % (2 * sizeof(E)) == 0;
 }
 
-template <typename E, int FORM, bool WIDE>
+// Whether the steps of a wave lie within 32-bit offsets.
+static bool near(const glr_seq& q, int size) { return !q.data || q.stride_t * size < (1LL << 27); }
+
+template <typename E, int FORM>
 static void glr_start(const GlrArgs& a, bool backward, unsigned grid, hipStream_t s) {
-  const int H = a.c.H;
+  const int H = a.c.H, e = sizeof(E);
   bool al = pairs<E>(a.gate, H) && pairs<E>(a.value, H);
   al = al && (backward ? pairs<E>(a.dh, H) && pairs<E>(a.dgate, H) && pairs<E>(a.dvalue, H) : pairs<E>(a.h, H));
+  const bool wide = a.s.lanes == (backward ? 32 : 64) && near(a.gate, e) && near(a.value, e) && near(a.h, e) &&
+                    near(a.dh, e) && near(a.dgate, e) && near(a.dvalue, e);
   const dim3 g(grid), t(GLR_THREADS);
   if (backward) {
-    if (al) hipLaunchKernelGGL((glr_backward_kernel<E, true, FORM, WIDE>), g, t, 0, s, a);
-    else hipLaunchKernelGGL((glr_backward_kernel<E, false, FORM, WIDE>), g, t, 0, s, a);
+    if (al && wide) hipLaunchKernelGGL((glr_backward_kernel<E, true, FORM, 32>), g, t, 0, s, a);
+    else if (al) hipLaunchKernelGGL((glr_backward_kernel<E, true, FORM, 0>), g, t, 0, s, a);
+    else if (wide) hipLaunchKernelGGL((glr_backward_kernel<E, false, FORM, 32>), g, t, 0, s, a);
+    else hipLaunchKernelGGL((glr_backward_kernel<E, false, FORM, 0>), g, t, 0, s, a);
   } else {
-    if (al) hipLaunchKernelGGL((glr_forward_kernel<E, true, FORM, WIDE>), g, t, 0, s, a);
-    else hipLaunchKernelGGL((glr_forward_kernel<E, false, FORM, WIDE>), g, t, 0, s, a);
+    if (al && wide) hipLaunchKernelGGL((glr_forward_kernel<E, true, FORM, 64>), g, t, 0, s, a);
+    else if (al) hipLaunchKernelGGL((glr_forward_kernel<E, true, FORM, 0>), g, t, 0, s, a);
+    else if (wide) hipLaunchKernelGGL((glr_forward_kernel<E, false, FORM, 64>), g, t, 0, s, a);
+    else hipLaunchKernelGGL((glr_forward_kernel<E, false, FORM, 0>), g, t, 0, s, a);
   }
 }
-// Whether the 16 steps of a run lie within 32-bit offsets.
-static bool near(const glr_seq& q, int size) { return !q.data || q.stride_t * size < (1LL << 27); }
 template <typename E>
 static void glr_form(const GlrArgs& a, bool backward, unsigned grid, hipStream_t s) {
-  const int e = sizeof(E);
-  const bool wide = a.s.lanes == 64 && near(a.gate, e) && near(a.value, e) && near(a.h, e) && near(a.dh, e) &&
-                    near(a.dgate, e) && near(a.dvalue, e);
-  if (a.c.form == GLR_MIX) {
-    if (wide) glr_start<E, GLR_MIX, true>(a, backward, grid, s);
-    else glr_start<E, GLR_MIX, false>(a, backward, grid, s);
-  } else {
-    if (wide) glr_start<E, GLR_DECAY, true>(a, backward, grid, s);
-    else glr_start<E, GLR_DECAY, false>(a, backward, grid, s);
-  }
+  if (a.c.form == GLR_MIX) glr_start<E, GLR_MIX>(a, backward, grid, s);
+  else glr_start<E, GLR_DECAY>(a, backward, grid, s);
 }
 static hipError_t glr_launch(const GlrArgs& a, bool backward, hipStream_t s) {
   if (a.s.words) {

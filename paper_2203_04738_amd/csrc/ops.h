@@ -7,21 +7,22 @@
 namespace mg {
 
 // ---- gated linear recurrence (kernels_glr.hip)
-// A workgroup of GLR_WAVES waves covers one row of the batch, 2 * lanes channels (two per lane) and
-// GLR_WAVES * (64 / lanes) * GLR_STEPS steps: a wave's lanes hold 64 / lanes runs of GLR_STEPS steps.
-constexpr int GLR_WAVES = 8, GLR_STEPS = 8;
+// A workgroup of GLR_WAVES waves covers one row of the batch, 2 * lanes channels (two per lane) and GLR_WAVES * (64 / lanes) *
+// run steps: a wave's lanes hold 64 / lanes runs.  Forward: runs of 16 steps over up to 128 channels; the adjoint, which
+// keeps three arrays where the forward sweep keeps two: runs of 8 steps over up to 64 channels.
+constexpr int GLR_WAVES = 8, GLR_RUN_FWD = 16, GLR_RUN_BWD = 8;
 struct GlrShape {
-  int lanes;                // lanes across the channels: 16, 32 or 64
+  int lanes;                // lanes across the channels: 16, 32 or (forward) 64
   int steps;                // of a tile
   int chunks;               // tiles along the sequence
   int cols;                 // tiles along the channels
   long long words;          // tiles' words in the workspace (none where a sequence is one tile)
 };
-inline GlrShape glr_shape(const glr_cfg& c) {
+inline GlrShape glr_shape(const glr_cfg& c, bool backward) {
   GlrShape s;
-  s.lanes = c.H > 64 ? 64 : c.H > 32 ? 32 : 16;
-  s.steps = GLR_WAVES * (64 / s.lanes) * GLR_STEPS;
-  s.chunks = (c.T + s.steps - 1) / s.steps;
+  s.lanes = c.H > 64 && !backward ? 64 : c.H > 32 ? 32 : 16;
+  s.steps = GLR_WAVES * (64 / s.lanes) * (backward ? GLR_RUN_BWD : GLR_RUN_FWD);
+  s.chunks = (int)(((long long)c.T + s.steps - 1) / s.steps);
   s.cols = (c.H + 2 * s.lanes - 1) / (2 * s.lanes);
   s.words = s.chunks > 1 ? (long long)s.chunks * c.B * s.cols * 2 * s.lanes : 0;
   return s;
@@ -33,7 +34,8 @@ struct GlrArgs {
   const float* h0;
   const uint8_t* reset;
   float* h_last;
-  float* saved;             // [chunks,B,H]: state before a tile's first step
+  float* saved;             // [.,B,H]: the state before every `save`-th step (the tiles of the adjoint)
+  int save;
   const float* dh_last;
   float* dh0;
   unsigned long long* words;

@@ -19,9 +19,11 @@ static int glr_check(const glr_cfg* c) {
   if ((long long)c->T * c->B > (1LL << 30) || (long long)c->B * c->H > (1LL << 30)) return MGRIT_E_SIZE;
   if (c->form != GLR_MIX && c->form != GLR_DECAY) return MGRIT_E_ENUM;
   if (!is_dtype(c->dtype)) return MGRIT_E_ENUM;
-  const GlrShape s = glr_shape(*c);
-  if ((long long)s.chunks * s.cols * c->B > 0x7fffffffLL) return MGRIT_E_SIZE;   // workgroups of a launch
-  if ((s.words + 255) / 256 > 0x7fffffffLL) return MGRIT_E_SIZE;
+  for (int backward = 0; backward < 2; ++backward) {                             // workgroups of a launch
+    const GlrShape s = glr_shape(*c, backward);
+    if ((long long)s.chunks * s.cols * c->B > 0x7fffffffLL || (s.words + 255) / 256 > 0x7fffffffLL)
+      return MGRIT_E_SIZE;
+  }
   return MGRIT_OK;
 }
 static int seq_check(const glr_cfg& c, const glr_seq* q, bool out) {
@@ -45,14 +47,19 @@ static int seq_check(const glr_cfg& c, const glr_seq* q, bool out) {
   return lo < c.H || hi / n < lo ? MGRIT_E_SIZE : MGRIT_OK;
 }
 static size_t glr_ws(const GlrShape& s) { return s.words ? 256 + 8 * (size_t)s.words : 0; }
-static size_t glr_save(const glr_cfg& c, const GlrShape& s) { return 4 * (size_t)s.chunks * c.B * c.H; }
+static size_t glr_save(const glr_cfg& c) { return 4 * (size_t)glr_shape(c, true).chunks * c.B * c.H; }
+static size_t glr_ws(const glr_cfg& c) {
+  const size_t f = glr_ws(glr_shape(c, false)), b = glr_ws(glr_shape(c, true));
+  return f > b ? f : b;
+}
 static int glr_space(const glr_cfg& c, const GlrShape& s, void* ws, size_t n, GlrArgs* a) {
-  const size_t need = glr_ws(s);
+  const size_t need = glr_ws(c);
   if (n < need) return MGRIT_E_WORKSPACE;
   if (need && !ws) return MGRIT_E_NULL;
   if (need && off16(ws)) return MGRIT_E_ALIGN;
   a->c = c;
   a->s = s;
+  a->save = glr_shape(c, true).steps;
   a->ticket = (int*)ws;
   a->words = need ? (unsigned long long*)((char*)ws + 256) : nullptr;
   return MGRIT_OK;
@@ -111,14 +118,14 @@ int glr_workspace_bytes(const glr_cfg* cfg, size_t* bytes) {
   const int rc = glr_check(cfg);
   if (rc) return rc;
   if (!bytes) return MGRIT_E_NULL;
-  *bytes = glr_ws(glr_shape(*cfg));
+  *bytes = glr_ws(*cfg);
   return MGRIT_OK;
 }
 int glr_saved_bytes(const glr_cfg* cfg, size_t* bytes) {
   const int rc = glr_check(cfg);
   if (rc) return rc;
   if (!bytes) return MGRIT_E_NULL;
-  *bytes = glr_save(*cfg, glr_shape(*cfg));
+  *bytes = glr_save(*cfg);
   return MGRIT_OK;
 }
 
@@ -133,9 +140,9 @@ int glr_forward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, c
   if ((rc = seq_check(*cfg, h, true))) return rc;
   if (off(h0, 4) || off(h_last, 4) || off16(saved)) return MGRIT_E_ALIGN;
   GlrArgs a{};
-  const GlrShape s = glr_shape(*cfg);
+  const GlrShape s = glr_shape(*cfg, false);
   if ((rc = glr_space(*cfg, s, workspace, workspace_bytes, &a))) return rc;
-  if (saved && saved_bytes < glr_save(*cfg, s)) return MGRIT_E_WORKSPACE;
+  if (saved && saved_bytes < glr_save(*cfg)) return MGRIT_E_WORKSPACE;
   a.gate = *gate;
   a.value = *value;
   a.h = *h;
@@ -160,9 +167,9 @@ int glr_backward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, 
   if (!saved) return MGRIT_E_NULL;
   if (off16(saved) || off(dh_last, 4) || off(dh0, 4)) return MGRIT_E_ALIGN;
   GlrArgs a{};
-  const GlrShape s = glr_shape(*cfg);
+  const GlrShape s = glr_shape(*cfg, true);
   if ((rc = glr_space(*cfg, s, workspace, workspace_bytes, &a))) return rc;
-  if (saved_bytes < glr_save(*cfg, s)) return MGRIT_E_WORKSPACE;
+  if (saved_bytes < glr_save(*cfg)) return MGRIT_E_WORKSPACE;
   a.gate = *gate;
   a.value = *value;
   a.dh = *dh;
