@@ -145,16 +145,13 @@ hipError_t launch_q8_quantize(const Q8Args& a, hipStream_t s) {
 // ---------------------------------------------------------------------------
 // products
 // ---------------------------------------------------------------------------
-// Four neighbouring channels n .. n+3 of a token, from their sums; wide: one store (the row's place allows it).
+// Four neighbouring channels n .. n+3 of a token, from their sums and the scales and biases of the channels; wide: in one
+// store (the row's place allows it).
 template <typename E>
-__device__ inline void put4(const Q8Args& a, E* y, int n, const intx4& sum, float sm, bool wide) {
-  float v[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = min(n + i, a.c.N - 1);
-    v[i] = (float)sum[i] * sm * a.w_scale[c];
-    if (a.bias) v[i] += a.bias[c];
-  }
+__device__ inline void put4(const Q8Args& a, E* y, int n, const intx4& sum, float sm, const float4& ws,
+                            const float4& bias, bool wide) {
+  const float v[4] = {(float)sum[0] * sm * ws.x + bias.x, (float)sum[1] * sm * ws.y + bias.y,
+                      (float)sum[2] * sm * ws.z + bias.z, (float)sum[3] * sm * ws.w + bias.w};
   if (wide && n + 3 < a.c.N) {
     if constexpr (sizeof(E) == 4)
       *reinterpret_cast<float4*>(y + n) = make_float4(v[0], v[1], v[2], v[3]);
@@ -165,6 +162,11 @@ __device__ inline void put4(const Q8Args& a, E* y, int n, const intx4& sum, floa
     for (int i = 0; i < 4; ++i)
       if (n + i < a.c.N) y[n + i] = elem_of<E>(v[i]);
   }
+}
+// Scales (or biases: zeros where there are none) of channels n .. n+3
+__device__ inline float4 channels4(const float* p, int n, int N) {
+  if (!p) return make_float4(0.f, 0.f, 0.f, 0.f);
+  return make_float4(p[min(n, N - 1)], p[min(n + 1, N - 1)], p[min(n + 2, N - 1)], p[min(n + 3, N - 1)]);
 }
 template <typename E>
 __device__ inline bool wide_rows(const Q8Args& a) {
@@ -209,13 +211,11 @@ __global__ __launch_bounds__(256) void q8_few_kernel(Q8Args a) {
 #pragma unroll
   for (int b = 0; b < MB; ++b) sums[wave][b][lane] = acc[b];
   __syncthreads();
-  const bool wide = wide_rows<E>(a);
-  for (int b = wave; b < MB; b += 4) {
-    const int m = 16 * b + (lane & 15), n = n0 + 4 * (lane >> 4);
-    if (m >= a.c.M || n >= a.c.N) continue;
-    const intx4 sum = sums[0][b][lane] + sums[1][b][lane] + sums[2][b][lane] + sums[3][b][lane];
-    put4<E>(a, (E*)a.y + (long long)m * a.c.ldy, n, sum, a.scale[m], wide);
-  }
+  const int n = n0 + 4 * (lane >> 4), m = 16 * wave + (lane & 15);
+  if (wave >= MB || m >= a.c.M || n >= a.c.N) return;
+  const float4 ws = channels4(a.w_scale, n, a.c.N), bias = channels4(a.bias, n, a.c.N);
+  const intx4 sum = sums[0][wave][lane] + sums[1][wave][lane] + sums[2][wave][lane] + sums[3][wave][lane];
+  put4<E>(a, (E*)a.y + (long long)m * a.c.ldy, n, sum, a.scale[m], ws, bias, wide_rows<E>(a));
 }
 
 // A tile of TM tokens x TN channels: four waves, each half of either.  Slices of 128 bytes of K go through one of two
@@ -297,23 +297,34 @@ __global__ __launch_bounds__(256) void q8_tile_kernel(Q8Args a, int tiles_m, int
           acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[kk & 1][i], fx[kk & 1][j], acc[i][j], 0, 0, 0);
     }
   }
-  const bool wide = wide_rows<E>(a);
-#pragma unroll
-  for (int j = 0; j < WM; ++j) {
-    const int m = m0 + wm + 32 * j + (lane & 31);
-    if (m >= a.c.M) continue;
-    const float sm = a.scale[m];
-    E* y = (E*)a.y + (long long)m * a.c.ldy;
-#pragma unroll
-    for (int i = 0; i < WN; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int n = n0 + wn + 32 * i + 8 * e + 4 * (lane >> 5);
-        if (n >= a.c.N) continue;
-        const intx4 sum = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
-        put4<E>(a, y, n, sum, sm, wide);
-      }
+  // scales and biases of the tile's channels through LDS
+  __syncthreads();
+  float4 *ws = reinterpret_cast<float4*>(lds[0]), *bias = ws + TN / 4;
+  if (tid < TN / 4) {
+    ws[tid] = channels4(a.w_scale, n0 + 4 * tid, a.c.N);
+    bias[tid] = channels4(a.bias, n0 + 4 * tid, a.c.N);
   }
+  float sm[WM];
+#pragma unroll
+  for (int j = 0; j < WM; ++j) sm[j] = a.scale[min(m0 + wm + 32 * j + (lane & 31), a.c.M - 1)];
+  __syncthreads();
+  const bool wide = wide_rows<E>(a);
+  E* y = (E*)a.y + (long long)m0 * a.c.ldy;
+#pragma unroll
+  for (int i = 0; i < WN; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int c = wn + 32 * i + 8 * e + 4 * (lane >> 5), n = n0 + c;
+      const float4 w4 = ws[c / 4], b4 = bias[c / 4];
+      if (n >= a.c.N) continue;
+#pragma unroll
+      for (int j = 0; j < WM; ++j) {
+        const int r = wm + 32 * j + (lane & 31);
+        if (m0 + r >= a.c.M) continue;
+        const intx4 sum = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+        put4<E>(a, y + (long long)r * a.c.ldy, n, sum, sm[j], w4, b4, wide);
+      }
+    }
 }
 
 template <typename E, int TM, int TN>
