@@ -297,9 +297,14 @@ __global__ __launch_bounds__(256) void q8_tile_kernel(Q8Args a, int tiles_m, int
           acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[kk & 1][i], fx[kk & 1][j], acc[i][j], 0, 0, 0);
     }
   }
-  // scales and biases of the tile's channels through LDS
+  // Scales and biases of the tile's channels through LDS; the results too, 32 tokens of a wave at a time, so that rows are
+  // stored whole (from the lanes' own places a store would write 16 bytes each of 32 rows).
   __syncthreads();
-  float4 *ws = reinterpret_cast<float4*>(lds[0]), *bias = ws + TN / 4;
+  constexpr int CH = TN / 2, ROW = CH * (int)sizeof(E) + 16, PIECES = CH * (int)sizeof(E) / 16;
+  constexpr int PER = 16 / (int)sizeof(E);
+  char* mine = reinterpret_cast<char*>(lds) + wave * 32 * ROW;
+  float4 *ws = reinterpret_cast<float4*>(reinterpret_cast<char*>(lds) + 4 * 32 * ROW), *bias = ws + TN / 4;
+  static_assert(4 * 32 * ROW + TN * 8 <= (int)sizeof(lds), "the tile's results and scales fit its buffers");
   if (tid < TN / 4) {
     ws[tid] = channels4(a.w_scale, n0 + 4 * tid, a.c.N);
     bias[tid] = channels4(a.bias, n0 + 4 * tid, a.c.N);
@@ -308,23 +313,48 @@ __global__ __launch_bounds__(256) void q8_tile_kernel(Q8Args a, int tiles_m, int
 #pragma unroll
   for (int j = 0; j < WM; ++j) sm[j] = a.scale[min(m0 + wm + 32 * j + (lane & 31), a.c.M - 1)];
   __syncthreads();
-  const bool wide = wide_rows<E>(a);
-  E* y = (E*)a.y + (long long)m0 * a.c.ldy;
+  const bool wide = (((uintptr_t)a.y | (uintptr_t)(a.c.ldy * (long long)sizeof(E))) & 15) == 0;
+  auto own_lanes = [&]() {                                   // what the wave's own lanes wrote and read
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+  };
 #pragma unroll
-  for (int i = 0; i < WN; ++i)
+  for (int j = 0; j < WM; ++j) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = wn + 32 * i + 8 * e + 4 * (lane >> 5), n = n0 + c;
-      const float4 w4 = ws[c / 4], b4 = bias[c / 4];
-      if (n >= a.c.N) continue;
+    for (int i = 0; i < WN; ++i)
 #pragma unroll
-      for (int j = 0; j < WM; ++j) {
-        const int r = wm + 32 * j + (lane & 31);
-        if (m0 + r >= a.c.M) continue;
-        const intx4 sum = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
-        put4<E>(a, y + (long long)r * a.c.ldy, n, sum, sm[j], w4, b4, wide);
+      for (int e = 0; e < 4; ++e) {
+        const int c = 32 * i + 8 * e + 4 * (lane >> 5);      // the wave's channel
+        const float4 w4 = ws[(wn + c) / 4], b4 = bias[(wn + c) / 4];
+        const float v0 = (float)acc[i][j][4 * e] * sm[j] * w4.x + b4.x;
+        const float v1 = (float)acc[i][j][4 * e + 1] * sm[j] * w4.y + b4.y;
+        const float v2 = (float)acc[i][j][4 * e + 2] * sm[j] * w4.z + b4.z;
+        const float v3 = (float)acc[i][j][4 * e + 3] * sm[j] * w4.w + b4.w;
+        char* to_row = mine + (lane & 31) * ROW + c * (int)sizeof(E);
+        if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(to_row) = make_float4(v0, v1, v2, v3);
+        else *reinterpret_cast<uint2*>(to_row) = make_uint2(pack2<E>(v0, v1), pack2<E>(v2, v3));
+      }
+    own_lanes();
+#pragma unroll
+    for (int p = 0; p < PIECES / 2; ++p) {                   // 32 rows of PIECES pieces, 64 at a time
+      const int k = p * 64 + lane, r = k / PIECES, q = k % PIECES;
+      const int m = m0 + wm + 32 * j + r, n = n0 + wn + q * PER;
+      const uintx4 v = *reinterpret_cast<const uintx4*>(mine + r * ROW + q * 16);
+      if (m >= a.c.M || n >= a.c.N) continue;
+      E* y = (E*)a.y + (long long)m * a.c.ldy + n;
+      if (wide && n + PER <= a.c.N) {
+        *reinterpret_cast<uintx4*>(y) = v;
+      } else {
+        E el[PER];
+        __builtin_memcpy(el, &v, 16);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (n + i < a.c.N) y[i] = el[i];
       }
     }
+    own_lanes();
+  }
 }
 
 template <typename E, int TM, int TN>
