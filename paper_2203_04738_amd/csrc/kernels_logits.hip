@@ -94,7 +94,12 @@ struct Held {
 #pragma unroll
     for (int j = 0; j < T::loads; ++j) {
       const int i = first + j * T::threads * T::per_load;
-      if (i >= lo && i + T::per_load <= hi) {
+      if (i >= hi) {
+        E e[T::per_load];
+#pragma unroll
+        for (int k = 0; k < T::per_load; ++k) e[k] = low();
+        raw[j] = __builtin_bit_cast(uintx4, e);
+      } else if (i >= lo && i + T::per_load <= hi) {
         raw[j] = *reinterpret_cast<const uintx4*>(row + i);
       } else {
         E e[T::per_load];
@@ -136,17 +141,20 @@ __device__ inline float exponent(const Exponent& x, float v) {
   return ONE ? fmaf(v, x.c, -x.r) : (v - x.m) * x.c;
 }
 
-// (largest: the thread's own largest value)
+// (largest: of each of the thread's loads)
 template <typename E, int NW, bool ENTROPY>
-__device__ inline Stats team_stats(const Held<E, NW>& x, float c, int tid, float (*part)[2], float* largest = nullptr) {
+__device__ inline Stats team_stats(const Held<E, NW>& x, float c, int tid, float (*part)[2],
+                                   float (&largest)[TeamOf<E, NW>::loads]) {
   using T = TeamOf<E, NW>;
   Stats st;
   float m = -__builtin_inff();
 #pragma unroll
-  for (int j = 0; j < T::loads; ++j)
+  for (int j = 0; j < T::loads; ++j) {
+    largest[j] = x.at(j, 0);
 #pragma unroll
-    for (int k = 0; k < T::per_load; ++k) m = fmaxf(m, x.at(j, k));
-  if (largest) *largest = m;
+    for (int k = 1; k < T::per_load; ++k) largest[j] = fmaxf(largest[j], x.at(j, k));
+    m = fmaxf(m, largest[j]);
+  }
   m = wave_max(m);
   if constexpr (NW > 1) {
     if ((tid & 63) == 0) part[tid >> 6][0] = m;
@@ -227,14 +235,17 @@ struct TopShared {
 };
 
 // The K largest of the entries lo .. hi-1 of a row that the team holds, in falling order: put(rank, full key).  largest:
-// the thread's own largest value; ordinary: no NaN and no +inf.  (What few rows need reads the row from the caches, in loops:
+// that of each of the thread's loads; ordinary: no NaN and no +inf.  (What few rows need reads the row from the caches, in loops:
 // it would cost the others registers.)
 template <typename E, int NW, typename PUT>
-__device__ inline void team_top(const Held<E, NW>& x, const E* row, int lo, int hi, int K, int tid, float largest,
-                                bool ordinary, TopShared<NW, TeamOf<E, NW>::cand>& sh, PUT put) {
+__device__ inline void team_top(const Held<E, NW>& x, const E* row, int lo, int hi, int K, int tid,
+                                const float (&largest)[TeamOf<E, NW>::loads], bool ordinary, TopShared<NW, TeamOf<E, NW>::cand>& sh, PUT put) {
   using T = TeamOf<E, NW>;
   // (-inf, all that lies outside the row is, cannot be told from what is in it: no bound then)
-  unsigned most = largest > -__builtin_inff() ? key_of(largest) : 0;
+  float own = largest[0];
+#pragma unroll
+  for (int j = 1; j < T::loads; ++j) own = fmaxf(own, largest[j]);
+  unsigned most = own > -__builtin_inff() ? key_of(own) : 0;
   if (tid == 0) sh.n = 0;
   unsigned threshold;
   if constexpr (NW == 1) {
@@ -267,14 +278,15 @@ __device__ inline void team_top(const Held<E, NW>& x, const E* row, int lo, int 
   const bool bounded = ordinary && threshold != 0;
   if (bounded) {                                             // values compare as their keys do
     const float bound = value_of(threshold);
-    if (largest >= bound)
 #pragma unroll
-      for (int j = 0; j < T::loads; ++j)
+    for (int j = 0; j < T::loads; ++j) {
+      if (!(largest[j] >= bound)) continue;
 #pragma unroll
-        for (int k = 0; k < T::per_load; ++k) {
-          const float v = x.at(j, k);
-          if (v >= bound) take(key_of(v), x.index(j, k));
-        }
+      for (int k = 0; k < T::per_load; ++k) {
+        const float v = x.at(j, k);
+        if (v >= bound) take(key_of(v), x.index(j, k));
+      }
+    }
   } else {                                                   // fewer than K groups above -inf: all that is
     for (int i = lo + tid; i < hi; i += T::threads) {
       const float v = elem_f32(row[i]);
@@ -388,8 +400,8 @@ __global__ __launch_bounds__((TeamOf<E, NW>::block), NW == 16 ? 8 : 4) void logp
   Held<E, NW> held;
   held.load(x, lo, hi, lo - begin, tid);
   const float c = a.inv_t * LOG2E;
-  float largest;
-  const Stats st = team_stats<E, NW, true>(held, c, tid, part, &largest);
+  float largest[T::loads];
+  const Stats st = team_stats<E, NW, true>(held, c, tid, part, largest);
   const bool ordinary = st.s == st.s;                        // (no NaN, no +inf)
   if constexpr (SEGS) {
     if (tid == 0) {
@@ -621,7 +633,8 @@ __global__ __launch_bounds__((TeamOf<E, NW>::block)) void distill_kernel(Distill
   held.load(x, 0, a.V, row_shift(x), tid);
   if (tid < 64) read_teacher(a.ids + row * a.K, a.teacher + row * a.K, a.K, a.V, a.inv_t, x, tid, t);
   team_sync<NW>();
-  const Stats st = team_stats<E, NW, false>(held, a.inv_t * LOG2E, tid, part);
+  float largest[T::loads];
+  const Stats st = team_stats<E, NW, false>(held, a.inv_t * LOG2E, tid, part, largest);
   const bool none = t.total == 0.f;
   if (tid < 64) {
     const float loss = teacher_loss(t, a.K, st.m, st.s, a.inv_t, tid);
@@ -652,7 +665,8 @@ __global__ __launch_bounds__(1024) void distill_segment_kernel(DistillArgs a) {
   const int lo = max(begin, 0), hi = (int)min((long long)a.V, begin + (long long)a.shape.seg * T::per_load);
   Held<E, 16> held;
   held.load(x, lo, hi, lo - begin, threadIdx.x);
-  const Stats st = team_stats<E, 16, false>(held, a.inv_t * LOG2E, threadIdx.x, part);
+  float largest[T::loads];
+  const Stats st = team_stats<E, 16, false>(held, a.inv_t * LOG2E, threadIdx.x, part, largest);
   if (threadIdx.x == 0) {
     a.out.m[blockIdx.x] = st.m;
     a.out.s[blockIdx.x] = st.s;

@@ -26,44 +26,75 @@ __device__ inline float wave_max(float v) {
   return v;
 }
 
-// A row per team of NW waves, held in registers: LOADS pieces of 16 bytes per thread.  A row that is not finite:
-// scale NaN, zeros.
-template <typename E, int NW, int LOADS>
-__global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void q8_quantize_kernel(Q8Args a) {
-  constexpr int PER = 16 / (int)sizeof(E), THREADS = NW * 64;
-  __shared__ float part[NW];
-  const int tid = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
-  const long long row = NW == 1 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x;
-  if (row >= a.c.M) return;                          // (teams of one wave: whole waves)
-  const E* x = (const E*)a.x + row * a.c.ldx;
-  const int K = a.c.K, pad = q8_pad(K);
-  const bool aligned = ((uintptr_t)x & 15) == 0;
+// A row in the registers of a team of THREADS threads: LOADS pieces of 16 bytes per thread, zeros behind its end.
+template <typename E, int THREADS, int LOADS>
+struct QuantRow {
+  static constexpr int PER = 16 / (int)sizeof(E);
   uintx4 raw[LOADS];
+  __device__ inline void load(const E* x, int K, int tid) {
+    if (((uintptr_t)x & 15) == 0 && K % PER == 0) {
 #pragma unroll
-  for (int j = 0; j < LOADS; ++j) {
-    const int i = (j * THREADS + tid) * PER;
-    if (aligned && i + PER <= K) {
-      raw[j] = *reinterpret_cast<const uintx4*>(x + i);
-    } else {
+      for (int j = 0; j < LOADS; ++j) {
+        const int i = (j * THREADS + tid) * PER;
+        raw[j] = uintx4{};
+        if (i < K) raw[j] = *reinterpret_cast<const uintx4*>(x + i);
+      }
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int i = (j * THREADS + tid) * PER;
       E e[PER];
 #pragma unroll
       for (int k = 0; k < PER; ++k) e[k] = i + k < K ? x[i + k] : elem_of<E>(0.f);
       raw[j] = __builtin_bit_cast(uintx4, e);
     }
   }
-  auto at = [&](int j, int k) {
+  __device__ inline float at(int j, int k) const {
     return word_elem<E>(raw[j][k / ELEMS_PER_WORD<E>], k % ELEMS_PER_WORD<E>);
-  };
-  // (the larger of a value and NaN is the value: a NaN is made an infinity first)
-  float m = 0.f;
+  }
+  // largest magnitude of what the wave holds; infinite where a value is not a number (the larger of a value and NaN
+  // would be the value)
+  __device__ inline float top() const {
+    float m = 0.f;
 #pragma unroll
-  for (int j = 0; j < LOADS; ++j)
+    for (int j = 0; j < LOADS; ++j)
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const float v = fabsf(at(j, k));
-      m = fmaxf(m, v == v ? v : __builtin_inff());
+      for (int k = 0; k < PER; ++k) {
+        const float v = fabsf(at(j, k));
+        m = fmaxf(m, v == v ? v : __builtin_inff());
+      }
+    return wave_max(m);
+  }
+  // the quantised row (zeros where it is not finite); out 4-byte aligned
+  __device__ inline void put(int8_t* out, int pad, int tid, bool finite, float scale) const {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int i = (j * THREADS + tid) * PER;
+      if (i >= pad) continue;
+#pragma unroll
+      for (int k = 0; k < PER; k += 4) {
+        unsigned w = 0;
+        if (finite)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) w |= quant(at(j, k + b), scale) << (8 * b);
+        *reinterpret_cast<unsigned*>(out + i + k) = w;
+      }
     }
-  m = wave_max(m);
+  }
+};
+
+// A row per team of NW waves.  A row that is not finite: scale NaN, zeros.
+template <typename E, int NW, int LOADS>
+__global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void q8_quantize_kernel(Q8Args a) {
+  __shared__ float part[NW];
+  const int tid = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const long long row = NW == 1 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x;
+  if (row >= a.c.M) return;                          // (teams of one wave: whole waves)
+  const int pad = q8_pad(a.c.K);
+  QuantRow<E, NW * 64, LOADS> r;
+  r.load((const E*)a.x + row * a.c.ldx, a.c.K, tid);
+  float m = r.top();
   if constexpr (NW > 1) {
     if ((tid & 63) == 0) part[tid >> 6] = m;
     __syncthreads();
@@ -73,20 +104,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void q8_quantize_kernel(Q8
   const bool finite = m < __builtin_inff();
   const float scale = quant_scale(finite ? m : 0.f);
   if (tid == 0) a.scale[row] = finite ? scale : __uint_as_float(0x7fc00000u);
-  int8_t* out = a.q + row * pad;
-#pragma unroll
-  for (int j = 0; j < LOADS; ++j) {
-    const int i = (j * THREADS + tid) * PER;
-    if (i >= pad) continue;
-#pragma unroll
-    for (int k = 0; k < PER; k += 4) {
-      unsigned w = 0;
-      if (finite)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) w |= quant(at(j, k + b), scale) << (8 * b);
-      *reinterpret_cast<unsigned*>(out + i + k) = w;
-    }
-  }
+  r.put(a.q + row * pad, pad, tid, finite, scale);
 }
 
 // Rows longer than that, in two passes; the second reads the row from the caches.
@@ -216,6 +234,56 @@ __global__ __launch_bounds__(256) void q8_few_kernel(Q8Args a) {
   const float4 ws = channels4(a.w_scale, n, a.c.N), bias = channels4(a.bias, n, a.c.N);
   const intx4 sum = sums[0][wave][lane] + sums[1][wave][lane] + sums[2][wave][lane] + sums[3][wave][lane];
   put4<E>(a, (E*)a.y + (long long)m * a.c.ldy, n, sum, a.scale[m], ws, bias, wide_rows<E>(a));
+}
+
+// Up to 16 tokens of rows that a wave holds: one launch.  Every workgroup quantises all of them into LDS, from the L2 that
+// they share, while its first weights are on their way.
+constexpr int FUSED_LDS = 52 << 10, FUSED_WAVES = 8;
+template <typename E>
+__global__ __launch_bounds__(64 * FUSED_WAVES) void q8_fused_kernel(Q8Args a) {
+  constexpr int U = 4;
+  extern __shared__ intx4 dyn[];                       // [M][pad + 16] bytes: rows on different banks
+  __shared__ intx4 sums[FUSED_WAVES][64];
+  __shared__ float scales[16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int pad = q8_pad(a.c.K), slices = pad / 64, n0 = blockIdx.x * 16;
+  const int8_t* w = a.w + (long long)min(n0 + (lane & 15), a.c.N - 1) * pad + (lane >> 4) * 16;
+  char* xq = reinterpret_cast<char*>(dyn);
+  const char* x = xq + min(lane & 15, a.c.M - 1) * (pad + 16) + (lane >> 4) * 16;
+  intx4 fw[U], acc = {};
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) fw[u] = *reinterpret_cast<const intx4*>(w + 64 * min(s0 + u, slices - 1));
+  };
+  load(wave * U);
+  for (int r = wave; r < a.c.M; r += FUSED_WAVES) {
+    QuantRow<E, 64, 8> row;
+    row.load((const E*)a.x + (long long)r * a.c.ldx, a.c.K, lane);
+    const float m = row.top();
+    const bool finite = m < __builtin_inff();
+    const float scale = quant_scale(finite ? m : 0.f);
+    if (lane == 0) scales[r] = finite ? scale : __uint_as_float(0x7fc00000u);
+    row.put(reinterpret_cast<int8_t*>(xq) + r * (pad + 16), pad, lane, finite, scale);
+  }
+  __syncthreads();
+  for (int s0 = wave * U; s0 < slices; s0 += FUSED_WAVES * U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s0 + u >= slices) break;
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+          fw[u], *reinterpret_cast<const intx4*>(x + 64 * (s0 + u)), acc, 0, 0, 0);
+    }
+    if (s0 + FUSED_WAVES * U < slices) load(s0 + FUSED_WAVES * U);
+  }
+  sums[wave][lane] = acc;
+  __syncthreads();
+  const int n = n0 + 4 * (lane >> 4), m = lane & 15;
+  if (wave != 0 || m >= a.c.M || n >= a.c.N) return;
+  const float4 ws = channels4(a.w_scale, n, a.c.N), bias = channels4(a.bias, n, a.c.N);
+  intx4 sum = sums[0][lane];
+#pragma unroll
+  for (int i = 1; i < FUSED_WAVES; ++i) sum += sums[i][lane];
+  put4<E>(a, (E*)a.y + (long long)m * a.c.ldy, n, sum, scales[m], ws, bias, wide_rows<E>(a));
 }
 
 // A tile of TM tokens x TN channels: four waves, each half of either.  Slices of 128 bytes of K go through one of two
@@ -379,7 +447,20 @@ static void q8_start(const Q8Args& a, hipStream_t s) {
   else if (tiles(128) >= 192) tile_start<E, 128, 128>(a, s);
   else tile_start<E, 64, 64>(a, s);
 }
+// Whether the tokens are quantised in the product's own launch: so few that every workgroup can do it.
+static size_t fused_lds(const Q8Args& a) {
+  const int pad = q8_pad(a.c.K), held = 8 * 64 * (a.c.dtype == MGRIT_F32 ? 4 : 8);
+  const size_t need = (size_t)a.c.M * (pad + 16);
+  return a.c.M <= 16 && pad <= held && need <= FUSED_LDS ? need : 0;
+}
 hipError_t launch_q8_linear(const Q8Args& a, hipStream_t s) {
+  if (const size_t lds = fused_lds(a)) {
+    const dim3 g((unsigned)(a.c.N + 15) / 16), t(64 * FUSED_WAVES);
+    if (a.c.dtype == MGRIT_F32) hipLaunchKernelGGL(q8_fused_kernel<float>, g, t, lds, s, a);
+    else if (a.c.dtype == MGRIT_BF16) hipLaunchKernelGGL(q8_fused_kernel<Bf16>, g, t, lds, s, a);
+    else hipLaunchKernelGGL(q8_fused_kernel<F16>, g, t, lds, s, a);
+    return hipGetLastError();
+  }
   const hipError_t e = launch_q8_quantize(a, s);
   if (e != hipSuccess) return e;
   if (a.c.dtype == MGRIT_F32) q8_start<float>(a, s);

@@ -85,7 +85,7 @@ def _lib() -> ctypes.CDLL:
 
 def _stream() -> int:
     """The current stream of the current device, as torch.cuda.current_stream().cuda_stream says."""
-    return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device())
+    return _torch._C._cuda_getCurrentRawStream(_torch._C._cuda_getDevice())
 
 
 def _size(name, cfg) -> int:
@@ -95,8 +95,9 @@ def _size(name, cfg) -> int:
 
 
 # An argument is a plain value or (tensor, name, dtype, shape, kind): shape None: any; kind _DENSE:
-# contiguous; _ROWS: the last stride is 1; _SEQ: the same, passed as a pointer to a ``GlrSeq``.
-_DENSE, _ROWS, _SEQ = 0, 1, 2
+# contiguous; _ROWS: the last stride is 1; _SEQ: the same, [T,B,H], passed as a pointer to a ``GlrSeq``;
+# _STEP: the same, [B,H].
+_DENSE, _ROWS, _SEQ, _STEP = 0, 1, 2, 3
 
 
 def _unit_rows(t):
@@ -123,15 +124,10 @@ def _explain(args):
             raise TypeError(f"{name}: expected a CUDA tensor")
 
 
-def _fits(t, dtype, shape, kind):
-    return (isinstance(t, _torch.Tensor) and (shape is None or t.shape == shape) and (dtype is None or t.dtype is dtype)
-            and t.is_cuda and (t.is_contiguous() if kind == _DENSE else _unit_rows(t)))
-
-
 def _call(name, cfg, *args) -> None:
     """Checks and marshals the arguments, then calls entry point `name` on the current stream.  (A call of a few
     microseconds' work is as long as this: one pass over the arguments, the reasons only where one does not fit.)"""
-    L, out = _lib(), []
+    L, tensor, out = _lib(), _torch.Tensor, []
     for a in args:
         if type(a) is not tuple:
             out.append(a)
@@ -139,14 +135,19 @@ def _call(name, cfg, *args) -> None:
         t, _, dtype, shape, kind = a
         if t is None:
             out.append(None)
-        elif not _fits(t, dtype, shape, kind):
+            continue
+        if not (isinstance(t, tensor) and (shape is None or t.shape == shape) and (dtype is None or t.dtype is dtype)
+                and t.is_cuda and (t.is_contiguous() if kind == 0 else _unit_rows(t))):
             _explain(args)
             raise AssertionError(a[1])                # (not reached: _explain says what is wrong)
-        elif kind == _SEQ:
-            out.append(ctypes.byref(GlrSeq(t.data_ptr(), t.stride(0), t.stride(1))))
-        else:
+        if kind < 2:
             out.append(t.data_ptr())
-    _check(getattr(L, name)(ctypes.byref(cfg), *out, _stream()), name)
+        else:
+            strides = t.stride()
+            out.append(ctypes.byref(GlrSeq(t.data_ptr(), strides[0] if kind == 2 else 0, strides[-2])))
+    rc = getattr(L, name)(ctypes.byref(cfg), *out, _stream())
+    if rc:
+        _check(rc, name)
 
 
 def _bytes_of(t, name):
@@ -197,16 +198,11 @@ def glr_backward(cfg, gate, value, reset, saved, dh, dh_last, dgate, dvalue, dh0
 
 def glr_step(cfg, gate, value, slots, reset, state_in, state_out, h) -> None:
     """gate, value, h: [B,H]; state_in, state_out: [n_slots,H]."""
-    _lib()
-    B, H = cfg.B, cfg.H
-    for t, name in ((gate, "gate"), (value, "value"), (h, "h"), (state_in, "state_in"), (state_out, "state_out")):
-        if isinstance(t, _torch.Tensor) and t.dim() != 2:
-            raise ValueError(f"{name}: expected two dimensions, got shape {tuple(t.shape)}")
-    one = lambda t: t[None] if isinstance(t, _torch.Tensor) else t  # noqa: E731
-    n = state_in.shape[0] if isinstance(state_in, _torch.Tensor) else 0
-    _call("glr_step", cfg, _seq(cfg, one(gate), "gate"), _seq(cfg, one(value), "value"),
+    B, H, dtype = cfg.B, cfg.H, _dtype(cfg)
+    n = state_in.shape[0] if isinstance(state_in, _torch.Tensor) and state_in.dim() == 2 else 0
+    _call("glr_step", cfg, (gate, "gate", dtype, (B, H), _STEP), (value, "value", dtype, (B, H), _STEP),
           (slots, "slots", _torch.int32, (B,), _DENSE), n, _reset(reset, B), _f32(state_in, "state_in", n, H),
-          _f32(state_out, "state_out", n, H), _seq(cfg, one(h), "h"))
+          _f32(state_out, "state_out", n, H), (h, "h", dtype, (B, H), _STEP))
 
 
 # ---- rows of logits
