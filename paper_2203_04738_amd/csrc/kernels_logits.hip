@@ -26,7 +26,7 @@ typedef unsigned long long u64;
 template <typename E, int NW>
 struct TeamOf {
   static constexpr int per_load = 16 / (int)sizeof(E);       // elements
-  static constexpr int loads = NW == 1 ? (sizeof(E) == 4 ? 4 : 2) : (sizeof(E) == 4 ? 8 : 4);
+  static constexpr int loads = NW == 1 ? (sizeof(E) == 4 ? 4 : 2) : sizeof(E) == 4 ? 8 : 4;
   static constexpr int threads = NW * 64;
   static constexpr int block = NW == 1 ? 256 : threads;      // threads of a workgroup
   static constexpr int teams = block / threads;
@@ -68,6 +68,14 @@ __device__ inline u64 wave_max(u64 v) {
   return v;
 }
 
+// The largest of three (of those that are not NaN), in one instruction: fmaxf would first make each of the stored values
+// canonical.
+__device__ inline float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 template <int NW>
 __device__ inline void team_sync() {
   if constexpr (NW > 1) {
@@ -79,6 +87,25 @@ __device__ inline void team_sync() {
   }
 }
 
+// The 16 bytes of a row from element i on, at a 16-byte boundary; what lies outside lo .. hi-1 is -inf.
+template <typename E>
+__device__ inline uintx4 load_piece(const E* row, int i, int lo, int hi) {
+  constexpr int PER = 16 / (int)sizeof(E);
+  if (i >= lo && i + PER <= hi) return *reinterpret_cast<const uintx4*>(row + i);
+  E e[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) e[k] = elem_of<E>(-__builtin_inff());
+  if (i < hi)
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (i + k >= lo && i + k < hi) e[k] = row[i + k];
+  return __builtin_bit_cast(uintx4, e);
+}
+template <typename E>
+__device__ inline float piece_at(const uintx4& raw, int k) {
+  return word_elem<E>(raw[k / ELEMS_PER_WORD<E>], k % ELEMS_PER_WORD<E>);
+}
+
 // The elements lo .. hi-1 of a row that a thread of the team holds: load j holds the 16 bytes (j * threads + thread) of the
 // segment, counted from the 16-byte boundary at or before the row's start.  What lies outside is -inf.
 template <typename E, int NW>
@@ -87,34 +114,17 @@ struct Held {
   uintx4 raw[T::loads];
   int first;                                                 // index of the thread's first element
 
-  static __device__ inline E low() { return elem_of<E>(-__builtin_inff()); }
   // base: the row; hi <= V
   __device__ inline void load(const E* row, int lo, int hi, int shift, int tid) {
     first = lo + tid * T::per_load - shift;
 #pragma unroll
     for (int j = 0; j < T::loads; ++j) {
-      const int i = first + j * T::threads * T::per_load;
-      if (i >= hi) {
-        E e[T::per_load];
-#pragma unroll
-        for (int k = 0; k < T::per_load; ++k) e[k] = low();
-        raw[j] = __builtin_bit_cast(uintx4, e);
-      } else if (i >= lo && i + T::per_load <= hi) {
-        raw[j] = *reinterpret_cast<const uintx4*>(row + i);
-      } else {
-        E e[T::per_load];
-#pragma unroll
-        for (int k = 0; k < T::per_load; ++k) {
-          e[k] = low();
-          if (i + k >= lo && i + k < hi) e[k] = row[i + k];
-        }
-        raw[j] = __builtin_bit_cast(uintx4, e);
-      }
+      raw[j] = load_piece(row, first + j * T::threads * T::per_load, lo, hi);
     }
   }
   __device__ inline int index(int j, int k) const { return first + j * T::threads * T::per_load + k; }
   __device__ inline float at(int j, int k) const {
-    return word_elem<E>(raw[j][k / ELEMS_PER_WORD<E>], k % ELEMS_PER_WORD<E>);
+    return piece_at<E>(raw[j], k);
   }
 };
 
@@ -126,12 +136,13 @@ struct Stats {
 __device__ inline float finite_max(float m) { return m == -__builtin_inff() ? 0.f : m; }
 
 // How an exponent c (x - m) is computed for every x of a row: as one multiply-add fma(x, c, -r) with r = c m rounded,
-// whose rounding d = c m - r is the same for the whole row, or, where r is not finite (rows whose largest
-// value is the type's lowest), as it is written.
+// whose rounding d = c m - r is the same for the whole row, or, where d could pass 1/2 (|r| from 2^24 on: rows whose
+// largest value is the type's lowest, for one), as it is written.
+constexpr float ONE_FMA = 0x1p24f;
 struct Exponent {
   float c, m, r;
   bool one;
-  __device__ inline Exponent(float c_, float max) : c(c_), m(finite_max(max)), r(m * c_), one(fabsf(r) < __builtin_inff()) {}
+  __device__ inline Exponent(float c_, float max) : c(c_), m(finite_max(max)), r(m * c_), one(fabsf(r) < ONE_FMA) {}
   // 2^-d, what a sum of 2^fma(x, c, -r) is to be multiplied by
   __device__ inline float scale() const { return one ? __builtin_amdgcn_exp2f(-rest()) : 1.f; }
   __device__ inline float rest() const { return one ? fmaf(m, c, -r) : 0.f; }
@@ -150,9 +161,9 @@ __device__ inline Stats team_stats(const Held<E, NW>& x, float c, int tid, float
   float m = -__builtin_inff();
 #pragma unroll
   for (int j = 0; j < T::loads; ++j) {
-    largest[j] = x.at(j, 0);
+    largest[j] = -__builtin_inff();
 #pragma unroll
-    for (int k = 1; k < T::per_load; ++k) largest[j] = fmaxf(largest[j], x.at(j, k));
+    for (int k = 0; k < T::per_load; k += 2) largest[j] = max3(largest[j], x.at(j, k), x.at(j, k + 1));
     m = fmaxf(m, largest[j]);
   }
   m = wave_max(m);
@@ -202,10 +213,15 @@ __device__ inline Stats team_stats(const Held<E, NW>& x, float c, int tid, float
   return st;
 }
 
+// w (x - m): the difference of two floats may be beyond them where w times it is not
+__device__ inline float below(float x, float m, float w) {
+  const float d = (x - m) * w;
+  return fabsf(d) == __builtin_inff() ? x * w - m * w : d;
+}
 // log p of a logit, from the statistics of its row
 __device__ inline float log_prob(float x, const Stats& r, float inv_t) {
   if (r.s == 0.f) return -__builtin_inff();
-  return (x - r.m) * inv_t - logf(r.s);
+  return below(x, r.m, inv_t) - logf(r.s);
 }
 __device__ inline float entropy_of(const Stats& r) { return r.s == 0.f ? 0.f : logf(r.s) - r.u * LN2 / r.s; }
 
@@ -234,17 +250,14 @@ struct TopShared {
   int n;
 };
 
-// The K largest of the entries lo .. hi-1 of a row that the team holds, in falling order: put(rank, full key).  largest:
-// that of each of the thread's loads; ordinary: no NaN and no +inf.  (What few rows need reads the row from the caches, in loops:
-// it would cost the others registers.)
-template <typename E, int NW, typename PUT>
-__device__ inline void team_top(const Held<E, NW>& x, const E* row, int lo, int hi, int K, int tid,
-                                const float (&largest)[TeamOf<E, NW>::loads], bool ordinary, TopShared<NW, TeamOf<E, NW>::cand>& sh, PUT put) {
-  using T = TeamOf<E, NW>;
+// The K largest of the entries lo .. hi-1 of a row, in falling order: put(rank, full key).  own: the thread's own largest value;
+// ordinary: no NaN and no +inf; scan(bound, take): calls take(key, index) for the thread's values >= bound.  (What few rows
+// need reads the row from the caches, in loops: it would cost the others registers.)
+template <typename E, int NW, int CAND, typename SCAN, typename PUT>
+__device__ inline void team_top(const E* row, int lo, int hi, int K, int tid, float own, bool ordinary,
+                                TopShared<NW, CAND>& sh, SCAN scan, PUT put) {
+  constexpr int THREADS = NW * 64;
   // (-inf, all that lies outside the row is, cannot be told from what is in it: no bound then)
-  float own = largest[0];
-#pragma unroll
-  for (int j = 1; j < T::loads; ++j) own = fmaxf(own, largest[j]);
   unsigned most = own > -__builtin_inff() ? key_of(own) : 0;
   if (tid == 0) sh.n = 0;
   unsigned threshold;
@@ -273,30 +286,20 @@ __device__ inline void team_top(const Held<E, NW>& x, const E* row, int lo, int 
   team_sync<NW>();
   auto take = [&](unsigned key, int i) {
     const int at = atomicAdd(&sh.n, 1);
-    if (at < T::cand) sh.cand[at] = full_key(key, (unsigned)i);
+    if (at < CAND) sh.cand[at] = full_key(key, (unsigned)i);
   };
-  const bool bounded = ordinary && threshold != 0;
-  if (bounded) {                                             // values compare as their keys do
-    const float bound = value_of(threshold);
-#pragma unroll
-    for (int j = 0; j < T::loads; ++j) {
-      if (!(largest[j] >= bound)) continue;
-#pragma unroll
-      for (int k = 0; k < T::per_load; ++k) {
-        const float v = x.at(j, k);
-        if (v >= bound) take(key_of(v), x.index(j, k));
-      }
-    }
+  if (ordinary && threshold != 0) {                          // values compare as their keys do
+    scan(value_of(threshold), take);
   } else {                                                   // fewer than K groups above -inf: all that is
-    for (int i = lo + tid; i < hi; i += T::threads) {
+    for (int i = lo + tid; i < hi; i += THREADS) {
       const float v = elem_f32(row[i]);
       if (ordinary ? v > -__builtin_inff() : key_of(v) >= threshold) take(key_of(v), i);
     }
   }
   team_sync<NW>();
   const int n = sh.n;
-  if (n <= T::cand) {
-    for (int i = tid; i < n; i += T::threads) {
+  if (n <= CAND) {
+    for (int i = tid; i < n; i += THREADS) {
       const u64 mine = sh.cand[i];
       int rank = 0;
       for (int j = 0; j < n; ++j) rank += sh.cand[j] > mine;
@@ -316,7 +319,7 @@ __device__ inline void team_top(const Held<E, NW>& x, const E* row, int lo, int 
     u64 last = ~0ull;
     for (int r = 0; r < K; ++r) {
       u64 best = 0;
-      for (int i = lo + tid; i < hi; i += T::threads) {
+      for (int i = lo + tid; i < hi; i += THREADS) {
         const u64 f = full_key(key_of(elem_f32(row[i])), (unsigned)i);
         if (f < last && f > best) best = f;
       }
@@ -334,6 +337,27 @@ __device__ inline void team_top(const Held<E, NW>& x, const E* row, int lo, int 
       __syncthreads();
     }
   }
+}
+// The same of what a team holds; largest: that of each of the thread's loads.
+template <typename E, int NW, typename PUT>
+__device__ inline void held_top(const Held<E, NW>& x, const E* row, int lo, int hi, int K, int tid,
+                                const float (&largest)[TeamOf<E, NW>::loads], bool ordinary,
+                                TopShared<NW, TeamOf<E, NW>::cand>& sh, PUT put) {
+  using T = TeamOf<E, NW>;
+  float own = largest[0];
+#pragma unroll
+  for (int j = 1; j < T::loads; ++j) own = fmaxf(own, largest[j]);
+  team_top<E, NW>(row, lo, hi, K, tid, own, ordinary, sh, [&](float bound, auto take) {
+#pragma unroll
+    for (int j = 0; j < T::loads; ++j) {
+      if (!(largest[j] >= bound)) continue;
+#pragma unroll
+      for (int k = 0; k < T::per_load; ++k) {
+        const float v = x.at(j, k);
+        if (v >= bound) take(key_of(v), x.index(j, k));
+      }
+    }
+  }, put);
 }
 
 // How the rows of a call are cut.
@@ -413,15 +437,173 @@ __global__ __launch_bounds__((TeamOf<E, NW>::block), NW == 16 ? 8 : 4) void logp
       u64* out = a.out.top + item * a.K;
       for (int i = tid; i < a.K; i += T::threads)
         if (i >= hi - lo) out[i] = 0;                        // (a last segment of fewer than K entries)
-      team_top<E, NW>(held, x, lo, hi, min(a.K, hi - lo), tid, largest, ordinary, top[team],
+      held_top<E, NW>(held, x, lo, hi, min(a.K, hi - lo), tid, largest, ordinary, top[team],
                      [&](int r, u64 f) { out[r] = f; });
     }
   } else {
     if (tid == 0) put_token(a, row, x, st);
     if (a.K > 0)
-      team_top<E, NW>(held, x, lo, hi, a.K, tid, largest, ordinary, top[team], [&](int r, u64 f) {
+      held_top<E, NW>(held, x, lo, hi, a.K, tid, largest, ordinary, top[team], [&](int r, u64 f) {
         a.top_logp[row * a.K + r] = log_prob(value_of((unsigned)(f >> 32)), st, a.inv_t);
         a.top_ids[row * a.K + r] = index_of(f);
+      });
+  }
+}
+
+// Many long rows.  What bounds them is arithmetic: an exponential and four operations on every value, and what each
+// wave does besides, so a thread goes through 128 values in a stream of pieces, four loaded ahead, and
+// keeps of each piece its largest value alone; the few pieces that hold an alternative are read again.  The exponents are
+// taken against a reference r of the thread's own, the largest of the first pieces, 2^(c x - r): it moves (and the
+// sums with it) where a later piece is 2^32 times as large; threads and waves are brought to one reference at the end.
+template <typename E>
+struct StreamOf {
+  static constexpr int per = 16 / (int)sizeof(E), batches = sizeof(E) == 4 ? 8 : 4;
+  static constexpr int chunks = batches * 4 * 256;           // 16-byte pieces of a workgroup: 2^15 values
+};
+template <typename E, bool SEGS>
+__global__ __launch_bounds__(256) void logprobs_stream_kernel(RowArgs a) {
+  using T = StreamOf<E>;
+  constexpr float NONE = -__builtin_inff();
+  __shared__ float part[4][4];
+  __shared__ TopShared<4, 1024> top;
+  const int tid = threadIdx.x;
+  const long long item = blockIdx.x, row = SEGS ? item / a.shape.segs : item;
+  const int seg = SEGS ? (int)(item - row * a.shape.segs) : 0;
+  const E* x = (const E*)a.logits + row * a.ld;
+  const int begin = (SEGS ? seg * a.shape.seg * T::per : 0) - row_shift(x);
+  const int lo = max(begin, 0);
+  const int hi = SEGS ? (int)min((long long)a.V, begin + (long long)a.shape.seg * T::per) : a.V;
+  const int first = begin + tid * T::per;
+  const float c = a.inv_t * LOG2E;
+  float largest[T::batches][4], r = NONE, s = 0.f, u = 0.f, own = NONE;
+  uintx4 ahead[4];
+  auto load = [&](int b) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) ahead[q] = load_piece(x, first + (4 * b + q) * 256 * T::per, lo, hi);
+  };
+  load(0);
+#pragma unroll
+  for (int b = 0; b < T::batches; ++b) {
+    uintx4 raw[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      raw[q] = ahead[q];
+      largest[b][q] = NONE;
+    }
+    if (begin + b * 1024 * T::per >= hi) continue;           // (the same in all threads)
+    if (b + 1 < T::batches) load(b + 1);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int k = 0; k < T::per; k += 2)
+        largest[b][q] = max3(largest[b][q], piece_at<E>(raw[q], k), piece_at<E>(raw[q], k + 1));
+    const float m = fmaxf(fmaxf(largest[b][0], largest[b][1]), fmaxf(largest[b][2], largest[b][3]));
+    own = fmaxf(own, m);
+    const float to = m * c;
+    if (to - r > 32.f && to > -ONE_FMA) {                    // (also from no reference to the first)
+      if (r != NONE) {
+        const float d = r - to, f = __builtin_amdgcn_exp2f(d);
+        u = fmaf(d, s, u) * f;
+        s *= f;
+      }
+      r = to;
+    }
+    const float ref = r == NONE ? 0.f : r;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int k = 0; k < T::per; ++k) {
+        const float z = fmaf(piece_at<E>(raw[q], k), c, -ref), e = __builtin_amdgcn_exp2f(z);
+        s += e;
+        u = fmaf(e, fmaxf(z, -1e30f), u);                    // (0 times -inf is 0 here)
+      }
+  }
+  // one reference R for all; m: the largest value
+  float m = wave_max(own), R = wave_max(r);
+  if ((tid & 63) == 0) {
+    part[tid >> 6][0] = m;
+    part[tid >> 6][1] = R;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    m = fmaxf(m, part[w][0]);
+    R = fmaxf(R, part[w][1]);
+  }
+  if (r != NONE) {
+    const float d = r - R, f = __builtin_amdgcn_exp2f(d);
+    u = fmaf(d, s, u) * f;
+    s *= f;
+  }
+  s = wave_sum(s);
+  u = wave_sum(u);
+  if ((tid & 63) == 0) {
+    part[tid >> 6][2] = s;
+    part[tid >> 6][3] = u;
+  }
+  __syncthreads();
+  s = (part[0][2] + part[1][2]) + (part[2][2] + part[3][2]);
+  u = (part[0][3] + part[1][3]) + (part[2][3] + part[3][3]);
+  Stats st = {m, s, u};
+  const float d = fmaf(m, c, -R);                            // from R to c m
+  if (fabsf(m * c) < ONE_FMA) {
+    const float f = __builtin_amdgcn_exp2f(-d);
+    st.u = fmaf(-d, s, u) * f;
+    st.s = s * f;
+  } else if (m != NONE && m < __builtin_inff()) {
+    // so large that c x - r is too coarse: against the value itself (from the caches)
+    s = u = 0.f;
+    for (int i = lo + tid; i < hi; i += 256) {
+      const float z = (elem_f32(x[i]) - m) * c, e = __builtin_amdgcn_exp2f(z);
+      s += e;
+      u = fmaf(e, fmaxf(z, -1e30f), u);
+    }
+    s = wave_sum(s);
+    u = wave_sum(u);
+    __syncthreads();
+    if ((tid & 63) == 0) {
+      part[tid >> 6][2] = s;
+      part[tid >> 6][3] = u;
+    }
+    __syncthreads();
+    st.s = (part[0][2] + part[1][2]) + (part[2][2] + part[3][2]);
+    st.u = (part[0][3] + part[1][3]) + (part[2][3] + part[3][3]);
+  }
+  const bool ordinary = st.s == st.s;                        // (no NaN, no +inf)
+  auto scan = [&](float bound, auto take) {
+#pragma unroll
+    for (int b = 0; b < T::batches; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (!(largest[b][q] >= bound)) continue;
+        const int i = first + (4 * b + q) * 256 * T::per;
+        const uintx4 raw = load_piece(x, i, lo, hi);
+#pragma unroll
+        for (int k = 0; k < T::per; ++k) {
+          const float v = piece_at<E>(raw, k);
+          if (v >= bound) take(key_of(v), i + k);
+        }
+      }
+  };
+  if constexpr (SEGS) {
+    if (tid == 0) {
+      a.out.m[item] = st.m;
+      a.out.s[item] = st.s;
+      a.out.u[item] = st.u;
+    }
+    if (a.K > 0) {
+      u64* out = a.out.top + item * a.K;
+      for (int i = tid; i < a.K; i += 256)
+        if (i >= hi - lo) out[i] = 0;
+      team_top<E, 4>(x, lo, hi, min(a.K, hi - lo), tid, own, ordinary, top, scan,
+                     [&](int rank, u64 f) { out[rank] = f; });
+    }
+  } else {
+    if (tid == 0) put_token(a, row, x, st);
+    if (a.K > 0)
+      team_top<E, 4>(x, lo, hi, a.K, tid, own, ordinary, top, scan, [&](int rank, u64 f) {
+        a.top_logp[row * a.K + rank] = log_prob(value_of((unsigned)(f >> 32)), st, a.inv_t);
+        a.top_ids[row * a.K + rank] = index_of(f);
       });
   }
 }
@@ -441,7 +623,7 @@ __device__ inline Stats join_stats(const SegOut& o, long long row, int segs, flo
   return {m, wave_sum(s), wave_sum(u)};
 }
 
-constexpr int JOIN_SEGS = 33;                                // of a row at most: 2^20 entries and a piece, 2^15 each, or 2^18, 2^13 each
+constexpr int JOIN_SEGS = 33;                                // of a row at most: 2^20 entries and a piece, 2^15 each
 template <typename E>
 __global__ __launch_bounds__(256) void logprobs_join_kernel(RowArgs a) {
   __shared__ u64 cand[JOIN_SEGS * LOGPROBS_MAX_K];
@@ -541,7 +723,7 @@ __device__ inline float teacher_loss(const Teacher& t, int K, float m, float s, 
   if (t.total == 0.f) return 0.f;
   float dot = 0.f;
   for (int k = lane; k < K; k += 64)
-    if (t.q[k] != 0.f) dot = fmaf(t.q[k], (t.x[k] - finite_max(m)) * inv_t, dot);
+    if (t.q[k] != 0.f) dot += below(t.x[k], finite_max(m), t.q[k] * inv_t);
   dot = wave_sum(dot);
   if (s == 0.f) return __builtin_inff() * t.total;
   return (t.qlogq - dot + logf(s)) * t.total;
@@ -717,7 +899,6 @@ __global__ __launch_bounds__((TeamOf<E, NW>::block)) void distill_grad_kernel(Di
 }
 
 // ---- launches
-constexpr int CUT_ROWS = 512;
 static int elem_size(int dtype) { return dtype == MGRIT_F32 ? 4 : 2; }
 static bool rows_aligned(const void* p, long long ld, int size) {
   return (uintptr_t)p % 16 == 0 && ld * size % 16 == 0;
@@ -731,32 +912,27 @@ static int team_waves(int V, int size, bool aligned) {
   if (need <= (size == 4 ? TeamOf<float, 16>::elems : TeamOf<Bf16, 16>::elems)) return 16;
   return 0;
 }
-// Segments of a row, all as long, for teams of `waves` (4 or 16) waves.
-static RowShape segments(int V, int size, bool aligned, int waves = 16) {
-  const int per = 16 / size;
-  const int most = (size == 4 ? TeamOf<float, 16>::chunks : TeamOf<Bf16, 16>::chunks) / 16 * waves;
+// Segments of a row, all as long, of at most 2^15 values: what a team of 16 waves holds or a workgroup streams.
+static RowShape segments(int V, int size, bool aligned) {
+  const int per = 16 / size, most = size == 4 ? TeamOf<float, 16>::chunks : TeamOf<Bf16, 16>::chunks;
+  static_assert(TeamOf<float, 16>::chunks == StreamOf<float>::chunks && TeamOf<Bf16, 16>::chunks == StreamOf<Bf16>::chunks,
+                "both forms take segments of the same length");
   const int pieces = (V + (aligned ? 0 : per - 1) + per - 1) / per;
   RowShape s;
   s.segs = (pieces + most - 1) / most;
   s.seg = (pieces + s.segs - 1) / s.segs;
   return s;
 }
-// Waves of the teams that token_logprobs cuts long rows up for (their segments are joined in a second launch), 0 where
-// it leaves rows whole.
-static int logprobs_cut(int N, int V, int size, bool aligned) {
-  const int whole = team_waves(V, size, aligned);
-  if (whole == 1 || whole == 4) return 0;
-  if (whole == 16 && N < CUT_ROWS) return 0;
-  return V <= (1 << 18) ? 4 : 16;
-}
+// Whether token_logprobs streams rows longer than four waves hold (a workgroup of four waves for each 2^15 values) instead of
+// holding them in teams of 16 waves.  K = 20, streamed : held, us: 32768 bf16, 512 rows 15.2 : 12.4, 768 rows 18.4 : 18.4, 2048
+// rows 33.9 : 39.8; 32768 floats, 512 rows 19.3 : 17.9, 2048 rows 48.2 : 50.4; 131072 bf16 (4 segments a row), 64 rows
+// 18.2 : 14.9, 192 rows 24.9 : 23.6, 256 rows 28.1 : 28.4.
+constexpr long long STREAM_SEGMENTS = 768;
 size_t logits_workspace(const logits_cfg& c) {
   const int size = elem_size(c.dtype);
   // (what is aligned is known with the arrays only: the larger of the two)
-  long long segs = team_waves(c.V, size, false) ? 0 : segments(c.V, size, false).segs;
-  const int cut = logprobs_cut(c.N, c.V, size, false);
-  if (cut) segs = segments(c.V, size, false, cut).segs;
-  if (!segs) return 0;
-  const long long n = c.N * segs;
+  if (team_waves(c.V, size, false)) return 0;
+  const long long n = (long long)c.N * segments(c.V, size, false).segs;
   return (size_t)((3 * n * 4 + 15) / 16 * 16 + 8 * n * (c.K > LOGPROBS_MAX_K ? 0 : c.K) + 8LL * c.N);
 }
 
@@ -777,27 +953,30 @@ static hipError_t logprobs_start(const LogitsArgs& a, hipStream_t s) {
   const bool aligned = rows_aligned(a.logits, a.c.ld, sizeof(E));
   r.shape = {1, 0};
   const unsigned N = (unsigned)a.c.N;
-  const int cut = logprobs_cut(a.c.N, a.c.V, sizeof(E), aligned);
-  if (cut) {
-    r.shape = segments(a.c.V, sizeof(E), aligned, cut);
-    r.out = seg_out(a.workspace, a.c.N, r.shape.segs);
-    const dim3 grid(N * (unsigned)r.shape.segs);
-    if (cut == 4) hipLaunchKernelGGL((logprobs_kernel<E, 4, true>), grid, dim3(256), 0, s, r);
-    else hipLaunchKernelGGL((logprobs_kernel<E, 16, true>), grid, dim3(1024), 0, s, r);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((logprobs_join_kernel<E>), dim3(N), dim3(256), 0, s, r);
-    return hipGetLastError();
-  }
-  switch (team_waves(a.c.V, sizeof(E), aligned)) {
+  const int waves = team_waves(a.c.V, sizeof(E), aligned);
+  const RowShape cut = segments(a.c.V, sizeof(E), aligned);
+  const bool stream = (long long)N * cut.segs >= STREAM_SEGMENTS;
+  const dim3 grid(N * (unsigned)cut.segs);
+  switch (waves) {
     case 1:
       hipLaunchKernelGGL((logprobs_kernel<E, 1, false>), dim3((N + 3) / 4), dim3(256), 0, s, r);
       break;
     case 4:
       hipLaunchKernelGGL((logprobs_kernel<E, 4, false>), dim3(N), dim3(256), 0, s, r);
       break;
-    default:
-      hipLaunchKernelGGL((logprobs_kernel<E, 16, false>), dim3(N), dim3(1024), 0, s, r);
+    case 16:
+      if (stream) hipLaunchKernelGGL((logprobs_stream_kernel<E, false>), dim3(N), dim3(256), 0, s, r);
+      else hipLaunchKernelGGL((logprobs_kernel<E, 16, false>), dim3(N), dim3(1024), 0, s, r);
+      break;
+    default: {
+      r.shape = cut;
+      r.out = seg_out(a.workspace, a.c.N, cut.segs);
+      if (stream) hipLaunchKernelGGL((logprobs_stream_kernel<E, true>), grid, dim3(256), 0, s, r);
+      else hipLaunchKernelGGL((logprobs_kernel<E, 16, true>), grid, dim3(1024), 0, s, r);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL((logprobs_join_kernel<E>), dim3(N), dim3(256), 0, s, r);
+    }
   }
   return hipGetLastError();
 }

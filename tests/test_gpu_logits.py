@@ -53,6 +53,7 @@ def check_logprobs(x, tokens, K, dtype, temperature=1.0, ids_too=True):
     for name, g, r in zip(("logp", "entropy", "top"), got, ref):
         if g is None:
             continue
+        r = np.where(np.abs(r) > np.finfo(np.float32).max, np.sign(r) * INF, r)   # (what a float can say)
         assert np.array_equal(np.isnan(g), np.isnan(r)), name
         assert np.array_equal(np.isneginf(g), np.isneginf(r)), name
         on = np.isfinite(r)
@@ -119,6 +120,51 @@ def test_some_outputs_are_left_out():
     top, ids = torch.empty(4, 5, device=DEV), torch.empty(4, 5, dtype=torch.int64, device=DEV)
     mg.token_logprobs(cfg, x, None, None, None, top, ids, space(cfg))
     assert np.array_equal(top.cpu().numpy(), full[2]) and np.array_equal(ids.cpu().numpy(), full[3])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V,offset,pad", [(800, 9000, 0, 0), (800, 8193, 3, 6), (400, 33001, 1, 2)])
+def test_many_long_rows(N, V, offset, pad, dtype):
+    x, _ = rows(N, N, V, dtype, offset, V + pad)
+    low = torch.finfo(TYPES[dtype][1]).min
+    x[0], x[1], x[2], x[3] = 0.5, -INF, low, -INF
+    x[3, V - 2] = 2.0
+    x[4, : V // 2] = -INF                            # whole pieces, also the first, that a mask leaves out
+    x[5, : V // 2] = low
+    x[6] = x[6].round()
+    x[7, 3000:] += 60                                # the reference moves on the way
+    x[8, :3000] += 60
+    x[9, 5], x[10, 6] = float("nan"), INF
+    tokens = np.arange(N) * 7 % V
+    tokens[20:30] = -1
+    check_logprobs(x, tokens, 20, dtype, temperature=0.7, ids_too=False)
+    keep = [n for n in range(N) if n not in (9, 10)]
+    ids = logprobs(x, tokens, 20, dtype, 0.7)[3]
+    ref = orc.token_logprobs(values(x), tokens, 20, 0.7)[3]
+    assert np.array_equal(ids[keep], ref[keep])
+    assert ids[9, 0] == 5 and ids[10, 0] == 6
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [3, 800])
+@pytest.mark.parametrize("temperature", [1.0, 4.0])
+def test_values_of_the_types_whole_range(N, temperature, dtype):
+    V = 9000
+    x, _ = rows(N, N, V, dtype)
+    info = torch.finfo(TYPES[dtype][1])
+    x[0] = info.min
+    x[1] = torch.where(torch.arange(V, device=DEV) % 3 == 0, info.max, info.min)
+    x[2] = x[2] * 3000
+    x[2, 77] = info.min
+    check_logprobs(x, np.arange(N), 5, dtype, temperature)
+    ids, t = teacher(1, N, V, 4)
+    w = np.ones(N, np.float32)
+    loss, grad = distill(x, ids, t, w, dtype, temperature)
+    ref = orc.distill(values(x), ids, t.astype(np.float64), w.astype(np.float64), temperature)
+    beyond = ref[0] > np.finfo(np.float32).max               # (what a float can say)
+    assert np.all(loss[beyond] == INF)
+    assert np.all((np.abs(loss - ref[0]) <= 2 * TOL * np.maximum(1.0, np.abs(ref[0]) / 20))[~beyond])
+    assert np.all(np.abs(grad - ref[1]) <= UNIT[dtype] * np.abs(ref[1]) + 2 * TOL / temperature)
 
 
 # ---------------------------------------------------------------------------
