@@ -146,9 +146,10 @@ __device__ inline unsigned long long load_word(const unsigned long long* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// (an even number of words)
 __global__ __launch_bounds__(256) void glr_clear_kernel(unsigned long long* words, long long n, int* ticket) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i < n) words[i] = ~0ull;
+  const long long i = 2 * ((long long)blockIdx.x * 256 + threadIdx.x);
+  if (i < n) *reinterpret_cast<ulonglong2*>(words + i) = make_ulonglong2(~0ull, ~0ull);
   if (i == 0) *ticket = 0;
 }
 
@@ -645,7 +646,7 @@ static void glr_form(const GlrArgs& a, bool backward, unsigned grid, hipStream_t
 static hipError_t glr_launch(const GlrArgs& a, bool backward, hipStream_t s) {
   if (a.s.words) {
     const long long n = a.s.words;
-    hipLaunchKernelGGL(glr_clear_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a.words, n,
+    hipLaunchKernelGGL(glr_clear_kernel, dim3((unsigned)((n + 511) / 512)), dim3(256), 0, s, a.words, n,
                        a.ticket);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

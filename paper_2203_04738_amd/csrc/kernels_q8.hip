@@ -4,6 +4,9 @@
 // per column of tiles); rows are padded with zeros to 128 bytes, so that the products look at no tail of K.  In the products the
 // channels are the rows of the matrix instruction and the tokens its columns: a lane ends up with four neighbouring
 // channels of one token.
+#include <algorithm>
+#include <cmath>
+
 #include "elem.h"
 #include "ops.h"
 
@@ -430,11 +433,18 @@ static void tile_start(const Q8Args& a, hipStream_t s) {
   const int tm = (a.c.M + TM - 1) / TM, tn = (a.c.N + TN - 1) / TN;
   hipLaunchKernelGGL((q8_tile_kernel<E, TM, TN>), dim3((unsigned)tm * (unsigned)tn), dim3(256), 0, s, a, tm, tn);
 }
+// Which product.  Measured with quantisation, K = 2048, bf16, us on the GPU:
+//  - few tokens : tiles of 64 x 64.  17 x 2048 7.7 : 11.8, 64 x 2048 10.2 : 12.0, 64 x 8192 15.2 : 12.3 (every workgroup of
+//    the former reads all tokens from the L2, and there are N / 16 of them), 48 x 8192 (K = 4096) 21.5 : 19.4;
+//  - tiles of 64 : 128 : 256.  1024 x 2048 17 : 21 : 44, 2048 x 2048 26 : 25 : 48, 4096 x 2048 47 : 37 : 53, 6144 x 2048
+//    69 : 52 : 57, 8192 x 2048 85 : 68 : 63, 1024 x 8192 49 : 33 : 48.  That is 20 us per 1024 tiles of 64 (four
+//    of them share a CU), 27 per 512 of 128 (two) and 50 per round of 256 of 256 (one), 7 and 19 at least.
 template <typename E>
 static void q8_start(const Q8Args& a, hipStream_t s) {
   const unsigned groups = (unsigned)(a.c.N + 15) / 16;
-  if (a.c.M <= 64) {
-    switch ((a.c.M + 15) / 16) {
+  const int blocks = (int)(((long long)a.c.M + 15) / 16);
+  if (blocks == 1 || (blocks <= 4 && (long long)blocks * a.c.N <= 16384)) {
+    switch (blocks) {
       case 1: hipLaunchKernelGGL((q8_few_kernel<E, 1>), dim3(groups), dim3(256), 0, s, a); break;
       case 2: hipLaunchKernelGGL((q8_few_kernel<E, 2>), dim3(groups), dim3(256), 0, s, a); break;
       case 3: hipLaunchKernelGGL((q8_few_kernel<E, 3>), dim3(groups), dim3(256), 0, s, a); break;
@@ -442,16 +452,22 @@ static void q8_start(const Q8Args& a, hipStream_t s) {
     }
     return;
   }
-  auto tiles = [&](int t) { return (long long)((a.c.M + t - 1) / t) * ((a.c.N + t - 1) / t); };
-  if (tiles(256) >= 192) tile_start<E, 256, 256>(a, s);
-  else if (tiles(128) >= 192) tile_start<E, 128, 128>(a, s);
+  auto tiles = [&](long long t) { return (double)((a.c.M + t - 1) / t) * (double)((a.c.N + t - 1) / t); };
+  const double c64 = std::max(7.0, tiles(64) / 1024 * 20), c128 = std::max(19.0, tiles(128) / 512 * 27);
+  const double c256 = std::ceil(tiles(256) / 256) * 50;
+  if (c256 <= c128 && c256 <= c64) tile_start<E, 256, 256>(a, s);
+  else if (c128 <= c64) tile_start<E, 128, 128>(a, s);
   else tile_start<E, 64, 64>(a, s);
 }
-// Whether the tokens are quantised in the product's own launch: so few that every workgroup can do it.
+// LDS of the product that quantises the tokens itself, 0 where that has a launch of its own.  One launch : two, K = 2048, us
+// on the GPU: 1 x 2048 6.3 : 6.3, 8 x 2048 7.4 : 6.9, 16 x 2048 10.9 : 7.2, 1 x 8192 (K = 4096) 10.5 : 10.9, 8 x 8192 (K =
+// 4096) 17.1 : 12.4; the second launch takes 2.5 us of the host.  So: as long as the workgroups together
+// quantise at most 1024 rows.
 static size_t fused_lds(const Q8Args& a) {
   const int pad = q8_pad(a.c.K), held = 8 * 64 * (a.c.dtype == MGRIT_F32 ? 4 : 8);
   const size_t need = (size_t)a.c.M * (pad + 16);
-  return a.c.M <= 16 && pad <= held && need <= FUSED_LDS ? need : 0;
+  const long long rows = (long long)a.c.M * ((a.c.N + 15) / 16);
+  return a.c.M <= 16 && rows <= 1024 && pad <= held && need <= FUSED_LDS ? need : 0;
 }
 hipError_t launch_q8_linear(const Q8Args& a, hipStream_t s) {
   if (const size_t lds = fused_lds(a)) {

@@ -55,31 +55,36 @@ class Q8Cfg(ctypes.Structure):
         super().__init__(M, N, K, dtype, K, N)
 
 
+def _prototypes(L):
+    """Argument types of the entry points in the library L."""
+    vp, sz, i32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
+    szp = ctypes.POINTER(sz)
+    for name, cfg, args in (
+            ("glr_workspace_bytes", GlrCfg, [szp]), ("glr_saved_bytes", GlrCfg, [szp]),
+            ("glr_forward", GlrCfg, [vp] * 7 + [sz, vp, sz, vp]),
+            ("glr_backward", GlrCfg, [vp] * 4 + [sz] + [vp] * 6 + [sz, vp]),
+            ("glr_step", GlrCfg, [vp] * 3 + [i32] + [vp] * 5),
+            ("logits_workspace_bytes", LogitsCfg, [szp]),
+            ("token_logprobs", LogitsCfg, [vp] * 7 + [sz, vp]),
+            ("distill_topk", LogitsCfg, [vp] * 8 + [sz, vp]),
+            ("distill_topk_backward", LogitsCfg, [vp] * 7),
+            ("q8_workspace_bytes", Q8Cfg, [szp]), ("q8_quantize", Q8Cfg, [vp] * 4),
+            ("q8_linear", Q8Cfg, [vp] * 6 + [sz, vp])):
+        fn = getattr(L, name)
+        fn.argtypes = [ctypes.POINTER(cfg)] + args
+        fn.restype = ctypes.c_int
+    L.q8_row_bytes.argtypes = [i32]
+    L.q8_row_bytes.restype = ctypes.c_int64
+    return L
+
+
 def _lib() -> ctypes.CDLL:
     global _ready, _torch, _TYPES
     if _ready is None:
         import torch
         _torch = torch
         _TYPES = {MGRIT_F32: torch.float32, MGRIT_BF16: torch.bfloat16, MGRIT_F16: torch.float16}
-        L, vp, sz, i32 = _base_lib(), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
-        szp = ctypes.POINTER(sz)
-        for name, cfg, args in (
-                ("glr_workspace_bytes", GlrCfg, [szp]), ("glr_saved_bytes", GlrCfg, [szp]),
-                ("glr_forward", GlrCfg, [vp] * 7 + [sz, vp, sz, vp]),
-                ("glr_backward", GlrCfg, [vp] * 4 + [sz] + [vp] * 6 + [sz, vp]),
-                ("glr_step", GlrCfg, [vp] * 3 + [i32] + [vp] * 5),
-                ("logits_workspace_bytes", LogitsCfg, [szp]),
-                ("token_logprobs", LogitsCfg, [vp] * 7 + [sz, vp]),
-                ("distill_topk", LogitsCfg, [vp] * 8 + [sz, vp]),
-                ("distill_topk_backward", LogitsCfg, [vp] * 7),
-                ("q8_workspace_bytes", Q8Cfg, [szp]), ("q8_quantize", Q8Cfg, [vp] * 4),
-                ("q8_linear", Q8Cfg, [vp] * 6 + [sz, vp])):
-            fn = getattr(L, name)
-            fn.argtypes = [ctypes.POINTER(cfg)] + args
-            fn.restype = ctypes.c_int
-        L.q8_row_bytes.argtypes = [i32]
-        L.q8_row_bytes.restype = ctypes.c_int64
-        _ready = L
+        _ready = _prototypes(_base_lib())
     return _ready
 
 
