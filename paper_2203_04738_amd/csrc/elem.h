@@ -56,4 +56,17 @@ __device__ inline unsigned pack2<Bf16>(float a, float b) {
   return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
 }
 
+// Stores a value, past the caches or not.  (The empty statements keep the compiler from making one ordinary store of
+// the two.)
+template <typename V>
+__device__ inline void store_as(V* p, const V& v, bool past) {
+  if (past) {
+    asm volatile("" ::: "memory");
+    __builtin_nontemporal_store(v, p);
+    asm volatile("" ::: "memory");
+  } else {
+    *p = v;
+  }
+}
+
 }  // namespace mg

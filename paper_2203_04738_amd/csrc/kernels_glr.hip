@@ -75,10 +75,15 @@ __device__ inline RawPair<E> load_pair(const E* p, bool second) {
   return r;
 }
 template <typename E, bool ALIGNED>
-__device__ inline void store_pair(E* p, float a, float b, bool second) {
+__device__ inline void store_pair(E* p, float a, float b, bool second, bool past = false) {
   if constexpr (ALIGNED) {
-    if constexpr (sizeof(E) == 4) *reinterpret_cast<float2*>(p) = make_float2(a, b);
-    else *reinterpret_cast<unsigned*>(p) = pack2<E>(a, b);
+    typedef float Word __attribute__((ext_vector_type(2)));
+    if constexpr (sizeof(E) == 4) {
+      const Word w = {a, b};
+      store_as(reinterpret_cast<Word*>(p), w, past);
+    } else {
+      store_as(reinterpret_cast<unsigned*>(p), pack2<E>(a, b), past);
+    }
   } else {
     p[0] = elem_of<E>(a);
     if (second) p[1] = elem_of<E>(b);
@@ -477,7 +482,7 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) 
     for (int r = 0; r < STEPS; ++r, out.next()) {
       const float x = MASKED ? behind(A[r][0], S[r][0], h.x) : fmaf(A[r][0], h.x, S[r][0]);
       const float y = MASKED ? behind(A[r][1], S[r][1], h.y) : fmaf(A[r][1], h.y, S[r][1]);
-      if (!MASKED || p.t0 + r < a.c.T) store_pair<E, ALIGNED>(out.at(), x, y, p.second);
+      if (!MASKED || p.t0 + r < a.c.T) store_pair<E, ALIGNED>(out.at(), x, y, p.second, a.past);
     }
   };
   if (whole) write(std::false_type{});
@@ -598,8 +603,8 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a)
         (k ? h.y : h.x) = MASKED && (resets >> r & 1) ? in : fmaf(ga, past, in);
       }
       if (!MASKED || p.t0 + r < a.c.T) {
-        store_pair<E, ALIGNED>(dg.at(), og[0], og[1], p.second);
-        store_pair<E, ALIGNED>(dv.at(), ov[0], ov[1], p.second);
+        store_pair<E, ALIGNED>(dg.at(), og[0], og[1], p.second, a.past);
+        store_pair<E, ALIGNED>(dv.at(), ov[0], ov[1], p.second, a.past);
       }
       dg.next();
       dv.next();

@@ -748,6 +748,7 @@ struct DistillArgs {
   float inv_t;
   RowShape shape;
   SegOut out;
+  bool past;                 // gradients past the caches
 };
 
 // w (p - q) of what a team holds of a row, stored; scale = w total / s, then the entries of the teacher.
@@ -773,7 +774,7 @@ __device__ inline void put_gradient(const DistillArgs& a, const Held<E, NW>& x, 
         else r[k / 2] = pack2<E>(g[0], g[1]);
       }
       if (wide && i >= lo && i + T::per_load <= hi) {
-        *reinterpret_cast<uintx4*>(out + i) = r;
+        store_as(reinterpret_cast<uintx4*>(out + i), r, a.past);
       } else {
         E e[T::per_load];
         __builtin_memcpy(e, &r, 16);
@@ -1002,6 +1003,7 @@ static DistillArgs distill_args(const LogitsArgs& a) {
   d.ld = a.c.ld;
   d.ld_grad = a.c.ld_grad;
   d.inv_t = 1.0f / a.c.temperature;
+  d.past = stores_past_caches(2.0 * elem_size(a.c.dtype) * a.c.N * a.c.V);
   return d;
 }
 template <typename E>

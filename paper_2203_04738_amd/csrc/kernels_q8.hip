@@ -415,7 +415,7 @@ __global__ __launch_bounds__(256) void q8_tile_kernel(Q8Args a, int tiles_m, int
       if (m >= a.c.M || n >= a.c.N) continue;
       E* y = (E*)a.y + (long long)m * a.c.ldy + n;
       if (wide && n + PER <= a.c.N) {
-        *reinterpret_cast<uintx4*>(y) = v;
+        store_as(reinterpret_cast<uintx4*>(y), v, a.past);
       } else {
         E el[PER];
         __builtin_memcpy(el, &v, 16);

@@ -6,6 +6,12 @@
 
 namespace mg {
 
+// Whether a call moves so much that what it writes would not stay in the last-level cache (256 MB) for the next kernel
+// anyway: it is then stored past the caches, which leaves them to what the call reads.  Plain : past them, us:
+// recurrence 128 x 100 x 1000 floats 93 : 88 (forward 154 MB, backward 256 MB), 16384 x 4 x 1024 bf16 282 : 272; gradient of 1003 x
+// 50021 floats behind the forward pass 130 : 103; 8-bit product of 32768 x 2048 x 2048 224 : 216.
+inline bool stores_past_caches(double bytes) { return bytes >= 128e6; }
+
 // ---- gated linear recurrence (kernels_glr.hip)
 // A workgroup of GLR_WAVES waves covers one row of the batch, 2 * lanes channels (two per lane) and GLR_WAVES * (64 / lanes) *
 // run steps: a wave's lanes hold 64 / lanes runs.  Forward: runs of 16 steps over up to 128 channels; the adjoint, which
@@ -40,6 +46,7 @@ struct GlrArgs {
   float* dh0;
   unsigned long long* words;
   int* ticket;
+  bool past;                // results past the caches
 };
 hipError_t launch_glr_forward(const GlrArgs& a, hipStream_t s);
 hipError_t launch_glr_backward(const GlrArgs& a, hipStream_t s);
@@ -83,6 +90,7 @@ struct Q8Args {
   void* y;
   int8_t* q;                // [M, q8_row_bytes(K)]
   float* scale;             // [M]
+  bool past;                // results past the caches
 };
 hipError_t launch_q8_quantize(const Q8Args& a, hipStream_t s);
 hipError_t launch_q8_linear(const Q8Args& a, hipStream_t s);

@@ -60,6 +60,7 @@ static int glr_space(const glr_cfg& c, const GlrShape& s, void* ws, size_t n, Gl
   a->c = c;
   a->s = s;
   a->save = glr_shape(c, true).steps;
+  a->past = false;
   a->ticket = (int*)ws;
   a->words = need ? (unsigned long long*)((char*)ws + 256) : nullptr;
   return MGRIT_OK;
@@ -150,6 +151,7 @@ int glr_forward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, c
   a.reset = reset;
   a.h_last = h_last;
   a.saved = (float*)saved;
+  a.past = stores_past_caches(3.0 * elem_bytes(cfg->dtype) * cfg->T * cfg->B * cfg->H);
   (void)hipGetLastError();   // an error left by earlier, unrelated work is not this call's
   return launch_glr_forward(a, (hipStream_t)stream) == hipSuccess ? MGRIT_OK : MGRIT_E_LAUNCH;
 }
@@ -179,6 +181,7 @@ int glr_backward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, 
   a.saved = (float*)const_cast<void*>(saved);
   a.dh_last = dh_last;
   a.dh0 = dh0;
+  a.past = stores_past_caches(5.0 * elem_bytes(cfg->dtype) * cfg->T * cfg->B * cfg->H);
   (void)hipGetLastError();
   return launch_glr_backward(a, (hipStream_t)stream) == hipSuccess ? MGRIT_OK : MGRIT_E_LAUNCH;
 }
@@ -315,6 +318,7 @@ int q8_linear(const q8_cfg* cfg, const void* x, const int8_t* w_q, const float* 
   a.y = y;
   a.scale = (float*)workspace;
   a.q = (int8_t*)workspace + q8_scales(*cfg);
+  a.past = stores_past_caches((double)cfg->M * ((double)e * cfg->K + (double)e * cfg->N));
   (void)hipGetLastError();
   return launch_q8_linear(a, (hipStream_t)stream) == hipSuccess ? MGRIT_OK : MGRIT_E_LAUNCH;
 }
