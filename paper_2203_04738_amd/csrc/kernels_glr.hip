@@ -107,27 +107,32 @@ struct Gate {
     }
   }
 };
-// The same in one float that the adjoint keeps between its sweeps: the smaller of a and 1 - a under the sign of g, which
-// says which of the two it is.
-template <int FORM>
+// The same as the adjoint keeps it between its sweeps.  BOTH: a and 1 - a (16-bit arrays leave the registers for it, and
+// arithmetic is what those wait for).  Otherwise one float, the smaller of the two under the sign of g, which says which it
+// is.
+template <int FORM, bool BOTH>
 struct KeptGate {
-  float v;
+  float v, w;
   __device__ inline void set(float g) {
-    if constexpr (FORM == GLR_MIX) {
+    if constexpr (FORM == GLR_MIX && !BOTH) {
       const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(g));
       v = copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), g);
     } else {
-      v = __builtin_amdgcn_exp2f(LOG2E * g);
+      const Gate<FORM> gt(g);
+      v = gt.a;
+      w = gt.na;
     }
   }
   // What was computed from it is computed again from here on rather than kept: registers are what the adjoint lacks.
-  __device__ inline void anew() { asm volatile("" : "+v"(v)); }
+  __device__ inline void anew() {
+    if constexpr (!BOTH) asm volatile("" : "+v"(v));
+  }
   __device__ inline bool small_a() const { return (int)__float_as_uint(v) < 0; }
   __device__ inline float a() const {
-    return FORM == GLR_DECAY ? v : small_a() ? fabsf(v) : 1.0f - fabsf(v);
+    return FORM == GLR_DECAY || BOTH ? v : small_a() ? fabsf(v) : 1.0f - fabsf(v);
   }
   __device__ inline float na() const {
-    return FORM == GLR_DECAY ? 1.0f : small_a() ? 1.0f - fabsf(v) : fabsf(v);
+    return FORM == GLR_DECAY ? 1.0f : BOTH ? w : small_a() ? 1.0f - fabsf(v) : fabsf(v);
   }
 };
 
@@ -514,7 +519,7 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a)
     if (p.second) h.y = s[1];
   }
   const bool whole = glr_whole(a, p, resets);
-  KeptGate<FORM> gk[STEPS][2];
+  KeptGate<FORM, sizeof(E) == 2> gk[STEPS][2];
   auto anew = [&]() {
 #pragma unroll
     for (int r = 0; r < STEPS; ++r) {
