@@ -264,3 +264,23 @@ def test_another_stream_and_a_graph():
         assert np.array_equal(h.double().cpu().numpy(), ref["h"])
         assert np.array_equal(dgv[..., :H].double().cpu().numpy(), ref["dgate"])
         (h.sum() + dgv.sum()).item()                             # eager work in between
+
+
+@pytest.mark.parametrize("T,stride", [(40000, 1 << 15), (40, (1 << 25) + 2)])
+def test_offsets_beyond_32_bits(T, stride):
+    # 5 GB between the first step and the last: by many steps, and by few that lie 128 MB apart
+    B, H = 1, 66
+    d, dev = problem(51, T, B, H)
+    mem = torch.empty((T - 1) * stride + 2 * H, device=DEV)
+    wide = torch.as_strided(mem, (T, B, 2 * H), (stride, 2 * H, 1))
+    wide[..., :H], wide[..., H:] = dev["gate"], dev["value"]
+    dev["gate"], dev["value"] = wide[..., :H], wide[..., H:]
+    close(run(dev, T, B, H, "f32", "mix"), expected(d, "mix"), "f32")
+    cfg = mg.GlrCfg(T, B, H)
+    ws = space(mg.glr_workspace_bytes(cfg))
+    gate, value = dev["gate"].clone(), dev["value"].clone()
+    mem.fill_(7.0)
+    mg.glr_forward(cfg, gate, value, dev["h0"], None, wide[..., :H], None, None, ws)
+    torch.cuda.synchronize()
+    close({"h": wide[..., :H].double().cpu().numpy()}, expected(d, "mix"), "f32")
+    assert torch.all(wide[..., H:] == 7)

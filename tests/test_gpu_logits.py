@@ -315,3 +315,16 @@ def test_graph_replays_and_repeats_give_the_same_bits():
         assert np.array_equal(logp.cpu().numpy(), tops[0]) and np.array_equal(top.cpu().numpy(), tops[2])
         assert np.array_equal(top_ids.cpu().numpy(), tops[3])
         grad.float().abs().sum().item()
+
+
+def test_rows_beyond_32_bit_offsets():
+    N, V, ld = 3, 9000, (1 << 30) + 3                 # bf16 rows 2 GB apart
+    mem = torch.empty((N - 1) * ld + V, dtype=torch.bfloat16, device=DEV)
+    x = torch.as_strided(mem, (N, V), (ld, 1))
+    x.copy_(rows(5, N, V, "bf16")[0])
+    check_logprobs(x, np.array([0, V - 1, 77]), 9, "bf16")
+    ids, t = teacher(5, N, V, 7)
+    y = x.clone()
+    loss, grad = distill(x, ids, t, np.ones(N, np.float32), "bf16", in_place=True)
+    ref = distill(y, ids, t, np.ones(N, np.float32), "bf16")
+    assert np.array_equal(loss, ref[0]) and np.array_equal(grad, ref[1])

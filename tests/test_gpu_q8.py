@@ -101,7 +101,7 @@ def test_sizes(M, N, K, dtype):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 4100, 4096), (9, 300, 20000), (513, 770, 640), (2048, 1024, 1024), (1025, 2100, 130),
-                                   (48, 2048, 8192)])
+                                   (48, 2048, 8192), (2100, 70, 1500), (8000, 2040, 200)])
 def test_larger_sizes(M, N, K):
     check(tokens(M, M, K, "bf16"), *weights(N, N, K), "bf16")
     q, scale, _ = weights(N, N, K)
@@ -127,3 +127,13 @@ def test_strides_and_what_lies_beside(M, dtype):
     y = mem[1:].view(M, N + 3)[:, :N]
     check(x, *weights(2, N, K), dtype, y)
     assert torch.all(mem[1:].view(M, N + 3)[:, N:] == 7) and mem[0] == 7
+
+
+@pytest.mark.parametrize("M", [3, 130])
+def test_rows_beyond_32_bit_offsets(M):
+    N, K = 70, 300
+    ld = ((3 << 30) // M + 8) // 4 * 4                # bf16 rows over 6 GB in all, of tokens and of results
+    x = torch.as_strided(torch.empty((M - 1) * ld + K, dtype=torch.bfloat16, device=DEV), (M, K), (ld, 1))
+    x.copy_(tokens(1, M, K, "bf16"))
+    y = torch.as_strided(torch.empty((M - 1) * ld + N, dtype=torch.bfloat16, device=DEV), (M, N), (ld, 1))
+    check(x, *weights(1, N, K), "bf16", y)

@@ -73,6 +73,8 @@ def call(runtime, entry, *sizes, **env):
     ("q8_linear", (16, 2048, 8192, 1), ["q8_quantize_kernel", "q8_few_kernel<mg::Bf16, 1>"]),
     ("q8_linear", (64, 2048, 2048), ["q8_quantize_kernel", "q8_few_kernel<float, 4>"]),
     ("q8_linear", (65, 2048, 2048), ["q8_quantize_kernel", "q8_tile_kernel<float, 64, 64>"]),
+    ("q8_linear", (8000, 2040, 200), ["q8_quantize_kernel", "q8_tile_kernel<float, 256, 256>"]),
+    ("q8_linear", (2048, 2048, 2048, 1), ["q8_quantize_kernel<mg::Bf16, 1, 4>", "q8_tile_kernel<mg::Bf16, 128, 128>"]),
     ("q8_linear", (32768, 2048, 2048, 1), ["q8_quantize_kernel", "q8_tile_kernel<mg::Bf16, 256, 256>"]),
     ("q8_linear", (65, 16, 131072, 4), ["q8_quantize_long_kernel<mg::F16>", "q8_tile_kernel<mg::F16, 64, 64>"])])
 def test_kernels_of_a_call_and_launches_that_fail(runtime, entry, sizes, kernels):
