@@ -87,7 +87,7 @@ struct QuantRow {
   }
 };
 
-// A row per team of NW waves.  A row that is not finite: scale NaN, zeros.  32768 x 2048 bf16: 201 MB in 39 us (5.1 TB/s).
+// A row per team of NW waves.  A row that is not finite: scale NaN, zeros.  32768 x 2048 bf16: 201 MB in 40-42 us (4.8-5.1 TB/s).
 template <typename E, int NW, int LOADS>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void q8_quantize_kernel(Q8Args a) {
   __shared__ float part[NW];
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(64 * FUSED_WAVES) void q8_fused_kernel(Q8Args a) {
 // LDS buffers; a row's 16-byte pieces lie in the order piece ^ (row & 7), which spreads a fragment's rows over the banks.
 // While the matrix instructions of slice s run, slice s + 1 goes from registers to the other buffer and slice
 // s + 2 is loaded; the fragments of a quarter of a slice are read during the instructions of the quarter before, the
-// first of the next slice behind the barrier in front of the last quarter.  32768 x 2048 x 2048: 183 us, 1.5 POP/s; 135 us of
+// first of the next slice behind the barrier in front of the last quarter.  32768 x 2048 x 2048: 186-188 us, 1.5 POP/s; 135 us of
 // them are the loop over K (2.0 POP/s; a library's 8192^3 reaches 2.1), the rest results, which a workgroup alone on its CU (all
 // registers are taken) does not overlap with anything.
 template <typename E, int TM, int TN>
