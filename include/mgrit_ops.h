@@ -65,7 +65,8 @@ MGRIT_API int glr_saved_bytes(const glr_cfg* cfg, size_t* bytes);
 
 /* Forward.
  *   h0[B,H] float or NULL (zeros); reset[T,B] bytes or NULL; h out; h_last[B,H] float out or NULL: h_T
- *   unrounded, the h0 of a call that goes on with the sequence (it may be h0 itself).
+ *   unrounded, the h0 of a call that goes on with the sequence (it may be h0 itself).  It is formed from
+ *   the tiles' maps as the states between tiles are; a float h_T may differ from it in the last bits.
  *   saved: out or NULL: the states (float) that glr_backward starts from, 16-byte aligned. */
 MGRIT_API int glr_forward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, const float* h0,
                           const uint8_t* reset, const glr_seq* h, float* h_last, void* saved,

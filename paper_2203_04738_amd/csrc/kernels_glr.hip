@@ -11,7 +11,8 @@
 // before (a reset, or the state itself: what a tile knows once it knows the state before it).  No other A is -0:
 // no a is negative, so that a product that underflows is +0: a NaN or an infinity in the state stays in it for as
 // long as no reset stands in between.  The state before a tile is always computed as S + A h
-// tile by tile, whether the states between were there to be read or not: the result does not depend on timing.
+// tile by tile, by the tile itself (glr_join) as by those behind it that find the map and not yet the state (window_state):
+// the two round alike, and the result does not depend on timing.
 //
 // Tiles are taken by a ticket, first tiles first (the adjoint: last tiles first), so that those a workgroup waits for
 // have been started, wait for none behind it, and every wait ends.
@@ -398,22 +399,23 @@ __device__ inline Pair glr_join(const GlrArgs& a, const GlrPlace<LANES, STEPS>& 
   unsigned long long* word =
       a.words + (((long long)p.chunk * a.c.B + p.b) * a.s.cols) * chans + p.ch;
   const bool last = place == runs - 1;
+  // the tile's own map (in the last run): what a reader composes and the state behind it are formed from the same A and S
+  const Pair tA = {both(A.x, pA.x), both(A.y, pA.y)}, tS = {behind(A.x, S.x, pS.x), behind(A.y, S.y, pS.y)};
   if (last && chain && !at_start) {
-    store_word(word, make_word(both(A.x, pA.x), behind(A.x, S.x, pS.x)));
-    store_word(word + 1, make_word(both(A.y, pA.y), behind(A.y, S.y, pS.y)));
+    store_word(word, make_word(tA.x, tS.x));
+    store_word(word + 1, make_word(tA.y, tS.y));
   }
   if (!at_start) glr_look_back(a, p, BACKWARD, sh);
-  Pair h = {sh.carry[c], sh.carry[c + 1]};
-  h.x = behind(pA.x, pS.x, h.x);
-  h.y = behind(pA.y, pS.y, h.y);
+  const Pair carry = {sh.carry[c], sh.carry[c + 1]};
   if (last) {
-    out.x = behind(A.x, S.x, h.x);
-    out.y = behind(A.y, S.y, h.y);
+    out.x = behind(tA.x, tS.x, carry.x);
+    out.y = behind(tA.y, tS.y, carry.y);
     if (chain) {
       store_word(word, make_word(-0.0f, out.x));
       store_word(word + 1, make_word(-0.0f, out.y));
     }
   }
+  const Pair h = {behind(pA.x, pS.x, carry.x), behind(pA.y, pS.y, carry.y)};
   return h;
 }
 

@@ -1,0 +1,134 @@
+"""Recurrences whose memory is longer than a tile: the state that a tile starts from is the tiles before it composed in one
+fixed way, bit for bit, whichever of them were done first."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2203_04738_amd as mg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": (mg.MGRIT_F32, torch.float32), "bf16": (mg.MGRIT_BF16, torch.bfloat16)}
+FORMS = {"mix": mg.GLR_MIX, "decay": mg.GLR_DECAY}
+TILE = 128                                # steps of a tile where a call has more than 64 channels, either direction
+
+
+def problem(seed, T, B, H, dtype, form):
+    """Every channel has a memory of its own: gates around sigmoid(0..6), or decays of e^-2 .. e^-0.002 a step."""
+    rng = np.random.default_rng(seed)
+    z, u = rng.standard_normal((T, B, H)), rng.random(H)
+    gate = z + 6 * u if form == "mix" else -np.exp(0.3 * z - 6 * u)
+    to = lambda a, dt: torch.from_numpy(np.ascontiguousarray(a)).to(DEV).to(dt)  # noqa: E731
+    dt = TYPES[dtype][1]
+    seq = [to(a, dt) for a in (gate, rng.standard_normal((T, B, H)), rng.standard_normal((T, B, H)))]
+    return seq, [to(rng.standard_normal((B, H)), torch.float32) for _ in range(2)]
+
+
+def space(n):
+    return torch.empty(n, dtype=torch.uint8, device=DEV)
+
+
+def forward(gate, value, h0, dtype, form):
+    T, B, H = gate.shape
+    cfg = mg.GlrCfg(T, B, H, FORMS[form], TYPES[dtype][0])
+    saved, h = space(mg.glr_saved_bytes(cfg)), torch.empty_like(gate)
+    last = torch.empty(B, H, device=DEV)
+    mg.glr_forward(cfg, gate, value, h0, None, h, last, saved, space(mg.glr_workspace_bytes(cfg)))
+    return h, last, saved
+
+
+def backward(gate, value, saved, dh, dh_last, dtype, form):
+    T, B, H = gate.shape
+    cfg = mg.GlrCfg(T, B, H, FORMS[form], TYPES[dtype][0])
+    dgate, dvalue, dh0 = torch.empty_like(gate), torch.empty_like(gate), torch.empty(B, H, device=DEV)
+    mg.glr_backward(cfg, gate, value, None, saved, dh, dh_last, dgate, dvalue, dh0, space(mg.glr_workspace_bytes(cfg)))
+    return dgate, dvalue, dh0
+
+
+def fma32(a, b, c):
+    """a b + c of float32 arrays, rounded once: the product is exact in 64 bits, the sum is rounded to odd there."""
+    p, c = a.astype(np.float64) * b.astype(np.float64), c.astype(np.float64)
+    s = p + c
+    part = s - p
+    rest = (p - (s - part)) + (c - part)
+    even = (s.view(np.int64) & 1) == 0
+    s = np.where((rest != 0) & even, np.nextafter(s, np.where(rest > 0, np.inf, -np.inf)), s)
+    return s.astype(np.float32)
+
+
+def host(t):
+    return t.float().cpu().numpy()
+
+
+def test_the_sum_of_the_check_is_rounded_once():
+    one, eps = np.float32([1.0]), np.float32([2.0 ** -12])
+    # (1 + 2^-12)^2 = 1 + 2^-11 + 2^-24: half a unit above, which a hair more or less decides
+    a = one + eps
+    for c, up in ((2.0 ** -60, 1), (-(2.0 ** -60), 0)):
+        assert fma32(a, a, np.float32([c]))[0] == np.float32(1 + 2.0 ** -11 + up * 2.0 ** -23)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("H", [100, 130])
+def test_states_of_tiles_are_the_maps_of_tiles_composed(H, form):
+    # a tile's map h -> A h + S, from calls of that tile alone: S from a zero state, A from a state of one and no inputs
+    n, B = 24, 3
+    (gate, value, _), (h0, _) = problem(H, n * TILE, B, H, "f32", form)
+    h, _, saved = forward(gate, value, h0, "f32", form)
+    carry = host(saved.view(torch.float32).view(n, B, H))
+    state = host(h0)
+    zero, one = torch.zeros(B, H, device=DEV), torch.ones(B, H, device=DEV)
+    for k in range(n):
+        assert np.array_equal(carry[k], state), (k, np.mean(carry[k] != state))
+        at = slice(k * TILE, (k + 1) * TILE)
+        S = host(forward(gate[at], value[at], zero, "f32", form)[1])
+        A = host(forward(gate[at], torch.zeros_like(value[at]), one, "f32", form)[1])
+        alone, _, _ = forward(gate[at], value[at], torch.from_numpy(state).to(DEV), "f32", form)
+        assert torch.equal(alone, h[at]), k
+        state = fma32(A, state, S)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("H", [100, 130])
+def test_adjoints_of_tiles_are_the_maps_of_tiles_composed(H, form):
+    n, B = 24, 3
+    (gate, value, dh), (h0, dh_last) = problem(H, n * TILE, B, H, "f32", form)
+    dh[TILE - 1::TILE] = 0                        # the gradient at a tile's last state is what the tiles behind it say
+    h, _, saved = forward(gate, value, h0, "f32", form)
+    dgate, dvalue, dh0 = backward(gate, value, saved, dh, dh_last, "f32", form)
+    states = saved.view(torch.float32).view(n, B, H)
+    mu = host(dh_last)
+    zero, one = torch.zeros(B, H, device=DEV), torch.ones(B, H, device=DEV)
+    for k in range(n - 1, -1, -1):
+        at = slice(k * TILE, (k + 1) * TILE)
+        args = gate[at], value[at], states[k].clone().view(torch.uint8).view(-1)
+        if form == "decay":                       # (there dvalue is the state's gradient itself)
+            got = host(dvalue[(k + 1) * TILE - 1])
+            assert np.array_equal(got, mu), (k, np.mean(got != mu))
+        alone = backward(*args, dh[at], torch.from_numpy(mu).to(DEV), "f32", form)
+        assert torch.equal(alone[0], dgate[at]) and torch.equal(alone[1], dvalue[at]), k
+        S = host(backward(*args, dh[at], zero, "f32", form)[2])
+        A = host(backward(*args, torch.zeros_like(dh[at]), one, "f32", form)[2])
+        mu = fma32(A, mu, S)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("H", [20, 50, 260])
+def test_repeats_beside_other_work_have_the_same_bits(H, form, dtype):
+    T, B = 30 * 512 + 77, 4
+    (gate, value, dh), (h0, dh_last) = problem(H, T, B, H, dtype, form)
+    side, a = torch.cuda.Stream(), torch.randn(2048, 2048, device=DEV)
+    first = None
+    for k in range(6):
+        if k % 2:
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                for _ in range(3):
+                    a @ a
+        h, last, saved = forward(gate, value, h0, dtype, form)
+        out = (h, last, saved.clone()) + backward(gate, value, saved, dh, dh_last, dtype, form)
+        torch.cuda.synchronize()
+        assert all(torch.isfinite(t.float()).all() for t in out[:2])
+        first = first or out
+        assert all(torch.equal(x, y) for x, y in zip(first, out)), k
