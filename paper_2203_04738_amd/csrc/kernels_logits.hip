@@ -213,10 +213,12 @@ __device__ inline Stats team_stats(const Held<E, NW>& x, float c, int tid, float
   return st;
 }
 
-// w (x - m): the difference of two floats may be beyond them where w times it is not
+// w (x - m), w >= 0: the difference of two floats may be beyond them where w times it is not.  What a mask leaves out (-inf)
+// stays that, also where w m is beyond the floats.
 __device__ inline float below(float x, float m, float w) {
-  const float d = (x - m) * w;
-  return fabsf(d) == __builtin_inff() ? x * w - m * w : d;
+  const float d = x - m;
+  if (x == -__builtin_inff()) return x;
+  return w < 1.f && fabsf(d) == __builtin_inff() ? x * w - m * w : d * w;
 }
 // log p of a logit, from the statistics of its row
 __device__ inline float log_prob(float x, const Stats& r, float inv_t) {
