@@ -623,7 +623,7 @@ __device__ inline Stats join_stats(const SegOut& o, long long row, int segs, flo
     const float d = (finite_max(o.m[row * segs + i]) - m0) * c, si = o.s[row * segs + i];
     const float f = si == 0.f ? 0.f : __builtin_amdgcn_exp2f(d);
     s += f * si;
-    if (si != 0.f) u += f * fmaf(si, d, o.u[row * segs + i]);
+    if (f != 0.f) u += f * fmaf(si, d, o.u[row * segs + i]);   // (d can be -inf: a segment of the lowest value)
   }
   return {m, wave_sum(s), wave_sum(u)};
 }

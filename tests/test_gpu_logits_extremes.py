@@ -80,3 +80,19 @@ def test_differences_beyond_a_float(V, temperature, dtype):
     x[3, 1] = -INF
     check_logprobs(x, np.array([0, 1, 2, 3]), min(V, 12), dtype, temperature)
     check_logprobs(x, np.array([1, 0, 1, 1]), 3, dtype, temperature)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [7, 400])                      # held by teams, and streamed
+@pytest.mark.parametrize("temperature", [1.0, 0.5])
+def test_whole_segments_at_the_lowest_value(N, temperature, dtype):
+    V = 70001                                                # three segments
+    x = rows(N, N, V, dtype)
+    low = torch.finfo(TYPES[dtype][1]).min
+    x[0, 20000:] = low                                       # what a mask leaves lies in the first segment, in the last,
+    x[1, :60000] = low                                       # in the middle,
+    x[2, :30000], x[2, 40000:] = low, low
+    x[3] = low                                               # nowhere
+    x[4, :], x[4, 50000] = low, 3.0
+    x[5, :40000], x[5, 40000:] = -INF, low                   # and beside segments that hold nothing at all
+    check_logprobs(x, np.arange(N) * 997 % V, 9, dtype, temperature)
