@@ -679,7 +679,8 @@ struct Teacher {
   float total;                                               // of the weights: 1, 0 (no teacher), NaN (an id >= V)
   float qlogq;                                               // sum q log q
 };
-// By one wave; row: the student's logits.
+// By one wave; row: the student's logits.  Weights from (teacher - largest) / t, as `below` has it: a teacher's value over t
+// may be beyond a float.
 template <typename E>
 __device__ inline void read_teacher(const int64_t* ids, const float* teacher, int K, int V, float inv_t,
                                     const E* row, int lane, Teacher& t) {
@@ -694,17 +695,19 @@ __device__ inline void read_teacher(const int64_t* ids, const float* teacher, in
     if (k >= K) continue;
     const long long id = ids[k];
     const bool entry = id >= 0;
-    if (entry) z[i] = teacher[k] * inv_t;
+    if (entry) z[i] = teacher[k];
     bad |= entry && id >= V;
     t.id[k] = entry && id < V ? (int)id : -1;
     t.x[k] = entry && id < V ? elem_f32(row[id]) : 0.f;
     m = fmaxf(m, z[i]);
   }
-  m = wave_max(m);
-  const float m0 = finite_max(m);
+  m = finite_max(wave_max(m));
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) s += __builtin_amdgcn_exp2f((z[i] - m0) * LOG2E);
+  for (int i = 0; i < PER; ++i) {
+    z[i] = below(z[i], m, inv_t);
+    s += __builtin_amdgcn_exp2f(z[i] * LOG2E);
+  }
   s = wave_sum(s);
   const float log_s = logf(s);
   float ql = 0.f;
@@ -712,9 +715,9 @@ __device__ inline void read_teacher(const int64_t* ids, const float* teacher, in
   for (int i = 0; i < PER; ++i) {
     const int k = lane + 64 * i;
     if (k >= K) continue;
-    const float q = s == 0.f ? 0.f : __builtin_amdgcn_exp2f((z[i] - m0) * LOG2E) / s;
+    const float q = s == 0.f ? 0.f : __builtin_amdgcn_exp2f(z[i] * LOG2E) / s;
     t.q[k] = q;
-    if (q != 0.f) ql = fmaf(q, z[i] - m0 - log_s, ql);
+    if (q != 0.f) ql = fmaf(q, z[i] - log_s, ql);
   }
   ql = wave_sum(ql);
   const bool any_bad = __any(bad);

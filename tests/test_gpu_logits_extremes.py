@@ -96,3 +96,43 @@ def test_whole_segments_at_the_lowest_value(N, temperature, dtype):
     x[4, :], x[4, 50000] = low, 3.0
     x[5, :40000], x[5, 40000:] = -INF, low                   # and beside segments that hold nothing at all
     check_logprobs(x, np.arange(N) * 997 % V, 9, dtype, temperature)
+
+
+def distill(x, ids, t, w, dtype, temperature, apart):
+    N, V = x.shape
+    cfg = mg.LogitsCfg(N, V, ids.shape[1], TYPES[dtype][0], temperature)
+    d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV)  # noqa: E731
+    loss, stats, grad = torch.full((N,), 9.0, device=DEV), torch.full((N, 2), 9.0, device=DEV), torch.full_like(x, 9.0)
+    if apart:
+        mg.distill_topk(cfg, x, d(ids), d(t), None, loss, stats, None, space(cfg))
+        mg.distill_topk_backward(cfg, x, d(ids), d(t), stats, d(w), grad)
+    else:
+        mg.distill_topk(cfg, x, d(ids), d(t), d(w), loss, None, grad, space(cfg))
+    torch.cuda.synchronize()
+    return loss.double().cpu().numpy(), grad.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [50, 3000, 20000, 70001])
+@pytest.mark.parametrize("temperature", [0.5, 0.01, 1.0, 50.0])
+def test_teachers_at_the_ends_of_the_range(V, temperature, dtype):
+    N, K = 7, 4
+    x = rows(V, N, V, dtype)
+    info = np.finfo(np.float32)
+    ids = np.stack([np.random.default_rng(n).choice(V, K, replace=False) for n in range(N)]).astype(np.int64)
+    t = np.random.default_rng(1).standard_normal((N, K)).astype(np.float32)
+    t[0] = info.min                                          # all alike: a quarter each
+    t[1], t[1, 2] = info.min, 1.0
+    t[2] = info.max
+    t[3] = info.min, info.max, info.max, -INF
+    t[4] = 3e37, 3e37, -INF, 1.0
+    t[5] = info.min, -INF, -INF, info.min
+    w = np.linspace(0.5, 1.5, N).astype(np.float32)
+    tau = float(np.float32(temperature))
+    for apart in (False, True):
+        loss, grad = distill(x, ids, t, w, dtype, temperature, apart)
+        ref = orc.distill(x.double().cpu().numpy(), ids, t.astype(np.float64), w.astype(np.float64), tau)
+        scale = 1 / min(1.0, tau)
+        assert np.all(np.abs(loss - ref[0]) <= 2 * TOL * scale * np.maximum(1.0, np.abs(ref[0]) / 20)), (loss, ref[0])
+        bound = UNIT[dtype] * np.abs(ref[1]) + 2 * TOL * scale * w[:, None] / tau + (2.0 ** -25 if dtype == "f16" else 0)
+        assert np.all(np.abs(grad - ref[1]) <= bound)
