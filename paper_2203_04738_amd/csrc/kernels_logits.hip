@@ -759,13 +759,14 @@ struct DistillArgs {
   bool past;                 // gradients past the caches
 };
 
-// w (p - q) of what a team holds of a row, stored; scale = w total / s, then the entries of the teacher.
+// w (p - q) of what a team holds of a row, stored; scale = w total / s, then the entries of the teacher.  A row of nothing but
+// -inf (s = 0) has p = 0, but for an id that does not exist (total is NaN), which makes it NaN.
 template <typename E, int NW>
 __device__ inline void put_gradient(const DistillArgs& a, const Held<E, NW>& x, E* out, int lo, int hi, float m,
                                     float s, float w, const Teacher& t, int tid) {
   using T = TeamOf<E, NW>;
   const Exponent ex(a.inv_t * LOG2E, m);
-  const float f = t.total == 0.f || s == 0.f ? 0.f * s : w * t.total / s * ex.scale();
+  const float f = s == 0.f ? 0.f * t.total : w * t.total / s * ex.scale();
   const bool wide = ((uintptr_t)(out + x.first) & 15) == 0;
   auto store = [&](auto one) {
 #pragma unroll
@@ -796,7 +797,6 @@ __device__ inline void put_gradient(const DistillArgs& a, const Held<E, NW>& x, 
   else store(std::false_type{});
   // the entries, over what was stored there before the barrier
   team_sync<NW>();
-  if (t.total == 0.f) return;
   for (int k = tid; k < a.K; k += T::threads) {
     const int id = t.id[k];
     if (id < lo || id >= hi) continue;

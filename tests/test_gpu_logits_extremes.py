@@ -136,3 +136,14 @@ def test_teachers_at_the_ends_of_the_range(V, temperature, dtype):
         assert np.all(np.abs(loss - ref[0]) <= 2 * TOL * scale * np.maximum(1.0, np.abs(ref[0]) / 20)), (loss, ref[0])
         bound = UNIT[dtype] * np.abs(ref[1]) + 2 * TOL * scale * w[:, None] / tau + (2.0 ** -25 if dtype == "f16" else 0)
         assert np.all(np.abs(grad - ref[1]) <= bound)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [50, 20000, 70001])
+def test_an_id_that_does_not_exist_makes_a_masked_row_nan_too(V, dtype):
+    x = rows(V, 2, V, dtype)
+    x[0] = -INF
+    ids = np.array([[1, V], [1, 2]], np.int64)
+    for apart in (False, True):
+        loss, grad = distill(x, ids, np.zeros((2, 2), np.float32), np.ones(2, np.float32), dtype, 1.0, apart)
+        assert np.isnan(loss[0]) and np.all(np.isnan(grad[0])) and np.all(np.isfinite(grad[1]))
