@@ -105,12 +105,12 @@ def distill(x, ids, teacher, weight, temperature=1.0):
 
 # ---- product in 8-bit integers
 def q8_quantize(x):
-    """(q, scale) of rows of float32 values; the scale and the quotient are rounded to float32 by definition."""
+    """(q, scale) of rows of float32 values; both quotients are rounded to float32 by definition."""
     x = np.asarray(x, dtype=np.float32)
     finite = np.isfinite(x).all(1, keepdims=True)
     clean = np.where(finite, x, np.float32(0))
     amax = np.abs(clean).max(1, keepdims=True)
-    scale = np.maximum(amax * (np.float32(1) / np.float32(127)), np.float32(2.0 ** -126))
+    scale = np.maximum(amax / np.float32(127), np.float32(2.0 ** -126))
     q = np.rint(clean / scale)
     return q.astype(np.int8), np.where(finite, scale, np.float32(np.nan))[:, 0]
 

@@ -21,7 +21,7 @@ __host__ __device__ inline int q8_pad(int K) { return (K + 127) / 128 * 128; }
 // ---------------------------------------------------------------------------
 // quantisation
 // ---------------------------------------------------------------------------
-__device__ inline float quant_scale(float amax) { return fmaxf(amax * (1.0f / 127.0f), 0x1p-126f); }
+__device__ inline float quant_scale(float amax) { return fmaxf(amax / 127.0f, 0x1p-126f); }
 __device__ inline unsigned quant(float x, float scale) { return (unsigned)(int)rintf(x / scale) & 255u; }
 __device__ inline float wave_max(float v) {
 #pragma unroll
