@@ -142,7 +142,7 @@ MGRIT_API int distill_topk_backward(const logits_cfg* cfg, const void* logits, c
 
 /* ------------------------------------------------------------------------
  * Product in 8-bit integers:  y[m,n] = xs_m ws_n sum_k xq[m,k] wq[n,k] + bias_n,
- * the sum exact (32-bit integers).  A row is quantised by
+ * the sum exact (32-bit integers), then multiplied by ws, by xs, and the bias added, in floats.  A row is quantised by
  *     scale = max(max|x| / 127, 2^-126),   q = x / scale rounded to nearest (ties to even),
  * both quotients rounded to float.  A row with an infinity or a NaN has scale NaN and q 0: its results are NaN.
  * Rows of q are q8_row_bytes(K) bytes apart, K rounded up to 128.

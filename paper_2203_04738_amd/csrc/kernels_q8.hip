@@ -169,12 +169,13 @@ hipError_t launch_q8_quantize(const Q8Args& a, hipStream_t s) {
 // products
 // ---------------------------------------------------------------------------
 // Four neighbouring channels n .. n+3 of a token, from their sums and the scales and biases of the channels; wide: in one
-// store (the row's place allows it).
+// store (the row's place allows it).  The channel's scale comes first: a sum times the scale of a token near a float's largest
+// value would be beyond it where the product of all three is not.
 template <typename E>
 __device__ inline void put4(const Q8Args& a, E* y, int n, const intx4& sum, float sm, const float4& ws,
                             const float4& bias, bool wide) {
-  const float v[4] = {(float)sum[0] * sm * ws.x + bias.x, (float)sum[1] * sm * ws.y + bias.y,
-                      (float)sum[2] * sm * ws.z + bias.z, (float)sum[3] * sm * ws.w + bias.w};
+  const float v[4] = {(float)sum[0] * ws.x * sm + bias.x, (float)sum[1] * ws.y * sm + bias.y,
+                      (float)sum[2] * ws.z * sm + bias.z, (float)sum[3] * ws.w * sm + bias.w};
   if (wide && n + 3 < a.c.N) {
     if constexpr (sizeof(E) == 4)
       *reinterpret_cast<float4*>(y + n) = make_float4(v[0], v[1], v[2], v[3]);
@@ -403,10 +404,10 @@ __global__ __launch_bounds__(256) void q8_tile_kernel(Q8Args a, int tiles_m, int
       for (int e = 0; e < 4; ++e) {
         const int c = 32 * i + 8 * e + 4 * (lane >> 5);      // the wave's channel
         const float4 w4 = ws[(wn + c) / 4], b4 = bias[(wn + c) / 4];
-        const float v0 = (float)acc[i][j][4 * e] * sm[j] * w4.x + b4.x;
-        const float v1 = (float)acc[i][j][4 * e + 1] * sm[j] * w4.y + b4.y;
-        const float v2 = (float)acc[i][j][4 * e + 2] * sm[j] * w4.z + b4.z;
-        const float v3 = (float)acc[i][j][4 * e + 3] * sm[j] * w4.w + b4.w;
+        const float v0 = (float)acc[i][j][4 * e] * w4.x * sm[j] + b4.x;
+        const float v1 = (float)acc[i][j][4 * e + 1] * w4.y * sm[j] + b4.y;
+        const float v2 = (float)acc[i][j][4 * e + 2] * w4.z * sm[j] + b4.z;
+        const float v3 = (float)acc[i][j][4 * e + 3] * w4.w * sm[j] + b4.w;
         char* to_row = mine + (lane & 31) * ROW + c * (int)sizeof(E);
         if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(to_row) = make_float4(v0, v1, v2, v3);
         else *reinterpret_cast<uint2*>(to_row) = make_uint2(pack2<E>(v0, v1), pack2<E>(v2, v3));

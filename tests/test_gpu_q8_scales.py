@@ -62,3 +62,18 @@ def test_ties_in_a_product(M):
     ref = orc.q8_linear(x, q[:, :x.shape[1]], scale)
     got = product(torch.from_numpy(x).to(DEV), q, scale)
     assert np.all(np.abs(got - ref) <= 4 * 2.0 ** -24 * np.abs(ref))    # an exact sum, rounded and multiplied twice
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [2, 40, 130, 3000])
+def test_large_tokens_and_small_weights(M):
+    # tokens near a float's largest: sums times the token's scale alone would be beyond it
+    rng = np.random.default_rng(M)
+    K = 300
+    x = (rng.uniform(-1, 1, (M, K)) * 3e38).astype(np.float32)
+    q = rng.integers(-128, 128, (70, mg.q8_row_bytes(K))).astype(np.int8)
+    scale = (rng.random(70) * 1e-9 + 1e-10).astype(np.float32)
+    ref = orc.q8_linear(x, q[:, :K], scale)
+    assert np.abs(ref / scale).max() > np.finfo(np.float32).max > np.abs(ref).max()
+    got = product(torch.from_numpy(x).to(DEV), q, scale)
+    assert np.all(np.abs(got - ref) <= 4 * 2.0 ** -24 * np.abs(ref))
