@@ -38,6 +38,9 @@ enum { MGRIT_F16 = 4 };
  *     h_t = a_t h_{t-1} + b_t,   t = 1..T,
  * GLR_MIX:   a = sigmoid(gate), b = (1 - a) value    (a GRU's update whose gates do not read the state)
  * GLR_DECAY: a = exp(gate),     b = value            (gate <= 0 is a decay; it is not enforced)
+ * A sequence is composed from runs of steps, h -> A h + S with A the product of the run's a.  Gates above 0 can carry A beyond
+ * the floats within some steps, where a state that is not zero becomes infinite or NaN; one of zero stays what its inputs make it.
+ * An infinite state, which nothing but a reset ends, may be NaN once A is below the floats.
  * A step whose `reset` byte is not zero forgets the past: h_t = b_t, whatever h_{t-1} was (infinities
  * and NaN included), and no gradient passes to the steps before it: sequences packed one behind the other.
  */

@@ -9,8 +9,8 @@
 // The word of a tile and channel is A in the low half and S in the high one, stored by one 64-bit store, so that a reader that
 // sees one sees the other.  All bits set: not written yet (no A is stored so).  A = -0: S does not depend on what was
 // before (a reset, or the state itself: what a tile knows once it knows the state before it).  No other A is -0:
-// no a is negative, so that a product that underflows is +0: a NaN or an infinity in the state stays in it for as
-// long as no reset stands in between.  The state before a tile is always computed as S + A h
+// no a is negative, so that a product that underflows is +0, and a state that is not finite does not become so again
+// (0 times it is NaN) as long as no reset stands in between.  The state before a tile is always computed as S + A h
 // tile by tile, by the tile itself (glr_join) as by those behind it that find the map and not yet the state (window_state):
 // the two round alike, and the result does not depend on timing.
 //
@@ -138,12 +138,23 @@ struct KeptGate {
 };
 
 __device__ inline bool is_free(float A) { return __float_as_uint(A) == GLR_FREE; }
+// GLR_DECAY: gates above 0 are allowed, and the product of a run's a can be beyond the floats.  A state of zero stays what it
+// is then, and what a run has forgotten stays forgotten (infinity times 0 would be NaN).
 // A of a run behind another run.
+template <int FORM>
 __device__ inline float both(float A, float before) {
-  return is_free(A) || is_free(before) ? -0.0f : A * before;
+  if (is_free(A) || is_free(before)) return -0.0f;
+  return FORM == GLR_DECAY && before == 0.f ? 0.f : A * before;
 }
-// The state behind a run (A, S) from the state h before it.
-__device__ inline float behind(float A, float S, float h) { return is_free(A) ? S : fmaf(A, h, S); }
+// The state behind a run (A, S) that knows no reset, and behind any run, from the state h before it.
+template <int FORM>
+__device__ inline float behind_whole(float A, float S, float h) {
+  return FORM == GLR_DECAY && h == 0.f ? S : fmaf(A, h, S);
+}
+template <int FORM>
+__device__ inline float behind(float A, float S, float h) {
+  return is_free(A) ? S : behind_whole<FORM>(A, S, h);
+}
 
 __device__ inline unsigned long long make_word(float A, float S) {
   unsigned a = __float_as_uint(A);
@@ -278,6 +289,7 @@ struct GlrShared {
 
 // The state before a tile from the n words of the tiles before it that the window holds for a channel (word 0 the
 // nearest): false where a word that is needed is not there yet.  The words are read four at a time.
+template <int FORM>
 __device__ inline bool window_state(const unsigned long long* w, int n, int stride, float& h) {
   int at = -1;
   bool stop = false;
@@ -300,14 +312,15 @@ __device__ inline bool window_state(const unsigned long long* w, int n, int stri
     for (int k = 0; k < 4; ++k) v[k] = w[min(i0 + k, at) * stride];
 #pragma unroll
     for (int k = 3; k >= 0; --k)
-      if (i0 + k < at) h = fmaf(__uint_as_float((unsigned)v[k]), h, __uint_as_float((unsigned)(v[k] >> 32)));
+      if (i0 + k < at)
+        h = behind_whole<FORM>(__uint_as_float((unsigned)v[k]), __uint_as_float((unsigned)(v[k] >> 32)), h);
   }
   return true;
 }
 
 // The state before tile `chunk` of the thread's two channels, in sh.carry, from the words of
 // the tiles before it (backward: behind it), whose distance is 1, 2, ...  All threads of the workgroup call it.
-template <int LANES, int STEPS>
+template <int FORM, int LANES, int STEPS>
 __device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, bool backward, GlrShared& sh) {
   const int before = backward ? a.s.chunks - 1 - p.chunk : p.chunk;
   const int runs = p.runs(), chans = 2 * p.lanes, n = min(before, GLR_WORDS / chans);
@@ -324,7 +337,7 @@ __device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace<LANES, STE
     int ok = 1;
     if (p.run < 2) {                                  // run 0: channel ch, run 1: ch + 1
       float h = 0.f;
-      ok = window_state(&sh.window[2 * p.lane_c + p.run], n, chans, h);
+      ok = window_state<FORM>(&sh.window[2 * p.lane_c + p.run], n, chans, h);
       sh.carry[2 * p.lane_c + p.run] = h;
     }
     if (__syncthreads_and(ok)) return;
@@ -334,14 +347,14 @@ __device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace<LANES, STE
 
 // (A, S) per channel of the runs before the thread's own in its tile, from the own one, through LDS (`all`).  32
 // lanes: the halves of a wave meet by exchange, the waves in LDS.  before_barrier() is called in front of the barrier.
-template <bool BACKWARD, int LANES, int STEPS, typename FN>
+template <bool BACKWARD, int FORM, int LANES, int STEPS, typename FN>
 __device__ inline void runs_before(const GlrPlace<LANES, STEPS>& p, Pair A, Pair S, float4* all, Pair& pA, Pair& pS,
                                    FN before_barrier) {
   auto behind_it = [&](const float4& x) {             // one more run: (A, S) of either channel
-    pS.x = behind(x.x, x.y, pS.x);
-    pS.y = behind(x.z, x.w, pS.y);
-    pA.x = both(x.x, pA.x);
-    pA.y = both(x.z, pA.y);
+    pS.x = behind<FORM>(x.x, x.y, pS.x);
+    pS.y = behind<FORM>(x.z, x.w, pS.y);
+    pA.x = both<FORM>(x.x, pA.x);
+    pA.y = both<FORM>(x.z, pA.y);
   };
   pA = {1.f, 1.f};
   pS = {0.f, 0.f};
@@ -355,8 +368,8 @@ __device__ inline void runs_before(const GlrPlace<LANES, STEPS>& p, Pair A, Pair
                           __shfl_xor(S.y, 32, 64));
     if (later)
       all[wave * LANES + p.lane_c] = LANES == 64 ? make_float4(A.x, S.x, A.y, S.y)
-                                                 : make_float4(both(A.x, other.x), behind(A.x, S.x, other.y),
-                                                               both(A.y, other.z), behind(A.y, S.y, other.w));
+                                                 : make_float4(both<FORM>(A.x, other.x), behind<FORM>(A.x, S.x, other.y),
+                                                               both<FORM>(A.y, other.z), behind<FORM>(A.y, S.y, other.w));
     before_barrier();
     __syncthreads();
     const int n = BACKWARD ? GLR_WAVES - 1 - wave : wave;
@@ -382,7 +395,7 @@ __device__ inline void runs_before(const GlrPlace<LANES, STEPS>& p, Pair A, Pair
 // What both directions do between their sweeps: from (A, S) of the thread's run, per channel, the state before
 // the run.  first: the state before the sequence's first tile (backward: behind its last one).  The threads of the
 // tile's last run (backward: its first) get in `out` the state behind the tile.
-template <bool BACKWARD, int LANES, int STEPS>
+template <bool BACKWARD, int FORM, int LANES, int STEPS>
 __device__ inline Pair glr_join(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, Pair A, Pair S, Pair first, Pair& out,
                                 GlrShared& sh) {
   const int chans = 2 * p.lanes, runs = p.runs(), c = 2 * p.lane_c;
@@ -390,7 +403,7 @@ __device__ inline Pair glr_join(const GlrArgs& a, const GlrPlace<LANES, STEPS>& 
   const bool chain = a.s.chunks > 1;
   const int place = BACKWARD ? runs - 1 - p.run : p.run;      // runs of the tile before this one
   Pair pA, pS;
-  runs_before<BACKWARD, LANES, STEPS>(p, A, S, sh.run, pA, pS, [&]() {
+  runs_before<BACKWARD, FORM, LANES, STEPS>(p, A, S, sh.run, pA, pS, [&]() {
     if (at_start && place == 0) {
       sh.carry[c] = first.x;
       sh.carry[c + 1] = first.y;
@@ -400,22 +413,22 @@ __device__ inline Pair glr_join(const GlrArgs& a, const GlrPlace<LANES, STEPS>& 
       a.words + (((long long)p.chunk * a.c.B + p.b) * a.s.cols) * chans + p.ch;
   const bool last = place == runs - 1;
   // the tile's own map (in the last run): what a reader composes and the state behind it are formed from the same A and S
-  const Pair tA = {both(A.x, pA.x), both(A.y, pA.y)}, tS = {behind(A.x, S.x, pS.x), behind(A.y, S.y, pS.y)};
+  const Pair tA = {both<FORM>(A.x, pA.x), both<FORM>(A.y, pA.y)}, tS = {behind<FORM>(A.x, S.x, pS.x), behind<FORM>(A.y, S.y, pS.y)};
   if (last && chain && !at_start) {
     store_word(word, make_word(tA.x, tS.x));
     store_word(word + 1, make_word(tA.y, tS.y));
   }
-  if (!at_start) glr_look_back(a, p, BACKWARD, sh);
+  if (!at_start) glr_look_back<FORM>(a, p, BACKWARD, sh);
   const Pair carry = {sh.carry[c], sh.carry[c + 1]};
   if (last) {
-    out.x = behind(tA.x, tS.x, carry.x);
-    out.y = behind(tA.y, tS.y, carry.y);
+    out.x = behind<FORM>(tA.x, tS.x, carry.x);
+    out.y = behind<FORM>(tA.y, tS.y, carry.y);
     if (chain) {
       store_word(word, make_word(-0.0f, out.x));
       store_word(word + 1, make_word(-0.0f, out.y));
     }
   }
-  const Pair h = {behind(pA.x, pS.x, carry.x), behind(pA.y, pS.y, carry.y)};
+  const Pair h = {behind<FORM>(pA.x, pS.x, carry.x), behind<FORM>(pA.y, pS.y, carry.y)};
   return h;
 }
 
@@ -473,7 +486,7 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) 
   }
   constexpr int L = STEPS - 1;
   Pair end = {0.f, 0.f};
-  const Pair h = glr_join<false, LANES, STEPS>(a, p, {A[L][0], A[L][1]}, {S[L][0], S[L][1]}, first, end, sh);
+  const Pair h = glr_join<false, FORM, LANES, STEPS>(a, p, {A[L][0], A[L][1]}, {S[L][0], S[L][1]}, first, end, sh);
   const long long at = (long long)p.b * a.c.H + p.ch;
   if (a.saved && p.t0 % a.save == 0 && p.t0 < a.c.T) {
     float* s = a.saved + (long long)(p.t0 / a.save) * a.c.B * a.c.H + at;
@@ -490,8 +503,8 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) 
     constexpr bool MASKED = decltype(masked)::value;
 #pragma unroll
     for (int r = 0; r < STEPS; ++r, out.next()) {
-      const float x = MASKED ? behind(A[r][0], S[r][0], h.x) : fmaf(A[r][0], h.x, S[r][0]);
-      const float y = MASKED ? behind(A[r][1], S[r][1], h.y) : fmaf(A[r][1], h.y, S[r][1]);
+      const float x = MASKED ? behind<FORM>(A[r][0], S[r][0], h.x) : behind_whole<FORM>(A[r][0], S[r][0], h.x);
+      const float y = MASKED ? behind<FORM>(A[r][1], S[r][1], h.y) : behind_whole<FORM>(A[r][1], S[r][1], h.y);
       if (!MASKED || p.t0 + r < a.c.T) store_pair<E, ALIGNED>(out.at(), x, y, p.second, a.past);
     }
   };
@@ -572,11 +585,11 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a)
   }
   anew();
   Pair fA, fS;
-  runs_before<false, LANES, STEPS>(p, {pA[0], pA[1]}, {pS[0], pS[1]}, fwd, fA, fS, []() {});
-  h.x = behind(fA.x, fS.x, h.x);
-  h.y = behind(fA.y, fS.y, h.y);
+  runs_before<false, FORM, LANES, STEPS>(p, {pA[0], pA[1]}, {pS[0], pS[1]}, fwd, fA, fS, []() {});
+  h.x = behind<FORM>(fA.x, fS.x, h.x);
+  h.y = behind<FORM>(fA.y, fS.y, h.y);
   Pair end = {0.f, 0.f};
-  const Pair mu = glr_join<true, LANES, STEPS>(a, p, {pA[0], pA[1]}, {qS[0], qS[1]}, first, end, sh);
+  const Pair mu = glr_join<true, FORM, LANES, STEPS>(a, p, {pA[0], pA[1]}, {qS[0], qS[1]}, first, end, sh);
   if (p.run == 0 && p.chunk == 0 && a.dh0) {
     if (p.has) a.dh0[at] = end.x;
     if (p.second) a.dh0[at + 1] = end.y;

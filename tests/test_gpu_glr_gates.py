@@ -1,0 +1,87 @@
+"""Gates of the recurrence at the ends of their range: how exact a and 1 - a are, and products of gates that a float cannot hold."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2203_04738_amd as mg
+from oracle import ops_oracle as orc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def space(n):
+    return torch.empty(n, dtype=torch.uint8, device=DEV)
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(DEV)
+
+
+def run(gate, value, h0, form, dh=None, dh_last=None):
+    T, B, H = gate.shape
+    cfg = mg.GlrCfg(T, B, H, form)
+    ws, saved = space(mg.glr_workspace_bytes(cfg)), space(mg.glr_saved_bytes(cfg))
+    h, last = torch.empty(T, B, H, device=DEV), torch.empty(B, H, device=DEV)
+    mg.glr_forward(cfg, dev(gate), dev(value), None if h0 is None else dev(h0), None, h, last, saved, ws)
+    out = {"h": h, "h_last": last}
+    if dh is not None:
+        out.update({k: torch.empty(T, B, H, device=DEV) for k in ("dgate", "dvalue")}, dh0=torch.empty(B, H, device=DEV))
+        mg.glr_backward(cfg, dev(gate), dev(value), None, saved, dev(dh), None if dh_last is None else dev(dh_last),
+                        out["dgate"], out["dvalue"], out["dh0"], ws)
+    return {k: v.double().cpu().numpy() for k, v in out.items()}
+
+
+def test_gates_that_are_not_finite():
+    inf, nan = np.inf, np.nan
+    g = np.array([inf, -inf, nan, 1e30, -1e30, 300.0, -300.0, 0.0], np.float32)[None, None]
+    two, three = 2 * np.ones((1, 1, 8)), 3 * np.ones((1, 8))
+    a = np.array([1, 0, nan, 1, 0, 1, 0, 0.5])
+    got = run(g, two, three, mg.GLR_MIX, two)
+    assert np.array_equal(got["h"][0, 0], 3 * a + 2 * (1 - a), equal_nan=True)
+    assert np.array_equal(got["dvalue"][0, 0], 2 * (1 - a), equal_nan=True)
+    got = run(g, two, three, mg.GLR_DECAY, two)
+    a = np.array([inf, 0, nan, inf, 0, inf, 0, 1])
+    on = np.isfinite(a)                             # (else infinite or NaN: an infinite a makes a NaN of a state of zero)
+    for k, r in (("h", 3 * a + 2), ("dh0", 2 * a)):
+        assert np.array_equal(got[k].ravel()[on], r[on]) and not np.isfinite(got[k].ravel()[~on]).any()
+
+
+@pytest.mark.parametrize("T", [9, 100, 700, 3000])
+@pytest.mark.parametrize("H", [5, 40, 130])
+def test_growth_of_a_state_of_zero(T, H):
+    # decays are not enforced: while state and inputs are zero, gates of any size leave it there
+    B = 2
+    rng = np.random.default_rng(T)
+    gate = -np.exp(rng.uniform(-4, 1, (T, B, H)))
+    value, dh = rng.standard_normal((T, B, H)), rng.standard_normal((T, B, H))
+    gate, value, dh = (a.astype(np.float32) for a in (gate, value, dh))
+    n = 2 * T // 3
+    gate[:n], value[:n] = 60.0, 0.0
+    got = run(gate, value, None, mg.GLR_DECAY)
+    ref = orc.glr_forward(gate[n:].astype(np.float64), value[n:].astype(np.float64), None, None, "decay")
+    assert np.all(got["h"][:n] == 0)
+    assert np.all(np.abs(got["h"][n:] - ref) <= 8e-6 * max(1.0, np.abs(ref).max()))
+    assert np.all(np.isfinite(got["h_last"]))
+    # the adjoint, from the other end: no gradient comes from the last steps
+    gate = -np.exp(rng.uniform(-4, 1, (T, B, H))).astype(np.float32)
+    value = rng.standard_normal((T, B, H)).astype(np.float32)
+    gate[T - n:], value[T - n:], dh[T - n:] = 20.0, 0.0, 0.0
+    gate[T - n], h0 = -np.inf, np.zeros((B, H), np.float32)         # (the states themselves are zero from here on)
+    got = run(gate, value, h0, mg.GLR_DECAY, dh)
+    m = T - n
+    h = orc.glr_forward(gate[:m].astype(np.float64), value[:m].astype(np.float64), h0, None, "decay")
+    ref = orc.glr_backward(gate[:m].astype(np.float64), value[:m].astype(np.float64), h, dh[:m].astype(np.float64), h0,
+                           None, None, "decay")
+    assert np.all(got["dvalue"][m:] == 0) and np.all(got["h"][m:] == 0)
+    for k, r in zip(("dgate", "dvalue"), ref):
+        assert np.all(np.abs(got[k][:m] - r) <= 2.5e-5 * max(1.0, np.abs(r).max())), k
+
+
+def test_a_state_that_is_not_finite_does_not_become_so():
+    # an infinite state stays infinite, or is NaN where the gates' product has left the floats; it is never a number again
+    T, B, H = 600, 1, 70
+    z = np.zeros((T, B, H))
+    for gate in (-30.0, 0.0, 5.0):
+        h = run(z + gate, z + 1, np.full((B, H), np.inf), mg.GLR_MIX)["h"]
+        assert not np.isfinite(h).any() and np.all(h[0] == np.inf)
