@@ -9,8 +9,8 @@
 // The word of a tile and channel is A in the low half and S in the high one, stored by one 64-bit store, so that a reader that
 // sees one sees the other.  All bits set: not written yet (no A is stored so).  A = -0: S does not depend on what was
 // before (a reset, or the state itself: what a tile knows once it knows the state before it).  No other A is -0:
-// no a is negative, so that a product that underflows is +0, and a state that is not finite does not become so again
-// (0 times it is NaN) as long as no reset stands in between.  The state before a tile is always computed as S + A h
+// no a is negative, so that a product that underflows is +0, and a state that is not finite does not become finite
+// again (0 times it is NaN) as long as no reset stands in between.  The state before a tile is always computed as S + A h
 // tile by tile, by the tile itself (glr_join) as by those behind it that find the map and not yet the state (window_state):
 // the two round alike, and the result does not depend on timing.
 //
@@ -26,7 +26,7 @@ namespace mg {
 constexpr int GLR_THREADS = GLR_WAVES * 64;
 constexpr int GLR_CHANNELS = 128;                   // channels of a tile at most
 constexpr int GLR_WORDS = 2048;                     // words looked at at a time: 16 tiles of 128 channels, 32 of 64
-constexpr float LOG2E = 1.44269504088896341f;
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 constexpr unsigned GLR_NONE = 0xffffffffu, GLR_FREE = 0x80000000u;
 
 struct Pair {
@@ -91,19 +91,26 @@ __device__ inline void store_pair(E* p, float a, float b, bool second, bool past
   }
 }
 
-// a and, for GLR_MIX, 1 - a of a gate, both to full precision: with e = exp(-|g|), the smaller of the two is
-// e / (1 + e) at any g, and the larger one 1 minus that.
+// exp(x), x of any size: 2^p with p = x log2(e) as rounded, and e^r for what the rounding left, r = x - p ln 2 (at most 2^-17
+// where 2^p is a number other than 0; where x is infinite, NaN, for which fminf takes the bound).  Without the second factor
+// the result is off by 7 units of 2^-24 at x = -6, 16 at -20, 62 at -80.
+__device__ inline float exp_of(float x) {
+  const float p = LOG2E * x, e = __builtin_amdgcn_exp2f(p);
+  return fmaf(e, fminf(fmaf(-p, LN2, x), 0x1p-16f), e);
+}
+// a and, for GLR_MIX, 1 - a of a gate, both to a few units of their own last place: with e = exp(-|g|), the smaller of the two
+// is e / (1 + e) at any g, and the larger one 1 minus that.
 template <int FORM>
 struct Gate {
   float a, na;
   __device__ inline explicit Gate(float g) {
     if constexpr (FORM == GLR_MIX) {
-      const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(g));
+      const float e = exp_of(-fabsf(g));
       const float s = e * __builtin_amdgcn_rcpf(1.0f + e), l = 1.0f - s;
       a = g < 0.0f ? s : l;
       na = g < 0.0f ? l : s;
     } else {
-      a = __builtin_amdgcn_exp2f(LOG2E * g);
+      a = exp_of(g);
       na = 1.0f;
     }
   }
@@ -116,7 +123,7 @@ struct KeptGate {
   float v, w;
   __device__ inline void set(float g) {
     if constexpr (FORM == GLR_MIX && !BOTH) {
-      const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(g));
+      const float e = exp_of(-fabsf(g));
       v = copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), g);
     } else {
       const Gate<FORM> gt(g);

@@ -32,6 +32,32 @@ def run(gate, value, h0, form, dh=None, dh_last=None):
     return {k: v.double().cpu().numpy() for k, v in out.items()}
 
 
+# The smaller of a and 1 - a is e / (1 + e), e = exp(-|g|): e to 1 unit of its last place and a rounding, the constant ln 2
+# to 2.8e-9 |g|, then a sum (1 rounding), a reciprocal (1 unit) and a product (1 rounding).  In units of 2^-24:
+# 2 + 1 + 0.05 |g| + 1 + 2 + 1; the larger one is 1 minus that.  exp(g) alone: 2 + 0.05 |g| + 3 roundings.
+@pytest.mark.parametrize("lo,hi", [(0, 4), (4, 10), (10, 30), (30, 80)])
+def test_a_and_1_minus_a_are_exact_to_some_units(lo, hi):
+    H = 4096
+    g = np.random.default_rng(lo).uniform(lo, hi, (1, 1, H)).astype(np.float32)
+    one, unit = np.ones((1, 1, H)), 2.0 ** -24
+    for gate in (g, -g):
+        a = 1 / (1 + np.exp(-gate.astype(np.float64)))
+        na = 1 / (1 + np.exp(gate.astype(np.float64)))
+        got = run(gate, 0 * one, one[0], mg.GLR_MIX, one)          # h = a, dvalue = 1 - a, dgate = (1 - a) a (1 - 0)
+        bound = (7 + 0.05 * np.abs(gate)) * unit
+        assert np.all(np.abs(got["h"] - a) <= bound * a)
+        assert np.all(np.abs(got["dvalue"] - na) <= bound * na)
+        assert np.all(np.abs(got["dgate"] - a * na) <= (2 * bound + 2 * unit) * a * na)
+        assert np.all(np.abs(run(gate, one, None, mg.GLR_MIX)["h"] - na) <= bound * na)
+        e = np.exp(gate.astype(np.float64))
+        assert np.all(np.abs(run(gate, 0 * one, one[0], mg.GLR_DECAY)["h"] - e) <= (5 + 0.05 * np.abs(gate)) * unit * e)
+        step = torch.empty(1, H, device=DEV)
+        state = torch.ones(1, H, device=DEV)
+        for form, ref, n in ((mg.GLR_MIX, a, 7), (mg.GLR_DECAY, e, 5)):
+            mg.glr_step(mg.GlrCfg(1, 1, H, form), dev(gate[0]), dev(0 * one[0]), None, None, state, torch.empty_like(state), step)
+            assert np.all(np.abs(step.double().cpu().numpy() - ref[0]) <= ((n + 0.05 * np.abs(gate)) * unit * ref)[0])
+
+
 def test_gates_that_are_not_finite():
     inf, nan = np.inf, np.nan
     g = np.array([inf, -inf, nan, 1e30, -1e30, 300.0, -300.0, 0.0], np.float32)[None, None]
