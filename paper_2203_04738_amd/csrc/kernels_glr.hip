@@ -501,6 +501,12 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) 
     if (p.second) s[1] = h.y;
   }
   if (p.run == runs - 1 && a.h_last && p.chunk == a.s.chunks - 1) {
+    // h_last may be h0 itself, and behind a reset nothing so far has waited for the first tile, whose word says that it has
+    // read h0 (that tile waits for none)
+    if (a.h_last == a.h0 && p.chunk > 0) {
+      const unsigned long long* w = a.words + (long long)p.b * a.s.cols * 2 * p.lanes + p.ch;
+      while ((unsigned)load_word(w) == GLR_NONE) __builtin_amdgcn_s_sleep(1);
+    }
     if (p.has) a.h_last[at] = end.x;
     if (p.second) a.h_last[at + 1] = end.y;
   }

@@ -132,3 +132,20 @@ def test_repeats_beside_other_work_have_the_same_bits(H, form, dtype):
         assert all(torch.isfinite(t.float()).all() for t in out[:2])
         first = first or out
         assert all(torch.equal(x, y) for x, y in zip(first, out)), k
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H", [20, 50, 1030])
+def test_a_state_replaced_in_place_behind_a_reset(H, dtype):
+    # h_last is h0 itself: the last tile, which a reset makes independent of the first, writes what the first reads
+    T, B = 6 * 512, 40
+    (gate, value, _), (h0, _) = problem(H, T, B, H, dtype, "mix")
+    reset = torch.zeros(T, B, dtype=torch.uint8, device=DEV)
+    reset[1400], reset[2900, ::2] = 1, 1
+    cfg = mg.GlrCfg(T, B, H, mg.GLR_MIX, TYPES[dtype][0])
+    ws, h, ref, last = space(mg.glr_workspace_bytes(cfg)), torch.empty_like(gate), torch.empty_like(gate), torch.empty_like(h0)
+    mg.glr_forward(cfg, gate, value, h0, reset, ref, last, None, ws)
+    for _ in range(4):
+        state = h0.clone()
+        mg.glr_forward(cfg, gate, value, state, reset, h, state, None, ws)
+        assert torch.equal(h, ref) and torch.equal(state, last)
