@@ -18,6 +18,9 @@
  * reproducible.  Buffers that a call writes must not overlap any other buffer of
  * the call unless its comment says so.  A workspace of 0 bytes may be NULL; other
  * workspaces are 16-byte aligned; calls that share one are ordered on one stream.
+ * A call whose launches would take 2^32 threads or more is refused with MGRIT_E_SIZE: from 2^23 tiles on for a sequence
+ * (128 to 512 steps of 32 to 128 channels of one batch row each), 2^22 for rows of logits (2^15 entries each) or tokens to
+ * quantise.
  * Nothing is kept in a workspace from call to call.
  */
 #ifndef MGRIT_OPS_H

@@ -939,6 +939,12 @@ static RowShape segments(int V, int size, bool aligned) {
 // rows 33.9 : 39.8; 32768 floats, 512 rows 19.3 : 17.9, 2048 rows 48.2 : 50.4; 131072 bf16 (4 segments a row), 64 rows
 // 18.2 : 14.9, 192 rows 24.9 : 23.6, 256 rows 28.1 : 28.4.
 constexpr long long STREAM_SEGMENTS = 768;
+// Whether rows, or their segments, can be a team each in one launch.
+static bool teams_launchable(const logits_cfg& c, int size, bool aligned) {
+  const int waves = team_waves(c.V, size, aligned);
+  if (waves == 1) return launchable(((long long)c.N + 3) / 4, 256);
+  return launchable((long long)c.N * segments(c.V, size, aligned).segs, waves == 4 ? 256 : 1024);
+}
 size_t logits_workspace(const logits_cfg& c) {
   const int size = elem_size(c.dtype);
   // (what is aligned is known with the arrays only: the larger of the two)
@@ -968,6 +974,9 @@ static hipError_t logprobs_start(const LogitsArgs& a, hipStream_t s) {
   const RowShape cut = segments(a.c.V, sizeof(E), aligned);
   const bool stream = (long long)N * cut.segs >= STREAM_SEGMENTS;
   const dim3 grid(N * (unsigned)cut.segs);
+  // (a row's segments, or four rows in one workgroup)
+  if (!launchable(waves == 1 ? (N + 3) / 4 : (long long)N * cut.segs, waves == 1 || waves == 4 || stream ? 256 : 1024))
+    return TOO_LARGE;
   switch (waves) {
     case 1:
       hipLaunchKernelGGL((logprobs_kernel<E, 1, false>), dim3((N + 3) / 4), dim3(256), 0, s, r);
@@ -1022,6 +1031,7 @@ static hipError_t grad_start(const LogitsArgs& a, const float* stats, hipStream_
   d.stats_in = stats;
   const bool aligned = rows_aligned(a.logits, a.c.ld, sizeof(E));
   const unsigned N = (unsigned)a.c.N;
+  if (!teams_launchable(a.c, sizeof(E), aligned)) return TOO_LARGE;
   // (the boundary of a row moves its segments: the whole row has to be within the last one)
   switch (team_waves(a.c.V, sizeof(E), aligned)) {
     case 1:
@@ -1047,6 +1057,7 @@ static hipError_t distill_start(const LogitsArgs& a, hipStream_t s) {
   DistillArgs d = distill_args(a);
   const bool aligned = rows_aligned(a.logits, a.c.ld, sizeof(E));
   const unsigned N = (unsigned)a.c.N;
+  if (!teams_launchable(a.c, sizeof(E), aligned)) return TOO_LARGE;
   switch (team_waves(a.c.V, sizeof(E), aligned)) {
     case 1:
       hipLaunchKernelGGL((distill_kernel<E, 1>), dim3((N + 3) / 4), dim3(256), 0, s, d);

@@ -142,23 +142,38 @@ __global__ __launch_bounds__(1024) void q8_quantize_long_kernel(Q8Args a) {
 
 // Teams that hold the row.  One wave per row : four, 2048 bf16, us: 512 rows 4.1 : 3.3, 2048 rows 5.6 : 5.9, 8192 rows
 // 14.2 : 16.6, 32768 rows 42.5 : 57; rows of 4096 take four (4096 rows 15.2 : 13.4).
+struct QuantTeam {
+  int waves, loads;                                  // of 16 bytes a thread; 0: the row is read twice
+};
+static QuantTeam quant_team(const q8_cfg& c) {
+  const int per = c.dtype == MGRIT_F32 ? 4 : 8, pad = q8_pad(c.K);
+  if (pad <= 2 * 64 * per) return {1, 2};
+  if (pad <= 4 * 64 * per && c.M >= 2048) return {1, 4};
+  if (pad <= 4 * 256 * per) return {4, 4};
+  if (pad <= 4 * 1024 * per) return {16, 4};
+  return {16, 0};
+}
+static bool quantize_launchable(const q8_cfg& c) {
+  const int waves = quant_team(c).waves;
+  return waves == 1 ? launchable(((long long)c.M + 3) / 4, 256) : launchable(c.M, waves * 64);
+}
 template <typename E>
 static void quantize_start(const Q8Args& a, hipStream_t s) {
-  constexpr int PER = 16 / (int)sizeof(E);
-  const int pad = q8_pad(a.c.K);
   const unsigned M = (unsigned)a.c.M;
-  if (pad <= 2 * 64 * PER)
+  const QuantTeam t = quant_team(a.c);
+  if (t.waves == 1 && t.loads == 2)
     hipLaunchKernelGGL((q8_quantize_kernel<E, 1, 2>), dim3((M + 3) / 4), dim3(256), 0, s, a);
-  else if (pad <= 4 * 64 * PER && M >= 2048)
+  else if (t.waves == 1)
     hipLaunchKernelGGL((q8_quantize_kernel<E, 1, 4>), dim3((M + 3) / 4), dim3(256), 0, s, a);
-  else if (pad <= 4 * 256 * PER)
+  else if (t.waves == 4)
     hipLaunchKernelGGL((q8_quantize_kernel<E, 4, 4>), dim3(M), dim3(256), 0, s, a);
-  else if (pad <= 4 * 1024 * PER)
+  else if (t.loads > 0)
     hipLaunchKernelGGL((q8_quantize_kernel<E, 16, 4>), dim3(M), dim3(1024), 0, s, a);
   else
     hipLaunchKernelGGL(q8_quantize_long_kernel<E>, dim3(M), dim3(1024), 0, s, a);
 }
 hipError_t launch_q8_quantize(const Q8Args& a, hipStream_t s) {
+  if (!quantize_launchable(a.c)) return TOO_LARGE;
   if (a.c.dtype == MGRIT_F32) quantize_start<float>(a, s);
   else if (a.c.dtype == MGRIT_BF16) quantize_start<Bf16>(a, s);
   else quantize_start<F16>(a, s);
@@ -436,7 +451,7 @@ __global__ __launch_bounds__(256) void q8_tile_kernel(Q8Args a, int tiles_m, int
 
 template <typename E, int TM, int TN>
 static void tile_start(const Q8Args& a, hipStream_t s) {
-  const int tm = (a.c.M + TM - 1) / TM, tn = (a.c.N + TN - 1) / TN;
+  const int tm = (int)(((long long)a.c.M + TM - 1) / TM), tn = (int)(((long long)a.c.N + TN - 1) / TN);
   hipLaunchKernelGGL((q8_tile_kernel<E, TM, TN>), dim3((unsigned)tm * (unsigned)tn), dim3(256), 0, s, a, tm, tn);
 }
 // Which product.  Measured with quantisation, K = 2048, bf16, us on the GPU:
@@ -445,25 +460,38 @@ static void tile_start(const Q8Args& a, hipStream_t s) {
 //  - tiles of 64 : 128 : 256.  1024 x 2048 17 : 21 : 44, 2048 x 2048 26 : 25 : 48, 4096 x 2048 47 : 37 : 53, 6144 x 2048
 //    69 : 52 : 57, 8192 x 2048 85 : 68 : 63, 1024 x 8192 49 : 33 : 48.  That is 20 us per 1024 tiles of 64 (four
 //    of them share a CU), 27 per 512 of 128 (two) and 50 per round of 256 of 256 (one), 7 and 19 at least.
+static double tiles_of(const q8_cfg& c, long long t) {
+  return (double)((c.M + t - 1) / t) * (double)((c.N + t - 1) / t);
+}
+static int product_tile(const q8_cfg& c) {                   // 0: few tokens
+  const long long blocks = ((long long)c.M + 15) / 16;
+  if (blocks == 1 || (blocks <= 4 && blocks * c.N <= 16384)) return 0;
+  const double c64 = std::max(7.0, tiles_of(c, 64) / 1024 * 20), c128 = std::max(19.0, tiles_of(c, 128) / 512 * 27);
+  const double c256 = std::ceil(tiles_of(c, 256) / 256) * 50;
+  return c256 <= c128 && c256 <= c64 ? 256 : c128 <= c64 ? 128 : 64;
+}
+static bool product_launchable(const q8_cfg& c) {
+  const int tile = product_tile(c);
+  return launchable(tile ? (long long)tiles_of(c, tile) : ((long long)c.N + 15) / 16, 256);
+}
 template <typename E>
 static void q8_start(const Q8Args& a, hipStream_t s) {
-  const unsigned groups = (unsigned)(a.c.N + 15) / 16;
-  const int blocks = (int)(((long long)a.c.M + 15) / 16);
-  if (blocks == 1 || (blocks <= 4 && (long long)blocks * a.c.N <= 16384)) {
-    switch (blocks) {
+  const int tile = product_tile(a.c);
+  if (tile == 0) {
+    const unsigned groups = ((unsigned)a.c.N + 15) / 16;
+    switch ((a.c.M + 15) / 16) {
       case 1: hipLaunchKernelGGL((q8_few_kernel<E, 1>), dim3(groups), dim3(256), 0, s, a); break;
       case 2: hipLaunchKernelGGL((q8_few_kernel<E, 2>), dim3(groups), dim3(256), 0, s, a); break;
       case 3: hipLaunchKernelGGL((q8_few_kernel<E, 3>), dim3(groups), dim3(256), 0, s, a); break;
       default: hipLaunchKernelGGL((q8_few_kernel<E, 4>), dim3(groups), dim3(256), 0, s, a);
     }
-    return;
+  } else if (tile == 256) {
+    tile_start<E, 256, 256>(a, s);
+  } else if (tile == 128) {
+    tile_start<E, 128, 128>(a, s);
+  } else {
+    tile_start<E, 64, 64>(a, s);
   }
-  auto tiles = [&](long long t) { return (double)((a.c.M + t - 1) / t) * (double)((a.c.N + t - 1) / t); };
-  const double c64 = std::max(7.0, tiles(64) / 1024 * 20), c128 = std::max(19.0, tiles(128) / 512 * 27);
-  const double c256 = std::ceil(tiles(256) / 256) * 50;
-  if (c256 <= c128 && c256 <= c64) tile_start<E, 256, 256>(a, s);
-  else if (c128 <= c64) tile_start<E, 128, 128>(a, s);
-  else tile_start<E, 64, 64>(a, s);
 }
 // LDS of the product that quantises the tokens itself, 0 where that has a launch of its own.  One launch : two, K = 2048, us
 // on the GPU: 1 x 2048 6.3 : 6.3, 8 x 2048 7.4 : 6.9, 16 x 2048 10.9 : 7.2, 1 x 8192 (K = 4096) 10.5 : 10.9, 8 x 8192 (K =
@@ -472,7 +500,7 @@ static void q8_start(const Q8Args& a, hipStream_t s) {
 static size_t fused_lds(const Q8Args& a) {
   const int pad = q8_pad(a.c.K), held = 8 * 64 * (a.c.dtype == MGRIT_F32 ? 4 : 8);
   const size_t need = (size_t)a.c.M * (pad + 16);
-  const long long rows = (long long)a.c.M * ((a.c.N + 15) / 16);
+  const long long rows = a.c.M * (((long long)a.c.N + 15) / 16);
   return a.c.M <= 16 && rows <= 1024 && pad <= held && need <= FUSED_LDS ? need : 0;
 }
 hipError_t launch_q8_linear(const Q8Args& a, hipStream_t s) {
@@ -483,6 +511,7 @@ hipError_t launch_q8_linear(const Q8Args& a, hipStream_t s) {
     else hipLaunchKernelGGL(q8_fused_kernel<F16>, g, t, lds, s, a);
     return hipGetLastError();
   }
+  if (!product_launchable(a.c)) return TOO_LARGE;
   const hipError_t e = launch_q8_quantize(a, s);
   if (e != hipSuccess) return e;
   if (a.c.dtype == MGRIT_F32) q8_start<float>(a, s);

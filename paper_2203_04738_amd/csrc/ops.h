@@ -12,6 +12,11 @@ namespace mg {
 // 50021 floats behind the forward pass 130 : 103; 8-bit product of 32768 x 2048 x 2048 224 : 216.
 inline bool stores_past_caches(double bytes) { return bytes >= 128e6; }
 
+// What a launch can be: fewer than 2^32 threads in all.
+inline bool launchable(long long groups, int threads) { return groups * threads <= 0xffffffffLL; }
+// What a launch function returns, before it has launched anything, for a call whose launches would be larger.
+constexpr hipError_t TOO_LARGE = hipErrorInvalidConfiguration;
+
 // ---- gated linear recurrence (kernels_glr.hip)
 // A workgroup of GLR_WAVES waves covers one row of the batch, 2 * lanes channels (two per lane) and GLR_WAVES * (64 / lanes) *
 // run steps: a wave's lanes hold 64 / lanes runs.  Forward: runs of 16 steps over up to 128 channels; the adjoint, which

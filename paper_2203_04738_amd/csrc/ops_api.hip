@@ -11,17 +11,25 @@ static bool off(const void* p, size_t n) { return (uintptr_t)p % n != 0; }
 static bool is_dtype(int d) { return d == MGRIT_F32 || d == MGRIT_BF16 || d == MGRIT_F16; }
 static size_t elem_bytes(int d) { return d == MGRIT_F32 ? 4 : 2; }
 static size_t up(size_t v, size_t n) { return (v + n - 1) / n * n; }
+static int code_of(hipError_t e) {
+  return e == hipSuccess ? MGRIT_OK : e == TOO_LARGE ? MGRIT_E_SIZE : MGRIT_E_LAUNCH;
+}
 
 // ---- gated linear recurrence
-static int glr_check(const glr_cfg* c) {
+static int glr_sizes(const glr_cfg* c) {
   if (!c) return MGRIT_E_NULL;
   if (c->T < 1 || c->B < 1 || c->H < 1) return MGRIT_E_SIZE;
   if ((long long)c->T * c->B > (1LL << 30) || (long long)c->B * c->H > (1LL << 30)) return MGRIT_E_SIZE;
   if (c->form != GLR_MIX && c->form != GLR_DECAY) return MGRIT_E_ENUM;
-  if (!is_dtype(c->dtype)) return MGRIT_E_ENUM;
-  for (int backward = 0; backward < 2; ++backward) {                             // workgroups of a launch
+  return is_dtype(c->dtype) ? MGRIT_OK : MGRIT_E_ENUM;
+}
+// Sequences: the tiles, and the threads that clear their words, are one launch each.
+static int glr_check(const glr_cfg* c) {
+  const int rc = glr_sizes(c);
+  if (rc) return rc;
+  for (int backward = 0; backward < 2; ++backward) {
     const GlrShape s = glr_shape(*c, backward);
-    if ((long long)s.chunks * s.cols * c->B > 0x7fffffffLL || (s.words + 255) / 256 > 0x7fffffffLL)
+    if (!launchable((long long)s.chunks * s.cols * c->B, GLR_WAVES * 64) || !launchable((s.words + 511) / 512, 256))
       return MGRIT_E_SIZE;
   }
   return MGRIT_OK;
@@ -70,7 +78,7 @@ static int glr_space(const glr_cfg& c, const GlrShape& s, void* ws, size_t n, Gl
 static int logits_check(const logits_cfg* c) {
   if (!c) return MGRIT_E_NULL;
   if (c->N < 1 || c->V < 1 || c->V > (1 << 20) || c->K < 0) return MGRIT_E_SIZE;
-  if ((long long)c->N * 33 > 0x7fffffffLL) return MGRIT_E_SIZE;                 // workgroups of a launch
+  if ((long long)c->N * 33 > 0x7fffffffLL) return MGRIT_E_SIZE;                 // segments of all rows
   if (c->ld < c->V || c->ld > (1LL << 40)) return MGRIT_E_SIZE;
   if (!is_dtype(c->dtype)) return MGRIT_E_ENUM;
   if (!std::isfinite(c->temperature) || c->temperature <= 0.f || !std::isfinite(1.0f / c->temperature))
@@ -153,7 +161,7 @@ int glr_forward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, c
   a.saved = (float*)saved;
   a.past = stores_past_caches(3.0 * elem_bytes(cfg->dtype) * cfg->T * cfg->B * cfg->H);
   (void)hipGetLastError();   // an error left by earlier, unrelated work is not this call's
-  return launch_glr_forward(a, (hipStream_t)stream) == hipSuccess ? MGRIT_OK : MGRIT_E_LAUNCH;
+  return code_of(launch_glr_forward(a, (hipStream_t)stream));
 }
 
 int glr_backward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, const uint8_t* reset,
@@ -183,13 +191,13 @@ int glr_backward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, 
   a.dh0 = dh0;
   a.past = stores_past_caches(5.0 * elem_bytes(cfg->dtype) * cfg->T * cfg->B * cfg->H);
   (void)hipGetLastError();
-  return launch_glr_backward(a, (hipStream_t)stream) == hipSuccess ? MGRIT_OK : MGRIT_E_LAUNCH;
+  return code_of(launch_glr_backward(a, (hipStream_t)stream));
 }
 
 int glr_step(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, const int32_t* slots,
              int32_t n_slots, const uint8_t* reset, const float* state_in, float* state_out, const glr_seq* h,
              void* stream) {
-  int rc = glr_check(cfg);
+  int rc = glr_sizes(cfg);
   if (rc) return rc;
   if (cfg->T != 1 || n_slots < 1 || (!slots && n_slots < cfg->B)) return MGRIT_E_SIZE;
   const glr_seq* in[2] = {gate, value};
@@ -200,7 +208,7 @@ int glr_step(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, cons
   if (off(state_in, 4) || off(state_out, 4) || off(slots, 4)) return MGRIT_E_ALIGN;
   GlrStepArgs a{*cfg, *gate, *value, *h, slots, n_slots, reset, state_in, state_out};
   (void)hipGetLastError();
-  return launch_glr_step(a, (hipStream_t)stream) == hipSuccess ? MGRIT_OK : MGRIT_E_LAUNCH;
+  return code_of(launch_glr_step(a, (hipStream_t)stream));
 }
 
 int logits_workspace_bytes(const logits_cfg* cfg, size_t* bytes) {
@@ -233,7 +241,7 @@ int token_logprobs(const logits_cfg* cfg, const void* logits, const int64_t* tok
   a.top_ids = top_ids;
   a.workspace = (char*)workspace;
   (void)hipGetLastError();
-  return launch_token_logprobs(a, (hipStream_t)stream) == hipSuccess ? MGRIT_OK : MGRIT_E_LAUNCH;
+  return code_of(launch_token_logprobs(a, (hipStream_t)stream));
 }
 
 int distill_topk(const logits_cfg* cfg, const void* logits, const int64_t* ids, const float* teacher,
@@ -255,7 +263,7 @@ int distill_topk(const logits_cfg* cfg, const void* logits, const int64_t* ids, 
   a.dlogits = dlogits;
   a.workspace = (char*)workspace;
   (void)hipGetLastError();
-  return launch_distill(a, (hipStream_t)stream) == hipSuccess ? MGRIT_OK : MGRIT_E_LAUNCH;
+  return code_of(launch_distill(a, (hipStream_t)stream));
 }
 
 int distill_topk_backward(const logits_cfg* cfg, const void* logits, const int64_t* ids, const float* teacher,
@@ -273,7 +281,7 @@ int distill_topk_backward(const logits_cfg* cfg, const void* logits, const int64
   a.stats_in = stats;
   a.dlogits = dlogits;
   (void)hipGetLastError();
-  return launch_distill_grad(a, (hipStream_t)stream) == hipSuccess ? MGRIT_OK : MGRIT_E_LAUNCH;
+  return code_of(launch_distill_grad(a, (hipStream_t)stream));
 }
 
 int64_t q8_row_bytes(int32_t K) { return ((int64_t)K + 127) / 128 * 128; }
@@ -297,7 +305,7 @@ int q8_quantize(const q8_cfg* cfg, const void* x, int8_t* q, float* scale, void*
   a.q = q;
   a.scale = scale;
   (void)hipGetLastError();
-  return launch_q8_quantize(a, (hipStream_t)stream) == hipSuccess ? MGRIT_OK : MGRIT_E_LAUNCH;
+  return code_of(launch_q8_quantize(a, (hipStream_t)stream));
 }
 
 int q8_linear(const q8_cfg* cfg, const void* x, const int8_t* w_q, const float* w_scale, const float* bias,
@@ -320,7 +328,7 @@ int q8_linear(const q8_cfg* cfg, const void* x, const int8_t* w_q, const float* 
   a.q = (int8_t*)workspace + q8_scales(*cfg);
   a.past = stores_past_caches((double)cfg->M * ((double)e * cfg->K + (double)e * cfg->N));
   (void)hipGetLastError();
-  return launch_q8_linear(a, (hipStream_t)stream) == hipSuccess ? MGRIT_OK : MGRIT_E_LAUNCH;
+  return code_of(launch_q8_linear(a, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -149,3 +149,15 @@ def test_a_state_replaced_in_place_behind_a_reset(H, dtype):
         state = h0.clone()
         mg.glr_forward(cfg, gate, value, state, reset, h, state, None, ws)
         assert torch.equal(h, ref) and torch.equal(state, last)
+
+
+def test_as_many_rows_as_a_launch_takes():
+    T, B, H = 2, (1 << 23) - 1, 2                           # a tile each: 2^32 - 512 threads
+    gate, value = torch.randn(T, B, H, device=DEV), torch.randn(T, B, H, device=DEV)
+    h, last, _ = forward(gate, value, None, "f32", "mix")
+    a = torch.sigmoid(gate)
+    ref = (1 - a) * value
+    ref[1] += a[1] * ref[0]
+    assert torch.all((h - ref).abs() <= 2.0 ** -20) and torch.equal(last, h[1])
+    with pytest.raises(mg.MgritGruError):
+        mg.glr_workspace_bytes(mg.GlrCfg(T, B + 1, H))
