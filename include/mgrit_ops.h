@@ -107,7 +107,7 @@ typedef struct {
   int32_t N, V;         /* rows >= 1; entries 1 .. 2^20 */
   int32_t K;            /* entries per row of the top / teacher arrays */
   int32_t dtype;
-  float temperature;    /* finite, > 0 */
+  float temperature;    /* finite, > 0, log2(e) / temperature finite (from 4.3e-39 on) */
   int64_t ld, ld_grad;  /* row strides of logits and dlogits */
 } logits_cfg;
 

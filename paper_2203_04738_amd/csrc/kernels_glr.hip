@@ -26,7 +26,6 @@ namespace mg {
 constexpr int GLR_THREADS = GLR_WAVES * 64;
 constexpr int GLR_CHANNELS = 128;                   // channels of a tile at most
 constexpr int GLR_WORDS = 2048;                     // words looked at at a time: 16 tiles of 128 channels, 32 of 64
-constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 constexpr unsigned GLR_NONE = 0xffffffffu, GLR_FREE = 0x80000000u;
 
 struct Pair {

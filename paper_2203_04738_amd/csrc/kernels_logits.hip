@@ -18,7 +18,6 @@
 
 namespace mg {
 
-constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 typedef unsigned long long u64;
 

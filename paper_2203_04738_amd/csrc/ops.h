@@ -6,6 +6,8 @@
 
 namespace mg {
 
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+
 // Whether a call moves so much that what it writes would not stay in the last-level cache (256 MB) for the next kernel
 // anyway: it is then stored past the caches, which leaves them to what the call reads.  Plain : past them, us:
 // recurrence 128 x 100 x 1000 floats 93 : 88 (forward 154 MB, backward 256 MB), 16384 x 4 x 1024 bf16 282 : 272; gradient of 1003 x

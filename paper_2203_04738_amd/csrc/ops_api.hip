@@ -81,7 +81,8 @@ static int logits_check(const logits_cfg* c) {
   if ((long long)c->N * 33 > 0x7fffffffLL) return MGRIT_E_SIZE;                 // segments of all rows
   if (c->ld < c->V || c->ld > (1LL << 40)) return MGRIT_E_SIZE;
   if (!is_dtype(c->dtype)) return MGRIT_E_ENUM;
-  if (!std::isfinite(c->temperature) || c->temperature <= 0.f || !std::isfinite(1.0f / c->temperature))
+  // (the exponents' factor log2(e) / t has to be a float)
+  if (!std::isfinite(c->temperature) || c->temperature <= 0.f || !std::isfinite(LOG2E * (1.0f / c->temperature)))
     return MGRIT_E_SIZE;
   return MGRIT_OK;
 }
