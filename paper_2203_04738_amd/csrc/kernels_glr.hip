@@ -736,11 +736,7 @@ __global__ __launch_bounds__(256) void glr_step_kernel(GlrStepArgs a) {
 
 template <typename E>
 static void glr_step_start(const GlrStepArgs& a, hipStream_t s) {
-  auto one = [&](glr_seq q) {
-    q.stride_t = 0;
-    return pairs<E>(q, a.c.H);
-  };
-  const bool al = one(a.gate) && one(a.value) && one(a.h);
+  const bool al = pairs<E>(a.gate, a.c.H) && pairs<E>(a.value, a.c.H) && pairs<E>(a.h, a.c.H);
   const dim3 g((unsigned)(((long long)a.c.B * ((a.c.H + 1) / 2) + 255) / 256)), t(256);
   if (a.c.form == GLR_MIX) {
     if (al) hipLaunchKernelGGL((glr_step_kernel<E, true, GLR_MIX>), g, t, 0, s, a);

@@ -60,7 +60,7 @@ hipError_t launch_glr_backward(const GlrArgs& a, hipStream_t s);
 
 struct GlrStepArgs {
   glr_cfg c;
-  glr_seq gate, value, h;
+  glr_seq gate, value, h;   // (stride_t 0)
   const int32_t* slots;
   int n_slots;
   const uint8_t* reset;

@@ -201,13 +201,16 @@ int glr_step(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, cons
   int rc = glr_sizes(cfg);
   if (rc) return rc;
   if (cfg->T != 1 || n_slots < 1 || (!slots && n_slots < cfg->B)) return MGRIT_E_SIZE;
-  const glr_seq* in[2] = {gate, value};
-  for (const glr_seq* q : in)
-    if ((rc = seq_check(*cfg, q, false))) return rc;
-  if ((rc = seq_check(*cfg, h, true))) return rc;
+  glr_seq rows[3] = {};                               // gate, value, h
+  const glr_seq* given[3] = {gate, value, h};
+  for (int i = 0; i < 3; ++i) {
+    if (given[i]) rows[i] = *given[i];
+    rows[i].stride_t = 0;
+    if ((rc = seq_check(*cfg, &rows[i], i == 2))) return rc;
+  }
   if (!state_in || !state_out) return MGRIT_E_NULL;
   if (off(state_in, 4) || off(state_out, 4) || off(slots, 4)) return MGRIT_E_ALIGN;
-  GlrStepArgs a{*cfg, *gate, *value, *h, slots, n_slots, reset, state_in, state_out};
+  GlrStepArgs a{*cfg, rows[0], rows[1], rows[2], slots, n_slots, reset, state_in, state_out};
   (void)hipGetLastError();
   return code_of(launch_glr_step(a, (hipStream_t)stream));
 }

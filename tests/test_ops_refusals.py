@@ -17,3 +17,34 @@ def test_temperatures_whose_exponents_are_floats(t, ok):
     with np.errstate(over="ignore"):
         assert np.isfinite(np.float32(1.442695) / np.float32(t)) == ok
     assert ops._lib().logits_workspace_bytes(ctypes.byref(cfg), ctypes.byref(n)) == (0 if ok else SIZE)
+
+
+def test_a_step_does_not_read_the_stride_of_time(tmp_path):
+    """(on the host's runtime: nothing may be refused for it, nothing launched differently)"""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = str(tmp_path / "libfake_hip.so")
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-o", out,
+                           os.path.join(root, "tests", "fake_hip_runtime.cpp")])
+    code = """
+import ctypes, sys
+ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
+from ctypes import byref
+from paper_2203_04738_amd import binding, ops
+L = ops._prototypes(binding.lib())
+for t in (0, 3, -7, 1 << 62, -1 << 63):
+    s = [byref(ops.GlrSeq((i + 1) << 40, t, 8)) for i in range(3)]
+    print("returned", L.glr_step(byref(ops.GlrCfg(1, 4, 8)), s[0], s[1], None, 4, None, 5 << 40, 6 << 40, s[2], None))
+for i in range(3):
+    s = [byref(ops.GlrSeq((i + 1) << 40, 0, 8)) for i in range(3)]
+    s[i] = None
+    print("returned", L.glr_step(byref(ops.GlrCfg(1, 4, 8)), s[0], s[1], None, 4, None, 5 << 40, 6 << 40, s[2], None))
+"""
+    r = subprocess.run([sys.executable, "-c", code, out], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
+    lines = r.stdout.splitlines()
+    assert [int(n.split()[1]) for n in lines if n.startswith("returned")] == [0] * 5 + [-1] * 3
+    assert [n for n in lines if n.startswith("launched")] == [
+        "launched 1 void mg::glr_step_kernel<float, true, 0>(mg::GlrStepArgs)"] * 5
