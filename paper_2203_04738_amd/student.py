@@ -119,7 +119,9 @@ class Served:
         self.layers = [self._pack(W) + (b.clone(),) for W, b in student.params]
         self.head = self._pack(student.head[0]) + (student.head[1].clone(),)
         dev = student.head[0].device
-        self.state = [torch.zeros(slots, self.H, device=dev) for _ in self.layers]
+        # (a row more than the pool has, for what `read` leaves of idle rows)
+        self._pool = [torch.zeros(slots + 1, self.H, device=dev) for _ in self.layers]
+        self.state = [p[:slots] for p in self._pool]
 
     @staticmethod
     def _pack(W):
@@ -141,18 +143,20 @@ class Served:
         return y
 
     def read(self, x, slots):
-        """Takes prompts x[T,B,D] in from zero states and leaves their states in the pool rows `slots` (int32 [B]);
-        returns the logits [B,V] behind their last step."""
+        """Takes prompts x[T,B,D] in from zero states and leaves their states in the pool rows `slots` (int32 [B]; a row whose slot
+        is outside the pool is idle, as in `next`: no state is touched); returns the logits [B,V] behind their last step."""
         import torch
         T, B, H = x.shape[0], x.shape[1], self.H
+        n = len(self.state[0])
+        to = torch.where((slots >= 0) & (slots < n), slots, n).long()
         cfg = _o.GlrCfg(T, B, H)
         ws = _empty(_o.glr_workspace_bytes(cfg), x)
         h = x
-        for layer, state in zip(self.layers, self.state):
+        for layer, pool in zip(self.layers, self._pool):
             gv = self._linear(h.reshape(T * B, -1), layer).view(T, B, 2 * H)
             h, last = torch.empty(T, B, H, device=x.device), torch.empty(B, H, device=x.device)
             _o.glr_forward(cfg, gv[..., :H], gv[..., H:], None, None, h, last, None, ws)
-            state[slots.long()] = last
+            pool.index_copy_(0, to, last)
         return self._linear(h[-1], self.head)
 
     def next(self, x, slots):
