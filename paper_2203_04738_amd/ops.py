@@ -37,7 +37,7 @@ class GlrSeq(ctypes.Structure):
 
 
 class LogitsCfg(ctypes.Structure):
-    """Mirror of ``logits_cfg``; the row strides are filled in from the tensors of a call."""
+    """Mirror of ``logits_cfg``; a call passes the row strides of its tensors, in a copy."""
 
     _fields_ = (_fields(ctypes.c_int32, ("N", "V", "K", "dtype")) + [("temperature", ctypes.c_float)]
                 + _fields(ctypes.c_int64, ("ld", "ld_grad")))
@@ -47,7 +47,7 @@ class LogitsCfg(ctypes.Structure):
 
 
 class Q8Cfg(ctypes.Structure):
-    """Mirror of ``q8_cfg``; the row strides are filled in from the tensors of a call."""
+    """Mirror of ``q8_cfg``; a call passes the row strides of its tensors, in a copy."""
 
     _fields_ = _fields(ctypes.c_int32, ("M", "N", "K", "dtype")) + _fields(ctypes.c_int64, ("ldx", "ldy"))
 
@@ -227,13 +227,21 @@ def _ld(t, cols):
     return t.stride(0)
 
 
+def _strided(cfg, **strides):
+    """A copy of a configuration with the row strides of a call: the caller's own may be in another thread's call."""
+    c = type(cfg).from_buffer_copy(cfg)
+    for name, ld in strides.items():
+        setattr(c, name, ld)
+    return c
+
+
 def _i64(t, name, *shape):
     return t, name, _torch.int64, shape, _DENSE
 
 
 def token_logprobs(cfg, logits, tokens, logp, entropy, top_logp, top_ids, workspace) -> None:
     N, V, K = cfg.N, cfg.V, cfg.K
-    cfg.ld = _ld(logits, V)
+    cfg = _strided(cfg, ld=_ld(logits, V))
     _call("token_logprobs", cfg, _matrix(cfg, logits, "logits", N, V), _i64(tokens, "tokens", N),
           _f32(logp, "logp", N), _f32(entropy, "entropy", N), _f32(top_logp, "top_logp", N, K),
           _i64(top_ids, "top_ids", N, K), *_bytes_of(workspace, "workspace"))
@@ -241,7 +249,7 @@ def token_logprobs(cfg, logits, tokens, logp, entropy, top_logp, top_ids, worksp
 
 def distill_topk(cfg, logits, ids, teacher, weight, loss, stats, dlogits, workspace) -> None:
     N, V, K = cfg.N, cfg.V, cfg.K
-    cfg.ld, cfg.ld_grad = _ld(logits, V), _ld(dlogits, V)
+    cfg = _strided(cfg, ld=_ld(logits, V), ld_grad=_ld(dlogits, V))
     _call("distill_topk", cfg, _matrix(cfg, logits, "logits", N, V), _i64(ids, "ids", N, K),
           _f32(teacher, "teacher", N, K), _f32(weight, "weight", N), _f32(loss, "loss", N),
           _f32(stats, "stats", N, 2), _matrix(cfg, dlogits, "dlogits", N, V), *_bytes_of(workspace, "workspace"))
@@ -249,7 +257,7 @@ def distill_topk(cfg, logits, ids, teacher, weight, loss, stats, dlogits, worksp
 
 def distill_topk_backward(cfg, logits, ids, teacher, stats, dloss, dlogits) -> None:
     N, V, K = cfg.N, cfg.V, cfg.K
-    cfg.ld, cfg.ld_grad = _ld(logits, V), _ld(dlogits, V)
+    cfg = _strided(cfg, ld=_ld(logits, V), ld_grad=_ld(dlogits, V))
     _call("distill_topk_backward", cfg, _matrix(cfg, logits, "logits", N, V), _i64(ids, "ids", N, K),
           _f32(teacher, "teacher", N, K), _f32(stats, "stats", N, 2), _f32(dloss, "dloss", N),
           _matrix(cfg, dlogits, "dlogits", N, V))
@@ -267,14 +275,14 @@ def q8_workspace_bytes(cfg: Q8Cfg) -> int:
 def q8_quantize(cfg, x, q, scale) -> None:
     """Rows x[M,K] -> q[M, q8_row_bytes(K)] int8, scale[M]."""
     M, K = cfg.M, cfg.K
-    cfg.ldx = _ld(x, K)
+    cfg = _strided(cfg, ldx=_ld(x, K))
     _call("q8_quantize", cfg, _matrix(cfg, x, "x", M, K), (q, "q", _torch.int8, (M, q8_row_bytes(K)), _DENSE),
           _f32(scale, "scale", M))
 
 
 def q8_linear(cfg, x, w_q, w_scale, bias, y, workspace) -> None:
     M, N, K = cfg.M, cfg.N, cfg.K
-    cfg.ldx, cfg.ldy = _ld(x, K), _ld(y, N)
+    cfg = _strided(cfg, ldx=_ld(x, K), ldy=_ld(y, N))
     _call("q8_linear", cfg, _matrix(cfg, x, "x", M, K), (w_q, "w_q", _torch.int8, (N, q8_row_bytes(K)), _DENSE),
           _f32(w_scale, "w_scale", N), _f32(bias, "bias", N), _matrix(cfg, y, "y", M, N),
           *_bytes_of(workspace, "workspace"))

@@ -48,3 +48,38 @@ for i in range(3):
     assert [int(n.split()[1]) for n in lines if n.startswith("returned")] == [0] * 5 + [-1] * 3
     assert [n for n in lines if n.startswith("launched")] == [
         "launched 1 void mg::glr_step_kernel<float, true, 0>(mg::GlrStepArgs)"] * 5
+
+
+def test_a_call_leaves_the_configuration_alone():
+    # (host memory: every call ends in an error, behind its look at the strides)
+    import torch
+    z = torch.zeros
+    ws, ids = z(0, dtype=torch.uint8), z(3, 2, dtype=torch.int64)
+    x, grad = z(3, 20)[:, :10], z(3, 30)[:, :10]
+    lc, qc = mg.LogitsCfg(3, 10, 2), mg.Q8Cfg(3, 5, 10)
+    w, y = z(5, 128, dtype=torch.int8), z(3, 9)[:, :5]
+    for call in (lambda: mg.token_logprobs(lc, x, None, None, z(3), z(3, 2), ids, ws),
+                 lambda: mg.distill_topk(lc, x, ids, z(3, 2), None, z(3), None, grad, ws),
+                 lambda: mg.distill_topk_backward(lc, x, ids, z(3, 2), z(3, 2), None, grad),
+                 lambda: mg.q8_quantize(qc, x, z(3, 128, dtype=torch.int8), z(3)),
+                 lambda: mg.q8_linear(qc, x, w, z(5), None, y, ws)):
+        with pytest.raises(TypeError):
+            call()
+        assert (lc.ld, lc.ld_grad, qc.ldx, qc.ldy) == (10, 10, 10, 5)
+
+
+def test_threads_that_share_a_configuration_pass_their_own_strides(monkeypatch):
+    # what reaches the library while another thread's call has just looked at its own tensors
+    import torch
+    x = {20: torch.zeros(3, 20)[:, :10], 50: torch.zeros(3, 50)[:, :10]}
+    cfg, seen = mg.LogitsCfg(3, 10, 0), []
+
+    def call(name, c, *args):
+        if len(seen) == 0:                                   # (the other thread's call, in the middle of this one)
+            seen.append(None)
+            mg.token_logprobs(cfg, x[50], None, None, None, None, None, None)
+        seen.append((args[0][0], c.ld))
+
+    monkeypatch.setattr(ops, "_call", call)
+    mg.token_logprobs(cfg, x[20], None, None, None, None, None, None)
+    assert [(t is x[n], ld) for n, (t, ld) in zip((50, 20), seen[1:])] == [(True, 50), (True, 20)]
