@@ -1021,7 +1021,7 @@ static DistillArgs distill_args(const LogitsArgs& a) {
   d.ld = a.c.ld;
   d.ld_grad = a.c.ld_grad;
   d.inv_t = 1.0f / a.c.temperature;
-  d.past = stores_past_caches(2.0 * elem_size(a.c.dtype) * a.c.N * a.c.V);
+  d.past = results_past_caches((double)elem_size(a.c.dtype) * a.c.N * a.c.V, 180e6);
   return d;
 }
 template <typename E>
@@ -1065,6 +1065,7 @@ static hipError_t distill_start(const LogitsArgs& a, hipStream_t s) {
       hipLaunchKernelGGL((distill_kernel<E, 4>), dim3(N), dim3(256), 0, s, d);
       return hipGetLastError();
     case 16:
+      if (sizeof(E) == 2) d.past = results_past_caches(2.0 * a.c.N * a.c.V, 180e6, 450e6);
       hipLaunchKernelGGL((distill_kernel<E, 16>), dim3(N), dim3(1024), 0, s, d);
       return hipGetLastError();
   }

@@ -60,6 +60,10 @@ static size_t glr_ws(const glr_cfg& c) {
   const size_t f = glr_ws(glr_shape(c, false)), b = glr_ws(glr_shape(c, true));
   return f > b ? f : b;
 }
+static bool glr_past(const glr_cfg& c, int results) {
+  return results_past_caches((double)results * elem_bytes(c.dtype) * c.T * c.B * c.H, 95e6,
+                             c.dtype == MGRIT_F32 ? 150e6 : 1e300);
+}
 static int glr_space(const glr_cfg& c, const GlrShape& s, void* ws, size_t n, GlrArgs* a) {
   const size_t need = glr_ws(c);
   if (n < need) return MGRIT_E_WORKSPACE;
@@ -160,7 +164,7 @@ int glr_forward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, c
   a.reset = reset;
   a.h_last = h_last;
   a.saved = (float*)saved;
-  a.past = stores_past_caches(3.0 * elem_bytes(cfg->dtype) * cfg->T * cfg->B * cfg->H);
+  a.past = glr_past(*cfg, 1);
   (void)hipGetLastError();   // an error left by earlier, unrelated work is not this call's
   return code_of(launch_glr_forward(a, (hipStream_t)stream));
 }
@@ -190,7 +194,7 @@ int glr_backward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, 
   a.saved = (float*)const_cast<void*>(saved);
   a.dh_last = dh_last;
   a.dh0 = dh0;
-  a.past = stores_past_caches(5.0 * elem_bytes(cfg->dtype) * cfg->T * cfg->B * cfg->H);
+  a.past = glr_past(*cfg, 2);
   (void)hipGetLastError();
   return code_of(launch_glr_backward(a, (hipStream_t)stream));
 }
@@ -330,7 +334,7 @@ int q8_linear(const q8_cfg* cfg, const void* x, const int8_t* w_q, const float* 
   a.y = y;
   a.scale = (float*)workspace;
   a.q = (int8_t*)workspace + q8_scales(*cfg);
-  a.past = stores_past_caches((double)cfg->M * ((double)e * cfg->K + (double)e * cfg->N));
+  a.past = results_past_caches((double)e * cfg->M * cfg->N, 95e6);
   (void)hipGetLastError();
   return code_of(launch_q8_linear(a, (hipStream_t)stream));
 }
