@@ -1065,7 +1065,6 @@ static hipError_t distill_start(const LogitsArgs& a, hipStream_t s) {
       hipLaunchKernelGGL((distill_kernel<E, 4>), dim3(N), dim3(256), 0, s, d);
       return hipGetLastError();
     case 16:
-      if (sizeof(E) == 2) d.past = results_past_caches(2.0 * a.c.N * a.c.V, 180e6, 450e6);
       hipLaunchKernelGGL((distill_kernel<E, 16>), dim3(N), dim3(1024), 0, s, d);
       return hipGetLastError();
   }

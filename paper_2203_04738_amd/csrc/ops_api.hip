@@ -60,8 +60,8 @@ static size_t glr_ws(const glr_cfg& c) {
   const size_t f = glr_ws(glr_shape(c, false)), b = glr_ws(glr_shape(c, true));
   return f > b ? f : b;
 }
-static bool glr_past(const glr_cfg& c, int results) {
-  return results_past_caches((double)results * elem_bytes(c.dtype) * c.T * c.B * c.H, 95e6,
+static bool glr_past(const glr_cfg& c, bool backward) {
+  return results_past_caches((backward ? 2.0 : 1.0) * elem_bytes(c.dtype) * c.T * c.B * c.H, backward ? 95e6 : 45e6,
                              c.dtype == MGRIT_F32 ? 150e6 : 1e300);
 }
 static int glr_space(const glr_cfg& c, const GlrShape& s, void* ws, size_t n, GlrArgs* a) {
@@ -164,7 +164,7 @@ int glr_forward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, c
   a.reset = reset;
   a.h_last = h_last;
   a.saved = (float*)saved;
-  a.past = glr_past(*cfg, 1);
+  a.past = glr_past(*cfg, false);
   (void)hipGetLastError();   // an error left by earlier, unrelated work is not this call's
   return code_of(launch_glr_forward(a, (hipStream_t)stream));
 }
@@ -194,7 +194,7 @@ int glr_backward(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, 
   a.saved = (float*)const_cast<void*>(saved);
   a.dh_last = dh_last;
   a.dh0 = dh0;
-  a.past = glr_past(*cfg, 2);
+  a.past = glr_past(*cfg, true);
   (void)hipGetLastError();
   return code_of(launch_glr_backward(a, (hipStream_t)stream));
 }
