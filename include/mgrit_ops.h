@@ -14,13 +14,15 @@
  *
  * Conventions are those of mgrit_gru.h: device pointers, everything enqueued on
  * `stream`, no allocation, no synchronisation, arguments checked on the host before
- * anything is launched, MGRIT_E_* codes, outputs overwritten, never accumulated, no exception crosses the ABI.  Every output is bitwise
- * reproducible.  Buffers that a call writes must not overlap any other buffer of
- * the call unless its comment says so.  A workspace of 0 bytes may be NULL; other
- * workspaces are 16-byte aligned; calls that share one are ordered on one stream.
- * A call whose launches would take 2^32 threads or more is refused with MGRIT_E_SIZE: from 2^23 tiles on for a sequence
- * (128 to 512 steps of 32 to 128 channels of one batch row each), 2^22 for rows of logits (2^15 entries each) or tokens to
- * quantise.
+ * anything is launched, MGRIT_E_* codes, outputs overwritten, never accumulated, no
+ * exception crosses the ABI.  Every output is bitwise reproducible.  Buffers that a
+ * call writes must not overlap any other buffer of the call unless its comment says so.
+ * A workspace of 0 bytes may be NULL; other workspaces are 16-byte aligned; calls that
+ * share one are ordered on one stream.
+ * A call whose launches would take 2^32 threads or more is refused with MGRIT_E_SIZE:
+ * from 2^23 tiles on for a sequence (128 to 512 steps of 32 to 128 channels of one batch
+ * row each), from 2^22 on for rows of logits (of up to 2^15 entries; longer ones count
+ * as several) or tokens to quantise, more where they are short.
  * Nothing is kept in a workspace from call to call.
  */
 #ifndef MGRIT_OPS_H
@@ -41,9 +43,10 @@ enum { MGRIT_F16 = 4 };
  *     h_t = a_t h_{t-1} + b_t,   t = 1..T,
  * GLR_MIX:   a = sigmoid(gate), b = (1 - a) value    (a GRU's update whose gates do not read the state)
  * GLR_DECAY: a = exp(gate),     b = value            (gate <= 0 is a decay; it is not enforced)
- * A sequence is composed from runs of steps, h -> A h + S with A the product of the run's a.  Gates above 0 can carry A beyond
- * the floats within some steps, where a state that is not zero becomes infinite or NaN; one of zero stays what its inputs make it.
- * An infinite state, which nothing but a reset ends, may be NaN once A is below the floats.
+ * A sequence is composed from runs of steps, h -> A h + S with A the product of the run's a.  Gates above 0
+ * can carry A beyond the floats within some steps, where a state that is not zero becomes infinite or NaN; one
+ * of zero stays what its inputs make it.  An infinite state, which nothing but a reset ends, may be NaN once A
+ * is below the floats.
  * A step whose `reset` byte is not zero forgets the past: h_t = b_t, whatever h_{t-1} was (infinities
  * and NaN included), and no gradient passes to the steps before it: sequences packed one behind the other.
  */
@@ -90,10 +93,10 @@ MGRIT_API int glr_backward(const glr_cfg* cfg, const glr_seq* gate, const glr_se
                            void* workspace, size_t workspace_bytes, void* stream);
 
 /* One step of B running sequences whose states live in a pool of n_slots rows (cfg->T is 1).
- *   gate, value, h: arrays [1,B,H] as above (stride_t is not read); slots[B] int32 or NULL (row b is slot b; then n_slots >= B):
- *   a row whose slot is outside 0..n_slots-1 is idle: its h is zero and no state is touched.  Two rows must not
- *   name the same slot.  reset[B] or NULL.  state_in, state_out[n_slots,H] float; they may be the same
- *   array, and slots that no row names are left alone. */
+ *   gate, value, h: arrays [1,B,H] as above (stride_t is not read); slots[B] int32 or NULL (row b is
+ *   slot b; then n_slots >= B): a row whose slot is outside 0..n_slots-1 is idle: its h is zero and no
+ *   state is touched.  Two rows must not name the same slot.  reset[B] or NULL.  state_in,
+ *   state_out[n_slots,H] float; they may be the same array, and slots that no row names are left alone. */
 MGRIT_API int glr_step(const glr_cfg* cfg, const glr_seq* gate, const glr_seq* value, const int32_t* slots,
                        int32_t n_slots, const uint8_t* reset, const float* state_in, float* state_out,
                        const glr_seq* h, void* stream);
@@ -148,7 +151,8 @@ MGRIT_API int distill_topk_backward(const logits_cfg* cfg, const void* logits, c
 
 /* ------------------------------------------------------------------------
  * Product in 8-bit integers:  y[m,n] = xs_m ws_n sum_k xq[m,k] wq[n,k] + bias_n,
- * the sum exact (32-bit integers), then multiplied by ws, by xs, and the bias added, in floats.  A row is quantised by
+ * the sum exact (32-bit integers), then multiplied by ws, by xs, and the bias added, in floats.
+ * A row is quantised by
  *     scale = max(max|x| / 127, 2^-126),   q = x / scale rounded to nearest (ties to even),
  * both quotients rounded to float.  A row with an infinity or a NaN has scale NaN and q 0: its results are NaN.
  * Rows of q are q8_row_bytes(K) bytes apart, K rounded up to 128.
@@ -162,7 +166,8 @@ typedef struct {
 MGRIT_API int64_t q8_row_bytes(int32_t K);
 /* Host only: workspace of q8_linear. */
 MGRIT_API int q8_workspace_bytes(const q8_cfg* cfg, size_t* bytes);
-/* Quantises rows x[M,K] of the dtype (tokens, or the output channels of a weight matrix); cfg->N and ldy are not read.
+/* Quantises rows x[M,K] of the dtype (tokens, or the output channels of a weight matrix); cfg->N and
+ * ldy are not read.
  *   q[M, q8_row_bytes(K)] int8, 16-byte aligned, zeros beyond K; scale[M] float. */
 MGRIT_API int q8_quantize(const q8_cfg* cfg, const void* x, int8_t* q, float* scale, void* stream);
 /* w_q[N, q8_row_bytes(K)] int8 (16-byte aligned; what lies beyond K does not matter), w_scale[N] float,

@@ -1,18 +1,19 @@
 // Gated linear recurrence h_t = a_t h_{t-1} + b_t (include/mgrit_ops.h), its adjoint, and one step of it.
 //
 // A run of steps is the map h -> A h + S with A = prod a, S its result from a zero state, and two runs behind each
-// other compose to (A2 A1, A2 S1 + S2): that is all a sequence needs to be cut up.  A workgroup reads its
-// tile once, into registers; every lane goes through its run of 8 or 16 steps from a zero state; the runs of the tile meet in
-// LDS; the tiles of a sequence meet in the workspace, where each leaves its (A, S) as soon as it has read its
-// tile and, once it knows the state before it, the state behind it.  The bytes are those of the arrays, each read or written once.
+// other compose to (A2 A1, A2 S1 + S2): that is all a sequence needs to be cut up.  A workgroup reads its tile once,
+// into registers; every lane goes through its run of 8 or 16 steps from a zero state; the runs of the tile meet in
+// LDS; the tiles of a sequence meet in the workspace, where each leaves its (A, S) as soon as it has read its tile
+// and, once it knows the state before it, the state behind it.  The bytes are those of the arrays, each read or
+// written once.
 //
-// The word of a tile and channel is A in the low half and S in the high one, stored by one 64-bit store, so that a reader that
-// sees one sees the other.  All bits set: not written yet (no A is stored so).  A = -0: S does not depend on what was
-// before (a reset, or the state itself: what a tile knows once it knows the state before it).  No other A is -0:
-// no a is negative, so that a product that underflows is +0, and a state that is not finite does not become finite
-// again (0 times it is NaN) as long as no reset stands in between.  The state before a tile is always computed as S + A h
-// tile by tile, by the tile itself (glr_join) as by those behind it that find the map and not yet the state (window_state):
-// the two round alike, and the result does not depend on timing.
+// The word of a tile and channel is A in the low half and S in the high one, stored by one 64-bit store, so that a
+// reader that sees one sees the other.  All bits set: not written yet (no A is stored so).  A = -0: S does not depend
+// on what was before (a reset, or the state itself: what a tile knows once it knows the state before it).  No other A
+// is -0: no a is negative, so that a product that underflows is +0, and a state that is not finite does not become
+// finite again (0 times it is NaN) as long as no reset stands in between.  The state before a tile is always computed
+// as S + A h tile by tile, by the tile itself (glr_join) as by those behind it that find the map and not yet the
+// state (window_state): the two round alike, and the result does not depend on timing.
 //
 // Tiles are taken by a ticket, first tiles first (the adjoint: last tiles first), so that those a workgroup waits for
 // have been started, wait for none behind it, and every wait ends.
@@ -90,15 +91,15 @@ __device__ inline void store_pair(E* p, float a, float b, bool second, bool past
   }
 }
 
-// exp(x), x of any size: 2^p with p = x log2(e) as rounded, and e^r for what the rounding left, r = x - p ln 2 (at most 2^-17
-// where 2^p is a number other than 0; where x is infinite, NaN, for which fminf takes the bound).  Without the second factor
-// the result is off by 7 units of 2^-24 at x = -6, 16 at -20, 62 at -80.
+// exp(x), x of any size: 2^p with p = x log2(e) as rounded, and e^r for what the rounding left, r = x - p ln 2 (at
+// most 2^-17 where 2^p is a number other than 0; where x is infinite, NaN, for which fminf takes the bound).  Without
+// the second factor the result is off by 7 units of 2^-24 at x = -6, 16 at -20, 62 at -80.
 __device__ inline float exp_of(float x) {
   const float p = LOG2E * x, e = __builtin_amdgcn_exp2f(p);
   return fmaf(e, fminf(fmaf(-p, LN2, x), 0x1p-16f), e);
 }
-// a and, for GLR_MIX, 1 - a of a gate, both to a few units of their own last place: with e = exp(-|g|), the smaller of the two
-// is e / (1 + e) at any g, and the larger one 1 minus that.
+// a and, for GLR_MIX, 1 - a of a gate, both to a few units of their own last place: with e = exp(-|g|), the smaller
+// of the two is e / (1 + e) at any g, and the larger one 1 minus that.
 template <int FORM>
 struct Gate {
   float a, na;
@@ -114,9 +115,9 @@ struct Gate {
     }
   }
 };
-// The same as the adjoint keeps it between its sweeps.  BOTH: a and 1 - a (16-bit arrays leave the registers for it, and
-// arithmetic is what those wait for).  Otherwise one float, the smaller of the two under the sign of g, which says which it
-// is.
+// The same as the adjoint keeps it between its sweeps.  BOTH: a and 1 - a (16-bit arrays leave the registers for it,
+// and arithmetic is what those wait for).  Otherwise one float, the smaller of the two under the sign of g, which
+// says which it is.
 template <int FORM, bool BOTH>
 struct KeptGate {
   float v, w;
@@ -144,8 +145,9 @@ struct KeptGate {
 };
 
 __device__ inline bool is_free(float A) { return __float_as_uint(A) == GLR_FREE; }
-// GLR_DECAY: gates above 0 are allowed, and the product of a run's a can be beyond the floats.  A state of zero stays what it
-// is then, and what a run has forgotten stays forgotten (infinity times 0 would be NaN).
+// GLR_DECAY: gates above 0 are allowed, and the product of a run's a can be beyond the floats.  A state of zero stays
+// what it is then, and what a run has forgotten stays forgotten (infinity times 0 would be NaN).
+
 // A of a run behind another run.
 template <int FORM>
 __device__ inline float both(float A, float before) {
@@ -182,11 +184,12 @@ __global__ __launch_bounds__(256) void glr_clear_kernel(unsigned long long* word
 }
 
 // Where a thread stands.  LANES > 0: that many lanes across the channels, and strides that allow 32-bit offsets
-// within a wave: tile, channels and steps are the wave's (in scalar registers), and a lane has an offset in it.  0: as the
-// shape says, any strides.  STEPS: of a run.
+// within a wave: tile, channels and steps are the wave's (in scalar registers), and a lane has an offset in it.  0:
+// as the shape says, any strides.  STEPS: of a run.
 template <int LANES, int STEPS>
 struct GlrPlace {
-  int lanes, lane_c, run, chunk, b;    // lanes across the channels, this one's place; run of the tile, tile, batch row
+  int lanes, lane_c;                   // lanes across the channels, this one's place
+  int run, chunk, b;                   // run of the tile, tile, batch row
   int ch0, ch;                         // first channel of the tile, of the lane
   int t0, wave_t0;                     // first step of the run, of the wave
   bool has, second;                    // whether channels ch and ch + 1 exist
@@ -222,15 +225,15 @@ __device__ inline unsigned reset_bits(const GlrArgs& a, const GlrPlace<LANES, ST
   const unsigned long long all = __ballot(r);
   return (unsigned)(LANES == 64 ? all : all >> ((threadIdx.x & 63) / p.lanes * p.lanes)) & ((1u << STEPS) - 1);
 }
-// Whether no step of the wave's runs resets or lies behind the sequence's end: the same answer in all lanes of the wave,
-// whose sweeps then look at neither.
+// Whether no step of the wave's runs resets or lies behind the sequence's end: the same answer in all lanes of the
+// wave, whose sweeps then look at neither.
 template <int LANES, int STEPS>
 __device__ inline bool glr_whole(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, unsigned resets) {
   return p.inside(a) && !__any(resets != 0);
 }
 
-// The steps of a thread's run in an array, from step t on.  LANES > 0: the wave's place and a 32-bit offset (the host has
-// looked at the strides).
+// The steps of a thread's run in an array, from step t on.  LANES > 0: the wave's place and a 32-bit offset (the host
+// has looked at the strides).
 template <typename E, int LANES, int STEPS>
 struct RunOf {
   char* base;
@@ -327,7 +330,8 @@ __device__ inline bool window_state(const unsigned long long* w, int n, int stri
 // The state before tile `chunk` of the thread's two channels, in sh.carry, from the words of
 // the tiles before it (backward: behind it), whose distance is 1, 2, ...  All threads of the workgroup call it.
 template <int FORM, int LANES, int STEPS>
-__device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, bool backward, GlrShared& sh) {
+__device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, bool backward,
+                                     GlrShared& sh) {
   const int before = backward ? a.s.chunks - 1 - p.chunk : p.chunk;
   const int runs = p.runs(), chans = 2 * p.lanes, n = min(before, GLR_WORDS / chans);
   const long long per_tile = (long long)a.c.B * a.s.cols * chans;
@@ -352,7 +356,8 @@ __device__ inline void glr_look_back(const GlrArgs& a, const GlrPlace<LANES, STE
 }
 
 // (A, S) per channel of the runs before the thread's own in its tile, from the own one, through LDS (`all`).  32
-// lanes: the halves of a wave meet by exchange, the waves in LDS.  before_barrier() is called in front of the barrier.
+// lanes: the halves of a wave meet by exchange, the waves in LDS.  before_barrier() is called in front of the
+// barrier.
 template <bool BACKWARD, int FORM, int LANES, int STEPS, typename FN>
 __device__ inline void runs_before(const GlrPlace<LANES, STEPS>& p, Pair A, Pair S, float4* all, Pair& pA, Pair& pS,
                                    FN before_barrier) {
@@ -372,10 +377,11 @@ __device__ inline void runs_before(const GlrPlace<LANES, STEPS>& p, Pair A, Pair
     if constexpr (LANES == 32)
       other = make_float4(__shfl_xor(A.x, 32, 64), __shfl_xor(S.x, 32, 64), __shfl_xor(A.y, 32, 64),
                           __shfl_xor(S.y, 32, 64));
-    if (later)
-      all[wave * LANES + p.lane_c] = LANES == 64 ? make_float4(A.x, S.x, A.y, S.y)
-                                                 : make_float4(both<FORM>(A.x, other.x), behind<FORM>(A.x, S.x, other.y),
-                                                               both<FORM>(A.y, other.z), behind<FORM>(A.y, S.y, other.w));
+    float4 mine = {A.x, S.x, A.y, S.y};
+    if constexpr (LANES == 32)
+      mine = make_float4(both<FORM>(A.x, other.x), behind<FORM>(A.x, S.x, other.y), both<FORM>(A.y, other.z),
+                         behind<FORM>(A.y, S.y, other.w));
+    if (later) all[wave * LANES + p.lane_c] = mine;
     before_barrier();
     __syncthreads();
     const int n = BACKWARD ? GLR_WAVES - 1 - wave : wave;
@@ -402,8 +408,8 @@ __device__ inline void runs_before(const GlrPlace<LANES, STEPS>& p, Pair A, Pair
 // the run.  first: the state before the sequence's first tile (backward: behind its last one).  The threads of the
 // tile's last run (backward: its first) get in `out` the state behind the tile.
 template <bool BACKWARD, int FORM, int LANES, int STEPS>
-__device__ inline Pair glr_join(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, Pair A, Pair S, Pair first, Pair& out,
-                                GlrShared& sh) {
+__device__ inline Pair glr_join(const GlrArgs& a, const GlrPlace<LANES, STEPS>& p, Pair A, Pair S, Pair first,
+                                Pair& out, GlrShared& sh) {
   const int chans = 2 * p.lanes, runs = p.runs(), c = 2 * p.lane_c;
   const bool at_start = BACKWARD ? p.chunk == a.s.chunks - 1 : p.chunk == 0;
   const bool chain = a.s.chunks > 1;
@@ -418,8 +424,10 @@ __device__ inline Pair glr_join(const GlrArgs& a, const GlrPlace<LANES, STEPS>& 
   unsigned long long* word =
       a.words + (((long long)p.chunk * a.c.B + p.b) * a.s.cols) * chans + p.ch;
   const bool last = place == runs - 1;
-  // the tile's own map (in the last run): what a reader composes and the state behind it are formed from the same A and S
-  const Pair tA = {both<FORM>(A.x, pA.x), both<FORM>(A.y, pA.y)}, tS = {behind<FORM>(A.x, S.x, pS.x), behind<FORM>(A.y, S.y, pS.y)};
+  // the tile's own map (in the last run): what a reader composes and the state behind it are formed from the same A
+  // and S
+  const Pair tA = {both<FORM>(A.x, pA.x), both<FORM>(A.y, pA.y)};
+  const Pair tS = {behind<FORM>(A.x, S.x, pS.x), behind<FORM>(A.y, S.y, pS.y)};
   if (last && chain && !at_start) {
     store_word(word, make_word(tA.x, tS.x));
     store_word(word + 1, make_word(tA.y, tS.y));
@@ -445,9 +453,10 @@ __device__ inline int glr_tile(const GlrArgs& a, GlrShared& sh) {
   return sh.tile;
 }
 
-// Memory bounds it where a sequence is one tile (128 x 100 x 1000 floats: 154 MB in 29 us, 5.3 TB/s); over several
-// tiles it is the wait for those before (16384 x 4 x 1024 bf16: 403 MB in 98 us; copies whose tiles did not wait took
-// 78).  Runs of 16 steps halve the tiles against runs of 8 (143 us), and 128 channels make a row's piece 256 bytes.
+// Memory bounds it where a sequence is one tile (128 x 100 x 1000 floats: 154 MB in 30 us, 5.2 TB/s); over several
+// tiles it is the wait for those before (16384 x 4 x 1024 bf16: 403 MB in 102 us; copies whose tiles did not wait
+// took 78).  Runs of 16 steps halve the tiles against runs of 8 (143 us), and 128 channels make a row's piece 256
+// bytes.
 template <typename E, bool ALIGNED, int FORM, int LANES>
 __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) {
   constexpr int STEPS = GLR_RUN_FWD;
@@ -500,8 +509,8 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) 
     if (p.second) s[1] = h.y;
   }
   if (p.run == runs - 1 && a.h_last && p.chunk == a.s.chunks - 1) {
-    // h_last may be h0 itself, and behind a reset nothing so far has waited for the first tile, whose word says that it has
-    // read h0 (that tile waits for none)
+    // h_last may be h0 itself, and behind a reset nothing so far has waited for the first tile, whose word says that
+    // it has read h0 (that tile waits for none)
     if (a.h_last == a.h0 && p.chunk > 0) {
       const unsigned long long* w = a.words + (long long)p.b * a.s.cols * 2 * p.lanes + p.ch;
       while ((unsigned)load_word(w) == GLR_NONE) __builtin_amdgcn_s_sleep(1);
@@ -525,9 +534,10 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_forward_kernel(GlrArgs a) 
 }
 
 // mu_t = a_t l_t is what step t hands on to step t - 1: mu -> a (dh + mu), the same composition from the other end.
-// 128 x 100 x 1000 floats: 256 MB in 55 us (4.7 TB/s); 16384 x 4 x 1024 bf16: 671 MB in 166 us, where its arithmetic, some
-// fifty vector instructions a value, and the wait for tiles behind take as long as memory.  Runs of 8 steps: with 16 the three
-// arrays, the gates and the adjoints do not fit 128 registers (267 us).
+// 128 x 100 x 1000 floats: 256 MB in 58 us (4.4 TB/s); 16384 x 4 x 1024 bf16: 671 MB in 174 us (3.9 TB/s), where its
+// waves wait for 57 % of their cycles, for the tiles behind and for memory, two workgroups a CU; arithmetic, 54
+// vector instructions a value, is next.  Runs of 8 steps: with 16 the three arrays, the gates and the adjoints do not
+// fit 128 registers (267 us).
 template <typename E, bool ALIGNED, int FORM, int LANES>
 __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a) {
   constexpr int STEPS = GLR_RUN_BWD;
@@ -607,7 +617,8 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a)
     if (p.second) a.dh0[at + 1] = end.y;
   }
   if (!p.has) return;
-  RunOf<E, LANES, STEPS> dg(a.dgate, a, p, min(p.t0, a.c.T - 1), p.lane_c), dv(a.dvalue, a, p, min(p.t0, a.c.T - 1), p.lane_c);
+  const int from = min(p.t0, a.c.T - 1);
+  RunOf<E, LANES, STEPS> dg(a.dgate, a, p, from, p.lane_c), dv(a.dvalue, a, p, from, p.lane_c);
   auto write = [&](auto masked) {
     constexpr bool MASKED = decltype(masked)::value;
     float l[STEPS][2], m[2] = {mu.x, mu.y};
@@ -703,8 +714,8 @@ static hipError_t glr_launch(const GlrArgs& a, bool backward, hipStream_t s) {
 hipError_t launch_glr_forward(const GlrArgs& a, hipStream_t s) { return glr_launch(a, false, s); }
 hipError_t launch_glr_backward(const GlrArgs& a, hipStream_t s) { return glr_launch(a, true, s); }
 
-// One step: two channels per thread.  100 rows of 1024 bf16: 3.1 us, the latency of slot, gates and state one after the
-// other.
+// One step: two channels per thread.  100 rows of 1024 bf16: 3.0 us, the latency of slot, gates and state one after
+// the other.
 template <typename E, bool ALIGNED, int FORM>
 __global__ __launch_bounds__(256) void glr_step_kernel(GlrStepArgs a) {
   const int pairs = (a.c.H + 1) / 2;

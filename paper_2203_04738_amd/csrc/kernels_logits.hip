@@ -1,16 +1,16 @@
-// Rows of logits (include/mgrit_ops.h): log probabilities with entropy and top alternatives, and the
-// distillation loss with its gradient.
+// Rows of logits (include/mgrit_ops.h): log probabilities with entropy and top alternatives, and the distillation
+// loss with its gradient.
 //
-// A team of 1, 4 or 16 waves holds a row, or a segment of a long one, in registers as it was stored, 16 bytes
-// per load: one pass over memory, and everything after it (maximum, sums, alternatives, gradient) reads
-// registers.  Rows longer than a team holds are cut into segments whose statistics a second kernel joins.
+// A team of 1, 4 or 16 waves holds a row, or a segment of a long one, in registers as it was stored, 16 bytes per
+// load: one pass over memory, and everything after it (maximum, sums, alternatives, gradient) reads registers.  Rows
+// longer than a team holds are cut into segments whose statistics a second kernel joins.
 //
-// Alternatives.  A value's key is a whole number that rises with it; the largest key of a group of lanes is a lower bound
-// of the k-th largest of all, if there are k groups with keys as large.  The K-th largest of the groups' largest
-// keys (found bit by bit, by counting) leaves little more than K candidates of the whole row, which go to LDS with their indices and
-// are ranked by counting how many beat each.  Keys with indices are all different, so the result does not
-// depend on the order in which candidates arrive.  Where there are more candidates than LDS takes (rows of
-// equal values), the alternatives are found one after the other, each the largest below the last.
+// Alternatives.  A value's key is a whole number that rises with it; the largest key of a group of lanes is a lower
+// bound of the k-th largest of all, if there are k groups with keys as large.  The K-th largest of the groups'
+// largest keys (found bit by bit, by counting) leaves little more than K candidates of the whole row, which go to LDS
+// with their indices and are ranked by counting how many beat each.  Keys with indices are all different, so the
+// result does not depend on the order in which candidates arrive.  Where there are more candidates than LDS takes
+// (rows of equal values), the alternatives are found one after the other, each the largest below the last.
 #include <type_traits>
 
 #include "elem.h"
@@ -67,8 +67,8 @@ __device__ inline u64 wave_max(u64 v) {
   return v;
 }
 
-// The largest of three (of those that are not NaN), in one instruction: fmaxf would first make each of the stored values
-// canonical.
+// The largest of three (of those that are not NaN), in one instruction: fmaxf would first make each of the stored
+// values canonical.
 __device__ inline float max3(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
@@ -105,8 +105,8 @@ __device__ inline float piece_at(const uintx4& raw, int k) {
   return word_elem<E>(raw[k / ELEMS_PER_WORD<E>], k % ELEMS_PER_WORD<E>);
 }
 
-// The elements lo .. hi-1 of a row that a thread of the team holds: load j holds the 16 bytes (j * threads + thread) of the
-// segment, counted from the 16-byte boundary at or before the row's start.  What lies outside is -inf.
+// The elements lo .. hi-1 of a row that a thread of the team holds: load j holds the 16 bytes (j * threads + thread)
+// of the segment, counted from the 16-byte boundary at or before the row's start.  What lies outside is -inf.
 template <typename E, int NW>
 struct Held {
   using T = TeamOf<E, NW>;
@@ -212,8 +212,8 @@ __device__ inline Stats team_stats(const Held<E, NW>& x, float c, int tid, float
   return st;
 }
 
-// w (x - m), w >= 0: the difference of two floats may be beyond them where w times it is not.  What a mask leaves out (-inf)
-// stays that, also where w m is beyond the floats.
+// w (x - m), w >= 0: the difference of two floats may be beyond them where w times it is not.  What a mask leaves out
+// (-inf) stays that, also where w m is beyond the floats.
 __device__ inline float below(float x, float m, float w) {
   const float d = x - m;
   if (x == -__builtin_inff()) return x;
@@ -251,9 +251,9 @@ struct TopShared {
   int n;
 };
 
-// The K largest of the entries lo .. hi-1 of a row, in falling order: put(rank, full key).  own: the thread's own largest value;
-// ordinary: no NaN and no +inf; scan(bound, take): calls take(key, index) for the thread's values >= bound.  (What few rows
-// need reads the row from the caches, in loops: it would cost the others registers.)
+// The K largest of the entries lo .. hi-1 of a row, in falling order: put(rank, full key).  own: the thread's own
+// largest value; ordinary: no NaN and no +inf; scan(bound, take): calls take(key, index) for the thread's values >=
+// bound.  (What few rows need reads the row from the caches, in loops: it would cost the others registers.)
 template <typename E, int NW, int CAND, typename SCAN, typename PUT>
 __device__ inline void team_top(const E* row, int lo, int hi, int K, int tid, float own, bool ordinary,
                                 TopShared<NW, CAND>& sh, SCAN scan, PUT put) {
@@ -407,8 +407,8 @@ __device__ inline void put_token(const RowArgs& a, long long row, const E* x, co
   }
 }
 
-// A team per row or segment.  What bounds few rows is latency: 8 rows of 32768 bf16, K = 20: 8.9 us for load, two
-// sums, the search of the bound and the ranking; 100 rows of 51 floats: 6.2 us.
+// A team per row or segment.  What bounds few rows is latency: 8 rows of 32768 bf16, K = 20: 8.8 us for load, two
+// sums, the search of the bound and the ranking; 100 rows of 51 floats: 6.1 us.
 template <typename E, int NW, bool SEGS>
 __global__ __launch_bounds__((TeamOf<E, NW>::block), NW == 16 ? 8 : 4) void logprobs_kernel(RowArgs a) {
   using T = TeamOf<E, NW>;
@@ -454,11 +454,12 @@ __global__ __launch_bounds__((TeamOf<E, NW>::block), NW == 16 ? 8 : 4) void logp
 }
 
 // Many long rows.  What bounds them is arithmetic: an exponential and four operations on every value, and what each
-// wave does besides, so a thread goes through 128 values in a stream of pieces, four loaded ahead, and
-// keeps of each piece its largest value alone; the few pieces that hold an alternative are read again.  The exponents are
-// taken against a reference r of the thread's own, the largest of the first pieces, 2^(c x - r): it moves (and the
-// sums with it) where a later piece is 2^32 times as large; threads and waves are brought to one reference at the end.
-// 2048 x 131072 bf16, K = 8: 537 MB in 108 us (5.0 TB/s); held by teams of 4 waves, 32 values a thread, 182 us.
+// wave does besides, so a thread goes through 128 values in a stream of pieces, four loaded ahead, and keeps of each
+// piece its largest value alone; the few pieces that hold an alternative are read again.  The exponents are taken
+// against a reference r of the thread's own, the largest of the first pieces, 2^(c x - r): it moves (and the sums
+// with it) where a later piece is 2^32 times as large; threads and waves are brought to one reference at the end.
+// 2048 x 131072 bf16, K = 8: 537 MB in 114 us traced (4.7 TB/s; calls behind each other 106 us with the join); held
+// by teams of 4 waves, 32 values a thread, 182 us.
 template <typename E>
 struct StreamOf {
   static constexpr int per = 16 / (int)sizeof(E), batches = sizeof(E) == 4 ? 8 : 4;
@@ -678,8 +679,8 @@ struct Teacher {
   float total;                                               // of the weights: 1, 0 (no teacher), NaN (an id >= V)
   float qlogq;                                               // sum q log q
 };
-// By one wave; row: the student's logits.  Weights from (teacher - largest) / t, as `below` has it: a teacher's value over t
-// may be beyond a float.
+// By one wave; row: the student's logits.  Weights from (teacher - largest) / t, as `below` has it: a teacher's value
+// over t may be beyond a float.
 template <typename E>
 __device__ inline void read_teacher(const int64_t* ids, const float* teacher, int K, int V, float inv_t,
                                     const E* row, int lane, Teacher& t) {
@@ -758,8 +759,8 @@ struct DistillArgs {
   bool past;                 // gradients past the caches
 };
 
-// w (p - q) of what a team holds of a row, stored; scale = w total / s, then the entries of the teacher.  A row of nothing but
-// -inf (s = 0) has p = 0, but for an id that does not exist (total is NaN), which makes it NaN.
+// w (p - q) of what a team holds of a row, stored; scale = w total / s, then the entries of the teacher.  A row of
+// nothing but -inf (s = 0) has p = 0, but for an id that does not exist (total is NaN), which makes it NaN.
 template <typename E, int NW>
 __device__ inline void put_gradient(const DistillArgs& a, const Held<E, NW>& x, E* out, int lo, int hi, float m,
                                     float s, float w, const Teacher& t, int tid) {
@@ -808,8 +809,8 @@ __device__ inline void put_zeros(E* out, int lo, int hi, int tid, int threads) {
   for (int i = lo + tid; i < hi; i += threads) out[i] = elem_of<E>(0.f);
 }
 
-// A row in one team: loss, statistics and, where it is asked for, the gradient.  8192 x 32768 bf16, 64 teacher logits:
-// 1.07 GB in 215 us (5.0 TB/s), as a copy.
+// A row in one team: loss, statistics and, where it is asked for, the gradient.  8192 x 32768 bf16, 64 teacher
+// logits: 1.07 GB in 215 us where calls follow each other (5.0 TB/s, a copy's is 6.2), 256 us as traced.
 template <typename E, int NW>
 __global__ __launch_bounds__((TeamOf<E, NW>::block)) void distill_kernel(DistillArgs a) {
   using T = TeamOf<E, NW>;
@@ -844,8 +845,8 @@ __global__ __launch_bounds__((TeamOf<E, NW>::block)) void distill_kernel(Distill
   else put_gradient<E, NW>(a, held, out, 0, a.V, st.m, st.s, w, t, tid);
 }
 
-// Statistics of a segment of a long row: 1003 x 50021 floats, 201 MB in 30 us (from the last-level cache in part), the gradient
-// below 402 MB in 70 us.
+// Statistics of a segment of a long row: 1003 x 50021 floats, 201 MB in 30 us (from the last-level cache in part),
+// the gradient below 402 MB in 69 us (the logits from that cache in part).
 template <typename E>
 __global__ __launch_bounds__(1024) void distill_segment_kernel(DistillArgs a) {
   using T = TeamOf<E, 16>;
@@ -925,7 +926,8 @@ static int team_waves(int V, int size, bool aligned) {
 // Segments of a row, all as long, of at most 2^15 values: what a team of 16 waves holds or a workgroup streams.
 static RowShape segments(int V, int size, bool aligned) {
   const int per = 16 / size, most = size == 4 ? TeamOf<float, 16>::chunks : TeamOf<Bf16, 16>::chunks;
-  static_assert(TeamOf<float, 16>::chunks == StreamOf<float>::chunks && TeamOf<Bf16, 16>::chunks == StreamOf<Bf16>::chunks,
+  static_assert(TeamOf<float, 16>::chunks == StreamOf<float>::chunks &&
+                    TeamOf<Bf16, 16>::chunks == StreamOf<Bf16>::chunks,
                 "both forms take segments of the same length");
   const int pieces = (V + (aligned ? 0 : per - 1) + per - 1) / per;
   RowShape s;
@@ -933,10 +935,10 @@ static RowShape segments(int V, int size, bool aligned) {
   s.seg = (pieces + s.segs - 1) / s.segs;
   return s;
 }
-// Whether token_logprobs streams rows longer than four waves hold (a workgroup of four waves for each 2^15 values) instead of
-// holding them in teams of 16 waves.  K = 20, streamed : held, us: 32768 bf16, 512 rows 15.2 : 12.4, 768 rows 18.4 : 18.4, 2048
-// rows 33.9 : 39.8; 32768 floats, 512 rows 19.3 : 17.9, 2048 rows 48.2 : 50.4; 131072 bf16 (4 segments a row), 64 rows
-// 18.2 : 14.9, 192 rows 24.9 : 23.6, 256 rows 28.1 : 28.4.
+// Whether token_logprobs streams rows longer than four waves hold (a workgroup of four waves for each 2^15 values)
+// instead of holding them in teams of 16 waves.  K = 20, streamed : held, us: 32768 bf16, 512 rows 15.2 : 12.4, 768
+// rows 18.4 : 18.4, 2048 rows 33.9 : 39.8; 32768 floats, 512 rows 19.3 : 17.9, 2048 rows 48.2 : 50.4; 131072 bf16 (4
+// segments a row), 64 rows 18.2 : 14.9, 192 rows 24.9 : 23.6, 256 rows 28.1 : 28.4.
 constexpr long long STREAM_SEGMENTS = 768;
 // Whether rows, or their segments, can be a team each in one launch.
 static bool teams_launchable(const logits_cfg& c, int size, bool aligned) {
@@ -974,8 +976,8 @@ static hipError_t logprobs_start(const LogitsArgs& a, hipStream_t s) {
   const bool stream = (long long)N * cut.segs >= STREAM_SEGMENTS;
   const dim3 grid(N * (unsigned)cut.segs);
   // (a row's segments, or four rows in one workgroup)
-  if (!launchable(waves == 1 ? (N + 3) / 4 : (long long)N * cut.segs, waves == 1 || waves == 4 || stream ? 256 : 1024))
-    return TOO_LARGE;
+  const int threads = waves == 1 || waves == 4 || stream ? 256 : 1024;
+  if (!launchable(waves == 1 ? ((long long)N + 3) / 4 : (long long)N * cut.segs, threads)) return TOO_LARGE;
   switch (waves) {
     case 1:
       hipLaunchKernelGGL((logprobs_kernel<E, 1, false>), dim3((N + 3) / 4), dim3(256), 0, s, r);

@@ -1,9 +1,9 @@
 // Product in 8-bit integers with a scale for each token and channel (include/mgrit_ops.h).
 //
-// The tokens are quantised into the workspace by a kernel of their own (each row once; the product's tiles would do it once
-// per column of tiles); rows are padded with zeros to 128 bytes, so that the products look at no tail of K.  In the products the
-// channels are the rows of the matrix instruction and the tokens its columns: a lane ends up with four neighbouring
-// channels of one token.
+// The tokens are quantised into the workspace by a kernel of their own (each row once; the product's tiles would do
+// it once per column of tiles); rows are padded with zeros to 128 bytes, so that the products look at no tail of K.
+// In the products the channels are the rows of the matrix instruction and the tokens its columns: a lane ends up with
+// four neighbouring channels of one token.
 #include <algorithm>
 #include <cmath>
 
@@ -87,7 +87,8 @@ struct QuantRow {
   }
 };
 
-// A row per team of NW waves.  A row that is not finite: scale NaN, zeros.  32768 x 2048 bf16: 201 MB in 40-42 us (4.8-5.1 TB/s).
+// A row per team of NW waves.  A row that is not finite: scale NaN, zeros.  32768 x 2048 bf16: 201 MB in 42 us (4.8
+// TB/s).
 template <typename E, int NW, int LOADS>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void q8_quantize_kernel(Q8Args a) {
   __shared__ float part[NW];
@@ -140,8 +141,8 @@ __global__ __launch_bounds__(1024) void q8_quantize_long_kernel(Q8Args a) {
   }
 }
 
-// Teams that hold the row.  One wave per row : four, 2048 bf16, us: 512 rows 4.1 : 3.3, 2048 rows 5.6 : 5.9, 8192 rows
-// 14.2 : 16.6, 32768 rows 42.5 : 57; rows of 4096 take four (4096 rows 15.2 : 13.4).
+// Teams that hold the row.  One wave per row : four, 2048 bf16, us: 512 rows 4.1 : 3.3, 2048 rows 5.6 : 5.9, 8192
+// rows 14.2 : 16.6, 32768 rows 42.5 : 57; rows of 4096 take four (4096 rows 15.2 : 13.4).
 struct QuantTeam {
   int waves, loads;                                  // of 16 bytes a thread; 0: the row is read twice
 };
@@ -180,12 +181,11 @@ hipError_t launch_q8_quantize(const Q8Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// ---------------------------------------------------------------------------
-// products
-// ---------------------------------------------------------------------------
-// Four neighbouring channels n .. n+3 of a token, from their sums and the scales and biases of the channels; wide: in one
-// store (the row's place allows it).  The channel's scale comes first: a sum times the scale of a token near a float's largest
-// value would be beyond it where the product of all three is not.
+// --------------------------------------------------------------------------- products
+// --------------------------------------------------------------------------- Four neighbouring channels n .. n+3 of
+// a token, from their sums and the scales and biases of the channels; wide: in one store (the row's place allows it).
+//  The channel's scale comes first: a sum times the scale of a token near a float's largest value would be beyond it
+// where the product of all three is not.
 template <typename E>
 __device__ inline void put4(const Q8Args& a, E* y, int n, const intx4& sum, float sm, const float4& ws,
                             const float4& bias, bool wide) {
@@ -213,9 +213,9 @@ __device__ inline bool wide_rows(const Q8Args& a) {
 }
 
 // Few tokens (up to 16 MB): the weights are read once, straight into the operands of the matrix instruction, and
-// bound it.  A workgroup takes 16 channels; its four waves split K in turns of U slices of 64 bytes (two
-// neighbouring slices are a line of memory) and add their sums up in LDS.  8 tokens x 2048 x 2048: 4.2 MB in 4.0 us, a
-// trip to memory and the ends of a launch.
+// bound it.  A workgroup takes 16 channels; its four waves split K in turns of U slices of 64 bytes (two neighbouring
+// slices are a line of memory) and add their sums up in LDS.  8 tokens x 2048 x 2048: 4.2 MB in 4.0 us, a trip to
+// memory and the ends of a launch.
 template <typename E, int MB>
 __global__ __launch_bounds__(256) void q8_few_kernel(Q8Args a) {
   constexpr int U = MB == 1 ? 8 : 4;
@@ -258,8 +258,8 @@ __global__ __launch_bounds__(256) void q8_few_kernel(Q8Args a) {
   put4<E>(a, (E*)a.y + (long long)m * a.c.ldy, n, sum, a.scale[m], ws, bias, wide_rows<E>(a));
 }
 
-// Up to 16 tokens of rows that a wave holds: one launch (8 tokens x 2048 x 2048: 7.9 us).  Every workgroup quantises all of them into LDS, from the L2 that
-// they share, while its first weights are on their way.
+// Up to 16 tokens of rows that a wave holds: one launch (8 tokens x 2048 x 2048: 7.8 us).  Every workgroup quantises
+// all of them into LDS, from the L2 that they share, while its first weights are on their way.
 constexpr int FUSED_LDS = 52 << 10, FUSED_WAVES = 8;
 template <typename E>
 __global__ __launch_bounds__(64 * FUSED_WAVES) void q8_fused_kernel(Q8Args a) {
@@ -309,12 +309,12 @@ __global__ __launch_bounds__(64 * FUSED_WAVES) void q8_fused_kernel(Q8Args a) {
 }
 
 // A tile of TM tokens x TN channels: four waves, each half of either.  Slices of 128 bytes of K go through one of two
-// LDS buffers; a row's 16-byte pieces lie in the order piece ^ (row & 7), which spreads a fragment's rows over the banks.
-// While the matrix instructions of slice s run, slice s + 1 goes from registers to the other buffer and slice
+// LDS buffers; a row's 16-byte pieces lie in the order piece ^ (row & 7), which spreads a fragment's rows over the
+// banks.  While the matrix instructions of slice s run, slice s + 1 goes from registers to the other buffer and slice
 // s + 2 is loaded; the fragments of a quarter of a slice are read during the instructions of the quarter before, the
-// first of the next slice behind the barrier in front of the last quarter.  32768 x 2048 x 2048: 186-188 us, 1.5 POP/s; 135 us of
-// them are the loop over K (2.0 POP/s; a library's 8192^3 reaches 2.1), the rest results, which a workgroup alone on its CU (all
-// registers are taken) does not overlap with anything.
+// first of the next slice behind the barrier in front of the last quarter.  32768 x 2048 x 2048: 186-200 us over
+// traces, 1.4-1.5 POP/s; 135 us of them are the loop over K (2.0 POP/s; a library's 8192^3 reaches 2.1), the rest
+// results, which a workgroup alone on its CU (all registers are taken) does not overlap with anything.
 template <typename E, int TM, int TN>
 __global__ __launch_bounds__(256) void q8_tile_kernel(Q8Args a, int tiles_m, int tiles_n) {
   constexpr int WM = TM / 64, WN = TN / 64;              // 32 x 32 blocks of a wave
@@ -389,8 +389,8 @@ __global__ __launch_bounds__(256) void q8_tile_kernel(Q8Args a, int tiles_m, int
           acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[kk & 1][i], fx[kk & 1][j], acc[i][j], 0, 0, 0);
     }
   }
-  // Scales and biases of the tile's channels through LDS; the results too, 32 tokens of a wave at a time, so that rows are
-  // stored whole (from the lanes' own places a store would write 16 bytes each of 32 rows).
+  // Scales and biases of the tile's channels through LDS; the results too, 32 tokens of a wave at a time, so that
+  // rows are stored whole (from the lanes' own places a store would write 16 bytes each of 32 rows).
   __syncthreads();
   constexpr int CH = TN / 2, ROW = CH * (int)sizeof(E) + 16, PIECES = CH * (int)sizeof(E) / 16;
   constexpr int PER = 16 / (int)sizeof(E);
@@ -455,10 +455,11 @@ static void tile_start(const Q8Args& a, hipStream_t s) {
   hipLaunchKernelGGL((q8_tile_kernel<E, TM, TN>), dim3((unsigned)tm * (unsigned)tn), dim3(256), 0, s, a, tm, tn);
 }
 // Which product.  Measured with quantisation, K = 2048, bf16, us on the GPU:
-//  - few tokens : tiles of 64 x 64.  17 x 2048 7.7 : 11.8, 64 x 2048 10.2 : 12.0, 64 x 8192 15.2 : 12.3 (every workgroup of
-//    the former reads all tokens from the L2, and there are N / 16 of them), 48 x 8192 (K = 4096) 21.5 : 19.4;
-//  - tiles of 64 : 128 : 256.  1024 x 2048 17 : 21 : 44, 2048 x 2048 26 : 25 : 48, 4096 x 2048 47 : 37 : 53, 6144 x 2048
-//    69 : 52 : 57, 8192 x 2048 85 : 68 : 63, 1024 x 8192 49 : 33 : 48.  That is 20 us per 1024 tiles of 64 (four
+//  - few tokens : tiles of 64 x 64.  17 x 2048 7.7 : 11.8, 64 x 2048 10.2 : 12.0, 64 x 8192 15.2 : 12.3 (every
+//    workgroup of the former reads all tokens from the L2, and there are N / 16 of them), 48 x 8192 (K = 4096) 21.5 :
+//    19.4;
+//  - tiles of 64 : 128 : 256.  1024 x 2048 17 : 21 : 44, 2048 x 2048 26 : 25 : 48, 4096 x 2048 47 : 37 : 53, 6144 x
+//    2048 69 : 52 : 57, 8192 x 2048 85 : 68 : 63, 1024 x 8192 49 : 33 : 48.  That is 20 us per 1024 tiles of 64 (four
 //    of them share a CU), 27 per 512 of 128 (two) and 50 per round of 256 of 256 (one), 7 and 19 at least.
 static double tiles_of(const q8_cfg& c, long long t) {
   return (double)((c.M + t - 1) / t) * (double)((c.N + t - 1) / t);
@@ -493,10 +494,10 @@ static void q8_start(const Q8Args& a, hipStream_t s) {
     tile_start<E, 64, 64>(a, s);
   }
 }
-// LDS of the product that quantises the tokens itself, 0 where that has a launch of its own.  One launch : two, K = 2048, us
-// on the GPU: 1 x 2048 6.3 : 6.3, 8 x 2048 7.4 : 6.9, 16 x 2048 10.9 : 7.2, 1 x 8192 (K = 4096) 10.5 : 10.9, 8 x 8192 (K =
-// 4096) 17.1 : 12.4; the second launch takes 2.5 us of the host.  So: as long as the workgroups together
-// quantise at most 1024 rows.
+// LDS of the product that quantises the tokens itself, 0 where that has a launch of its own.  One launch : two, K =
+// 2048, us on the GPU: 1 x 2048 6.3 : 6.3, 8 x 2048 7.4 : 6.9, 16 x 2048 10.9 : 7.2, 1 x 8192 (K = 4096) 10.5 : 10.9,
+// 8 x 8192 (K = 4096) 17.1 : 12.4; the second launch takes 2.5 us of the host.  So: as long as the workgroups
+// together quantise at most 1024 rows.
 static size_t fused_lds(const Q8Args& a) {
   const int pad = q8_pad(a.c.K), held = 8 * 64 * (a.c.dtype == MGRIT_F32 ? 4 : 8);
   const size_t need = (size_t)a.c.M * (pad + 16);

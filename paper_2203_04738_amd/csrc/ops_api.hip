@@ -1,5 +1,5 @@
-// C ABI of the operators around a gated linear recurrent layer (include/mgrit_ops.h): arguments are checked on the host
-// before anything is launched.
+// C ABI of the operators around a gated linear recurrent layer (include/mgrit_ops.h): arguments are checked on the
+// host before anything is launched.
 #include <cmath>
 
 #include "ops.h"

@@ -11,12 +11,13 @@ layer j + 1 reads the states of layer j, the head reads the top layer's.
 * `step` is a training step: forward (`glr_forward`), loss and gradient with respect to the logits in one pass
   (`distill_topk`), backward (`glr_backward`), torch Adam.  The products of training are torch matrix
   products, as the head of `training.GruStackTrainer` is;
-* `Served` is the trained student for serving: its weights in 8 bits (`q8_quantize`), products `q8_linear`; `read` takes
-  whole prompts in, `next` one token of each running sequence (`glr_step` on a pool of states), both
+* `Served` is the trained student for serving: its weights in 8 bits (`q8_quantize`), products `q8_linear`; `read`
+  takes whole prompts in, `next` one token of each running sequence (`glr_step` on a pool of states), both
   return logits, and `alternatives` scores them (`token_logprobs`).
 
-Teachers are whatever gives logits per position; the states of a GRU layer (`gru_serial_scan`, `mgrit_gru_forward`) times a
-head are what this framework trains.  ``python -m paper_2203_04738_amd.student`` runs the whole path on a small example.
+Teachers are whatever gives logits per position; the states of a GRU layer (`gru_serial_scan`, `mgrit_gru_forward`)
+times a head are what this framework trains.  ``python -m paper_2203_04738_amd.student`` runs the whole path on a
+small example.
 """
 from __future__ import annotations
 
@@ -47,8 +48,8 @@ def _CODES():
 
 
 class LinearStudent:
-    """params: per layer [W[2H,D_j], b[2H]] (gates above candidates), head: [W_o[V,H], b_o[V]]; float32 CUDA tensors, updated
-    in place.  T, B: steps and batch of a training step."""
+    """params: per layer [W[2H,D_j], b[2H]] (gates above candidates), head: [W_o[V,H], b_o[V]]; float32 CUDA
+    tensors, updated in place.  T, B: steps and batch of a training step."""
 
     def __init__(self, T: int, B: int, params, head, *, K: int, temperature: float = 1.0, lr: float = 1e-3):
         import torch
@@ -143,8 +144,9 @@ class Served:
         return y
 
     def read(self, x, slots):
-        """Takes prompts x[T,B,D] in from zero states and leaves their states in the pool rows `slots` (int32 [B]; a row whose slot
-        is outside the pool is idle, as in `next`: no state is touched); returns the logits [B,V] behind their last step."""
+        """Takes prompts x[T,B,D] in from zero states and leaves their states in the pool rows `slots` (int32 [B]; a row
+        whose slot is outside the pool is idle, as in `next`: no state is touched); returns the logits [B,V] behind
+        their last step."""
         import torch
         T, B, H = x.shape[0], x.shape[1], self.H
         n = len(self.state[0])
