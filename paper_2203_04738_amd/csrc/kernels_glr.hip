@@ -116,7 +116,7 @@ struct Gate {
   }
 };
 // The same as the adjoint keeps it between its sweeps.  BOTH: a and 1 - a (16-bit arrays leave the registers for it,
-// and arithmetic is what those wait for).  Otherwise one float, the smaller of the two under the sign of g, which
+// and it saves instructions).  Otherwise one float, the smaller of the two under the sign of g, which
 // says which it is.
 template <int FORM, bool BOTH>
 struct KeptGate {
