@@ -132,7 +132,8 @@ MGRIT_API int token_logprobs(const logits_cfg* cfg, const void* logits, const in
  *     q = softmax over the row's entries of teacher / t,   loss = sum_k q_k (log q_k - log p[ids_k]),
  *     dlogits = weight / t (p - sum_k q_k e[ids_k]).
  *   ids[N,K] int64 (negative: padding, no entry; the same id twice: both count), teacher[N,K] float (-inf: no
- *   weight).  A row without any entry of weight has loss 0 and gradient 0.  K = 1 is cross entropy.
+ *   weight; nor has an entry whose q is below the smallest normal float).  A row without any entry of weight
+ *   has loss 0 and gradient 0.  K = 1 is cross entropy.
  *   An id >= V makes its row NaN.  K <= 256.
  *   weight[N] float or NULL (ones): dL/dloss of each row; a row of weight 0 has gradient 0 whatever it holds.
  *   loss[N] float (not multiplied by the weight).
