@@ -11,7 +11,8 @@ LIB = os.path.join(HERE, "libmgrit_gru.so")
 SOURCES = ["api.hip", "kernels_forward.hip", "kernels_adjoint.hip", "kernels_ode.hip",
            "kernels_lstm.hip", "kernels_misc.hip", "kernels_scan.hip",
            "kernels_scan_xcd.hip", "kernels_sweep.hip", "ops_api.hip", "kernels_glr.hip",
-           "kernels_logits.hip", "kernels_q8.hip"]
+           "kernels_logits.hip", "kernels_q8.hip", "tokens_api.hip", "kernels_embed.hip",
+           "kernels_conv.hip", "kernels_ssm.hip"]
 FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fvisibility=hidden",
     # packed fp32 instructions are kept off on the test machines

@@ -21,6 +21,7 @@
 
 #include "elem.h"
 #include "ops.h"
+#include "pairs.h"
 
 namespace mg {
 
@@ -33,71 +34,6 @@ struct Pair {
   float x, y;
 };
 
-// Raw words of two neighbouring channels of one step.
-template <typename E>
-struct RawPair {
-  unsigned w[sizeof(E) / 2];
-  __device__ inline void anew() {
-#pragma unroll
-    for (unsigned& x : w) asm volatile("" : "+v"(x));
-  }
-  __device__ inline void set(float x) {
-    const E e = elem_of<E>(x);
-    if constexpr (sizeof(E) == 4) w[0] = w[1] = __float_as_uint(e);
-    else w[0] = (unsigned)e.bits * 0x10001u;
-  }
-  __device__ inline float at(int i) const {
-    if constexpr (sizeof(E) == 4) return __uint_as_float(w[i]);
-    else return word_elem<E>(w[0], i);
-  }
-};
-// Channels c and c + 1 of a step at p; ALIGNED: as one word, with c + 1 < H.  Otherwise `second` says whether
-// there is a channel c + 1.
-template <typename E, bool ALIGNED>
-__device__ inline RawPair<E> load_pair(const E* p, bool second) {
-  RawPair<E> r;
-  if constexpr (ALIGNED) {
-    if constexpr (sizeof(E) == 4) {
-      const uint2 v = *reinterpret_cast<const uint2*>(p);
-      r.w[0] = v.x;
-      r.w[1] = v.y;
-    } else {
-      r.w[0] = *reinterpret_cast<const unsigned*>(p);
-    }
-  } else {
-    const E a = p[0], b = p[second ? 1 : 0];
-    if constexpr (sizeof(E) == 4) {
-      r.w[0] = __float_as_uint(a);
-      r.w[1] = __float_as_uint(b);
-    } else {
-      r.w[0] = (unsigned)a.bits | ((unsigned)b.bits << 16);
-    }
-  }
-  return r;
-}
-template <typename E, bool ALIGNED>
-__device__ inline void store_pair(E* p, float a, float b, bool second, bool past = false) {
-  if constexpr (ALIGNED) {
-    typedef float Word __attribute__((ext_vector_type(2)));
-    if constexpr (sizeof(E) == 4) {
-      const Word w = {a, b};
-      store_as(reinterpret_cast<Word*>(p), w, past);
-    } else {
-      store_as(reinterpret_cast<unsigned*>(p), pack2<E>(a, b), past);
-    }
-  } else {
-    p[0] = elem_of<E>(a);
-    if (second) p[1] = elem_of<E>(b);
-  }
-}
-
-// exp(x), x of any size: 2^p with p = x log2(e) as rounded, and e^r for what the rounding left, r = x - p ln 2 (at
-// most 2^-17 where 2^p is a number other than 0; where x is infinite, NaN, for which fminf takes the bound).  Without
-// the second factor the result is off by 7 units of 2^-24 at x = -6, 16 at -20, 62 at -80.
-__device__ inline float exp_of(float x) {
-  const float p = LOG2E * x, e = __builtin_amdgcn_exp2f(p);
-  return fmaf(e, fminf(fmaf(-p, LN2, x), 0x1p-16f), e);
-}
 // a and, for GLR_MIX, 1 - a of a gate, both to a few units of their own last place: with e = exp(-|g|), the smaller
 // of the two is e / (1 + e) at any g, and the larger one 1 minus that.
 template <int FORM>
@@ -661,12 +597,6 @@ __global__ __launch_bounds__(GLR_THREADS, 4) void glr_backward_kernel(GlrArgs a)
   };
   if (whole) write(std::false_type{});
   else write(std::true_type{});
-}
-
-// Whether two channels of every step of the array are one aligned word.
-template <typename E>
-static bool pairs(const glr_seq& q, int H) {
-  return H % 2 == 0 && q.stride_t % 2 == 0 && q.stride_b % 2 == 0 && (uintptr_t)q.data % (2 * sizeof(E)) == 0;
 }
 
 // Whether the steps of a wave lie within 32-bit offsets.

@@ -1,5 +1,5 @@
-// Rows of logits (include/mgrit_ops.h): log probabilities with entropy and top alternatives, and the distillation
-// loss with its gradient.
+// Rows of logits (include/mgrit_ops.h, mgrit_tokens.h): log probabilities with entropy and top alternatives, the
+// distillation loss and the policy loss with their gradients.
 //
 // A team of 1, 4 or 16 waves holds a row, or a segment of a long one, in registers as it was stored, 16 bytes per
 // load: one pass over memory, and everything after it (maximum, sums, alternatives, gradient) reads registers.  Rows
@@ -14,7 +14,8 @@
 #include <type_traits>
 
 #include "elem.h"
-#include "ops.h"
+#include "pairs.h"
+#include "tokens.h"
 
 namespace mg {
 
@@ -909,6 +910,154 @@ __global__ __launch_bounds__((TeamOf<E, NW>::block)) void distill_grad_kernel(Di
   else put_gradient<E, NW>(a, held, out, lo, hi, a.stats_in[2 * row], a.stats_in[2 * row + 1], w, t, tid);
 }
 
+// ---- policy loss
+struct PolicyRows {
+  DistillArgs d;             // (K = 1: the sampled token is all of the teacher's side)
+  policy_cfg rule;
+  float t;
+  const float *old_logp, *ref_logp, *advantage;
+  float *logp, *ratio, *kl;
+};
+// What a row's statistics make of its token.
+struct PolicyTerm {
+  float loss, logp, ratio, kl;
+  float slope;               // dloss / dlogp
+};
+// exp(d) - 1 - d.  Below 1/2 by its series, whose terms from d^11 / 11! on are below 2^-24 of it.
+__device__ inline float exp_beyond_line(float d) {
+  if (fabsf(d) < 0.5f) {
+    float p = fmaf(d, 1.f / 3628800, 1.f / 362880);
+    p = fmaf(d, p, 1.f / 40320);
+    p = fmaf(d, p, 1.f / 5040);
+    p = fmaf(d, p, 1.f / 720);
+    p = fmaf(d, p, 1.f / 120);
+    p = fmaf(d, p, 1.f / 24);
+    p = fmaf(d, p, 1.f / 6);
+    return d * d * fmaf(d, p, 0.5f);
+  }
+  return d == __builtin_inff() ? d : exp_of(d) - 1.f - d;
+}
+// x: the token's logit.  Differences of log probabilities are small beside them: those are kept in 64 bits.
+__device__ inline PolicyTerm policy_term(const PolicyRows& a, long long row, float x, float m, float s) {
+  PolicyTerm p;
+  double lp = -(double)__builtin_inff();
+  if (x != x || m != m || s != s) lp = (double)__uint_as_float(0x7fc00000u);
+  else if (s != 0.f && x != -__builtin_inff()) lp = ((double)x - (double)m) / (double)a.t - log((double)s);
+  p.logp = (float)lp;
+  const float A = a.advantage[row], r = exp_of((float)(lp - (double)a.old_logp[row]));
+  const float in = fminf(fmaxf(r, 1.f - a.rule.clip_low), 1.f + a.rule.clip_high);
+  const float gain = r * A, clipped = (r != r ? r : in) * A;
+  p.ratio = r;
+  p.loss = gain > clipped ? -clipped : -gain;
+  p.slope = gain > clipped ? 0.f : -gain;
+  p.kl = 0.f;
+  if (a.ref_logp) {
+    const float d = (float)((double)a.ref_logp[row] - lp);
+    p.kl = exp_beyond_line(d);
+    if (a.rule.kl != 0.f) {
+      p.loss = fmaf(a.rule.kl, p.kl, p.loss);
+      p.slope -= a.rule.kl * (p.kl + d);
+    }
+  }
+  return p;
+}
+// The same for any token, with what put_gradient needs in t, by one thread.
+template <typename E>
+__device__ inline PolicyTerm policy_row(const PolicyRows& a, long long row, const E* x, float m, float s, Teacher& t) {
+  const long long tok = a.d.ids[row];
+  PolicyTerm p = {0.f, 0.f, 0.f, 0.f, 0.f};
+  t.q[0] = 1.f;
+  t.id[0] = -1;
+  t.x[0] = 0.f;
+  t.total = tok < 0 ? 0.f : 1.f;
+  if (tok >= a.d.V) {
+    p.loss = p.logp = p.ratio = p.kl = p.slope = t.total = __uint_as_float(0x7fc00000u);
+  } else if (tok >= 0) {
+    t.id[0] = (int)tok;
+    t.x[0] = elem_f32(x[tok]);
+    p = policy_term(a, row, t.x[0], m, s);
+  }
+  return p;
+}
+__device__ inline void put_policy(const PolicyRows& a, long long row, const PolicyTerm& p, float m, float s) {
+  a.d.loss[row] = p.loss;
+  if (a.logp) a.logp[row] = p.logp;
+  if (a.ratio) a.ratio[row] = p.ratio;
+  if (a.kl) a.kl[row] = p.kl;
+  if (a.d.stats) {
+    a.d.stats[2 * row] = m;
+    a.d.stats[2 * row + 1] = s;
+  }
+}
+// w of put_gradient: the gradient is -weight slope / t (p - e[token]).
+__device__ inline float policy_weight(const PolicyRows& a, long long row, float slope) {
+  const float w = a.d.weight ? a.d.weight[row] : 1.f;
+  return w == 0.f ? 0.f : -(w * slope) * a.d.inv_t;
+}
+
+// A row in one team.
+template <typename E, int NW>
+__global__ __launch_bounds__((TeamOf<E, NW>::block)) void policy_kernel(PolicyRows a) {
+  using T = TeamOf<E, NW>;
+  __shared__ float part[NW == 1 ? 1 : NW][2];
+  __shared__ Teacher teachers[T::teams];
+  __shared__ float weights[T::teams];
+  const int team = NW == 1 ? threadIdx.x >> 6 : 0, tid = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const long long row = (long long)blockIdx.x * T::teams + team;
+  if (row >= a.d.N) return;
+  Teacher& t = teachers[team];
+  const E* x = (const E*)a.d.logits + row * a.d.ld;
+  Held<E, NW> held;
+  held.load(x, 0, a.d.V, row_shift(x), tid);
+  float largest[T::loads];
+  const Stats st = team_stats<E, NW, false>(held, a.d.inv_t * LOG2E, tid, part, largest);
+  if (tid == 0) {
+    const PolicyTerm p = policy_row<E>(a, row, x, st.m, st.s, t);
+    put_policy(a, row, p, st.m, st.s);
+    weights[team] = policy_weight(a, row, p.slope);
+  }
+  if (!a.d.dlogits) return;
+  team_sync<NW>();
+  E* out = (E*)a.d.dlogits + row * a.d.ld_grad;
+  const float w = weights[team];
+  if (t.total == 0.f || w == 0.f) put_zeros(out, 0, a.d.V, tid, T::threads);
+  else put_gradient<E, NW>(a.d, held, out, 0, a.d.V, st.m, st.s, w, t, tid);
+}
+// Loss of a long row from the statistics of its segments; one wave.
+template <typename E>
+__global__ __launch_bounds__(64) void policy_join_kernel(PolicyRows a) {
+  __shared__ Teacher t;
+  const long long row = blockIdx.x;
+  const Stats st = join_stats(a.d.out, row, a.d.shape.segs, a.d.inv_t * LOG2E, threadIdx.x);
+  if (threadIdx.x == 0)
+    put_policy(a, row, policy_row<E>(a, row, (const E*)a.d.logits + row * a.d.ld, st.m, st.s, t), st.m, st.s);
+}
+// Gradient of a row, or of a segment of one, from its statistics.
+template <typename E, int NW>
+__global__ __launch_bounds__((TeamOf<E, NW>::block)) void policy_grad_kernel(PolicyRows a) {
+  using T = TeamOf<E, NW>;
+  __shared__ Teacher teachers[T::teams];
+  __shared__ float weights[T::teams];
+  const int team = NW == 1 ? threadIdx.x >> 6 : 0, tid = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const long long item = (long long)blockIdx.x * T::teams + team;
+  const long long row = item / a.d.shape.segs;
+  const int seg = (int)(item - row * a.d.shape.segs);
+  if (row >= a.d.N) return;
+  Teacher& t = teachers[team];
+  const E* x = (const E*)a.d.logits + row * a.d.ld;
+  const int begin = seg * a.d.shape.seg * T::per_load - row_shift(x);
+  const int lo = max(begin, 0), hi = (int)min((long long)a.d.V, begin + (long long)a.d.shape.seg * T::per_load);
+  Held<E, NW> held;
+  held.load(x, lo, hi, lo - begin, tid);
+  const float m = a.d.stats_in[2 * row], s = a.d.stats_in[2 * row + 1];
+  if (tid == 0) weights[team] = policy_weight(a, row, policy_row<E>(a, row, x, m, s, t).slope);
+  team_sync<NW>();
+  E* out = (E*)a.d.dlogits + row * a.d.ld_grad;
+  const float w = weights[team];
+  if (t.total == 0.f || w == 0.f) put_zeros(out, lo, hi, tid, T::threads);
+  else put_gradient<E, NW>(a.d, held, out, lo, hi, m, s, w, t, tid);
+}
+
 // ---- launches
 static int elem_size(int dtype) { return dtype == MGRIT_F32 ? 4 : 2; }
 static bool rows_aligned(const void* p, long long ld, int size) {
@@ -1090,6 +1239,93 @@ hipError_t launch_distill_grad(const LogitsArgs& a, hipStream_t s) {
   if (a.c.dtype == MGRIT_F32) return grad_start<float>(a, a.stats_in, s);
   if (a.c.dtype == MGRIT_BF16) return grad_start<Bf16>(a, a.stats_in, s);
   return grad_start<F16>(a, a.stats_in, s);
+}
+
+static PolicyRows policy_rows(const PolicyArgs& a) {
+  PolicyRows p{};
+  LogitsArgs l{};
+  l.c = a.c;
+  l.c.K = 1;
+  l.logits = a.logits;
+  l.ids = a.tokens;
+  l.weight = a.weight;
+  l.loss = a.loss;
+  l.stats = a.stats;
+  l.dlogits = a.dlogits;
+  p.d = distill_args(l);
+  p.rule = a.rule;
+  p.t = a.c.temperature;
+  p.old_logp = a.old_logp;
+  p.ref_logp = a.ref_logp;
+  p.advantage = a.advantage;
+  p.logp = a.logp;
+  p.ratio = a.ratio;
+  p.kl = a.kl;
+  return p;
+}
+template <typename E>
+static hipError_t policy_grad_start(const PolicyArgs& a, const float* stats, hipStream_t s) {
+  PolicyRows p = policy_rows(a);
+  p.d.stats_in = stats;
+  const bool aligned = rows_aligned(a.logits, a.c.ld, sizeof(E));
+  const unsigned N = (unsigned)a.c.N;
+  if (!teams_launchable(a.c, sizeof(E), aligned)) return TOO_LARGE;
+  switch (team_waves(a.c.V, sizeof(E), aligned)) {
+    case 1:
+      p.d.shape = {1, TeamOf<E, 1>::chunks};
+      hipLaunchKernelGGL((policy_grad_kernel<E, 1>), dim3((N + 3) / 4), dim3(256), 0, s, p);
+      break;
+    case 4:
+      p.d.shape = {1, TeamOf<E, 4>::chunks};
+      hipLaunchKernelGGL((policy_grad_kernel<E, 4>), dim3(N), dim3(256), 0, s, p);
+      break;
+    case 16:
+      p.d.shape = {1, TeamOf<E, 16>::chunks};
+      hipLaunchKernelGGL((policy_grad_kernel<E, 16>), dim3(N), dim3(1024), 0, s, p);
+      break;
+    default:
+      p.d.shape = segments(a.c.V, sizeof(E), aligned);
+      hipLaunchKernelGGL((policy_grad_kernel<E, 16>), dim3(N * (unsigned)p.d.shape.segs), dim3(1024), 0, s, p);
+  }
+  return hipGetLastError();
+}
+template <typename E>
+static hipError_t policy_start(const PolicyArgs& a, hipStream_t s) {
+  PolicyRows p = policy_rows(a);
+  const bool aligned = rows_aligned(a.logits, a.c.ld, sizeof(E));
+  const unsigned N = (unsigned)a.c.N;
+  if (!teams_launchable(a.c, sizeof(E), aligned)) return TOO_LARGE;
+  switch (team_waves(a.c.V, sizeof(E), aligned)) {
+    case 1:
+      hipLaunchKernelGGL((policy_kernel<E, 1>), dim3((N + 3) / 4), dim3(256), 0, s, p);
+      return hipGetLastError();
+    case 4:
+      hipLaunchKernelGGL((policy_kernel<E, 4>), dim3(N), dim3(256), 0, s, p);
+      return hipGetLastError();
+    case 16:
+      hipLaunchKernelGGL((policy_kernel<E, 16>), dim3(N), dim3(1024), 0, s, p);
+      return hipGetLastError();
+  }
+  p.d.shape = segments(a.c.V, sizeof(E), aligned);
+  p.d.out = seg_out(a.workspace, a.c.N, p.d.shape.segs);
+  if (!p.d.stats) p.d.stats = (float*)p.d.out.top;           // (no alternatives here: the space behind)
+  hipLaunchKernelGGL((distill_segment_kernel<E>), dim3(N * (unsigned)p.d.shape.segs), dim3(1024), 0, s, p.d);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((policy_join_kernel<E>), dim3(N), dim3(64), 0, s, p);
+  e = hipGetLastError();
+  if (e != hipSuccess || !a.dlogits) return e;
+  return policy_grad_start<E>(a, p.d.stats, s);
+}
+hipError_t launch_policy(const PolicyArgs& a, hipStream_t s) {
+  if (a.c.dtype == MGRIT_F32) return policy_start<float>(a, s);
+  if (a.c.dtype == MGRIT_BF16) return policy_start<Bf16>(a, s);
+  return policy_start<F16>(a, s);
+}
+hipError_t launch_policy_grad(const PolicyArgs& a, hipStream_t s) {
+  if (a.c.dtype == MGRIT_F32) return policy_grad_start<float>(a, a.stats_in, s);
+  if (a.c.dtype == MGRIT_BF16) return policy_grad_start<Bf16>(a, a.stats_in, s);
+  return policy_grad_start<F16>(a, a.stats_in, s);
 }
 
 }  // namespace mg

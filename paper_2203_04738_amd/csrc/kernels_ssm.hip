@@ -1,0 +1,812 @@
+// Selective state space scan (include/mgrit_tokens.h), its adjoint, and one step of it.
+//
+// Four lanes are a channel, each with a quarter of its states; 16 channels are a wave.  What a channel has per step
+// (d, x, gates) is computed for four steps at a time, one by each of its lanes, and handed round by quad permutations;
+// sums over the states are exchanges between the four lanes.  b and c, the same for all channels, are staged in LDS a
+// tile of steps at a time.
+//
+// Where there are too few channels and batch rows to fill the card, a sequence is cut into chunks.  A chunk is the map
+// h -> P h + S with S its result from a zero state and P = exp(a sum d): first every chunk's S and sum of d, then the
+// states between chunks, one chunk after the other, then the chunks from their true states.
+#include <type_traits>
+
+#include "elem.h"
+#include "pairs.h"
+#include "tokens.h"
+
+namespace mg {
+
+constexpr int SSM_THREADS = 256, SSM_COLS = 64, SSM_TILE = 16;
+
+// ---- lanes of a channel
+template <int J>
+__device__ inline float quad_of(float v) {                // lane J of the four
+  return __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), J * 0x55, 0xf, 0xf, true));
+}
+__device__ inline float quad_xor1(float v) {
+  return __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0xb1, 0xf, 0xf, true));
+}
+__device__ inline float quad_xor2(float v) {
+  return __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x4e, 0xf, 0xf, true));
+}
+// p[j] of every lane: the sum over the four lanes of p[q] in lane q.
+__device__ inline float quad_sums(const float (&p)[4], int q) {
+  const bool odd = q & 1, high = q & 2;
+  const float a = (odd ? p[1] : p[0]) + quad_xor1(odd ? p[0] : p[1]);
+  const float b = (odd ? p[3] : p[2]) + quad_xor1(odd ? p[2] : p[3]);
+  return (high ? b : a) + quad_xor2(high ? a : b);
+}
+__device__ inline float quad_sum(float v) {
+  v += quad_xor1(v);
+  return v + quad_xor2(v);
+}
+
+// ---- elementwise
+// softplus(v) and its derivative sigmoid(v).  With e = exp(-|v|): softplus = max(v, 0) + log(1 + e), and log(1 + e) =
+// 2 atanh(s), s = e / (2 + e) <= 1/3, whose series in s^2 <= 1/9 ends below 2^-25 of it behind s^16.
+struct Softplus {
+  float d, slope;
+  __device__ inline explicit Softplus(float v) {
+    const float e = exp_of(-fabsf(v));
+    const float s = e * __builtin_amdgcn_rcpf(2.0f + e), w = s * s;
+    float p = fmaf(w, 1.f / 17, 1.f / 15);
+    p = fmaf(w, p, 1.f / 13);
+    p = fmaf(w, p, 1.f / 11);
+    p = fmaf(w, p, 1.f / 9);
+    p = fmaf(w, p, 1.f / 7);
+    p = fmaf(w, p, 1.f / 5);
+    p = fmaf(w, p, 1.f / 3);
+    const float l = fmaf(2.f * s * w, p, 2.f * s);
+    d = v > 0.f ? v + l : v == v ? l : v;
+    const float small = e * __builtin_amdgcn_rcpf(1.0f + e);
+    slope = v < 0.f ? small : 1.0f - small;
+    if (v != v) slope = v;
+  }
+};
+// sigmoid(z) and 1 - sigmoid(z)
+struct Sigmoid {
+  float s, n;
+  __device__ inline explicit Sigmoid(float z) {
+    const float e = exp_of(-fabsf(z));
+    const float small = e * __builtin_amdgcn_rcpf(1.0f + e), large = 1.0f - small;
+    s = z < 0.f ? small : large;
+    n = z < 0.f ? large : small;
+    if (z != z) s = n = z;
+  }
+};
+
+// ---- states of a lane
+typedef float Quad __attribute__((ext_vector_type(4), aligned(4)));
+template <int SP>
+__device__ inline void load_states(const float* p, int S, int n0, float (&v)[SP]) {
+  if constexpr (SP >= 4) {
+    if (S == 4 * SP) {
+#pragma unroll
+      for (int i = 0; i < SP; i += 4) {
+        const Quad w = *reinterpret_cast<const Quad*>(p + n0 + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[i + k] = w[k];
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < SP; ++i) v[i] = n0 + i < S ? p[n0 + i] : 0.f;
+}
+template <int SP>
+__device__ inline void store_states(float* p, int S, int n0, const float (&v)[SP]) {
+  if constexpr (SP >= 4) {
+    if (S == 4 * SP) {
+#pragma unroll
+      for (int i = 0; i < SP; i += 4) *reinterpret_cast<Quad*>(p + n0 + i) = Quad{v[i], v[i + 1], v[i + 2], v[i + 3]};
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < SP; ++i)
+    if (n0 + i < S) p[n0 + i] = v[i];
+}
+
+// Where a thread stands.
+struct SsmPlace {
+  int q, wave, b, chunk, ch, n0;                     // ch: channel (one that exists)
+  bool has;                                          // whether it is the thread's own
+  long long at;                                      // of (b, ch) in [B,H]
+  int t0, t1;                                        // steps of the chunk
+  template <int SP>
+  __device__ inline void set(const SsmArgs& a, int first_chunk, std::integral_constant<int, SP>) {
+    const int tid = threadIdx.x;
+    q = tid & 3;
+    wave = tid >> 6;
+    n0 = q * SP;
+    const unsigned across = (unsigned)a.s.cols * a.c.B;
+    const unsigned k = blockIdx.x / across, rest = blockIdx.x - k * across;
+    chunk = first_chunk + (int)k;
+    b = (int)(rest / a.s.cols);
+    const int col = (int)(rest - (unsigned)b * a.s.cols);
+    ch = col * SSM_COLS + (tid >> 2);
+    has = ch < a.c.H;
+    if (!has) ch = a.c.H - 1;
+    at = (long long)b * a.c.H + ch;
+    t0 = chunk * a.s.len;
+    t1 = min(a.c.T, t0 + a.s.len);
+  }
+};
+
+// One element per step of a channel, from step t on; steps behind the last are read at the last.
+template <typename E>
+struct Steps {
+  const E* p;
+  long long stride;
+  __device__ inline Steps(const glr_seq& s, const SsmPlace& at)
+      : p((const E*)s.data + at.b * s.stride_b + at.ch), stride(s.stride_t) {}
+  __device__ inline E load(int t, int last) const { return p[min(t, last) * stride]; }
+};
+template <typename E>
+__device__ inline void put(const glr_seq& s, const SsmPlace& at, int t, float v) {
+  ((E*)s.data)[t * s.stride_t + at.b * s.stride_b + at.ch] = elem_of<E>(v);
+}
+
+// b and c of a tile of TB steps in LDS, as floats: [step][lane of four][b SP | c SP]; zeros where there is no state or
+// step.
+template <typename E, int SP, int TB>
+struct BcTile {
+  static constexpr int row = 8 * SP, n = TB * row, per = (n + SSM_THREADS - 1) / SSM_THREADS;
+  E raw[per];
+  __device__ inline void load(const SsmArgs& a, int b, int t0) {
+#pragma unroll
+    for (int k = 0; k < per; ++k) {
+      const int e = threadIdx.x + k * SSM_THREADS;
+      const int r = e % row, which = r / (4 * SP), s = r % (4 * SP), t = t0 + e / row;
+      const glr_seq& q = which ? a.cc : a.b;
+      raw[k] = elem_of<E>(0.f);
+      if (e < n && s < a.c.S && t < a.c.T) raw[k] = ((const E*)q.data)[t * q.stride_t + b * q.stride_b + s];
+    }
+  }
+  __device__ inline void store(float* lds) const {
+#pragma unroll
+    for (int k = 0; k < per; ++k) {
+      const int e = threadIdx.x + k * SSM_THREADS;
+      const int r = e % row, which = r / (4 * SP), s = r % (4 * SP);
+      if (e < n) lds[e / row * row + s / SP * (2 * SP) + which * SP + s % SP] = elem_f32(raw[k]);
+    }
+  }
+};
+template <int SP>
+__device__ inline void read_bc(const float* lds, int step, int q, int which, float (&v)[SP]) {
+  const float* p = lds + step * 8 * SP + q * 2 * SP + which * SP;
+#pragma unroll
+  for (int i = 0; i < SP; ++i) v[i] = p[i];
+}
+
+// Bits of the steps t0 .. t0 + n - 1 that reset.
+__device__ inline unsigned ssm_resets(const SsmArgs& a, int b, int t0, int n) {
+  if (!a.reset) return 0;
+  const int lane = threadIdx.x & 63, t = t0 + lane;
+  bool r = false;
+  if (lane < n && t < a.c.T) r = a.reset[(long long)t * a.c.B + b] != 0;
+  return (unsigned)__ballot(r);
+}
+
+__device__ inline float decay(float d, float a2) { return __builtin_amdgcn_exp2f(d * a2); }
+
+// ---- forward
+// MAIN: results of a chunk from its state; otherwise its end state from zero and the sum of its d.
+template <typename E, int SP, bool MAIN>
+__global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
+  constexpr int TB = SSM_TILE, G = TB / 4;
+  using Tile = BcTile<E, SP, TB>;
+  __shared__ float bc[2][Tile::n];
+  SsmPlace p;
+  p.set(a, 0, std::integral_constant<int, SP>());
+  const int S = a.c.S, last = a.c.T - 1, q = p.q;
+  float A2[SP], h[SP];
+  load_states<SP>(a.a + (long long)p.ch * S, S, p.n0, A2);
+#pragma unroll
+  for (int i = 0; i < SP; ++i) {
+    A2[i] *= LOG2E;
+    h[i] = 0.f;
+  }
+  if (MAIN && p.has) {
+    const long long at = p.at * S;
+    if (p.chunk > 0) load_states<SP>(a.ends + (long long)p.chunk * a.c.B * a.c.H * S + at, S, p.n0, h);
+    else if (a.h0) load_states<SP>(a.h0 + at, S, p.n0, h);
+  }
+  const float bias = a.bias ? a.bias[p.ch] : 0.f, skip = MAIN && a.skip ? a.skip[p.ch] : 0.f;
+  const bool gated = MAIN && a.z.data;
+  const Steps<E> xs(a.x, p), ds(a.dt, p), zs(gated ? a.z : a.x, p);
+  Tile next;
+  E xn[G], dn[G], zn[G];
+  auto load = [&](int t) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      xn[g] = xs.load(t + 4 * g + q, last);
+      dn[g] = ds.load(t + 4 * g + q, last);
+      if (gated) zn[g] = zs.load(t + 4 * g + q, last);
+    }
+    next.load(a, p.b, t);
+  };
+  load(p.t0);
+  float sum = 0.f;
+  bool forgets = false;
+  int buf = 0;
+  for (int t = p.t0; t < p.t1; t += TB, buf ^= 1) {
+    float x[G], d[G], z[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      x[g] = elem_f32(xn[g]);
+      d[g] = elem_f32(dn[g]);
+      z[g] = gated ? elem_f32(zn[g]) : 0.f;
+    }
+    next.store(bc[buf]);
+    const unsigned resets = ssm_resets(a, p.b, t, TB);
+    __syncthreads();
+    if (t + TB < p.t1) load(t + TB);
+    forgets |= resets != 0;
+    auto tile = [&](auto cut_) {
+      constexpr bool CUT = decltype(cut_)::value;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const int ts = t + 4 * g;
+        if (MAIN && a.saved && ts % a.s.save == 0 && ts < a.c.T && p.has)
+          store_states<SP>(a.saved + (ts / a.s.save * (long long)a.c.B * a.c.H + p.at) * S, S, p.n0, h);
+        const bool in = p.has && ts + q < a.c.T;
+        const float delta = in ? Softplus(d[g] + bias).d : 0.f;
+        const float xv = in ? x[g] : 0.f, dx = delta * xv;
+        if (!MAIN) sum += delta;
+        float part[4];
+        auto step = [&](auto j_) {
+          constexpr int j = decltype(j_)::value;
+          const float dj = quad_of<j>(delta), xj = quad_of<j>(dx);
+          const bool cut = CUT && (resets >> (4 * g + j) & 1);
+          float b[SP], c[SP];
+          read_bc<SP>(bc[buf], 4 * g + j, q, 0, b);
+          if (MAIN) read_bc<SP>(bc[buf], 4 * g + j, q, 1, c);
+          float y = 0.f;
+#pragma unroll
+          for (int i = 0; i < SP; ++i) {
+            h[i] = cut ? xj * b[i] : fmaf(decay(dj, A2[i]), h[i], xj * b[i]);
+            if (MAIN) y = fmaf(h[i], c[i], y);
+          }
+          part[j] = y;
+        };
+        step(std::integral_constant<int, 0>());
+        step(std::integral_constant<int, 1>());
+        step(std::integral_constant<int, 2>());
+        step(std::integral_constant<int, 3>());
+        if constexpr (MAIN) {
+          float y = quad_sums(part, q);
+          y = fmaf(skip, xv, y);
+          if (gated) y *= z[g] * Sigmoid(z[g]).s;
+          if (in) put<E>(a.y, p, ts + q, y);
+        }
+      }
+    };
+    if (resets) tile(std::true_type{});
+    else tile(std::false_type{});
+  }
+  if (!p.has) return;
+  if (MAIN) {
+    if (a.h_last && p.chunk == a.s.chunks - 1) store_states<SP>(a.h_last + p.at * S, S, p.n0, h);
+  } else {
+    const long long k = (long long)p.chunk * a.c.B * a.c.H + p.at;
+    store_states<SP>(a.ends + k * S, S, p.n0, h);
+    sum = quad_sum(sum);
+    if (q == 0) a.sums[k] = forgets ? -1.f : sum;
+  }
+}
+
+// The states between chunks, in place of the chunks' own: forward before, backward behind each chunk.  A thread per
+// state.
+__global__ __launch_bounds__(256) void ssm_between_kernel(SsmArgs a, const float* first, bool backward) {
+  const long long n = (long long)a.c.B * a.c.H * a.c.S, i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const long long bh = i / a.c.S, per = (long long)a.c.B * a.c.H;
+  const float a2 = LOG2E * a.a[bh % a.c.H * a.c.S + (i - bh * a.c.S)];
+  float v = first ? first[i] : 0.f;
+  const int K = a.s.chunks;
+  for (int s0 = 0; s0 < K; s0 += 8) {
+    float e[8], d[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const int step = min(s0 + s, K - 1), k = backward ? K - 1 - step : step;
+      // (the last chunk of the way has no map, and needs none)
+      e[s] = step < K - 1 ? a.ends[k * n + i] : 0.f;
+      d[s] = step < K - 1 ? a.sums[k * per + bh] : -1.f;
+    }
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      if (s0 + s >= K) break;
+      const int k = backward ? K - 1 - (s0 + s) : s0 + s;
+      a.ends[k * n + i] = v;
+      v = d[s] < 0.f || v == 0.f ? e[s] : fmaf(decay(d[s], a2), v, e[s]);
+    }
+  }
+}
+
+// ---- backward
+// mu_t = exp(d_t a) lambda_t is what step t hands on to step t - 1.  What a chunk hands on from nothing, and the sum of
+// its d.  (Chunk 0 hands on to nobody.)
+template <typename E, int SP>
+__global__ __launch_bounds__(SSM_THREADS) void ssm_adjoint_ends_kernel(SsmArgs a) {
+  constexpr int TB = SSM_TILE, G = TB / 4;
+  using Tile = BcTile<E, SP, TB>;
+  __shared__ float bc[2][Tile::n];
+  SsmPlace p;
+  p.set(a, 1, std::integral_constant<int, SP>());
+  const int S = a.c.S, last = a.c.T - 1, q = p.q;
+  float A2[SP], mu[SP];
+  load_states<SP>(a.a + (long long)p.ch * S, S, p.n0, A2);
+#pragma unroll
+  for (int i = 0; i < SP; ++i) {
+    A2[i] *= LOG2E;
+    mu[i] = 0.f;
+  }
+  const float bias = a.bias ? a.bias[p.ch] : 0.f;
+  const bool gated = a.z.data;
+  const Steps<E> ys(a.dy, p), ds(a.dt, p), zs(gated ? a.z : a.dy, p);
+  Tile next;
+  E yn[G], dn[G], zn[G];
+  auto load = [&](int t) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      yn[g] = ys.load(t + 4 * g + q, last);
+      dn[g] = ds.load(t + 4 * g + q, last);
+      if (gated) zn[g] = zs.load(t + 4 * g + q, last);
+    }
+    next.load(a, p.b, t);
+  };
+  const int tiles = (p.t1 - p.t0 + TB - 1) / TB;
+  load(p.t0 + (tiles - 1) * TB);
+  float sum = 0.f;
+  bool forgets = false;
+  int buf = 0;
+  for (int k = tiles - 1; k >= 0; --k, buf ^= 1) {
+    const int t = p.t0 + k * TB;
+    float y[G], d[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const bool in = p.has && t + 4 * g + q < a.c.T;
+      const float z = gated ? elem_f32(zn[g]) : 0.f, dy = elem_f32(yn[g]);
+      y[g] = !in ? 0.f : gated ? dy * (z * Sigmoid(z).s) : dy;
+      d[g] = in ? Softplus(elem_f32(dn[g]) + bias).d : 0.f;
+      sum += d[g];
+    }
+    next.store(bc[buf]);
+    const unsigned resets = ssm_resets(a, p.b, t, TB);
+    __syncthreads();
+    if (k > 0) load(t - TB);
+    forgets |= resets != 0;
+#pragma unroll
+    for (int g = G - 1; g >= 0; --g) {
+      auto step = [&](auto j_) {
+        constexpr int j = decltype(j_)::value;
+        const float dj = quad_of<j>(d[g]), yj = quad_of<j>(y[g]);
+        const bool cut = resets >> (4 * g + j) & 1;
+        float c[SP];
+        read_bc<SP>(bc[buf], 4 * g + j, q, 1, c);
+#pragma unroll
+        for (int i = 0; i < SP; ++i) {
+          const float m = decay(dj, A2[i]) * fmaf(c[i], yj, mu[i]);
+          mu[i] = cut ? 0.f : m;
+        }
+      };
+      step(std::integral_constant<int, 3>());
+      step(std::integral_constant<int, 2>());
+      step(std::integral_constant<int, 1>());
+      step(std::integral_constant<int, 0>());
+    }
+  }
+  if (!p.has) return;
+  const long long k = (long long)p.chunk * a.c.B * a.c.H + p.at;
+  store_states<SP>(a.ends + k * S, S, p.n0, mu);
+  sum = quad_sum(sum);
+  if (q == 0) a.sums[k] = forgets ? -1.f : sum;
+}
+
+// Sums of b's and c's gradients over the 16 channels of a wave: v = (of b, of c) of a lane's states, to
+// out[which * 4 SP + n].
+template <int SP>
+__device__ inline void channel_sums(const float (&v)[2 * SP], float* out, int lane) {
+  float w[SP], u[(SP + 1) / 2];
+#pragma unroll
+  for (int i = 0; i < SP; ++i) {               // lower half of the wave: of b, upper half: of c
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + SP]), false, false);
+    w[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  constexpr int H2 = (SP + 1) / 2;
+#pragma unroll
+  for (int i = 0; i < H2; ++i) {               // even rows of 16 lanes: the lower half of the states
+    const unsigned other = SP > 1 ? __float_as_uint(w[(i + H2) % SP]) : __float_as_uint(w[i]);
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(w[i]), other, false, false);
+    u[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    // the four channels of a row
+    u[i] += __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(u[i]), 0x124, 0xf, 0xf, true));
+    u[i] += __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(u[i]), 0x128, 0xf, 0xf, true));
+  }
+  if ((lane & 12) == 0 && (SP > 1 || (lane & 16) == 0)) {
+    const int n0 = (lane >> 5) * 4 * SP + (lane & 3) * SP + (SP > 1 && (lane & 16) ? H2 : 0);
+#pragma unroll
+    for (int i = 0; i < H2; ++i) out[n0 + i] = u[i];
+  }
+}
+
+template <typename E, int SP, int R>
+__global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
+  constexpr int G = R / 4;
+  using Tile = BcTile<E, SP, R>;
+  __shared__ float bc[2][Tile::n];
+  __shared__ float red[4][R][8 * SP];
+  SsmPlace p;
+  p.set(a, 0, std::integral_constant<int, SP>());
+  const int S = a.c.S, last = a.c.T - 1, q = p.q, lane = threadIdx.x & 63;
+  const long long states = (long long)a.c.B * a.c.H * S;
+  float A[SP], mu[SP], dA[SP];
+  load_states<SP>(a.a + (long long)p.ch * S, S, p.n0, A);
+#pragma unroll
+  for (int i = 0; i < SP; ++i) mu[i] = dA[i] = 0.f;
+  if (p.has) {
+    if (p.chunk < a.s.chunks - 1) load_states<SP>(a.ends + p.chunk * states + p.at * S, S, p.n0, mu);
+    else if (a.dh_last) load_states<SP>(a.dh_last + p.at * S, S, p.n0, mu);
+  }
+  const float bias = a.bias ? a.bias[p.ch] : 0.f, skip = a.skip ? a.skip[p.ch] : 0.f;
+  const bool gated = a.z.data;
+  const Steps<E> xs(a.x, p), ds(a.dt, p), ys(a.dy, p), zs(gated ? a.z : a.x, p);
+  Tile next;
+  E xn[G], dn[G], yn[G], zn[G];
+  float hn[SP];
+  auto load = [&](int t) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      xn[g] = xs.load(t + 4 * g + q, last);
+      dn[g] = ds.load(t + 4 * g + q, last);
+      yn[g] = ys.load(t + 4 * g + q, last);
+      if (gated) zn[g] = zs.load(t + 4 * g + q, last);
+    }
+    next.load(a, p.b, t);
+    load_states<SP>(a.saved + t / R * states + p.at * S, S, p.n0, hn);
+  };
+  const int tiles = (p.t1 - p.t0 + R - 1) / R;
+  load(p.t0 + (tiles - 1) * R);
+  float dskip = 0.f, dbias = 0.f;
+  int buf = 0;
+  for (int k = tiles - 1; k >= 0; --k, buf ^= 1) {
+    const int t = p.t0 + k * R;
+    float x[G], delta[G], slope[G], dy[G], z[G], out[G];    // out: dL/d(sum c h + skip x)
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const bool in = p.has && t + 4 * g + q < a.c.T;
+      const Softplus sp(elem_f32(dn[g]) + bias);
+      x[g] = in ? elem_f32(xn[g]) : 0.f;
+      delta[g] = in ? sp.d : 0.f;
+      slope[g] = sp.slope;
+      dy[g] = in ? elem_f32(yn[g]) : 0.f;
+      z[g] = gated ? elem_f32(zn[g]) : 0.f;
+      out[g] = gated && in ? dy[g] * (z[g] * Sigmoid(z[g]).s) : dy[g];
+    }
+    float h[SP];
+#pragma unroll
+    for (int i = 0; i < SP; ++i) h[i] = p.has ? hn[i] : 0.f;
+    next.store(bc[buf]);
+    const unsigned resets = ssm_resets(a, p.b, t, R);
+    __syncthreads();                               // (and red has been read)
+    if (k > 0) load(t - R);
+    auto tile = [&](auto cut_) {
+      constexpr bool CUT = decltype(cut_)::value;
+      float keep[R][SP], past[R][SP], sum[G];
+      // forward, again
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const float dx = delta[g] * x[g];
+        float part[4];
+        auto step = [&](auto j_) {
+          constexpr int j = decltype(j_)::value;
+          const int r = 4 * g + j;
+          const float dj = quad_of<j>(delta[g]), xj = quad_of<j>(dx);
+          const bool cut = CUT && (resets >> r & 1);
+          float b[SP], c[SP];
+          read_bc<SP>(bc[buf], r, q, 0, b);
+          read_bc<SP>(bc[buf], r, q, 1, c);
+          float y = 0.f;
+#pragma unroll
+          for (int i = 0; i < SP; ++i) {
+            past[r][i] = h[i];
+            keep[r][i] = decay(dj, A[i] * LOG2E);
+            h[i] = cut ? xj * b[i] : fmaf(keep[r][i], h[i], xj * b[i]);
+            y = fmaf(h[i], c[i], y);
+          }
+          part[j] = y;
+        };
+        step(std::integral_constant<int, 0>());
+        step(std::integral_constant<int, 1>());
+        step(std::integral_constant<int, 2>());
+        step(std::integral_constant<int, 3>());
+        sum[g] = quad_sums(part, q);
+      }
+      // back
+#pragma unroll
+      for (int g = G - 1; g >= 0; --g) {
+        const float dx = delta[g] * x[g];
+        float of_x[4], of_d[4];
+        auto step = [&](auto j_) {
+          constexpr int j = decltype(j_)::value;
+          const int r = 4 * g + j;
+          const float dj = quad_of<j>(delta[g]), xj = quad_of<j>(dx), oj = quad_of<j>(out[g]);
+          const bool cut = CUT && (resets >> r & 1);
+          float b[SP], c[SP], v[2 * SP];
+          read_bc<SP>(bc[buf], r, q, 0, b);
+          read_bc<SP>(bc[buf], r, q, 1, c);
+          float lb = 0.f, ld = 0.f;
+#pragma unroll
+          for (int i = 0; i < SP; ++i) {
+            const float lam = fmaf(c[i], oj, mu[i]);
+            v[i] = lam * xj;
+            v[SP + i] = oj * h[i];
+            lb = fmaf(lam, b[i], lb);
+            mu[i] = cut ? 0.f : keep[r][i] * lam;
+            const float m = cut ? 0.f : mu[i] * past[r][i];
+            ld = fmaf(m, A[i], ld);
+            dA[i] = fmaf(m, dj, dA[i]);
+            h[i] = past[r][i];
+          }
+          of_x[j] = lb;
+          of_d[j] = ld;
+          channel_sums<SP>(v, red[p.wave][r], lane);
+        };
+        step(std::integral_constant<int, 3>());
+        step(std::integral_constant<int, 2>());
+        step(std::integral_constant<int, 1>());
+        step(std::integral_constant<int, 0>());
+        const float lb = quad_sums(of_x, q), ld = quad_sums(of_d, q);
+        const int ts = t + 4 * g + q;
+        if (p.has && ts < a.c.T) {
+          const float ddt = fmaf(lb, x[g], ld) * slope[g];
+          put<E>(a.dx, p, ts, fmaf(lb, delta[g], out[g] * skip));
+          put<E>(a.ddt, p, ts, ddt);
+          if (gated) {
+            const Sigmoid sg(z[g]);
+            put<E>(a.dz, p, ts, dy[g] * fmaf(skip, x[g], sum[g]) * (sg.s * fmaf(z[g], sg.n, 1.f)));
+          }
+          dskip = fmaf(out[g], x[g], dskip);
+          dbias += ddt;
+        }
+      }
+    };
+    if (resets) tile(std::true_type{});
+    else tile(std::false_type{});
+    __syncthreads();
+    // the waves' sums of the tile
+    const int col = (int)(blockIdx.x % (unsigned)a.s.cols);
+    for (int e = threadIdx.x; e < R * 8 * SP; e += SSM_THREADS) {
+      const int r = e / (8 * SP), which = e % (8 * SP) / (4 * SP), n = e % (4 * SP);
+      if (n < S && t + r < a.c.T) {
+        const float* f = &red[0][r][which * 4 * SP + n];
+        constexpr int W = R * 8 * SP;
+        a.part_bc[(((long long)col * a.c.T + t + r) * a.c.B + p.b) * (2 * S) + which * S + n] =
+            (f[0] + f[W]) + (f[2 * W] + f[3 * W]);
+      }
+    }
+  }
+  if (!p.has) return;
+  const long long k = (long long)p.chunk * a.c.B * a.c.H + p.at;
+  store_states<SP>(a.part_a + k * S, S, p.n0, dA);
+  dskip = quad_sum(dskip);
+  dbias = quad_sum(dbias);
+  if (q == 0) {
+    a.part_h[2 * k] = dskip;
+    a.part_h[2 * k + 1] = dbias;
+  }
+  if (a.dh0 && p.chunk == 0) store_states<SP>(a.dh0 + p.at * S, S, p.n0, mu);
+}
+
+// Gradients of b and c: the workgroups' sums across the channels.
+template <typename E>
+__global__ __launch_bounds__(256) void ssm_bc_kernel(SsmArgs a) {
+  const int S2 = 2 * a.c.S;
+  const long long n = (long long)a.c.T * a.c.B * S2, i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  float v = 0.f;
+  for (int c = 0; c < a.s.cols; ++c) v += a.part_bc[c * n + i];
+  const long long row = i / S2;
+  const int s = (int)(i - row * S2), t = (int)(row / a.c.B), b = (int)(row - (long long)t * a.c.B);
+  const glr_seq& o = s < a.c.S ? a.db : a.dc;
+  ((E*)o.data)[t * o.stride_t + b * o.stride_b + (s < a.c.S ? s : s - a.c.S)] = elem_of<E>(v);
+}
+
+// Gradients of a, skip and bias: sums over the chunks and batch rows, 64 of them side by side in four parts.
+__global__ __launch_bounds__(256) void ssm_params_kernel(SsmArgs a) {
+  __shared__ float part[4][64];
+  const long long HS = (long long)a.c.H * a.c.S, H2 = 2LL * a.c.H, i = (long long)blockIdx.x * 64 + (threadIdx.x & 63);
+  const int w = threadIdx.x >> 6;
+  const long long P = (long long)a.s.chunks * a.c.B;
+  const bool of_a = i < HS;
+  const float* f = of_a ? a.part_a + i : a.part_h + (i - HS);
+  const long long stride = of_a ? HS : H2;
+  float v = 0.f;
+  if (i < HS + H2)
+    for (long long k = w; k < P; k += 4) v += f[k * stride];
+  part[w][threadIdx.x & 63] = v;
+  __syncthreads();
+  if (w || i >= HS + H2) return;
+  v = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+  if (of_a) {
+    a.da[i] = v;
+  } else {
+    float* o = (i - HS) & 1 ? a.dbias : a.dskip;
+    if (o) o[(i - HS) >> 1] = v;
+  }
+}
+
+// ---- one step
+template <typename E, int SP>
+__global__ __launch_bounds__(SSM_THREADS) void ssm_step_kernel(SsmStepArgs a) {
+  const long long i = ((long long)blockIdx.x * SSM_THREADS + threadIdx.x) >> 2;
+  const int q = threadIdx.x & 3, H = a.c.H, S = a.c.S, b = (int)(i / H), ch = (int)(i - (long long)b * H);
+  if (b >= a.c.B) return;                             // (four lanes together)
+  E* y = (E*)a.y.data + b * a.y.stride_b + ch;
+  const int slot = a.slots ? a.slots[b] : b;
+  if (slot < 0 || slot >= a.n_slots) {
+    if (q == 0) *y = elem_of<E>(0.f);
+    return;
+  }
+  auto one = [&](const glr_seq& s) { return elem_f32(((const E*)s.data)[b * s.stride_b + ch]); };
+  const float x = one(a.x), d = Softplus(one(a.dt) + (a.bias ? a.bias[ch] : 0.f)).d;
+  const bool cut = a.reset && a.reset[b];
+  float A[SP], h[SP], sum = 0.f;
+  const long long at = ((long long)slot * H + ch) * S;
+  load_states<SP>(a.a + (long long)ch * S, S, q * SP, A);
+  load_states<SP>(a.state_in + at, S, q * SP, h);
+  const E *bs = (const E*)a.b.data + b * a.b.stride_b, *cs = (const E*)a.cc.data + b * a.cc.stride_b;
+#pragma unroll
+  for (int k = 0; k < SP; ++k) {
+    const int n = min(q * SP + k, S - 1);
+    const float keep = decay(d, A[k] * LOG2E), in = d * x * elem_f32(bs[n]);
+    h[k] = cut ? in : fmaf(keep, h[k], in);
+    if (q * SP + k < S) sum = fmaf(h[k], elem_f32(cs[n]), sum);
+  }
+  store_states<SP>(a.state_out + at, S, q * SP, h);
+  sum = quad_sum(sum);
+  if (q) return;
+  float v = fmaf(a.skip ? a.skip[ch] : 0.f, x, sum);
+  if (a.z.data) {
+    const float z = one(a.z);
+    v *= z * Sigmoid(z).s;
+  }
+  *y = elem_of<E>(v);
+}
+
+// ---- launches
+SsmShape ssm_shape(const ssm_cfg& c, bool backward) {
+  SsmShape s;
+  s.per = c.S <= 4 ? 1 : c.S <= 8 ? 2 : c.S <= 16 ? 4 : c.S <= 32 ? 8 : 16;
+  s.save = s.per <= 4 ? 16 : 64 / s.per;
+  s.cols = (c.H + SSM_COLS - 1) / SSM_COLS;
+  const long long across = (long long)s.cols * c.B, tiles = ((long long)c.T + SSM_TILE - 1) / SSM_TILE;
+  long long chunks = 1;
+  if (across < (backward ? 256 : 512)) {
+    chunks = ((backward ? 512 : 1024) + across - 1) / across;
+    chunks = chunks < (tiles + 1) / 2 ? chunks : (tiles + 1) / 2;
+  }
+  s.len = (int)((tiles + chunks - 1) / chunks) * SSM_TILE;
+  s.chunks = (int)(((long long)c.T + s.len - 1) / s.len);
+  return s;
+}
+static size_t piece(size_t n) { return (n + 255) / 256 * 256; }
+namespace {
+struct SsmSpace {
+  size_t ends, sums, bc, pa, ph, total;
+  SsmSpace(const ssm_cfg& c, bool backward) {
+    const SsmShape s = ssm_shape(c, backward);
+    const size_t bh = (size_t)c.B * c.H;
+    total = 0;
+    auto take = [&](size_t n) {
+      const size_t at = total;
+      total += piece(n);
+      return at;
+    };
+    ends = take(s.chunks > 1 ? 4 * s.chunks * bh * c.S : 0);
+    sums = take(s.chunks > 1 ? 4 * s.chunks * bh : 0);
+    bc = take(backward ? 4 * (size_t)s.cols * c.T * c.B * 2 * c.S : 0);
+    pa = take(backward ? 4 * s.chunks * bh * c.S : 0);
+    ph = take(backward ? 8 * s.chunks * bh : 0);
+  }
+};
+}  // namespace
+size_t ssm_workspace(const ssm_cfg& c) {
+  const size_t f = SsmSpace(c, false).total, b = SsmSpace(c, true).total;
+  return f > b ? f : b;
+}
+size_t ssm_saved(const ssm_cfg& c) {
+  const SsmShape s = ssm_shape(c, true);
+  return 4 * (((size_t)c.T + s.save - 1) / s.save) * c.B * c.H * c.S;
+}
+static unsigned blocks(long long n) { return (unsigned)((n + 255) / 256); }
+bool ssm_launchable(const ssm_cfg& c) {
+  for (int backward = 0; backward < 2; ++backward) {
+    const SsmShape s = ssm_shape(c, backward);
+    if (!launchable((long long)s.chunks * s.cols * c.B, SSM_THREADS)) return false;
+  }
+  return launchable(((long long)c.B * c.H * c.S + 255) / 256, 256) &&
+         launchable(((long long)c.T * c.B * 2 * c.S + 255) / 256, 256) &&
+         launchable(((long long)c.H * (c.S + 2) + 63) / 64, 256);
+}
+static void ssm_place(SsmArgs& a, char* ws, bool backward) {
+  const SsmSpace w(a.c, backward);
+  a.s = ssm_shape(a.c, backward);
+  a.ends = (float*)(ws + w.ends);
+  a.sums = (float*)(ws + w.sums);
+  a.part_bc = (float*)(ws + w.bc);
+  a.part_a = (float*)(ws + w.pa);
+  a.part_h = (float*)(ws + w.ph);
+}
+static hipError_t ssm_between(const SsmArgs& a, const float* first, bool backward, hipStream_t s) {
+  hipLaunchKernelGGL(ssm_between_kernel, dim3(blocks((long long)a.c.B * a.c.H * a.c.S)), dim3(256), 0, s, a, first,
+                     backward);
+  return hipGetLastError();
+}
+template <typename E, int SP>
+static hipError_t ssm_forward_start(const SsmArgs& a, hipStream_t s) {
+  const long long across = (long long)a.s.cols * a.c.B;
+  if (a.s.chunks > 1) {
+    hipLaunchKernelGGL((ssm_forward_kernel<E, SP, false>), dim3((unsigned)(across * (a.s.chunks - 1))),
+                       dim3(SSM_THREADS), 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || (e = ssm_between(a, a.h0, false, s)) != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((ssm_forward_kernel<E, SP, true>), dim3((unsigned)(across * a.s.chunks)), dim3(SSM_THREADS), 0, s, a);
+  return hipGetLastError();
+}
+template <typename E, int SP>
+static hipError_t ssm_backward_start(const SsmArgs& a, hipStream_t s) {
+  const long long across = (long long)a.s.cols * a.c.B;
+  hipError_t e;
+  if (a.s.chunks > 1) {
+    hipLaunchKernelGGL((ssm_adjoint_ends_kernel<E, SP>), dim3((unsigned)(across * (a.s.chunks - 1))),
+                       dim3(SSM_THREADS), 0, s, a);
+    if ((e = hipGetLastError()) != hipSuccess || (e = ssm_between(a, a.dh_last, true, s)) != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((ssm_backward_kernel<E, SP, (SP <= 4 ? 16 : 64 / SP)>), dim3((unsigned)(across * a.s.chunks)),
+                     dim3(SSM_THREADS), 0, s, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL((ssm_bc_kernel<E>), dim3(blocks((long long)a.c.T * a.c.B * 2 * a.c.S)), dim3(256), 0, s, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL(ssm_params_kernel, dim3((unsigned)(((long long)a.c.H * (a.c.S + 2) + 63) / 64)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <typename E, int SP>
+static hipError_t ssm_step_start(const SsmStepArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((ssm_step_kernel<E, SP>), dim3((unsigned)(((long long)a.c.B * a.c.H * 4 + 255) / 256)), dim3(256), 0,
+                     s, a);
+  return hipGetLastError();
+}
+// F<type, states of a lane>(arguments)
+#define SSM_DISPATCH(F, a, s)                                                  \
+  auto by_states = [&](auto e) -> hipError_t {                                 \
+    using E = decltype(e);                                                     \
+    switch (ssm_shape(a.c, false).per) {                                       \
+      case 1: return F<E, 1>(a, s);                                            \
+      case 2: return F<E, 2>(a, s);                                            \
+      case 4: return F<E, 4>(a, s);                                            \
+      case 8: return F<E, 8>(a, s);                                            \
+      default: return F<E, 16>(a, s);                                          \
+    }                                                                          \
+  };                                                                           \
+  if (a.c.dtype == MGRIT_F32) return by_states(float());                       \
+  if (a.c.dtype == MGRIT_BF16) return by_states(Bf16());                       \
+  return by_states(F16())
+
+hipError_t launch_ssm_forward(SsmArgs a, char* ws, hipStream_t s) {
+  ssm_place(a, ws, false);
+  a.s.save = ssm_shape(a.c, true).save;
+  SSM_DISPATCH(ssm_forward_start, a, s);
+}
+hipError_t launch_ssm_backward(SsmArgs a, char* ws, hipStream_t s) {
+  ssm_place(a, ws, true);
+  SSM_DISPATCH(ssm_backward_start, a, s);
+}
+hipError_t launch_ssm_step(const SsmStepArgs& a, hipStream_t s) {
+  if (!launchable(((long long)a.c.B * a.c.H * 4 + 255) / 256, 256)) return TOO_LARGE;
+  SSM_DISPATCH(ssm_step_start, a, s);
+}
+
+}  // namespace mg

@@ -2,18 +2,9 @@
 // host before anything is launched.
 #include <cmath>
 
-#include "ops.h"
+#include "checks.h"
 
 namespace mg {
-
-static bool off16(const void* p) { return ((uintptr_t)p & 15) != 0; }
-static bool off(const void* p, size_t n) { return (uintptr_t)p % n != 0; }
-static bool is_dtype(int d) { return d == MGRIT_F32 || d == MGRIT_BF16 || d == MGRIT_F16; }
-static size_t elem_bytes(int d) { return d == MGRIT_F32 ? 4 : 2; }
-static size_t up(size_t v, size_t n) { return (v + n - 1) / n * n; }
-static int code_of(hipError_t e) {
-  return e == hipSuccess ? MGRIT_OK : e == TOO_LARGE ? MGRIT_E_SIZE : MGRIT_E_LAUNCH;
-}
 
 // ---- gated linear recurrence
 static int glr_sizes(const glr_cfg* c) {
@@ -33,26 +24,6 @@ static int glr_check(const glr_cfg* c) {
       return MGRIT_E_SIZE;
   }
   return MGRIT_OK;
-}
-static int seq_check(const glr_cfg& c, const glr_seq* q, bool out) {
-  if (!q || !q->data) return MGRIT_E_NULL;
-  if (off(q->data, elem_bytes(c.dtype))) return MGRIT_E_ALIGN;
-  if (q->stride_t < 0 || q->stride_b < 0) return MGRIT_E_SIZE;
-  // the last element's offset has to be a number of bytes
-  const long double last = (long double)(c.T - 1) * q->stride_t + (long double)(c.B - 1) * q->stride_b + c.H;
-  if (last > 1e18L) return MGRIT_E_SIZE;
-  if (!out) return MGRIT_OK;
-  long long lo = q->stride_t, hi = q->stride_b, n = c.T;      // smaller stride and its extent
-  if (c.T == 1 && c.B == 1) return MGRIT_OK;
-  if (c.T == 1) return q->stride_b < c.H ? MGRIT_E_SIZE : MGRIT_OK;
-  if (c.B == 1) return q->stride_t < c.H ? MGRIT_E_SIZE : MGRIT_OK;
-  if (lo > hi) {
-    const long long t = lo;
-    lo = hi;
-    hi = t;
-    n = c.B;
-  }
-  return lo < c.H || hi / n < lo ? MGRIT_E_SIZE : MGRIT_OK;
 }
 static size_t glr_ws(const GlrShape& s) { return s.words ? 256 + 8 * (size_t)s.words : 0; }
 static size_t glr_save(const glr_cfg& c) { return 4 * (size_t)glr_shape(c, true).chunks * c.B * c.H; }
@@ -79,23 +50,6 @@ static int glr_space(const glr_cfg& c, const GlrShape& s, void* ws, size_t n, Gl
 }
 
 // ---- rows of logits
-static int logits_check(const logits_cfg* c) {
-  if (!c) return MGRIT_E_NULL;
-  if (c->N < 1 || c->V < 1 || c->V > (1 << 20) || c->K < 0) return MGRIT_E_SIZE;
-  if ((long long)c->N * 33 > 0x7fffffffLL) return MGRIT_E_SIZE;                 // segments of all rows
-  if (c->ld < c->V || c->ld > (1LL << 40)) return MGRIT_E_SIZE;
-  if (!is_dtype(c->dtype)) return MGRIT_E_ENUM;
-  // (the exponents' factor log2(e) / t has to be a float)
-  if (!std::isfinite(c->temperature) || c->temperature <= 0.f || !std::isfinite(LOG2E * (1.0f / c->temperature)))
-    return MGRIT_E_SIZE;
-  return MGRIT_OK;
-}
-static int logits_space(const logits_cfg& c, const void* ws, size_t n) {
-  const size_t need = logits_workspace(c);
-  if (n < need) return MGRIT_E_WORKSPACE;
-  if (need && !ws) return MGRIT_E_NULL;
-  return need && off16(ws) ? MGRIT_E_ALIGN : MGRIT_OK;
-}
 static int distill_check(const logits_cfg* c, const void* logits, const int64_t* ids, const float* teacher,
                          const float* weight, const void* dlogits) {
   const int rc = logits_check(c);

@@ -1,0 +1,193 @@
+"""Policy loss and its gradient on the GPU against the float64 oracle."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2203_04738_amd as mg
+from oracle import token_ops_oracle as orc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": (mg.MGRIT_F32, torch.float32, 2.0 ** -24), "bf16": (mg.MGRIT_BF16, torch.bfloat16, 2.0 ** -8),
+         "f16": (mg.MGRIT_F16, torch.float16, 2.0 ** -11)}
+LOW, HIGH = 0.2, 0.28
+
+
+def problem(seed, N, V, dtype, t, masked=False):
+    rng = np.random.default_rng(seed)
+    dt = TYPES[dtype][1]
+    x = 2 * rng.standard_normal((N, V))
+    if masked and V > 8:
+        x[:, V - V // 8:] = -np.inf
+    logits = torch.from_numpy(x).to(DEV, dt)
+    d = {"x": logits.double().cpu().numpy(), "tok": rng.integers(0, max(1, V - V // 8), N)}
+    m = d["x"].max(1, keepdims=True)
+    lse = m[:, 0] / t + np.log(np.exp((d["x"] - m) / t).sum(1))
+    lp = d["x"][np.arange(N), d["tok"]] / t - lse
+    moved = 0.4 * rng.standard_normal(N)
+    for border in (np.log(1 - LOW), np.log(1 + HIGH)):         # nothing where 32 bits decide
+        moved = np.where(np.abs(moved - border) < 1e-3, moved + 3e-3, moved)
+    d.update(old=(lp - moved).astype(np.float32), ref=(lp + 0.3 * rng.standard_normal(N)).astype(np.float32),
+             adv=rng.standard_normal(N).astype(np.float32), weight=rng.random(N).astype(np.float32))
+    d["tok"][rng.random(N) < 0.1] = -3
+    d["weight"][rng.random(N) < 0.1] = 0
+    dev = {k: torch.from_numpy(v).to(DEV) for k, v in d.items() if k != "x"}
+    dev["x"] = logits
+    return d, dev
+
+
+def call(dev, dtype, t, beta, apart=False, inplace=False, weight=True, pad=0):
+    code, dt, _ = TYPES[dtype]
+    N, V = dev["x"].shape
+    cfg, rule = mg.LogitsCfg(N, V, 0, code, t), mg.PolicyCfg(LOW, HIGH, beta)
+    ws = torch.full((mg.policy_workspace_bytes(cfg),), 255, dtype=torch.uint8, device=DEV)
+    rows = [torch.full((N,), float("nan"), device=DEV) for _ in range(4)]
+    grad = dev["x"] if inplace else torch.full((N, V + pad), 77.0, dtype=dt, device=DEV)[:, :V]
+    ref, w = dev["ref"] if beta else None, dev["weight"] if weight else None
+    given = (dev["x"], dev["tok"], dev["old"], ref, dev["adv"])
+    if apart:
+        stats = torch.full((N, 2), float("nan"), device=DEV)
+        mg.policy_loss(cfg, rule, *given, None, *rows, stats, None, ws)
+        mg.policy_loss_backward(cfg, rule, *given, stats, w, grad)
+    else:
+        mg.policy_loss(cfg, rule, *given, w, *rows, None, grad, ws)
+    torch.cuda.synchronize()
+    return rows, grad
+
+
+def compare(d, rows, grad, dtype, t, beta, weight=True):
+    want = orc.policy_loss(d["x"], d["tok"], d["old"].astype(float), d["ref"].astype(float) if beta else None,
+                           d["adv"].astype(float), d["weight"].astype(float) if weight else None, t, LOW, HIGH, beta)
+    # a row's sum of exponentials is known to 2e-7 or so plus |x - max| / t (up to 20) units of 2^-24 from the factor log2(e) / t:
+    # 2e-6 of a ratio, a log probability known to that absolutely, and to 2^-24 of itself when it is stored
+    for got, ref, name in zip(rows, want, ("loss", "logp", "ratio", "kl")):
+        got = got.double().cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.isnan(ref)), name
+        fin = np.isfinite(ref)
+        assert np.array_equal(got[~fin & ~np.isnan(ref)], ref[~fin & ~np.isnan(ref)]), name
+        size = np.fmax(1.0, np.abs(want[2][fin] * d["adv"][fin]))    # (1 where a row has no ratio)
+        assert (np.abs(got - ref)[fin] <= 4e-6 * (np.abs(ref[fin]) + size)).all(), name
+    got, unit = grad.double().cpu().numpy(), TYPES[dtype][2]
+    fin = np.isfinite(want[4]).all(1)
+    # the coefficient as the loss is known, plus the exponential; 16-bit subnormals to half their step
+    top = np.abs(want[4][fin]).max(1, keepdims=True, initial=0)
+    floor = {"f32": 0.0, "bf16": 0.0, "f16": 2.0 ** -25}[dtype]
+    size = np.maximum(1.0, np.abs(d["adv"][fin])) * (d["weight"][fin] if weight else 1.0) / t
+    assert (np.abs(got[fin] - want[4][fin])
+            <= unit * np.abs(want[4][fin]) + 8e-6 * np.abs(want[4][fin]) + 2e-6 * size[:, None] * (top > 0) + floor).all()
+    assert (got[fin][top[:, 0] == 0] == 0).all()
+    return want
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("N,V,t,beta", [(1, 1, 1.0, 0.0), (5, 2, 0.7, 0.1), (33, 51, 1.0, 0.05), (7, 1023, 2.0, 0.0),
+                                        (6, 4097, 1.0, 0.2), (9, 20000, 0.7, 0.05), (5, 33333, 1.0, 0.05), (3, 70001, 1.3, 0.1)])
+@pytest.mark.parametrize("apart", [False, True])
+def test_rows(dtype, N, V, t, beta, apart):
+    d, dev = problem(V, N, V, dtype, t, masked=True)
+    rows, grad = call(dev, dtype, t, beta, apart)
+    compare(d, rows, grad, dtype, t, beta)
+
+
+@pytest.mark.parametrize("V", [40, 2000, 40000])
+def test_in_place_padded_and_without_weights(V):
+    d, dev = problem(V, 12, V, "bf16", 1.0)
+    rows, grad = call(dev, "bf16", 1.0, 0.05, weight=False, pad=5)
+    compare(d, rows, grad, "bf16", 1.0, 0.05, weight=False)
+    assert (torch.as_strided(grad, (12, 5), (V + 5, 1), V) == 77).all()
+    rows, grad = call(dev, "bf16", 1.0, 0.05, inplace=True)
+    compare(d, rows, grad, "bf16", 1.0, 0.05)
+
+
+@pytest.mark.parametrize("V", [30, 3000, 50000])
+@pytest.mark.parametrize("beta", [0.0, 0.1])
+def test_rows_that_masks_tokens_and_values_leave_empty(V, beta):
+    d, dev = problem(1, 9, V, "f32", 1.0)
+    x, tok = dev["x"], dev["tok"]
+    tok.copy_(torch.tensor([3, 4, V, V + 2 ** 40, -1, 5, 6, 2, 1]))
+    dev["weight"].copy_(torch.tensor([1., 1., 1., 0., 1., 1., 0., 1., 1.]))
+    x[0] = -float("inf")                                       # nothing left
+    x[1, 4] = -float("inf")                                    # the token is masked
+    x[4] = float("nan")                                        # not sampled
+    x[5, 0] = float("nan")
+    x[6, 1] = float("nan")                                     # of weight 0
+    x[7] = torch.finfo(torch.float32).min
+    x[7, :4] = 0
+    d["x"], d["tok"], d["weight"] = x.double().cpu().numpy(), tok.cpu().numpy(), dev["weight"].cpu().numpy()
+    for apart in (False, True):
+        rows, grad = call(dev, "f32", 1.0, beta, apart)
+        want = compare(d, rows, grad, "f32", 1.0, beta)
+        for n in (2, 5):
+            assert torch.isnan(grad[n]).all(), n
+        for n in (3, 4, 6):
+            assert (grad[n] == 0).all(), n
+        if beta:
+            assert np.isinf(want[0][[0, 1]]).all() and (~torch.isfinite(grad[[0, 1]])).any(1).all()
+        else:
+            assert (grad[[0, 1]] == 0).all()                   # a ratio of 0
+
+
+def test_borders_and_signs():
+    # ratios on either side of both borders, and 1; advantages of both signs and 0; logits of two classes
+    ratio = torch.tensor([0.5, 0.79, 0.81, 1.0, 1.27, 1.29, 3.0])
+    adv = torch.tensor([1.0, -1.0, 0.0])
+    r, A = (v.reshape(-1) for v in torch.meshgrid(ratio, adv, indexing="ij"))
+    N = len(r)
+    d = {"x": np.tile([0.3, -0.4], (N, 1)), "tok": np.zeros(N, dtype=np.int64)}
+    lp = float(torch.log_softmax(torch.tensor([0.3, -0.4], dtype=torch.float64), 0)[0])
+    d.update(old=(lp - np.log(r.double().numpy())).astype(np.float32), adv=A.numpy(), weight=np.ones(N, dtype=np.float32),
+             ref=np.zeros(N, dtype=np.float32))
+    d["x"] = d["x"].astype(np.float32).astype(np.float64)
+    dev = {k: torch.from_numpy(v).to(DEV) for k, v in d.items()}
+    dev["x"] = dev["x"].float()
+    rows, grad = call(dev, "f32", 1.0, 0.0)
+    compare(d, rows, grad, "f32", 1.0, 0.0)
+    moved = (grad != 0).any(1).cpu()
+    assert torch.equal(moved, ((A > 0) & (r < 1.28)) | ((A < 0) & (r > 0.8)))
+
+
+def test_kl_of_small_and_large_differences():
+    diff = torch.cat([torch.logspace(-4, 1.5, 60), -torch.logspace(-4, 2.5, 60), torch.tensor([0.0])]).double()
+    N = len(diff)
+    x = np.zeros((N, 2))
+    lp = np.full(N, -np.log(2.0))
+    old = lp.astype(np.float32)
+    ref = (lp + diff.numpy()).astype(np.float32)
+    dev = {"x": torch.zeros(N, 2, device=DEV), "tok": torch.zeros(N, dtype=torch.int64, device=DEV),
+           "old": torch.from_numpy(old).to(DEV), "ref": torch.from_numpy(ref).to(DEV), "adv": torch.zeros(N, device=DEV),
+           "weight": torch.ones(N, device=DEV)}
+    rows, _ = call(dev, "f32", 1.0, 1.0)
+    d = ref.astype(float) - lp
+    want = np.expm1(d) - d
+    # log 2 from a float's sum that is exact; d rounded once (2^-24 d, which moves k by (e^d - 1) times that), then 20 roundings;
+    # d of 0 is what rounding leaves of it
+    tol = 2.0 ** -24 * (np.abs(np.expm1(d) * d) + 20 * want + np.abs(np.expm1(d)) * 1e-9) + 1e-37
+    assert (np.abs(rows[3].double().cpu().numpy() - want) <= tol).all()
+
+
+def test_captured_and_replayed():
+    N, V = 40, 40000
+    d, dev = problem(2, N, V, "bf16", 1.0)
+    cfg, rule = mg.LogitsCfg(N, V, 0, mg.MGRIT_BF16), mg.PolicyCfg(LOW, HIGH, 0.1)
+    ws = torch.empty(mg.policy_workspace_bytes(cfg), dtype=torch.uint8, device=DEV)
+    loss, grad = torch.zeros(N, device=DEV), torch.zeros(N, V, dtype=torch.bfloat16, device=DEV)
+
+    def one(loss, grad):
+        mg.policy_loss(cfg, rule, dev["x"], dev["tok"], dev["old"], dev["ref"], dev["adv"], dev["weight"], loss, None, None, None,
+                       None, grad, ws)
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        one(loss, grad)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one(loss, grad)
+    for _ in range(3):
+        dev["adv"].mul_(-1.5)
+        l2, g2 = torch.zeros_like(loss), torch.zeros_like(grad)
+        one(l2, g2)
+        loss.zero_(), grad.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(loss, l2) and torch.equal(grad, g2) and float(loss.abs().max()) > 0
