@@ -5,6 +5,7 @@
 // few steps before (backward: around) each thread's own.
 #include "elem.h"
 #include "pairs.h"
+#include "row_sums.h"
 #include "tokens.h"
 
 namespace mg {
@@ -238,18 +239,12 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, int lane
     }
   }
 }
-// Gradients of the weights and biases from the groups' sums, 64 of them side by side in four parts.
-__global__ __launch_bounds__(256) void conv_params_kernel(ConvArgs a) {
-  __shared__ float part[4][64];
-  const int W1 = a.c.W + 1, w = threadIdx.x >> 6;
-  const long long n = (long long)a.c.H * W1, i = (long long)blockIdx.x * 64 + (threadIdx.x & 63);
-  float v = 0.f;
-  if (i < n)
-    for (int g = w; g < a.groups; g += 4) v += a.part[g * n + i];
-  part[w][threadIdx.x & 63] = v;
-  __syncthreads();
-  if (w || i >= n) return;
-  v = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+// Gradients of the weights and biases from the groups' sums.
+__global__ __launch_bounds__(SUM_THREADS) void conv_params_kernel(ConvArgs a) {
+  const int W1 = a.c.W + 1;
+  const long long n = (long long)a.c.H * W1, i = sum_column();
+  float v;
+  if (!sum_rows(a.part + i, n, a.groups, i < n, v)) return;
   const int ch = (int)(i / W1), k = (int)(i - (long long)ch * W1);
   if (k < a.c.W) {
     if (a.dweight) a.dweight[(long long)ch * a.c.W + k] = v;
@@ -303,7 +298,7 @@ static long long conv_forward_groups(const conv_cfg& c) {
   return ((c.T + CONV_RUN - 1LL) / CONV_RUN * c.B * ((c.H + 1LL) / 2) + 255) / 256;
 }
 bool conv_launchable(const conv_cfg& c) {
-  return launchable(conv_forward_groups(c), 256) && launchable(((long long)c.H * (c.W + 1) + 63) / 64, 256);
+  return launchable(conv_forward_groups(c), 256) && launchable(sum_groups((long long)c.H * (c.W + 1)), SUM_THREADS);
 }
 template <typename E, bool ALIGNED>
 static void conv_forward_taps(const ConvArgs& a, hipStream_t s) {
@@ -338,7 +333,7 @@ static hipError_t conv_start(const ConvArgs& a, bool backward, hipStream_t s) {
   else conv_backward_taps<E, false>(a, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || (!a.dweight && !a.dbias)) return e;
-  hipLaunchKernelGGL(conv_params_kernel, dim3((unsigned)(((long long)H * (a.c.W + 1) + 63) / 64)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(conv_params_kernel, dim3(sum_groups((long long)H * (a.c.W + 1))), dim3(SUM_THREADS), 0, s, a);
   return hipGetLastError();
 }
 static hipError_t conv_typed(const ConvArgs& a, bool backward, hipStream_t s) {

@@ -12,9 +12,13 @@
 
 #include "elem.h"
 #include "pairs.h"
+#include "row_sums.h"
 #include "tokens.h"
 
 namespace mg {
+
+// (arrays that a call takes by reference would be in memory)
+#define SSM_INLINE __attribute__((always_inline))
 
 constexpr int SSM_THREADS = 256, SSM_COLS = 64, SSM_TILE = 16;
 
@@ -42,38 +46,33 @@ __device__ inline float quad_sum(float v) {
 }
 
 // ---- elementwise
-// softplus(v) and its derivative sigmoid(v).  With e = exp(-|v|): softplus = max(v, 0) + log(1 + e), and log(1 + e) =
-// 2 atanh(s), s = e / (2 + e) <= 1/3, whose series in s^2 <= 1/9 ends below 2^-25 of it behind s^16.
+// softplus(v) and its derivative sigmoid(v).  With e = exp(-|v|): softplus = max(v, 0) + log(1 + e), and log(1 + e) is
+// log u + c for u = 1 + e as rounded and c = e - (u - 1) what the rounding left (exact; c / u would be nearer by c e / u, at
+// most 2^-24 of the result).
 struct Softplus {
-  float d, slope;
+  float d, e;
   __device__ inline explicit Softplus(float v) {
-    const float e = exp_of(-fabsf(v));
-    const float s = e * __builtin_amdgcn_rcpf(2.0f + e), w = s * s;
-    float p = fmaf(w, 1.f / 17, 1.f / 15);
-    p = fmaf(w, p, 1.f / 13);
-    p = fmaf(w, p, 1.f / 11);
-    p = fmaf(w, p, 1.f / 9);
-    p = fmaf(w, p, 1.f / 7);
-    p = fmaf(w, p, 1.f / 5);
-    p = fmaf(w, p, 1.f / 3);
-    const float l = fmaf(2.f * s * w, p, 2.f * s);
-    d = v > 0.f ? v + l : v == v ? l : v;
-    const float small = e * __builtin_amdgcn_rcpf(1.0f + e);
-    slope = v < 0.f ? small : 1.0f - small;
-    if (v != v) slope = v;
+    e = exp_of(-fabsf(v));
+    const float u = 1.0f + e, c = e - (u - 1.0f);
+    d = fmaxf(v, 0.f) + fmaf(__builtin_amdgcn_logf(u), LN2, c);
+  }
+  __device__ inline float slope(float v) const {
+    const float r = __builtin_amdgcn_rcpf(1.0f + e);
+    return v < 0.f ? e * r : r;
   }
 };
-// sigmoid(z) and 1 - sigmoid(z)
+// s = sigmoid(z), n = sigmoid(-z).  (Of a NaN they are numbers: each use multiplies by z.)
 struct Sigmoid {
   float s, n;
   __device__ inline explicit Sigmoid(float z) {
-    const float e = exp_of(-fabsf(z));
-    const float small = e * __builtin_amdgcn_rcpf(1.0f + e), large = 1.0f - small;
-    s = z < 0.f ? small : large;
-    n = z < 0.f ? large : small;
-    if (z != z) s = n = z;
+    const float x = __builtin_amdgcn_fmed3f(-z, -104.f, 88.f), p = x * LOG2E;
+    float e = __builtin_amdgcn_exp2f(p);
+    e = fmaf(e, fmaf(-p, LN2, x), e);
+    s = __builtin_amdgcn_rcpf(1.0f + e);
+    n = e * s;
   }
 };
+__device__ inline float silu(float z) { return z * Sigmoid(z).s; }
 
 // ---- states of a lane
 typedef float Quad __attribute__((ext_vector_type(4), aligned(4)));
@@ -133,43 +132,67 @@ struct SsmPlace {
   }
 };
 
-// One element per step of a channel, from step t on; steps behind the last are read at the last.
-template <typename E>
-struct Steps {
-  const E* p;
-  long long stride;
-  __device__ inline Steps(const glr_seq& s, const SsmPlace& at)
-      : p((const E*)s.data + at.b * s.stride_b + at.ch), stride(s.stride_t) {}
-  __device__ inline E load(int t, int last) const { return p[min(t, last) * stride]; }
-};
-template <typename E>
-__device__ inline void put(const glr_seq& s, const SsmPlace& at, int t, float v) {
-  ((E*)s.data)[t * s.stride_t + at.b * s.stride_b + at.ch] = elem_of<E>(v);
+// (field by field: a choice between structures would go through memory)
+__device__ inline glr_seq one_of(bool first, const glr_seq& x, const glr_seq& y) {
+  return {first ? x.data : y.data, first ? x.stride_t : y.stride_t, first ? x.stride_b : y.stride_b};
 }
 
-// b and c of a tile of TB steps in LDS, as floats: [step][lane of four][b SP | c SP]; zeros where there is no state or
-// step.
+// A channel's elements of a sequence, one step for each of its four lanes, at a tile that starts at step t and moves on by
+// whole tiles: a lane's own address and scalar distances, without products.  FULL: the tile's steps all exist; otherwise
+// the last one is read for those behind it.
+template <typename E>
+struct Steps {
+  char* p;                                           // of step t + q
+  long long stride;                                  // bytes
+  __device__ inline Steps(const glr_seq& s, const SsmPlace& at, int t) : stride(s.stride_t * (long long)sizeof(E)) {
+    p = (char*)s.data + (at.b * s.stride_b + at.ch) * (long long)sizeof(E) + (t + at.q) * stride;
+  }
+  __device__ inline void move(int steps) { p += steps * stride; }
+  template <bool FULL, int G>
+  __device__ inline void load(E (&v)[G], int left) const {      // left: steps behind t + q
+#pragma unroll
+    for (int g = 0; g < G; ++g) v[g] = *(const E*)(p + (FULL ? 4 * g : min(4 * g, left)) * stride);
+  }
+  __device__ inline void put(int g, float v) const { *(E*)(p + 4 * g * stride) = elem_of<E>(v); }
+};
+
+// b and c of a tile of TB steps in LDS, as floats: [step][lane of four][b SP | c SP]; zeros where there is no state.  Half of
+// the waves read b, half c.
 template <typename E, int SP, int TB>
 struct BcTile {
-  static constexpr int row = 8 * SP, n = TB * row, per = (n + SSM_THREADS - 1) / SSM_THREADS;
+  static constexpr int row = 8 * SP, n = TB * row;
+  static constexpr int steps = SSM_THREADS / row;    // of the tile between a thread's elements
+  static constexpr int per = (TB + steps - 1) / steps;
   E raw[per];
-  __device__ inline void load(const SsmArgs& a, int b, int t0) {
+  const char* p;                                     // the thread's element of the tile that starts at step t
+  long long stride;
+  int step, to;
+  bool has;
+  __device__ inline BcTile(const SsmArgs& a, int b, int t) {
+    const int which = __builtin_amdgcn_readfirstlane(threadIdx.x / (SSM_THREADS / 2)), r = threadIdx.x % (SSM_THREADS / 2);
+    const int s = r % (4 * SP);
+    const glr_seq& q = which ? a.cc : a.b;
+    step = r / (4 * SP);
+    has = s < a.c.S;
+    stride = q.stride_t * (long long)sizeof(E);
+    p = (const char*)q.data + (b * q.stride_b + (t + step) * q.stride_t + (has ? s : 0)) * (long long)sizeof(E);
+    to = step * row + s / SP * (2 * SP) + which * SP + s % SP;
+  }
+  __device__ inline bool mine(int k) const { return TB % steps == 0 || step + k * steps < TB; }
+  __device__ inline void move(int n) { p += n * stride; }
+  __device__ inline void load(int t, int last) {
+    const bool full = t + TB - 1 <= last;
 #pragma unroll
     for (int k = 0; k < per; ++k) {
-      const int e = threadIdx.x + k * SSM_THREADS;
-      const int r = e % row, which = r / (4 * SP), s = r % (4 * SP), t = t0 + e / row;
-      const glr_seq& q = which ? a.cc : a.b;
-      raw[k] = elem_of<E>(0.f);
-      if (e < n && s < a.c.S && t < a.c.T) raw[k] = ((const E*)q.data)[t * q.stride_t + b * q.stride_b + s];
+      if (!mine(k)) continue;
+      if (full) raw[k] = *(const E*)(p + k * steps * stride);
+      else raw[k] = *(const E*)(p + min(k * steps, last - t - step) * stride);
     }
   }
   __device__ inline void store(float* lds) const {
 #pragma unroll
-    for (int k = 0; k < per; ++k) {
-      const int e = threadIdx.x + k * SSM_THREADS;
-      const int r = e % row, which = r / (4 * SP), s = r % (4 * SP);
-      if (e < n) lds[e / row * row + s / SP * (2 * SP) + which * SP + s % SP] = elem_f32(raw[k]);
-    }
+    for (int k = 0; k < per; ++k)
+      if (mine(k)) lds[to + k * steps * row] = has ? elem_f32(raw[k]) : 0.f;
   }
 };
 template <int SP>
@@ -214,17 +237,23 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
   }
   const float bias = a.bias ? a.bias[p.ch] : 0.f, skip = MAIN && a.skip ? a.skip[p.ch] : 0.f;
   const bool gated = MAIN && a.z.data;
-  const Steps<E> xs(a.x, p), ds(a.dt, p), zs(gated ? a.z : a.x, p);
-  Tile next;
+  Steps<E> xs(a.x, p, p.t0), ds(a.dt, p, p.t0), zs(one_of(gated, a.z, a.x), p, p.t0), ys(one_of(MAIN, a.y, a.x), p, p.t0);
+  Tile next(a, p.b, p.t0);
   E xn[G], dn[G], zn[G];
-  auto load = [&](int t) {
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      xn[g] = xs.load(t + 4 * g + q, last);
-      dn[g] = ds.load(t + 4 * g + q, last);
-      if (gated) zn[g] = zs.load(t + 4 * g + q, last);
-    }
-    next.load(a, p.b, t);
+  auto load = [&](int t) SSM_INLINE {
+    auto steps = [&](auto full) SSM_INLINE {
+      constexpr bool FULL = decltype(full)::value;
+      xs.template load<FULL>(xn, last - t - q);
+      ds.template load<FULL>(dn, last - t - q);
+      if (gated) zs.template load<FULL>(zn, last - t - q);
+    };
+    if (t + TB <= a.c.T) steps(std::true_type{});
+    else steps(std::false_type{});
+    next.load(t, last);
+    xs.move(TB);
+    ds.move(TB);
+    zs.move(TB);
+    next.move(TB);
   };
   load(p.t0);
   float sum = 0.f;
@@ -235,7 +264,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       x[g] = elem_f32(xn[g]);
-      d[g] = elem_f32(dn[g]);
+      d[g] = elem_f32(dn[g]) + bias;
       z[g] = gated ? elem_f32(zn[g]) : 0.f;
     }
     next.store(bc[buf]);
@@ -243,22 +272,23 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
     __syncthreads();
     if (t + TB < p.t1) load(t + TB);
     forgets |= resets != 0;
-    auto tile = [&](auto cut_) {
-      constexpr bool CUT = decltype(cut_)::value;
+    // PLAIN: every step exists and none resets.  (Lanes without a channel go through another one's and store nothing.)
+    auto tile = [&](auto plain) SSM_INLINE {
+      constexpr bool PLAIN = decltype(plain)::value;
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         const int ts = t + 4 * g;
         if (MAIN && a.saved && ts % a.s.save == 0 && ts < a.c.T && p.has)
           store_states<SP>(a.saved + (ts / a.s.save * (long long)a.c.B * a.c.H + p.at) * S, S, p.n0, h);
-        const bool in = p.has && ts + q < a.c.T;
-        const float delta = in ? Softplus(d[g] + bias).d : 0.f;
+        const bool in = PLAIN || ts + q < a.c.T;
+        const float delta = in ? Softplus(d[g]).d : 0.f;
         const float xv = in ? x[g] : 0.f, dx = delta * xv;
         if (!MAIN) sum += delta;
         float part[4];
-        auto step = [&](auto j_) {
+        auto step = [&](auto j_) SSM_INLINE {
           constexpr int j = decltype(j_)::value;
           const float dj = quad_of<j>(delta), xj = quad_of<j>(dx);
-          const bool cut = CUT && (resets >> (4 * g + j) & 1);
+          const bool cut = !PLAIN && (resets >> (4 * g + j) & 1);
           float b[SP], c[SP];
           read_bc<SP>(bc[buf], 4 * g + j, q, 0, b);
           if (MAIN) read_bc<SP>(bc[buf], 4 * g + j, q, 1, c);
@@ -277,13 +307,14 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
         if constexpr (MAIN) {
           float y = quad_sums(part, q);
           y = fmaf(skip, xv, y);
-          if (gated) y *= z[g] * Sigmoid(z[g]).s;
-          if (in) put<E>(a.y, p, ts + q, y);
+          if (gated) y *= silu(z[g]);
+          if (in && p.has) ys.put(g, y);
         }
       }
     };
-    if (resets) tile(std::true_type{});
+    if (!resets && t + TB <= a.c.T) tile(std::true_type{});
     else tile(std::false_type{});
+    if (MAIN) ys.move(TB);
   }
   if (!p.has) return;
   if (MAIN) {
@@ -344,20 +375,26 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_adjoint_ends_kernel(SsmArgs a
   }
   const float bias = a.bias ? a.bias[p.ch] : 0.f;
   const bool gated = a.z.data;
-  const Steps<E> ys(a.dy, p), ds(a.dt, p), zs(gated ? a.z : a.dy, p);
-  Tile next;
+  const int tiles = (p.t1 - p.t0 + TB - 1) / TB, end = p.t0 + (tiles - 1) * TB;
+  Steps<E> ys(a.dy, p, end), ds(a.dt, p, end), zs(one_of(gated, a.z, a.dy), p, end);
+  Tile next(a, p.b, end);
   E yn[G], dn[G], zn[G];
-  auto load = [&](int t) {
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      yn[g] = ys.load(t + 4 * g + q, last);
-      dn[g] = ds.load(t + 4 * g + q, last);
-      if (gated) zn[g] = zs.load(t + 4 * g + q, last);
-    }
-    next.load(a, p.b, t);
+  auto load = [&](int t) SSM_INLINE {
+    auto steps = [&](auto full) SSM_INLINE {
+      constexpr bool FULL = decltype(full)::value;
+      ys.template load<FULL>(yn, last - t - q);
+      ds.template load<FULL>(dn, last - t - q);
+      if (gated) zs.template load<FULL>(zn, last - t - q);
+    };
+    if (t + TB <= a.c.T) steps(std::true_type{});
+    else steps(std::false_type{});
+    next.load(t, last);
+    ys.move(-TB);
+    ds.move(-TB);
+    zs.move(-TB);
+    next.move(-TB);
   };
-  const int tiles = (p.t1 - p.t0 + TB - 1) / TB;
-  load(p.t0 + (tiles - 1) * TB);
+  load(end);
   float sum = 0.f;
   bool forgets = false;
   int buf = 0;
@@ -366,9 +403,9 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_adjoint_ends_kernel(SsmArgs a
     float y[G], d[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      const bool in = p.has && t + 4 * g + q < a.c.T;
+      const bool in = t + 4 * g + q < a.c.T;
       const float z = gated ? elem_f32(zn[g]) : 0.f, dy = elem_f32(yn[g]);
-      y[g] = !in ? 0.f : gated ? dy * (z * Sigmoid(z).s) : dy;
+      y[g] = !in ? 0.f : gated ? dy * silu(z) : dy;
       d[g] = in ? Softplus(elem_f32(dn[g]) + bias).d : 0.f;
       sum += d[g];
     }
@@ -379,7 +416,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_adjoint_ends_kernel(SsmArgs a
     forgets |= resets != 0;
 #pragma unroll
     for (int g = G - 1; g >= 0; --g) {
-      auto step = [&](auto j_) {
+      auto step = [&](auto j_) SSM_INLINE {
         constexpr int j = decltype(j_)::value;
         const float dj = quad_of<j>(d[g]), yj = quad_of<j>(y[g]);
         const bool cut = resets >> (4 * g + j) & 1;
@@ -441,48 +478,62 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
   p.set(a, 0, std::integral_constant<int, SP>());
   const int S = a.c.S, last = a.c.T - 1, q = p.q, lane = threadIdx.x & 63;
   const long long states = (long long)a.c.B * a.c.H * S;
-  float A[SP], mu[SP], dA[SP];
-  load_states<SP>(a.a + (long long)p.ch * S, S, p.n0, A);
+  float A2[SP], mu[SP], dA[SP];
+  load_states<SP>(a.a + (long long)p.ch * S, S, p.n0, A2);
 #pragma unroll
-  for (int i = 0; i < SP; ++i) mu[i] = dA[i] = 0.f;
+  for (int i = 0; i < SP; ++i) {
+    A2[i] *= LOG2E;
+    mu[i] = dA[i] = 0.f;
+  }
   if (p.has) {
     if (p.chunk < a.s.chunks - 1) load_states<SP>(a.ends + p.chunk * states + p.at * S, S, p.n0, mu);
     else if (a.dh_last) load_states<SP>(a.dh_last + p.at * S, S, p.n0, mu);
   }
   const float bias = a.bias ? a.bias[p.ch] : 0.f, skip = a.skip ? a.skip[p.ch] : 0.f;
   const bool gated = a.z.data;
-  const Steps<E> xs(a.x, p), ds(a.dt, p), ys(a.dy, p), zs(gated ? a.z : a.x, p);
-  Tile next;
+  const int tiles = (p.t1 - p.t0 + R - 1) / R, end = p.t0 + (tiles - 1) * R;
+  Steps<E> xs(a.x, p, end), ds(a.dt, p, end), ys(a.dy, p, end), zs(one_of(gated, a.z, a.x), p, end);
+  Steps<E> xo(a.dx, p, end), dto(a.ddt, p, end), zo(one_of(gated, a.dz, a.dx), p, end);
+  Tile next(a, p.b, end);
+  const float* saved = a.saved + end / R * states + p.at * S;
   E xn[G], dn[G], yn[G], zn[G];
   float hn[SP];
-  auto load = [&](int t) {
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      xn[g] = xs.load(t + 4 * g + q, last);
-      dn[g] = ds.load(t + 4 * g + q, last);
-      yn[g] = ys.load(t + 4 * g + q, last);
-      if (gated) zn[g] = zs.load(t + 4 * g + q, last);
-    }
-    next.load(a, p.b, t);
-    load_states<SP>(a.saved + t / R * states + p.at * S, S, p.n0, hn);
+  auto load = [&](int t) SSM_INLINE {
+    auto steps = [&](auto full) SSM_INLINE {
+      constexpr bool FULL = decltype(full)::value;
+      xs.template load<FULL>(xn, last - t - q);
+      ds.template load<FULL>(dn, last - t - q);
+      ys.template load<FULL>(yn, last - t - q);
+      if (gated) zs.template load<FULL>(zn, last - t - q);
+    };
+    if (t + R <= a.c.T) steps(std::true_type{});
+    else steps(std::false_type{});
+    next.load(t, last);
+    load_states<SP>(saved, S, p.n0, hn);
+    xs.move(-R);
+    ds.move(-R);
+    ys.move(-R);
+    zs.move(-R);
+    next.move(-R);
+    saved -= states;
   };
-  const int tiles = (p.t1 - p.t0 + R - 1) / R;
-  load(p.t0 + (tiles - 1) * R);
+  load(end);
+  // the thread's place in the tile's sums (those i * SSM_THREADS behind it are of the same state): [col][T,B,2S]
+  const int own = threadIdx.x % (8 * SP), own_n = own % (4 * SP) < S ? own / (4 * SP) * S + own % (4 * SP) : -1;
+  float* part_bc =
+      a.part_bc + (((long long)(blockIdx.x % (unsigned)a.s.cols) * a.c.T + end + threadIdx.x / (8 * SP)) * a.c.B + p.b) * (2 * S) + own_n;
+  const long long row = 2LL * a.c.B * S;                // of a step
   float dskip = 0.f, dbias = 0.f;
   int buf = 0;
   for (int k = tiles - 1; k >= 0; --k, buf ^= 1) {
     const int t = p.t0 + k * R;
-    float x[G], delta[G], slope[G], dy[G], z[G], out[G];    // out: dL/d(sum c h + skip x)
+    E xr[G], dr[G], yr[G], zr[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      const bool in = p.has && t + 4 * g + q < a.c.T;
-      const Softplus sp(elem_f32(dn[g]) + bias);
-      x[g] = in ? elem_f32(xn[g]) : 0.f;
-      delta[g] = in ? sp.d : 0.f;
-      slope[g] = sp.slope;
-      dy[g] = in ? elem_f32(yn[g]) : 0.f;
-      z[g] = gated ? elem_f32(zn[g]) : 0.f;
-      out[g] = gated && in ? dy[g] * (z[g] * Sigmoid(z[g]).s) : dy[g];
+      xr[g] = xn[g];
+      dr[g] = dn[g];
+      yr[g] = yn[g];
+      if (gated) zr[g] = zn[g];
     }
     float h[SP];
 #pragma unroll
@@ -491,19 +542,33 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
     const unsigned resets = ssm_resets(a, p.b, t, R);
     __syncthreads();                               // (and red has been read)
     if (k > 0) load(t - R);
-    auto tile = [&](auto cut_) {
-      constexpr bool CUT = decltype(cut_)::value;
+    auto tile = [&](auto plain) SSM_INLINE {
+      constexpr bool PLAIN = decltype(plain)::value;
+      // (Lanes without a channel go through another one's, with dy = 0: they add nothing to the sums over channels.)
+      float x[G], delta[G], slope[G], dy[G], z[G], sz[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const bool in = PLAIN || t + 4 * g + q < a.c.T;
+        const float v = elem_f32(dr[g]) + bias;
+        const Softplus sp(v);
+        x[g] = in ? elem_f32(xr[g]) : 0.f;
+        delta[g] = in ? sp.d : 0.f;
+        slope[g] = sp.slope(v);
+        dy[g] = in && p.has ? elem_f32(yr[g]) : 0.f;
+        z[g] = in && gated ? elem_f32(zr[g]) : 1.f;
+        sz[g] = gated ? Sigmoid(z[g]).s : 1.f;
+      }
       float keep[R][SP], past[R][SP], sum[G];
       // forward, again
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         const float dx = delta[g] * x[g];
         float part[4];
-        auto step = [&](auto j_) {
+        auto step = [&](auto j_) SSM_INLINE {
           constexpr int j = decltype(j_)::value;
           const int r = 4 * g + j;
           const float dj = quad_of<j>(delta[g]), xj = quad_of<j>(dx);
-          const bool cut = CUT && (resets >> r & 1);
+          const bool cut = !PLAIN && (resets >> r & 1);
           float b[SP], c[SP];
           read_bc<SP>(bc[buf], r, q, 0, b);
           read_bc<SP>(bc[buf], r, q, 1, c);
@@ -511,7 +576,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
 #pragma unroll
           for (int i = 0; i < SP; ++i) {
             past[r][i] = h[i];
-            keep[r][i] = decay(dj, A[i] * LOG2E);
+            keep[r][i] = decay(dj, A2[i]);
             h[i] = cut ? xj * b[i] : fmaf(keep[r][i], h[i], xj * b[i]);
             y = fmaf(h[i], c[i], y);
           }
@@ -526,13 +591,14 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
       // back
 #pragma unroll
       for (int g = G - 1; g >= 0; --g) {
-        const float dx = delta[g] * x[g];
+        // dL/d(sum c h + skip x)
+        const float dx = delta[g] * x[g], out = dy[g] * (z[g] * sz[g]);
         float of_x[4], of_d[4];
-        auto step = [&](auto j_) {
+        auto step = [&](auto j_) SSM_INLINE {
           constexpr int j = decltype(j_)::value;
           const int r = 4 * g + j;
-          const float dj = quad_of<j>(delta[g]), xj = quad_of<j>(dx), oj = quad_of<j>(out[g]);
-          const bool cut = CUT && (resets >> r & 1);
+          const float dj = quad_of<j>(delta[g]), xj = quad_of<j>(dx), oj = quad_of<j>(out);
+          const bool cut = !PLAIN && (resets >> r & 1);
           float b[SP], c[SP], v[2 * SP];
           read_bc<SP>(bc[buf], r, q, 0, b);
           read_bc<SP>(bc[buf], r, q, 1, c);
@@ -545,7 +611,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
             lb = fmaf(lam, b[i], lb);
             mu[i] = cut ? 0.f : keep[r][i] * lam;
             const float m = cut ? 0.f : mu[i] * past[r][i];
-            ld = fmaf(m, A[i], ld);
+            ld = fmaf(m, A2[i], ld);
             dA[i] = fmaf(m, dj, dA[i]);
             h[i] = past[r][i];
           }
@@ -558,34 +624,32 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
         step(std::integral_constant<int, 1>());
         step(std::integral_constant<int, 0>());
         const float lb = quad_sums(of_x, q), ld = quad_sums(of_d, q);
-        const int ts = t + 4 * g + q;
-        if (p.has && ts < a.c.T) {
-          const float ddt = fmaf(lb, x[g], ld) * slope[g];
-          put<E>(a.dx, p, ts, fmaf(lb, delta[g], out[g] * skip));
-          put<E>(a.ddt, p, ts, ddt);
-          if (gated) {
-            const Sigmoid sg(z[g]);
-            put<E>(a.dz, p, ts, dy[g] * fmaf(skip, x[g], sum[g]) * (sg.s * fmaf(z[g], sg.n, 1.f)));
-          }
-          dskip = fmaf(out[g], x[g], dskip);
+        const float ddt = fmaf(lb, x[g], ld * LN2) * slope[g];
+        if (p.has && (PLAIN || t + 4 * g + q < a.c.T)) {
+          xo.put(g, fmaf(lb, delta[g], out * skip));
+          dto.put(g, ddt);
+          if (gated) zo.put(g, dy[g] * fmaf(skip, x[g], sum[g]) * (sz[g] * fmaf(z[g], 1.f - sz[g], 1.f)));
+          dskip = fmaf(out, x[g], dskip);
           dbias += ddt;
         }
       }
     };
-    if (resets) tile(std::true_type{});
+    if (!resets && t + R <= a.c.T) tile(std::true_type{});
     else tile(std::false_type{});
     __syncthreads();
     // the waves' sums of the tile
-    const int col = (int)(blockIdx.x % (unsigned)a.s.cols);
-    for (int e = threadIdx.x; e < R * 8 * SP; e += SSM_THREADS) {
-      const int r = e / (8 * SP), which = e % (8 * SP) / (4 * SP), n = e % (4 * SP);
-      if (n < S && t + r < a.c.T) {
-        const float* f = &red[0][r][which * 4 * SP + n];
-        constexpr int W = R * 8 * SP;
-        a.part_bc[(((long long)col * a.c.T + t + r) * a.c.B + p.b) * (2 * S) + which * S + n] =
-            (f[0] + f[W]) + (f[2 * W] + f[3 * W]);
-      }
+    constexpr int W = R * 8 * SP;                  // of a wave
+#pragma unroll
+    for (int i = 0; i < (W + SSM_THREADS - 1) / SSM_THREADS; ++i) {
+      const int e = threadIdx.x + i * SSM_THREADS, r = e / (8 * SP);
+      if (own_n < 0 || (W % SSM_THREADS != 0 && e >= W) || t + r >= a.c.T) continue;
+      const float* f = &red[0][0][0] + e;
+      part_bc[i * (SSM_THREADS / (8 * SP)) * row] = (f[0] + f[W]) + (f[2 * W] + f[3 * W]);
     }
+    part_bc -= R * row;
+    xo.move(-R);
+    dto.move(-R);
+    zo.move(-R);
   }
   if (!p.has) return;
   const long long k = (long long)p.chunk * a.c.B * a.c.H + p.at;
@@ -603,32 +667,32 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
 template <typename E>
 __global__ __launch_bounds__(256) void ssm_bc_kernel(SsmArgs a) {
   const int S2 = 2 * a.c.S;
-  const long long n = (long long)a.c.T * a.c.B * S2, i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  float v = 0.f;
-  for (int c = 0; c < a.s.cols; ++c) v += a.part_bc[c * n + i];
-  const long long row = i / S2;
-  const int s = (int)(i - row * S2), t = (int)(row / a.c.B), b = (int)(row - (long long)t * a.c.B);
-  const glr_seq& o = s < a.c.S ? a.db : a.dc;
-  ((E*)o.data)[t * o.stride_t + b * o.stride_b + (s < a.c.S ? s : s - a.c.S)] = elem_of<E>(v);
+  const long long n = (long long)a.c.T * a.c.B * S2, i = 2 * ((long long)blockIdx.x * 256 + threadIdx.x);
+  if (i >= n) return;                                // (n is even)
+  float x = 0.f, y = 0.f;
+  const float* f = a.part_bc + i;
+#pragma unroll 8
+  for (int c = 0; c < a.s.cols; ++c, f += n) {
+    const float2 v = *reinterpret_cast<const float2*>(f);
+    x += v.x;
+    y += v.y;
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const long long row = (i + k) / S2;
+    const int s = (int)(i + k - row * S2), t = (int)(row / a.c.B), b = (int)(row - (long long)t * a.c.B);
+    const glr_seq& o = s < a.c.S ? a.db : a.dc;
+    ((E*)o.data)[t * o.stride_t + b * o.stride_b + (s < a.c.S ? s : s - a.c.S)] = elem_of<E>(k ? y : x);
+  }
 }
 
-// Gradients of a, skip and bias: sums over the chunks and batch rows, 64 of them side by side in four parts.
-__global__ __launch_bounds__(256) void ssm_params_kernel(SsmArgs a) {
-  __shared__ float part[4][64];
-  const long long HS = (long long)a.c.H * a.c.S, H2 = 2LL * a.c.H, i = (long long)blockIdx.x * 64 + (threadIdx.x & 63);
-  const int w = threadIdx.x >> 6;
-  const long long P = (long long)a.s.chunks * a.c.B;
+// Gradients of a, skip and bias: sums over the chunks and batch rows.
+__global__ __launch_bounds__(SUM_THREADS) void ssm_params_kernel(SsmArgs a) {
+  const long long HS = (long long)a.c.H * a.c.S, H2 = 2LL * a.c.H, i = sum_column();
   const bool of_a = i < HS;
-  const float* f = of_a ? a.part_a + i : a.part_h + (i - HS);
-  const long long stride = of_a ? HS : H2;
-  float v = 0.f;
-  if (i < HS + H2)
-    for (long long k = w; k < P; k += 4) v += f[k * stride];
-  part[w][threadIdx.x & 63] = v;
-  __syncthreads();
-  if (w || i >= HS + H2) return;
-  v = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+  float v;
+  if (!sum_rows(of_a ? a.part_a + i : a.part_h + (i - HS), of_a ? HS : H2, (long long)a.s.chunks * a.c.B, i < HS + H2, v))
+    return;
   if (of_a) {
     a.da[i] = v;
   } else {
@@ -670,7 +734,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_step_kernel(SsmStepArgs a) {
   float v = fmaf(a.skip ? a.skip[ch] : 0.f, x, sum);
   if (a.z.data) {
     const float z = one(a.z);
-    v *= z * Sigmoid(z).s;
+    v *= silu(z);
   }
   *y = elem_of<E>(v);
 }
@@ -679,12 +743,12 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_step_kernel(SsmStepArgs a) {
 SsmShape ssm_shape(const ssm_cfg& c, bool backward) {
   SsmShape s;
   s.per = c.S <= 4 ? 1 : c.S <= 8 ? 2 : c.S <= 16 ? 4 : c.S <= 32 ? 8 : 16;
-  s.save = s.per <= 4 ? 16 : 64 / s.per;
+  s.save = s.per <= 8 ? 8 : 4;
   s.cols = (c.H + SSM_COLS - 1) / SSM_COLS;
   const long long across = (long long)s.cols * c.B, tiles = ((long long)c.T + SSM_TILE - 1) / SSM_TILE;
   long long chunks = 1;
   if (across < (backward ? 256 : 512)) {
-    chunks = ((backward ? 512 : 1024) + across - 1) / across;
+    chunks = (1024 + across - 1) / across;
     chunks = chunks < (tiles + 1) / 2 ? chunks : (tiles + 1) / 2;
   }
   s.len = (int)((tiles + chunks - 1) / chunks) * SSM_TILE;
@@ -728,7 +792,7 @@ bool ssm_launchable(const ssm_cfg& c) {
   }
   return launchable(((long long)c.B * c.H * c.S + 255) / 256, 256) &&
          launchable(((long long)c.T * c.B * 2 * c.S + 255) / 256, 256) &&
-         launchable(((long long)c.H * (c.S + 2) + 63) / 64, 256);
+         launchable(((long long)c.H * (c.S + 2) + SUM_COLS - 1) / SUM_COLS, SUM_THREADS);
 }
 static void ssm_place(SsmArgs& a, char* ws, bool backward) {
   const SsmSpace w(a.c, backward);
@@ -747,31 +811,34 @@ static hipError_t ssm_between(const SsmArgs& a, const float* first, bool backwar
 template <typename E, int SP>
 static hipError_t ssm_forward_start(const SsmArgs& a, hipStream_t s) {
   const long long across = (long long)a.s.cols * a.c.B;
+  const dim3 t(SSM_THREADS);
   if (a.s.chunks > 1) {
-    hipLaunchKernelGGL((ssm_forward_kernel<E, SP, false>), dim3((unsigned)(across * (a.s.chunks - 1))),
-                       dim3(SSM_THREADS), 0, s, a);
+    hipLaunchKernelGGL((ssm_forward_kernel<E, SP, false>), dim3((unsigned)(across * (a.s.chunks - 1))), t, 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || (e = ssm_between(a, a.h0, false, s)) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((ssm_forward_kernel<E, SP, true>), dim3((unsigned)(across * a.s.chunks)), dim3(SSM_THREADS), 0, s, a);
+  hipLaunchKernelGGL((ssm_forward_kernel<E, SP, true>), dim3((unsigned)(across * a.s.chunks)), t, 0, s, a);
   return hipGetLastError();
 }
 template <typename E, int SP>
 static hipError_t ssm_backward_start(const SsmArgs& a, hipStream_t s) {
   const long long across = (long long)a.s.cols * a.c.B;
+  const dim3 t(SSM_THREADS);
   hipError_t e;
   if (a.s.chunks > 1) {
-    hipLaunchKernelGGL((ssm_adjoint_ends_kernel<E, SP>), dim3((unsigned)(across * (a.s.chunks - 1))),
-                       dim3(SSM_THREADS), 0, s, a);
+    hipLaunchKernelGGL((ssm_adjoint_ends_kernel<E, SP>), dim3((unsigned)(across * (a.s.chunks - 1))), t, 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess || (e = ssm_between(a, a.dh_last, true, s)) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((ssm_backward_kernel<E, SP, (SP <= 4 ? 16 : 64 / SP)>), dim3((unsigned)(across * a.s.chunks)),
-                     dim3(SSM_THREADS), 0, s, a);
+  hipLaunchKernelGGL((ssm_backward_kernel<E, SP, (SP <= 8 ? 8 : 4)>), dim3((unsigned)(across * a.s.chunks)), t, 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL((ssm_bc_kernel<E>), dim3(blocks((long long)a.c.T * a.c.B * 2 * a.c.S)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((ssm_bc_kernel<E>), dim3(blocks((long long)a.c.T * a.c.B * a.c.S)), dim3(256), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(ssm_params_kernel, dim3((unsigned)(((long long)a.c.H * (a.c.S + 2) + 63) / 64)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(ssm_params_kernel, dim3(sum_groups((long long)a.c.H * (a.c.S + 2))), dim3(SUM_THREADS), 0, s, a);
   return hipGetLastError();
+}
+template <typename E, int SP>
+static hipError_t ssm_run(const SsmArgs& a, bool backward, hipStream_t s) {
+  return backward ? ssm_backward_start<E, SP>(a, s) : ssm_forward_start<E, SP>(a, s);
 }
 template <typename E, int SP>
 static hipError_t ssm_step_start(const SsmStepArgs& a, hipStream_t s) {
@@ -779,34 +846,45 @@ static hipError_t ssm_step_start(const SsmStepArgs& a, hipStream_t s) {
                      s, a);
   return hipGetLastError();
 }
-// F<type, states of a lane>(arguments)
-#define SSM_DISPATCH(F, a, s)                                                  \
-  auto by_states = [&](auto e) -> hipError_t {                                 \
-    using E = decltype(e);                                                     \
-    switch (ssm_shape(a.c, false).per) {                                       \
-      case 1: return F<E, 1>(a, s);                                            \
-      case 2: return F<E, 2>(a, s);                                            \
-      case 4: return F<E, 4>(a, s);                                            \
-      case 8: return F<E, 8>(a, s);                                            \
-      default: return F<E, 16>(a, s);                                          \
-    }                                                                          \
-  };                                                                           \
-  if (a.c.dtype == MGRIT_F32) return by_states(float());                       \
-  if (a.c.dtype == MGRIT_BF16) return by_states(Bf16());                       \
-  return by_states(F16())
+template <typename E>
+static hipError_t ssm_by_states(const SsmArgs& a, bool backward, hipStream_t s) {
+  switch (a.s.per) {
+    case 1: return ssm_run<E, 1>(a, backward, s);
+    case 2: return ssm_run<E, 2>(a, backward, s);
+    case 4: return ssm_run<E, 4>(a, backward, s);
+    case 8: return ssm_run<E, 8>(a, backward, s);
+    default: return ssm_run<E, 16>(a, backward, s);
+  }
+}
+static hipError_t ssm_typed(const SsmArgs& a, bool backward, hipStream_t s) {
+  if (a.c.dtype == MGRIT_F32) return ssm_by_states<float>(a, backward, s);
+  if (a.c.dtype == MGRIT_BF16) return ssm_by_states<Bf16>(a, backward, s);
+  return ssm_by_states<F16>(a, backward, s);
+}
+template <typename E>
+static hipError_t ssm_step_by_states(const SsmStepArgs& a, hipStream_t s) {
+  switch (ssm_shape(a.c, false).per) {
+    case 1: return ssm_step_start<E, 1>(a, s);
+    case 2: return ssm_step_start<E, 2>(a, s);
+    case 4: return ssm_step_start<E, 4>(a, s);
+    case 8: return ssm_step_start<E, 8>(a, s);
+    default: return ssm_step_start<E, 16>(a, s);
+  }
+}
 
 hipError_t launch_ssm_forward(SsmArgs a, char* ws, hipStream_t s) {
   ssm_place(a, ws, false);
-  a.s.save = ssm_shape(a.c, true).save;
-  SSM_DISPATCH(ssm_forward_start, a, s);
+  return ssm_typed(a, false, s);
 }
 hipError_t launch_ssm_backward(SsmArgs a, char* ws, hipStream_t s) {
   ssm_place(a, ws, true);
-  SSM_DISPATCH(ssm_backward_start, a, s);
+  return ssm_typed(a, true, s);
 }
 hipError_t launch_ssm_step(const SsmStepArgs& a, hipStream_t s) {
   if (!launchable(((long long)a.c.B * a.c.H * 4 + 255) / 256, 256)) return TOO_LARGE;
-  SSM_DISPATCH(ssm_step_start, a, s);
+  if (a.c.dtype == MGRIT_F32) return ssm_step_by_states<float>(a, s);
+  if (a.c.dtype == MGRIT_BF16) return ssm_step_by_states<Bf16>(a, s);
+  return ssm_step_by_states<F16>(a, s);
 }
 
 }  // namespace mg

@@ -56,7 +56,7 @@ hipError_t launch_conv_step(const ConvStepArgs& a, hipStream_t s);
 // chunk of steps.
 struct SsmShape {
   int per;                  // states of a lane: 1, 2, 4, 8, 16
-  int save;                 // steps between saved states, the tile of the adjoint: 16, 8, 4
+  int save;                 // steps between saved states, the tile of the adjoint: 8 or 4
   int cols;                 // workgroups across the channels
   int chunks, len;          // chunks of a sequence, their steps (a multiple of 16)
 };

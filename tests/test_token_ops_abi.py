@@ -162,7 +162,7 @@ def test_scan_refusals():
         assert size("ssm_workspace_bytes", cfg)[0] == code and size("ssm_saved_bytes", cfg)[0] == code
         assert forward(cfg) == code and backward(cfg) == code
     (_, n), (_, saved) = size("ssm_workspace_bytes", ok), size("ssm_saved_bytes", ok)
-    assert n > 0 and saved == 4 * 7 * 2 * 8 * 4
+    assert n > 0 and saved == 4 * 13 * 2 * 8 * 4
     assert forward(i=None) == NULL and forward(i=inputs(a=None)) == NULL and forward(y=seq(None)) == NULL
     for k in ("x", "dt", "b", "c"):
         assert forward(i=inputs(**{k: ops.GlrSeq()})) == NULL and backward(i=inputs(**{k: ops.GlrSeq()})) == NULL
