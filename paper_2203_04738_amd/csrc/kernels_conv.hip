@@ -1,8 +1,10 @@
 // Causal convolution of every channel over its last few inputs (include/mgrit_tokens.h), its gradient, and one step.
 //
-// A thread has two neighbouring channels and goes along time with the window of inputs that the next step sees in
-// registers; a reset empties the window.  What bounds it is memory: every array is read or written once but for the
-// few steps before (backward: around) each thread's own.
+// A thread has VEC neighbouring channels, as one word (forward four, backward, which carries twice as much, two; one where
+// the arrays are not aligned to that), and goes along time with the window of inputs that the next step sees in registers; a reset empties the window.  What bounds it is
+// memory: every array is read or written once but for the few steps before (backward: behind) each thread's own.
+#include <type_traits>
+
 #include "elem.h"
 #include "pairs.h"
 #include "row_sums.h"
@@ -11,209 +13,300 @@
 namespace mg {
 
 constexpr int CONV_RUN = 16;                         // steps of a thread, forward
-constexpr int CONV_SEG = 64;                         // steps that a thread looks at in a segment, backward
+constexpr int CONV_SEG = 64, CONV_BLOCK = 8;         // steps of a segment and of a block of it, backward
 
-// The window of a thread's two channels, oldest first; WT >= W taps, those before the last W never used.
-template <int WT>
+// One step of a thread's channels as it is stored.
+template <typename E, int VEC>
+struct ConvRaw {
+  static constexpr int words = VEC * (int)sizeof(E) >= 4 ? VEC * (int)sizeof(E) / 4 : 1;
+  typedef unsigned Word __attribute__((ext_vector_type(words)));
+  unsigned w[words];
+  __device__ inline void load(const E* p) {
+    if constexpr (VEC == 1) {
+      const E e = *p;
+      if constexpr (sizeof(E) == 4) w[0] = __float_as_uint(e);
+      else w[0] = e.bits;
+    } else {
+      const Word v = *reinterpret_cast<const Word*>(p);
+#pragma unroll
+      for (int i = 0; i < words; ++i) w[i] = v[i];
+    }
+  }
+  __device__ inline float at(int c) const { return word_elem<E>(w[c / ELEMS_PER_WORD<E>], c % ELEMS_PER_WORD<E>); }
+};
+template <typename E, int VEC>
+__device__ inline void conv_store(E* p, const float (&v)[VEC], bool past) {
+  if constexpr (VEC == 1) {
+    *p = elem_of<E>(v[0]);
+  } else {
+    typename ConvRaw<E, VEC>::Word w;
+#pragma unroll
+    for (int c = 0; c < VEC; c += ELEMS_PER_WORD<E>) {
+      if constexpr (sizeof(E) == 4) w[c] = __float_as_uint(v[c]);
+      else w[c / 2] = pack2<E>(v[c], v[c + 1]);
+    }
+    store_as(reinterpret_cast<typename ConvRaw<E, VEC>::Word*>(p), w, past);
+  }
+}
+
+// The window of a thread's channels, oldest first; WT >= W taps, those before the last W never used.
+template <int WT, int VEC>
 struct Window {
-  float v[WT - 1][2];
+  float v[WT - 1][VEC];
   __device__ inline void clear() {
 #pragma unroll
-    for (int i = 0; i < WT - 1; ++i) v[i][0] = v[i][1] = 0.f;
-  }
-  __device__ inline void push(float x, float y) {
+    for (int i = 0; i < WT - 1; ++i)
 #pragma unroll
-    for (int i = 0; i + 1 < WT - 1; ++i) {
-      v[i][0] = v[i + 1][0];
-      v[i][1] = v[i + 1][1];
-    }
-    v[WT - 2][0] = x;
-    v[WT - 2][1] = y;
+      for (int c = 0; c < VEC; ++c) v[i][c] = 0.f;
+  }
+  template <typename FN>
+  __device__ inline void push(FN x) {                // x(c): the newest input of channel c
+#pragma unroll
+    for (int i = 0; i + 1 < WT - 1; ++i)
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) v[i][c] = v[i + 1][c];
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) v[WT - 2][c] = x(c);
   }
 };
-template <int WT>
+template <int WT, int VEC>
 struct Taps {
-  float w[WT][2], bias[2];
+  float w[WT][VEC], bias[VEC];
   int skip;                                          // taps that do not exist
-  __device__ inline Taps(const float* weight, const float* b, int W, int ch, bool second) : skip(WT - W) {
-    const int c1 = second ? ch + 1 : ch;
+  __device__ inline Taps(const float* weight, const float* b, int W, int ch) : skip(WT - W) {
 #pragma unroll
-    for (int k = 0; k < WT; ++k) {
-      w[k][0] = k >= skip ? weight[(long long)ch * W + k - skip] : 0.f;
-      w[k][1] = k >= skip ? weight[(long long)c1 * W + k - skip] : 0.f;
+    for (int c = 0; c < VEC; ++c) {
+#pragma unroll
+      for (int k = 0; k < WT; ++k) w[k][c] = k >= skip ? weight[(long long)(ch + c) * W + k - skip] : 0.f;
+      bias[c] = b ? b[ch + c] : 0.f;
     }
-    bias[0] = b ? b[ch] : 0.f;
-    bias[1] = b ? b[c1] : 0.f;
   }
-  __device__ inline float apply(const Window<WT>& win, float x, int c) const {
+  __device__ inline bool exists(int k) const { return WT < 8 || k >= skip; }
+  __device__ inline float apply(const Window<WT, VEC>& win, float x, int c) const {
     float p = bias[c];
 #pragma unroll
     for (int k = 0; k < WT - 1; ++k)
-      if (WT < 8 || k >= skip) p = fmaf(w[k][c], win.v[k][c], p);
+      if (exists(k)) p = fmaf(w[k][c], win.v[k][c], p);
     return fmaf(w[WT - 1][c], x, p);
   }
 };
-__device__ inline float conv_sigmoid(float z) {
-  const float e = exp_of(-fabsf(z));
-  const float small = e * __builtin_amdgcn_rcpf(1.0f + e);
-  return z != z ? z : z < 0.f ? small : 1.0f - small;
-}
 
-// Input s < 0 of a batch row's channel: from `past`, or zero.
-__device__ inline float past_input(const float* past, int W, int H, int b, int s, int ch) {
-  return past && s >= 1 - W ? past[((long long)b * (W - 1) + s + W - 1) * H + ch] : 0.f;
-}
+// Where a thread stands: `lanes` threads side by side across the channels, 64 / lanes runs (segments) of steps in a wave.
+struct ConvPlace {
+  int lanes, lane_c, ch, row, rows;                  // row: the run of the workgroup's `rows`
+  bool has;
+  __device__ inline ConvPlace(int lanes_, int col, int H, int vec) : lanes(lanes_) {
+    lane_c = threadIdx.x & (lanes - 1);
+    row = threadIdx.x / lanes;
+    rows = 256 / lanes;
+    ch = (col * lanes + lane_c) * vec;
+    has = ch < H;
+    if (!has) ch = 0;
+  }
+  // Bits of the steps t .. t + n - 1 (n <= 24, at least 16 lanes a run) that reset; those outside the sequence do not.
+  __device__ inline unsigned resets(const ConvArgs& a, int b, int t, int n) const {
+    if (!a.reset) return 0;
+    auto look = [&](int i) { return i < n && t + i >= 0 && t + i < a.c.T && a.reset[(long long)(t + i) * a.c.B + b] != 0; };
+    unsigned bits = mine(__ballot(look(lane_c)));
+    if (n > lanes) bits |= mine(__ballot(look(lane_c + lanes))) << lanes;
+    return bits;
+  }
+  __device__ inline unsigned mine(unsigned long long all) const {
+    if (lanes == 64) return (unsigned)all;
+    return (unsigned)(all >> ((threadIdx.x & 63) / lanes * lanes)) & (unsigned)((1ull << lanes) - 1);
+  }
+};
 
-// Fills the window with the inputs before step t0.
-template <typename E, bool ALIGNED, int WT>
-__device__ inline void fill_window(const ConvArgs& a, int b, int ch, bool second, int t0, Window<WT>& win) {
+// Fills the window with the inputs before step t0; bit i of `resets`: step t0 - (WT - 1) + i resets.
+template <typename E, int VEC, int WT>
+__device__ inline void fill_window(const ConvArgs& a, int b, int ch, int t0, unsigned resets, Window<WT, VEC>& win) {
   win.clear();
   const E* x = (const E*)a.x.data + b * a.x.stride_b + ch;
 #pragma unroll
   for (int i = 0; i < WT - 1; ++i) {
     const int s = t0 - (WT - 1) + i;
     if (s >= 0) {
-      const RawPair<E> r = load_pair<E, ALIGNED>(x + s * a.x.stride_t, second);
-      if (a.reset && a.reset[(long long)s * a.c.B + b]) win.clear();
-      win.push(r.at(0), r.at(1));
+      ConvRaw<E, VEC> r;
+      r.load(x + s * a.x.stride_t);
+      if (resets >> i & 1) win.clear();
+      win.push([&](int c) { return r.at(c); });
     } else {
-      win.push(past_input(a.past, a.c.W, a.c.H, b, s, ch), past_input(a.past, a.c.W, a.c.H, b, s, second ? ch + 1 : ch));
+      const bool given = a.past && s >= 1 - a.c.W;
+      const float* past = a.past + ((long long)b * (a.c.W - 1) + s + a.c.W - 1) * a.c.H + ch;
+      win.push([&](int c) { return given ? past[c] : 0.f; });
     }
   }
 }
 
-template <typename E, bool ALIGNED, int WT>
-__global__ __launch_bounds__(256) void conv_forward_kernel(ConvArgs a) {
-  const int pairs = (a.c.H + 1) / 2, T = a.c.T;
-  const int runs = (T + CONV_RUN - 1) / CONV_RUN;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x, br = i / pairs;
-  const int ch = 2 * (int)(i - br * pairs);
-  const int b = (int)(br / runs), t0 = (int)(br - (long long)b * runs) * CONV_RUN;
-  if (b >= a.c.B) return;
-  const bool second = ch + 1 < a.c.H;
-  RawPair<E> raw[CONV_RUN];
+template <typename E, int VEC, int WT>
+__global__ __launch_bounds__(256) void conv_forward_kernel(ConvArgs a, int lanes, int cols) {
+  const int T = a.c.T, runs = (T + CONV_RUN - 1) / CONV_RUN;
+  const unsigned group = blockIdx.x / (unsigned)cols;
+  const ConvPlace at(lanes, (int)(blockIdx.x - group * cols), a.c.H, VEC);
+  const long long item = (long long)group * at.rows + at.row;
+  const bool run_exists = item < (long long)runs * a.c.B, has = at.has && run_exists;     // (all lanes of a run look at its resets)
+  const int b = run_exists ? (int)(item / runs) : 0, t0 = run_exists ? (int)(item - (long long)b * runs) * CONV_RUN : 0;
+  const int ch = at.ch;
+  ConvRaw<E, VEC> raw[CONV_RUN];
   const E* x = (const E*)a.x.data + b * a.x.stride_b + ch;
 #pragma unroll
-  for (int r = 0; r < CONV_RUN; ++r) raw[r] = load_pair<E, ALIGNED>(x + min(t0 + r, T - 1) * a.x.stride_t, second);
-  const Taps<WT> taps(a.weight, a.bias, a.c.W, ch, second);
-  Window<WT> win;
-  fill_window<E, ALIGNED, WT>(a, b, ch, second, t0, win);
+  for (int r = 0; r < CONV_RUN; ++r) raw[r].load(x + min(t0 + r, T - 1) * a.x.stride_t);
+  const Taps<WT, VEC> taps(a.weight, a.bias, a.c.W, ch);
+  const unsigned resets = at.resets(a, b, t0 - (WT - 1), WT - 1 + CONV_RUN);
+  Window<WT, VEC> win;
+  fill_window<E, VEC, WT>(a, b, ch, t0, resets, win);
+  if (!has) return;
   E* y = (E*)a.y.data + b * a.y.stride_b + ch;
+  auto run = [&](auto plain) __attribute__((always_inline)) {     // plain: every step exists and none resets
+    constexpr bool PLAIN = decltype(plain)::value;
 #pragma unroll
-  for (int r = 0; r < CONV_RUN; ++r) {
-    const int t = t0 + r;
-    if (t >= T) break;
-    if (a.reset && a.reset[(long long)t * a.c.B + b]) win.clear();
-    float p[2];
+    for (int r = 0; r < CONV_RUN; ++r) {
+      const int t = t0 + r;
+      if (!PLAIN && t >= T) break;
+      if (!PLAIN && (resets >> (WT - 1 + r) & 1)) win.clear();
+      float p[VEC];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      p[c] = taps.apply(win, raw[r].at(c), c);
-      if (a.c.act == CONV_SILU) p[c] *= conv_sigmoid(p[c]);
+      for (int c = 0; c < VEC; ++c) {
+        p[c] = taps.apply(win, raw[r].at(c), c);
+        if (a.c.act == CONV_SILU) p[c] = silu(p[c]);
+      }
+      conv_store<E, VEC>(y + t * a.y.stride_t, p, a.past_caches);
+      win.push([&](int c) { return raw[r].at(c); });
     }
-    store_pair<E, ALIGNED>(y + t * a.y.stride_t, p[0], p[1], second, a.past_caches);
-    win.push(raw[r].at(0), raw[r].at(1));
-  }
+  };
+  if (!resets && t0 + CONV_RUN <= T) run(std::true_type{});
+  else run(std::false_type{});
   if (!a.last || t0 + CONV_RUN < T) return;
 #pragma unroll
   for (int k = 0; k < WT - 1; ++k)
     if (k >= taps.skip) {
       float* o = a.last + ((long long)b * (a.c.W - 1) + k - taps.skip) * a.c.H + ch;
-      o[0] = win.v[k][0];
-      if (second) o[1] = win.v[k][1];
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) o[c] = win.v[k][c];
     }
 }
 
-// A thread goes through segments of CONV_SEG - WT + 1 steps, and the WT - 1 behind each, whose outputs its inputs reach.
-// LANES threads are side by side across the channels.
-template <typename E, bool ALIGNED, int WT>
-__global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, int lanes) {
-  constexpr int OWN = CONV_SEG - (WT - 1), BLOCK = 8;
-  const int T = a.c.T, B = a.c.B, H = a.c.H, W = a.c.W;
-  const int cols = (H + 2 * lanes - 1) / (2 * lanes), rows = 256 / lanes;
+// What a thread carries along a segment: the window, and the gradients of the inputs t - WT + 1 .. t.
+template <typename E, int VEC, int WT>
+struct ConvBack {
+  const ConvArgs& a;
+  Window<WT, VEC> win;
+  float g[WT][VEC], dw[WT][VEC], dbias[VEC];
+  int b, ch, t0, t1, last_reset;                     // last_reset: the last step so far that resets
+
+  __device__ inline ConvBack(const ConvArgs& a_) : a(a_) {
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) {
+      dbias[c] = 0.f;
+#pragma unroll
+      for (int k = 0; k < WT; ++k) dw[k][c] = 0.f;
+    }
+  }
+  // Step t's own output.  PLAIN: it exists, is the segment's and sees all of the window.
+  template <bool PLAIN>
+  __device__ inline void step(const Taps<WT, VEC>& taps, int t, const ConvRaw<E, VEC>& x, const ConvRaw<E, VEC>& dy) {
+    const bool own = PLAIN || t < t1;
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) {
+      const float xv = x.at(c);
+      float dp = dy.at(c);
+      if (a.c.act == CONV_SILU) {
+        const float p = taps.apply(win, xv, c);
+        const Sigmoid s(p);
+        dp *= s.s * fmaf(p, s.n, 1.f);
+      }
+#pragma unroll
+      for (int k = 0; k < WT; ++k) {
+        if (!taps.exists(k) || (!PLAIN && t - (WT - 1) + k < last_reset)) continue;
+        g[k][c] = fmaf(taps.w[k][c], dp, g[k][c]);
+        if (own) dw[k][c] = fmaf(dp, k == WT - 1 ? xv : win.v[k < WT - 1 ? k : 0][c], dw[k][c]);
+      }
+      if (own) dbias[c] += dp;
+    }
+    win.push([&](int c) { return x.at(c); });
+  }
+  // The input t - (WT - 1), whose outputs are complete.
+  template <bool PLAIN>
+  __device__ inline void emit(int t) {
+    const int s = t - (WT - 1), T = a.c.T, W = a.c.W, H = a.c.H;
+    if (!PLAIN && a.dlast && s >= T - (W - 1) && s >= last_reset) {
+      const float* d = a.dlast + ((long long)b * (W - 1) + s - (T - (W - 1))) * H + ch;
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) g[0][c] += d[c];
+    }
+    if (s >= t0 && (PLAIN || s < t1)) {
+      conv_store<E, VEC>((E*)a.dx.data + s * a.dx.stride_t + b * a.dx.stride_b + ch, g[0], a.past_caches);
+    } else if (t0 == 0 && s < 0 && s >= 1 - W && a.dpast) {
+      float* d = a.dpast + ((long long)b * (W - 1) + s + W - 1) * H + ch;
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) d[c] = g[0][c];
+    }
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) {
+#pragma unroll
+      for (int k = 0; k + 1 < WT; ++k) g[k][c] = g[k + 1][c];
+      g[WT - 1][c] = 0.f;
+    }
+  }
+};
+
+// A thread goes through segments of CONV_SEG steps, and the WT - 1 behind each, whose outputs its inputs reach.
+template <typename E, int VEC, int WT>
+__global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, int lanes, int cols) {
+  const int T = a.c.T, W = a.c.W, H = a.c.H;
   const int group = blockIdx.x / cols, col = blockIdx.x - group * cols;
-  const int lane = threadIdx.x & (lanes - 1), row = threadIdx.x / lanes;
-  const int ch = (col * lanes + lane) * 2;
-  const bool has = ch < H, second = ch + 1 < H;
-  __shared__ float part[256][2];
-  float dw[WT][2], dbias[2] = {0.f, 0.f};
+  const ConvPlace at(lanes, col, H, VEC);
+  __shared__ float part[256][VEC];
+  ConvBack<E, VEC, WT> v(a);
+  v.ch = at.ch;
+  const Taps<WT, VEC> taps(a.weight, a.bias, W, at.ch);
+  const int segs = (T + CONV_SEG - 1) / CONV_SEG;
+  const long long all = (long long)segs * a.c.B;
+  // (the threads of a wave go through as many segments: they look at resets together)
+  for (long long first = (long long)group * at.rows; first < all; first += (long long)a.groups * at.rows) {
+    const long long item = first + at.row;
+    const bool real = at.has && item < all;
+    const int b = item < all ? (int)(item / segs) : 0;
+    v.b = b;
+    v.t0 = item < all ? (int)(item - (long long)b * segs) * CONV_SEG : 0;
+    v.t1 = min(v.t0 + CONV_SEG, T);
+    const E* x = (const E*)a.x.data + b * a.x.stride_b + at.ch;
+    const E* dy = (const E*)a.dy.data + b * a.dy.stride_b + at.ch;
+    const unsigned before = at.resets(a, b, v.t0 - (WT - 1), WT - 1);
+    fill_window<E, VEC, WT>(a, b, at.ch, v.t0, before, v.win);
+    v.last_reset = before ? v.t0 - (WT - 1) + 31 - __builtin_clz(before) : -(1 << 30);
 #pragma unroll
-  for (int k = 0; k < WT; ++k) dw[k][0] = dw[k][1] = 0.f;
-  const int segs = (T + OWN - 1) / OWN;
-  const long long all = (long long)segs * B;
-  if (has) {
-    const Taps<WT> taps(a.weight, a.bias, W, ch, second);
-    for (long long item = (long long)group * rows + row; item < all; item += (long long)a.groups * rows) {
-      const int b = (int)(item / segs), t0 = (int)(item - (long long)b * segs) * OWN, t1 = min(t0 + OWN, T);
-      const E* x = (const E*)a.x.data + b * a.x.stride_b + ch;
-      const E* dy = (const E*)a.dy.data + b * a.dy.stride_b + ch;
-      Window<WT> win;
-      fill_window<E, ALIGNED, WT>(a, b, ch, second, t0, win);
-      int last_reset = -(1 << 30);                   // the last step so far that resets
-      if (a.reset)
-        for (int s = max(0, t0 - (WT - 1)); s < t0; ++s)
-          if (a.reset[(long long)s * B + b]) last_reset = s;
-      float g[WT][2];                                // gradients of the inputs t - WT + 1 .. t
+    for (int k = 0; k < WT; ++k)
 #pragma unroll
-      for (int k = 0; k < WT; ++k) g[k][0] = g[k][1] = 0.f;
-      for (int base = t0; base < t1 + WT - 1; base += BLOCK) {
-        RawPair<E> xr[BLOCK], dr[BLOCK];
+      for (int c = 0; c < VEC; ++c) v.g[k][c] = 0.f;
+    for (int off = 0; off < CONV_SEG + WT - 1; off += CONV_BLOCK) {
+      const int base = v.t0 + off;
+      const unsigned resets = at.resets(a, b, base, CONV_BLOCK);
+      if (!real || base >= v.t1 + WT - 1) continue;
+      ConvRaw<E, VEC> xr[CONV_BLOCK], dr[CONV_BLOCK];
 #pragma unroll
-        for (int r = 0; r < BLOCK; ++r) {
-          const long long t = min(base + r, T - 1);
-          xr[r] = load_pair<E, ALIGNED>(x + t * a.x.stride_t, second);
-          dr[r] = load_pair<E, ALIGNED>(dy + t * a.dy.stride_t, second);
+      for (int r = 0; r < CONV_BLOCK; ++r) {
+        const long long t = min(base + r, T - 1);
+        xr[r].load(x + t * a.x.stride_t);
+        dr[r].load(dy + t * a.dy.stride_t);
+      }
+      if (!resets && base - (WT - 1) >= v.last_reset && base + CONV_BLOCK <= v.t1) {
+#pragma unroll
+        for (int r = 0; r < CONV_BLOCK; ++r) {
+          v.template step<true>(taps, base + r, xr[r], dr[r]);
+          v.template emit<true>(base + r);
         }
+      } else {
 #pragma unroll
-        for (int r = 0; r < BLOCK; ++r) {
+        for (int r = 0; r < CONV_BLOCK; ++r) {
           const int t = base + r;
-          if (t >= t1 + WT - 1) break;
-          if (t < T) {
-            if (a.reset && a.reset[(long long)t * B + b]) {
-              win.clear();
-              last_reset = t;
-            }
-            const bool own = t < t1;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const float xv = xr[r].at(c);
-              float dp = dr[r].at(c);
-              if (a.c.act == CONV_SILU) {
-                const float p = taps.apply(win, xv, c), s = conv_sigmoid(p);
-                dp *= s * fmaf(p, 1.f - s, 1.f);
-              }
-#pragma unroll
-              for (int k = 0; k < WT; ++k) {
-                const bool seen = (WT < 8 || k >= taps.skip) && t - (WT - 1) + k >= last_reset;
-                if (seen) {
-                  g[k][c] = fmaf(taps.w[k][c], dp, g[k][c]);
-                  if (own) dw[k][c] = fmaf(dp, k == WT - 1 ? xv : win.v[k < WT - 1 ? k : 0][c], dw[k][c]);
-                }
-              }
-              if (own) dbias[c] += dp;
-            }
-            win.push(xr[r].at(0), xr[r].at(1));
+          if (t >= v.t1 + WT - 1) break;
+          if (resets >> r & 1) {
+            v.win.clear();
+            v.last_reset = t;
           }
-          // the input whose outputs are complete
-          const int s = t - (WT - 1);
-          if (a.dlast && s >= T - (W - 1) && s >= last_reset) {
-            const float* d = a.dlast + ((long long)b * (W - 1) + s - (T - (W - 1))) * H + ch;
-            g[0][0] += d[0];
-            if (second) g[0][1] += d[1];
-          }
-          if (s >= t0 && s < t1) {
-            store_pair<E, ALIGNED>((E*)a.dx.data + s * a.dx.stride_t + b * a.dx.stride_b + ch, g[0][0], g[0][1], second,
-                                   a.past_caches);
-          } else if (t0 == 0 && s < 0 && s >= 1 - W && a.dpast) {
-            float* d = a.dpast + ((long long)b * (W - 1) + s + W - 1) * H + ch;
-            d[0] = g[0][0];
-            if (second) d[1] = g[0][1];
-          }
-#pragma unroll
-          for (int k = 0; k + 1 < WT; ++k) {
-            g[k][0] = g[k + 1][0];
-            g[k][1] = g[k + 1][1];
-          }
-          g[WT - 1][0] = g[WT - 1][1] = 0.f;
+          if (t < T) v.template step<false>(taps, t, xr[r], dr[r]);
+          v.template emit<false>(t);
         }
       }
     }
@@ -224,18 +317,15 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, int lane
   for (int k = 0; k <= WT; ++k) {
     if (k < skip) continue;
     __syncthreads();
-    part[threadIdx.x][0] = k < WT ? dw[k < WT ? k : 0][0] : dbias[0];
-    part[threadIdx.x][1] = k < WT ? dw[k < WT ? k : 0][1] : dbias[1];
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) part[threadIdx.x][c] = k < WT ? v.dw[k < WT ? k : 0][c] : v.dbias[c];
     __syncthreads();
-    if (row == 0 && has) {
-      float u = 0.f, v = 0.f;
-      for (int r = 0; r < rows; ++r) {
-        u += part[r * lanes + lane][0];
-        v += part[r * lanes + lane][1];
-      }
-      float* o = a.part + ((long long)group * H + ch) * (W + 1) + k - skip;
-      o[0] = u;
-      if (second) o[W + 1] = v;
+    for (int i = threadIdx.x; i < lanes * VEC; i += 256) {
+      const int lane = i / VEC, c = i % VEC, ch = (col * lanes + lane) * VEC + c;
+      if (ch >= H) continue;
+      float sum = 0.f;
+      for (int r = 0; r < at.rows; ++r) sum += part[r * lanes + lane][c];
+      a.part[((long long)group * H + ch) * (W + 1) + k - skip] = sum;
     }
   }
 }
@@ -280,72 +370,88 @@ __global__ __launch_bounds__(256) void conv_step_kernel(ConvStepArgs a) {
       a.past_out[at + (long long)k * H] = k + 1 < W - 1 ? past[k + 1 < CONV_MAX_W - 1 ? k + 1 : k] : x;
     }
   p = fmaf(w[W - 1], x, p);
-  if (a.c.act == CONV_SILU) p *= conv_sigmoid(p);
+  if (a.c.act == CONV_SILU) p = silu(p);
   *y = elem_of<E>(p);
 }
 
 // ---- launches
 static int conv_taps(int W) { return W == 2 || W == 3 || W == 4 ? W : 8; }
-static int conv_lanes(int H) { return H > 64 ? 64 : H > 32 ? 32 : 16; }
-static int conv_groups(const conv_cfg& c) {
-  const int lanes = conv_lanes(c.H), own = CONV_SEG - (conv_taps(c.W) - 1);
-  const long long cols = (c.H + 2LL * lanes - 1) / (2 * lanes), rows = 256 / lanes;
-  const long long all = (((c.T + own - 1LL) / own) * c.B + rows - 1) / rows, most = (2047 + cols) / cols;
+// Threads of `vec` channels.  (The workspace and the limits hold for any.)
+struct ConvShape {
+  int lanes, cols, rows;                             // threads side by side, workgroups across, runs of a workgroup
+  ConvShape(int H, int vec) {
+    const long long n = ((long long)H + vec - 1) / vec;
+    lanes = n > 32 ? 64 : n > 16 ? 32 : 16;
+    cols = (int)((n + lanes - 1) / lanes);
+    rows = 256 / lanes;
+  }
+};
+static long long conv_runs(const conv_cfg& c, const ConvShape& s) {
+  return ((c.T + CONV_RUN - 1LL) / CONV_RUN * c.B + s.rows - 1) / s.rows;
+}
+static int conv_groups(const conv_cfg& c, const ConvShape& s) {
+  const long long all = (((c.T + CONV_SEG - 1LL) / CONV_SEG) * c.B + s.rows - 1) / s.rows, most = (2047 + s.cols) / s.cols;
   return (int)(all < most ? all : most);
 }
-size_t conv_workspace(const conv_cfg& c) { return 4 * (size_t)conv_groups(c) * c.H * (c.W + 1); }
-static long long conv_forward_groups(const conv_cfg& c) {
-  return ((c.T + CONV_RUN - 1LL) / CONV_RUN * c.B * ((c.H + 1LL) / 2) + 255) / 256;
+size_t conv_workspace(const conv_cfg& c) {
+  const int two = conv_groups(c, ConvShape(c.H, 2)), one = conv_groups(c, ConvShape(c.H, 1));
+  return 4 * (size_t)(two > one ? two : one) * c.H * (c.W + 1);
 }
 bool conv_launchable(const conv_cfg& c) {
-  return launchable(conv_forward_groups(c), 256) && launchable(sum_groups((long long)c.H * (c.W + 1)), SUM_THREADS);
+  const ConvShape s(c.H, 1);
+  return launchable(conv_runs(c, s) * s.cols, 256) && launchable((long long)conv_groups(c, s) * s.cols, 256) &&
+         launchable(sum_groups((long long)c.H * (c.W + 1)), SUM_THREADS);
 }
-template <typename E, bool ALIGNED>
-static void conv_forward_taps(const ConvArgs& a, hipStream_t s) {
-  const dim3 g((unsigned)conv_forward_groups(a.c)), t(256);
-  switch (conv_taps(a.c.W)) {
-    case 2: hipLaunchKernelGGL((conv_forward_kernel<E, ALIGNED, 2>), g, t, 0, s, a); break;
-    case 3: hipLaunchKernelGGL((conv_forward_kernel<E, ALIGNED, 3>), g, t, 0, s, a); break;
-    case 4: hipLaunchKernelGGL((conv_forward_kernel<E, ALIGNED, 4>), g, t, 0, s, a); break;
-    default: hipLaunchKernelGGL((conv_forward_kernel<E, ALIGNED, 8>), g, t, 0, s, a);
+template <typename E>
+static bool conv_words(const glr_seq& q, int H, int vec) {
+  return H % vec == 0 && q.stride_t % vec == 0 && q.stride_b % vec == 0 && (uintptr_t)q.data % (vec * sizeof(E)) == 0;
+}
+template <typename E, int VEC, int WT, bool BACKWARD>
+static hipError_t conv_kernel(ConvArgs a, hipStream_t s) {
+  const ConvShape c(a.c.H, VEC);
+  const dim3 t(256);
+  if constexpr (!BACKWARD) {
+    hipLaunchKernelGGL((conv_forward_kernel<E, VEC, WT>), dim3((unsigned)(conv_runs(a.c, c) * c.cols)), t, 0, s, a, c.lanes,
+                       c.cols);
+    return hipGetLastError();
+  } else {
+    a.groups = conv_groups(a.c, c);
+    hipLaunchKernelGGL((conv_backward_kernel<E, VEC, WT>), dim3((unsigned)((long long)a.groups * c.cols)), t, 0, s, a, c.lanes,
+                       c.cols);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || (!a.dweight && !a.dbias)) return e;
+    hipLaunchKernelGGL(conv_params_kernel, dim3(sum_groups((long long)a.c.H * (a.c.W + 1))), dim3(SUM_THREADS), 0, s, a);
+    return hipGetLastError();
   }
 }
-template <typename E, bool ALIGNED>
-static void conv_backward_taps(const ConvArgs& a, hipStream_t s) {
-  const int lanes = conv_lanes(a.c.H);
-  const dim3 g((unsigned)(a.groups * ((a.c.H + 2LL * lanes - 1) / (2 * lanes)))), t(256);
+template <typename E, int VEC, bool BACKWARD>
+static hipError_t conv_start(const ConvArgs& a, hipStream_t s) {
   switch (conv_taps(a.c.W)) {
-    case 2: hipLaunchKernelGGL((conv_backward_kernel<E, ALIGNED, 2>), g, t, 0, s, a, lanes); break;
-    case 3: hipLaunchKernelGGL((conv_backward_kernel<E, ALIGNED, 3>), g, t, 0, s, a, lanes); break;
-    case 4: hipLaunchKernelGGL((conv_backward_kernel<E, ALIGNED, 4>), g, t, 0, s, a, lanes); break;
-    default: hipLaunchKernelGGL((conv_backward_kernel<E, ALIGNED, 8>), g, t, 0, s, a, lanes);
+    case 2: return conv_kernel<E, VEC, 2, BACKWARD>(a, s);
+    case 3: return conv_kernel<E, VEC, 3, BACKWARD>(a, s);
+    case 4: return conv_kernel<E, VEC, 4, BACKWARD>(a, s);
+    default: return conv_kernel<E, VEC, 8, BACKWARD>(a, s);
   }
 }
 template <typename E>
-static hipError_t conv_start(const ConvArgs& a, bool backward, hipStream_t s) {
-  const int H = a.c.H;
-  if (!backward) {
-    if (pairs<E>(a.x, H) && pairs<E>(a.y, H)) conv_forward_taps<E, true>(a, s);
-    else conv_forward_taps<E, false>(a, s);
-    return hipGetLastError();
-  }
-  if (pairs<E>(a.x, H) && pairs<E>(a.dy, H) && pairs<E>(a.dx, H)) conv_backward_taps<E, true>(a, s);
-  else conv_backward_taps<E, false>(a, s);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || (!a.dweight && !a.dbias)) return e;
-  hipLaunchKernelGGL(conv_params_kernel, dim3(sum_groups((long long)H * (a.c.W + 1))), dim3(SUM_THREADS), 0, s, a);
-  return hipGetLastError();
+static hipError_t conv_forward_start(const ConvArgs& a, hipStream_t s) {
+  const bool words = conv_words<E>(a.x, a.c.H, 4) && conv_words<E>(a.y, a.c.H, 4);
+  return words ? conv_start<E, 4, false>(a, s) : conv_start<E, 1, false>(a, s);
 }
-static hipError_t conv_typed(const ConvArgs& a, bool backward, hipStream_t s) {
-  if (a.c.dtype == MGRIT_F32) return conv_start<float>(a, backward, s);
-  if (a.c.dtype == MGRIT_BF16) return conv_start<Bf16>(a, backward, s);
-  return conv_start<F16>(a, backward, s);
+template <typename E>
+static hipError_t conv_backward_start(const ConvArgs& a, hipStream_t s) {
+  const bool words = conv_words<E>(a.x, a.c.H, 2) && conv_words<E>(a.dy, a.c.H, 2) && conv_words<E>(a.dx, a.c.H, 2);
+  return words ? conv_start<E, 2, true>(a, s) : conv_start<E, 1, true>(a, s);
 }
-hipError_t launch_conv_forward(const ConvArgs& a, hipStream_t s) { return conv_typed(a, false, s); }
-hipError_t launch_conv_backward(const ConvArgs& a_, hipStream_t s) {
-  ConvArgs a = a_;
-  a.groups = conv_groups(a.c);
-  return conv_typed(a, true, s);
+hipError_t launch_conv_forward(const ConvArgs& a, hipStream_t s) {
+  if (a.c.dtype == MGRIT_F32) return conv_forward_start<float>(a, s);
+  if (a.c.dtype == MGRIT_BF16) return conv_forward_start<Bf16>(a, s);
+  return conv_forward_start<F16>(a, s);
+}
+hipError_t launch_conv_backward(const ConvArgs& a, hipStream_t s) {
+  if (a.c.dtype == MGRIT_F32) return conv_backward_start<float>(a, s);
+  if (a.c.dtype == MGRIT_BF16) return conv_backward_start<Bf16>(a, s);
+  return conv_backward_start<F16>(a, s);
 }
 hipError_t launch_conv_step(const ConvStepArgs& a, hipStream_t s) {
   const long long n = ((long long)a.c.B * a.c.H + 255) / 256;

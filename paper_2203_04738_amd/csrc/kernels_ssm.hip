@@ -61,19 +61,6 @@ struct Softplus {
     return v < 0.f ? e * r : r;
   }
 };
-// s = sigmoid(z), n = sigmoid(-z).  (Of a NaN they are numbers: each use multiplies by z.)
-struct Sigmoid {
-  float s, n;
-  __device__ inline explicit Sigmoid(float z) {
-    const float x = __builtin_amdgcn_fmed3f(-z, -104.f, 88.f), p = x * LOG2E;
-    float e = __builtin_amdgcn_exp2f(p);
-    e = fmaf(e, fmaf(-p, LN2, x), e);
-    s = __builtin_amdgcn_rcpf(1.0f + e);
-    n = e * s;
-  }
-};
-__device__ inline float silu(float z) { return z * Sigmoid(z).s; }
-
 // ---- states of a lane
 typedef float Quad __attribute__((ext_vector_type(4), aligned(4)));
 template <int SP>

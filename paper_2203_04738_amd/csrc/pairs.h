@@ -1,4 +1,4 @@
-// Two neighbouring channels of one step of a sequence, and exponentials of any size.
+// Two neighbouring channels of one step of a sequence, exponentials and sigmoids of any size.
 #pragma once
 #include "elem.h"
 #include "ops.h"
@@ -76,4 +76,16 @@ __device__ inline float exp_of(float x) {
   const float p = LOG2E * x, e = __builtin_amdgcn_exp2f(p);
   return fmaf(e, fminf(fmaf(-p, LN2, x), 0x1p-16f), e);
 }
+// s = sigmoid(z), n = sigmoid(-z).  (Of a NaN they are numbers: each use multiplies by z.)
+struct Sigmoid {
+  float s, n;
+  __device__ inline explicit Sigmoid(float z) {
+    const float x = __builtin_amdgcn_fmed3f(-z, -104.f, 88.f), p = x * LOG2E;
+    float e = __builtin_amdgcn_exp2f(p);
+    e = fmaf(e, fmaf(-p, LN2, x), e);
+    s = __builtin_amdgcn_rcpf(1.0f + e);
+    n = e * s;
+  }
+};
+__device__ inline float silu(float z) { return z * Sigmoid(z).s; }
 }  // namespace mg
