@@ -1,7 +1,6 @@
 // Causal convolution of every channel over its last few inputs (include/mgrit_tokens.h), its gradient, and one step.
 //
-// A thread has VEC neighbouring channels, as one word (forward four, backward, which carries twice as much, two; one where
-// the arrays are not aligned to that), and goes along time with the window of inputs that the next step sees in registers; a reset empties the window.  What bounds it is
+// A thread has VEC neighbouring channels (two, as one word, where the arrays are aligned to that) and goes along time with the window of inputs that the next step sees in registers; a reset empties the window.  What bounds it is
 // memory: every array is read or written once but for the few steps before (backward: behind) each thread's own.
 #include <type_traits>
 
@@ -13,7 +12,7 @@
 namespace mg {
 
 constexpr int CONV_RUN = 16;                         // steps of a thread, forward
-constexpr int CONV_SEG = 64, CONV_BLOCK = 8;         // steps of a segment and of a block of it, backward
+constexpr int CONV_BLOCK = 4;                        // steps of a block of a segment, backward
 
 // One step of a thread's channels as it is stored.
 template <typename E, int VEC>
@@ -250,7 +249,7 @@ struct ConvBack {
   }
 };
 
-// A thread goes through segments of CONV_SEG steps, and the WT - 1 behind each, whose outputs its inputs reach.
+// A thread goes through segments of a.seg steps, and the WT - 1 behind each, whose outputs its inputs reach.
 template <typename E, int VEC, int WT>
 __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, int lanes, int cols) {
   const int T = a.c.T, W = a.c.W, H = a.c.H;
@@ -260,7 +259,7 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, int lane
   ConvBack<E, VEC, WT> v(a);
   v.ch = at.ch;
   const Taps<WT, VEC> taps(a.weight, a.bias, W, at.ch);
-  const int segs = (T + CONV_SEG - 1) / CONV_SEG;
+  const int segs = (T + a.seg - 1) / a.seg;
   const long long all = (long long)segs * a.c.B;
   // (the threads of a wave go through as many segments: they look at resets together)
   for (long long first = (long long)group * at.rows; first < all; first += (long long)a.groups * at.rows) {
@@ -268,8 +267,8 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, int lane
     const bool real = at.has && item < all;
     const int b = item < all ? (int)(item / segs) : 0;
     v.b = b;
-    v.t0 = item < all ? (int)(item - (long long)b * segs) * CONV_SEG : 0;
-    v.t1 = min(v.t0 + CONV_SEG, T);
+    v.t0 = item < all ? (int)(item - (long long)b * segs) * a.seg : 0;
+    v.t1 = min(v.t0 + a.seg, T);
     const E* x = (const E*)a.x.data + b * a.x.stride_b + at.ch;
     const E* dy = (const E*)a.dy.data + b * a.dy.stride_b + at.ch;
     const unsigned before = at.resets(a, b, v.t0 - (WT - 1), WT - 1);
@@ -279,7 +278,7 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, int lane
     for (int k = 0; k < WT; ++k)
 #pragma unroll
       for (int c = 0; c < VEC; ++c) v.g[k][c] = 0.f;
-    for (int off = 0; off < CONV_SEG + WT - 1; off += CONV_BLOCK) {
+    for (int off = 0; off < a.seg + WT - 1; off += CONV_BLOCK) {
       const int base = v.t0 + off;
       const unsigned resets = at.resets(a, b, base, CONV_BLOCK);
       if (!real || base >= v.t1 + WT - 1) continue;
@@ -389,8 +388,15 @@ struct ConvShape {
 static long long conv_runs(const conv_cfg& c, const ConvShape& s) {
   return ((c.T + CONV_RUN - 1LL) / CONV_RUN * c.B + s.rows - 1) / s.rows;
 }
+// Steps of a segment: as many as leave the card full, since each is followed by W - 1 that are looked at again.
+static int conv_seg(const conv_cfg& c, const ConvShape& s) {
+  int seg = 128;
+  while (seg > 16 && (c.T + seg - 1LL) / seg * c.B * s.cols < 2048LL * s.rows / 4) seg /= 2;
+  return seg;
+}
 static int conv_groups(const conv_cfg& c, const ConvShape& s) {
-  const long long all = (((c.T + CONV_SEG - 1LL) / CONV_SEG) * c.B + s.rows - 1) / s.rows, most = (2047 + s.cols) / s.cols;
+  const int seg = conv_seg(c, s);
+  const long long all = ((c.T + seg - 1LL) / seg * c.B + s.rows - 1) / s.rows, most = (2047 + s.cols) / s.cols;
   return (int)(all < most ? all : most);
 }
 size_t conv_workspace(const conv_cfg& c) {
@@ -402,10 +408,6 @@ bool conv_launchable(const conv_cfg& c) {
   return launchable(conv_runs(c, s) * s.cols, 256) && launchable((long long)conv_groups(c, s) * s.cols, 256) &&
          launchable(sum_groups((long long)c.H * (c.W + 1)), SUM_THREADS);
 }
-template <typename E>
-static bool conv_words(const glr_seq& q, int H, int vec) {
-  return H % vec == 0 && q.stride_t % vec == 0 && q.stride_b % vec == 0 && (uintptr_t)q.data % (vec * sizeof(E)) == 0;
-}
 template <typename E, int VEC, int WT, bool BACKWARD>
 static hipError_t conv_kernel(ConvArgs a, hipStream_t s) {
   const ConvShape c(a.c.H, VEC);
@@ -416,6 +418,7 @@ static hipError_t conv_kernel(ConvArgs a, hipStream_t s) {
     return hipGetLastError();
   } else {
     a.groups = conv_groups(a.c, c);
+    a.seg = conv_seg(a.c, c);
     hipLaunchKernelGGL((conv_backward_kernel<E, VEC, WT>), dim3((unsigned)((long long)a.groups * c.cols)), t, 0, s, a, c.lanes,
                        c.cols);
     const hipError_t e = hipGetLastError();
@@ -435,12 +438,12 @@ static hipError_t conv_start(const ConvArgs& a, hipStream_t s) {
 }
 template <typename E>
 static hipError_t conv_forward_start(const ConvArgs& a, hipStream_t s) {
-  const bool words = conv_words<E>(a.x, a.c.H, 4) && conv_words<E>(a.y, a.c.H, 4);
-  return words ? conv_start<E, 4, false>(a, s) : conv_start<E, 1, false>(a, s);
+  const bool words = pairs<E>(a.x, a.c.H) && pairs<E>(a.y, a.c.H);
+  return words ? conv_start<E, 2, false>(a, s) : conv_start<E, 1, false>(a, s);
 }
 template <typename E>
 static hipError_t conv_backward_start(const ConvArgs& a, hipStream_t s) {
-  const bool words = conv_words<E>(a.x, a.c.H, 2) && conv_words<E>(a.dy, a.c.H, 2) && conv_words<E>(a.dx, a.c.H, 2);
+  const bool words = pairs<E>(a.x, a.c.H) && pairs<E>(a.dy, a.c.H) && pairs<E>(a.dx, a.c.H);
   return words ? conv_start<E, 2, true>(a, s) : conv_start<E, 1, true>(a, s);
 }
 hipError_t launch_conv_forward(const ConvArgs& a, hipStream_t s) {

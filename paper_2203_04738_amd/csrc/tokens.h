@@ -31,7 +31,7 @@ struct ConvArgs {
   const uint8_t* reset;
   float *last, *dweight, *dbias, *dpast;
   float* part;              // [groups][H][W + 1]
-  int groups;
+  int groups, seg;          // backward: of workgroups along the sequences; steps of a thread's segment
   bool past_caches;
 };
 size_t conv_workspace(const conv_cfg& c);
