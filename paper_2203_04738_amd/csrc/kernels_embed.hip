@@ -3,9 +3,9 @@
 // The gradient sorts: a workgroup owns a range of the vocabulary and looks through all tokens of the call twice.  The
 // first time it counts those below its range, which is where its own will stand, and, per wave, those of each of its
 // own tokens; the second time every wave puts the places of its part behind those of the waves before it.  Places are
-// therefore in order of token and place, whatever runs first.  The same workgroup clears the rows that no token names.
-// Then a wave adds up a block of sorted places, however they fall into runs of one token, so that a token that is half
-// of all is no longer than many; sums of runs that cross blocks meet in a third launch.
+// therefore in order of token and place, whatever runs first.  Then a wave adds up a block of sorted places, however they
+// fall into runs of one token, so that a token that is half of all takes no longer than many, while other workgroups of the
+// launch clear the rows that no token names; sums of runs that cross blocks meet in a third launch.
 #include "elem.h"
 #include "tokens.h"
 
@@ -60,12 +60,11 @@ __global__ __launch_bounds__(256) void embed_lookup_kernel(EmbedArgs a) {
   v.store((E*)a.out + row * a.c.ld_out + col, tok < 0 ? 1.f : a.c.scale);
 }
 
-// ---- gradient: places of the tokens of a range, in order; rows without a token
+// ---- gradient: places of the tokens of a range, in order, and which of them occur
 constexpr int PLAN_WAVES = 16, PLAN_THREADS = 64 * PLAN_WAVES;
-template <typename E, bool WIDE, int RANGE>
+template <int RANGE>
 __global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a) {
   __shared__ int count[PLAN_WAVES][RANGE];
-  __shared__ int start[RANGE];
   __shared__ int part[PLAN_WAVES], below;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lo = blockIdx.x * RANGE, hi = min(lo + RANGE, a.c.V);
@@ -74,13 +73,17 @@ __global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a) {
   __syncthreads();
   const int per = ((a.c.N + PLAN_THREADS - 1) / PLAN_THREADS) * 64;      // places of a wave
   const int begin = (int)min((long long)a.c.N, (long long)wave * per), end = (int)min((long long)a.c.N, (long long)begin + per);
+  // (eight tokens a lane at a time: what the loads wait for is most of the time)
+  auto load = [&](int i0, long long (&k)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) k[j] = i0 + 64 * j + lane < end ? a.tokens[i0 + 64 * j + lane] : -1;
+  };
   int less = 0;
-  for (int i0 = begin; i0 < end; i0 += 256) {
-    long long k[4];
+  for (int i0 = begin; i0 < end; i0 += 512) {
+    long long k[8];
+    load(i0, k);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) k[j] = i0 + 64 * j + lane < end ? a.tokens[i0 + 64 * j + lane] : -1;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 8; ++j) {
       less += k[j] >= 0 && k[j] < lo;
       if (k[j] >= lo && k[j] < hi) atomicAdd(&count[wave][(int)k[j] - lo], 1);
     }
@@ -112,7 +115,6 @@ __global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a) {
   for (int j = 0; j < PER; ++j) {
     const int r = tid * PER + j;
     if (r >= RANGE) break;
-    start[r] = own[j];                               // (how many, from here on)
     int pos = at;
     for (int w = 0; w < PLAN_WAVES; ++w) {
       const int n = count[w][r];
@@ -122,43 +124,74 @@ __global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a) {
     at = pos;
   }
   if (blockIdx.x == gridDim.x - 1 && tid == PLAN_THREADS - 1) *a.total = at;
+  // (PER words for each 64 PER tokens, token i of them in word i % PER)
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const unsigned long long bits = __ballot(own[j] > 0);
+    if (lane == 0 && wave * 64 * PER < RANGE) a.occurs[(blockIdx.x * RANGE + wave * 64 * PER) / 64 + j] = bits;
+  }
   __syncthreads();
-  for (int i0 = begin; i0 < end; i0 += 64) {
-    const long long k = i0 + lane < end ? a.tokens[i0 + lane] : -1;
-    const bool mine = k >= lo && k < hi;
-    const int r = (int)k - lo;
-    unsigned long long left = __ballot(mine);
-    while (left) {                                   // (each pass takes one token's lanes)
-      const int key = __builtin_amdgcn_readlane(r, __builtin_ctzll(left));
-      const bool same = mine && r == key;
-      const unsigned long long who = __ballot(same);
-      const int pos = count[wave][key];
-      if (same) {
-        const int to = pos + __popcll(who & ((1ull << lane) - 1));
-        a.place[to] = i0 + lane;
-        a.token[to] = (int)k;
+  for (int i0 = begin; i0 < end; i0 += 512) {
+    long long k[8];
+    load(i0, k);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const bool mine = k[j] >= lo && k[j] < hi;
+      const unsigned long long some = __ballot(mine);
+      if (!some) continue;
+      // the lanes with the same token, bit by bit
+      const int r = mine ? (int)k[j] - lo : 0;
+      unsigned who[2] = {(unsigned)some, (unsigned)(some >> 32)};
+#pragma unroll
+      for (int bit = 0; 1 << bit < RANGE; ++bit) {
+        const unsigned long long set = __ballot(r >> bit & 1);
+        const unsigned without = (r >> bit & 1) - 1;   // all bits where the lane's is 0
+        who[0] &= (unsigned)set ^ without;
+        who[1] &= (unsigned)(set >> 32) ^ without;
       }
-      if (lane == 0) count[wave][key] = pos + __popcll(who);
-      left &= ~who;
+      if (mine) {
+        const int before = __builtin_amdgcn_mbcnt_hi(who[1], __builtin_amdgcn_mbcnt_lo(who[0], 0));
+        const int pos = count[wave][r], to = pos + before;
+        a.place[to] = i0 + 64 * j + lane;
+        a.token[to] = (int)k[j];
+        if (before == 0) count[wave][r] = pos + __popc(who[0]) + __popc(who[1]);
+      }
+      // (what one lane has written, all lanes of the wave read in the next round: LDS serves a wave in order, and nothing
+      // has to wait for the places to be stored)
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
   }
+}
+
+// Clears the rows of 64 tokens that do not occur, a wave a row.
+template <typename E, bool WIDE, int PER>
+__device__ inline void clear_rows(const EmbedArgs& a, int group) {
   using P = Piece<E, WIDE>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int pieces = (a.c.D + P::n - 1) / P::n;
   P zero;
 #pragma unroll
   for (int k = 0; k < P::n; ++k) zero.v[k] = 0.f;
-  const long long all = (long long)(hi - lo) * pieces;
-  for (long long i = tid; i < all; i += PLAN_THREADS) {
-    const int r = (int)(i / pieces);
-    if (start[r] == 0) zero.store((E*)a.out + (lo + r) * a.c.ld_table + (i - (long long)r * pieces) * P::n, 1.f);
+  for (int r = wave; r < 64; r += 4) {
+    const int token = 64 * group + r, in = token % (64 * PER);
+    if (token >= a.c.V) break;
+    if (a.occurs[token / (64 * PER) * PER + in % PER] >> (in / PER) & 1) continue;
+    E* out = (E*)a.out + token * a.c.ld_table;
+    for (int i = lane; i < pieces; i += 64) zero.store(out + (long long)i * P::n, 1.f);
   }
 }
 
 // ---- gradient: sums of a block of sorted places, in one wave per 64 pieces of the width
-template <typename E, bool WIDE>
-__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a) {
+template <typename E, bool WIDE, int PER>
+__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, unsigned sum_groups) {
   using P = Piece<E, WIDE>;
   constexpr int AHEAD = 8;
+  if (blockIdx.x >= sum_groups) {
+    clear_rows<E, WIDE, PER>(a, (int)(blockIdx.x - sum_groups));
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int pieces = (a.c.D + P::n - 1) / P::n, across = (pieces + 63) / 64;
   const long long item = (long long)blockIdx.x * 4 + wave;
@@ -174,6 +207,11 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a) {
   const bool ends = lane < n && (i + 1 >= M || a.token[i + 1] != tok);
   const unsigned long long breaks = __ballot(ends);
   const bool before = first > 0 && a.token[first - 1] == __builtin_amdgcn_readfirstlane(tok);
+  // for the join: the token of a run that begins here and goes on
+  const int tail = __builtin_amdgcn_readlane(tok, n - 1);
+  const bool goes_on = !(breaks >> (n - 1) & 1);
+  if (piece == 0)
+    a.crosses[block] = goes_on && !(before && tail == __builtin_amdgcn_readfirstlane(tok)) ? tail : -1;
   P sum;
 #pragma unroll
   for (int k = 0; k < P::n; ++k) sum.v[k] = 0.f;
@@ -205,28 +243,26 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a) {
       }
     }
   }
-  if (!(breaks >> (n - 1) & 1) && has) partial(open ? 0 : 1);
+  if (goes_on && has) partial(open ? 0 : 1);
 }
 
 // ---- gradient: runs that cross blocks, at the block where they begin; the blocks behind it in four parts
+constexpr int JOIN_WAVES = 4;
 template <typename E, bool WIDE>
-__global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a) {
+__global__ __launch_bounds__(64 * JOIN_WAVES) void embed_join_kernel(EmbedArgs a) {
   using P = Piece<E, WIDE>;
-  __shared__ float part[4][64][P::n];
+  __shared__ float part[JOIN_WAVES][64][P::n];
   __shared__ int found;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int pieces = (a.c.D + P::n - 1) / P::n, across = (pieces + 63) / 64;
   const int block = blockIdx.x / across, piece = (blockIdx.x - block * across) * 64 + lane;
   const int M = *a.total;
-  const long long next = (long long)(block + 1) * EMBED_RUN;
-  if (next >= M) return;
-  const int first = block * EMBED_RUN, tok = a.token[next - 1];
-  if (a.token[next] != tok) return;
-  if (a.token[first] == tok && first > 0 && a.token[first - 1] == tok) return;
+  const int tok = a.crosses[block];                  // (anything, where no place of the block is used)
+  if ((block + 1LL) * EMBED_RUN >= M || tok < 0) return;
   // blocks behind this one that begin with the token
   const int blocks = (int)((M + EMBED_RUN - 1LL) / EMBED_RUN);
   int end = blocks;
-  for (int b0 = block + 1; b0 < blocks; b0 += 256) {
+  for (int b0 = block + 1; b0 < blocks; b0 += 64 * JOIN_WAVES) {
     if (threadIdx.x == 0) found = blocks;
     __syncthreads();
     const int b = b0 + threadIdx.x;
@@ -236,23 +272,29 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a) {
     __syncthreads();
     if (end < blocks) break;
   }
-  const int n = end - (block + 1), per = (n + 3) / 4;
+  const int n = end - (block + 1), per = (n + JOIN_WAVES - 1) / JOIN_WAVES;
   const int from = block + 1 + wave * per, to = min(from + per, end);
   const int col = min(piece, pieces - 1) * P::n;
   float sum[P::n];
 #pragma unroll
   for (int k = 0; k < P::n; ++k) sum[k] = wave == 0 ? a.part[(2LL * block + 1) * a.c.D + col + k] : 0.f;
-  for (int b = from; b < to; ++b)
+#pragma unroll 8
+  for (int b = from; b < to; ++b) {
+    const float* p = a.part + 2LL * b * a.c.D + col;
 #pragma unroll
-    for (int k = 0; k < P::n; ++k) sum[k] += a.part[2LL * b * a.c.D + col + k];
+    for (int k = 0; k < P::n; ++k) sum[k] += p[k];
+  }
 #pragma unroll
   for (int k = 0; k < P::n; ++k) part[wave][lane][k] = sum[k];
   __syncthreads();
   if (wave || piece >= pieces) return;
   P v;
 #pragma unroll
-  for (int k = 0; k < P::n; ++k)
-    v.v[k] = (part[0][lane][k] + part[1][lane][k]) + (part[2][lane][k] + part[3][lane][k]);
+  for (int k = 0; k < P::n; ++k) {
+    v.v[k] = part[0][lane][k];
+#pragma unroll
+    for (int w = 1; w < JOIN_WAVES; ++w) v.v[k] += part[w][lane][k];
+  }
   v.store((E*)a.out + (long long)tok * a.c.ld_table + col, a.c.scale);
 }
 
@@ -261,9 +303,11 @@ static bool wide_rows(const void* p, long long ld, int D, int size) {
   return (uintptr_t)p % 16 == 0 && ld * size % 16 == 0 && (long long)D * size % 16 == 0;
 }
 static size_t embed_piece(size_t n) { return (n + 255) / 256 * 256; }
+// The total, the bits of the tokens that occur (of whole ranges), places, tokens, runs that cross blocks, sums.
+static size_t embed_bits(const embed_cfg& c) { return embed_piece(8 * ((size_t)c.V / 64 + 64)); }
 size_t embed_workspace(const embed_cfg& c) {
   const size_t N = (size_t)c.N, blocks = (N + EMBED_RUN - 1) / EMBED_RUN;
-  return 256 + 2 * embed_piece(4 * N) + 8 * blocks * c.D;
+  return 256 + embed_bits(c) + 2 * embed_piece(4 * N) + embed_piece(4 * blocks) + 8 * blocks * c.D;
 }
 template <typename E, bool WIDE>
 static hipError_t embed_lookup_start(const EmbedArgs& a, hipStream_t s) {
@@ -272,23 +316,27 @@ static hipError_t embed_lookup_start(const EmbedArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((embed_lookup_kernel<E, WIDE>), dim3((unsigned)n), dim3(256), 0, s, a);
   return hipGetLastError();
 }
-template <typename E, bool WIDE>
-static hipError_t embed_backward_start(const EmbedArgs& a, hipStream_t s) {
+// RANGE tokens of the vocabulary for a workgroup of the sort.
+template <typename E, bool WIDE, int RANGE>
+static hipError_t embed_backward_range(const EmbedArgs& a, hipStream_t s) {
+  constexpr int PER = (RANGE + PLAN_THREADS - 1) / PLAN_THREADS;
   const long long pieces = (a.c.D + Piece<E, WIDE>::n - 1) / Piece<E, WIDE>::n, across = (pieces + 63) / 64;
-  const long long items = ((a.c.N + EMBED_RUN - 1LL) / EMBED_RUN) * across;
-  if (!launchable(items, 256)) return TOO_LARGE;
-  // ranges that leave a few hundred workgroups
-  const int V = a.c.V;
-  const dim3 t(PLAN_THREADS);
-  if (V <= 256 * 128) hipLaunchKernelGGL((embed_plan_kernel<E, WIDE, 128>), dim3((V + 127) / 128), t, 0, s, a);
-  else if (V <= 256 * 512) hipLaunchKernelGGL((embed_plan_kernel<E, WIDE, 512>), dim3((V + 511) / 512), t, 0, s, a);
-  else hipLaunchKernelGGL((embed_plan_kernel<E, WIDE, 2048>), dim3((V + 2047) / 2048), t, 0, s, a);
+  const long long items = ((a.c.N + EMBED_RUN - 1LL) / EMBED_RUN) * across, sums = (items + 3) / 4, clears = (a.c.V + 63) / 64;
+  if (!launchable(items, 64 * JOIN_WAVES) || !launchable(sums + clears, 256)) return TOO_LARGE;
+  hipLaunchKernelGGL((embed_plan_kernel<RANGE>), dim3((a.c.V + RANGE - 1) / RANGE), dim3(PLAN_THREADS), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((embed_sum_kernel<E, WIDE>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((embed_sum_kernel<E, WIDE, PER>), dim3((unsigned)(sums + clears)), dim3(256), 0, s, a, (unsigned)sums);
   if ((e = hipGetLastError()) != hipSuccess || a.c.N <= EMBED_RUN) return e;
-  hipLaunchKernelGGL((embed_join_kernel<E, WIDE>), dim3((unsigned)items), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((embed_join_kernel<E, WIDE>), dim3((unsigned)items), dim3(64 * JOIN_WAVES), 0, s, a);
   return hipGetLastError();
+}
+template <typename E, bool WIDE>
+static hipError_t embed_backward_start(const EmbedArgs& a, hipStream_t s) {
+  // ranges that leave some hundred workgroups, each of which looks through all tokens
+  if (a.c.V <= 256 * 128) return embed_backward_range<E, WIDE, 128>(a, s);
+  if (a.c.V <= 256 * 512) return embed_backward_range<E, WIDE, 512>(a, s);
+  return embed_backward_range<E, WIDE, 2048>(a, s);
 }
 template <typename E>
 static hipError_t embed_start(const EmbedArgs& a, bool backward, hipStream_t s) {
@@ -305,9 +353,16 @@ static hipError_t embed_typed(const EmbedArgs& a, bool backward, hipStream_t s) 
 hipError_t launch_embed_lookup(const EmbedArgs& a, hipStream_t s) { return embed_typed(a, false, s); }
 hipError_t launch_embed_backward(EmbedArgs a, char* ws, hipStream_t s) {
   a.total = (int*)ws;
-  a.place = (int*)(ws + 256);
-  a.token = (int*)(ws + 256 + embed_piece(4 * (size_t)a.c.N));
-  a.part = (float*)(ws + 256 + 2 * embed_piece(4 * (size_t)a.c.N));
+  ws += 256;
+  a.occurs = (unsigned long long*)ws;
+  ws += embed_bits(a.c);
+  a.place = (int*)ws;
+  ws += embed_piece(4 * (size_t)a.c.N);
+  a.token = (int*)ws;
+  ws += embed_piece(4 * (size_t)a.c.N);
+  a.crosses = (int*)ws;
+  ws += embed_piece(4 * (((size_t)a.c.N + EMBED_RUN - 1) / EMBED_RUN));
+  a.part = (float*)ws;
   return embed_typed(a, true, s);
 }
 

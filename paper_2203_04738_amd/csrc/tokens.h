@@ -6,17 +6,17 @@
 namespace mg {
 
 // ---- embedding (kernels_embed.hip)
-// The sort: a workgroup owns EMBED_RANGE tokens of the vocabulary, looks through all tokens of the call and leaves the
-// places of its own, in order, behind those of smaller ones.  The sums: a wave adds EMBED_RUN sorted places.
-constexpr int EMBED_RANGE = 128, EMBED_RUN = 32;
+constexpr int EMBED_RUN = 32;                        // sorted places that a wave adds up
 struct EmbedArgs {
   embed_cfg c;
   const int64_t* tokens;
   const void* in;           // table, or dout
   void* out;                // out, or dtable
   int* total;               // tokens that name a row
+  unsigned long long* occurs;   // bits of the tokens that occur
   int* place;               // [N]: places of the tokens in order of token and place
   int* token;               // [N]: their tokens
+  int* crosses;             // [ceil(N / EMBED_RUN)]: the token of a run that begins in the block and goes on, or -1
   float* part;              // [ceil(N / EMBED_RUN)][2][D]: sums of runs that go on beyond their block
 };
 size_t embed_workspace(const embed_cfg& c);
