@@ -8,6 +8,7 @@ enqueued on its current stream.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 from . import ops as _o
 from .binding import MGRIT_F32, _check
@@ -106,46 +107,62 @@ def _size(name, cfg) -> int:
 
 
 class _Group(tuple):
-    """Arguments that one C structure holds: (structure, arguments)."""
+    """Arguments that one C structure holds, sequences and pointers: a tuple of them."""
+
+
+_SEQS = {n: struct.Struct(f"{n}q") for n in range(1, 24)}
+_NO_SEQ = (0, 0, 0)
 
 
 def _explain(args, device):
-    flat = [b for a in args for b in (a[1] if type(a) is _Group else (a,))]
+    flat = [b for a in args for b in (a if type(a) is _Group else (a,))]
     _o._explain(flat)
     for a in flat:
         if type(a) is tuple and a[0] is not None and a[0].get_device() != device:
             raise ValueError(f"{a[1]}: tensor on cuda:{a[0].get_device()}, the current device is cuda:{device}")
 
 
+def _fits(a, device):
+    t, _, dtype, shape, kind = a
+    return (isinstance(t, _o._torch.Tensor) and (shape is None or t.shape == shape) and (dtype is None or t.dtype is dtype)
+            and t.get_device() == device and (t.is_contiguous() if kind == 0 else _o._unit_rows(t)))
+
+
 def _call(name, cfg, *args) -> None:
     """Checks and marshals the arguments, then calls entry point `name` on the current stream (ops._call, with
     structures of arguments, and all tensors on the current device)."""
     L, torch = _lib(), _o._torch
-    tensor, device = torch.Tensor, torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
-
-    def value(a):
-        t, _, dtype, shape, kind = a
-        if t is None:
-            return None
-        if not (isinstance(t, tensor) and (shape is None or t.shape == shape) and (dtype is None or t.dtype is dtype)
-                and t.get_device() == device and (t.is_contiguous() if kind == 0 else _o._unit_rows(t))):
-            _explain(args, device)
-            raise AssertionError(a[1])                # (not reached: _explain says what is wrong)
-        if kind < 2:
-            return t.data_ptr()
-        strides = t.stride()
-        return GlrSeq(t.data_ptr(), strides[0] if kind == _SEQ else 0, strides[-2])
-
+    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
     out = []
     for a in args:
         kind = type(a)
         if kind is tuple:
-            v = value(a)
-            out.append(ctypes.byref(v) if type(v) is GlrSeq else v)
+            t = a[0]
+            if t is None:
+                out.append(None)
+            elif not _fits(a, device):
+                _explain(args, device)
+                raise AssertionError(a[1])            # (not reached: _explain says what is wrong)
+            elif a[4] < 2:
+                out.append(t.data_ptr())
+            else:
+                strides = t.stride()
+                out.append(_SEQS[3].pack(t.data_ptr(), strides[0] if a[4] == _SEQ else 0, strides[-2]))
         elif kind is _Group:
-            none = GlrSeq()
-            vs = [value(b) for b in a[1]]
-            out.append(ctypes.byref(a[0](*(none if v is None and b[4] >= 2 else v for v, b in zip(vs, a[1])))))
+            words = []
+            for b in a:
+                t = b[0]
+                if t is None:
+                    words += _NO_SEQ if b[4] >= 2 else (0,)
+                elif not _fits(b, device):
+                    _explain(args, device)
+                    raise AssertionError(b[1])
+                elif b[4] < 2:
+                    words.append(t.data_ptr())
+                else:
+                    strides = t.stride()
+                    words += (t.data_ptr(), strides[0] if b[4] == _SEQ else 0, strides[-2])
+            out.append(_SEQS[len(words)].pack(*words))
         elif isinstance(a, ctypes.Structure):
             out.append(ctypes.byref(a))
         else:
@@ -230,8 +247,8 @@ def ssm_saved_bytes(cfg: SsmCfg) -> int:
 
 def _ssm_inputs(cfg, one, x, dt, b, c, z, a, skip, bias):
     H, S = cfg.H, cfg.S
-    return _Group((SsmInputs, (one(cfg, x, "x"), one(cfg, dt, "dt"), one(cfg, b, "b", S), one(cfg, c, "c", S),
-                               one(cfg, z, "z"), _f32(a, "a", H, S), _f32(skip, "skip", H), _f32(bias, "bias", H))))
+    return _Group((one(cfg, x, "x"), one(cfg, dt, "dt"), one(cfg, b, "b", S), one(cfg, c, "c", S), one(cfg, z, "z"),
+                   _f32(a, "a", H, S), _f32(skip, "skip", H), _f32(bias, "bias", H)))            # (SsmInputs)
 
 
 def ssm_forward(cfg, x, dt, b, c, z, a, skip, bias, h0, reset, y, h_last, saved, workspace) -> None:
@@ -245,9 +262,9 @@ def ssm_forward(cfg, x, dt, b, c, z, a, skip, bias, h0, reset, y, h_last, saved,
 def ssm_backward(cfg, x, dt, b, c, z, a, skip, bias, reset, saved, dy, dh_last, dx, ddt, db, dc, dz, da, dskip, dbias,
                  dh0, workspace) -> None:
     T, B, H, S = cfg.T, cfg.B, cfg.H, cfg.S
-    grads = _Group((SsmGrads, (_seq(cfg, dx, "dx"), _seq(cfg, ddt, "ddt"), _seq(cfg, db, "db", S), _seq(cfg, dc, "dc", S),
-                               _seq(cfg, dz, "dz"), _f32(da, "da", H, S), _f32(dskip, "dskip", H),
-                               _f32(dbias, "dbias", H), _f32(dh0, "dh0", B, H, S))))
+    grads = _Group((_seq(cfg, dx, "dx"), _seq(cfg, ddt, "ddt"), _seq(cfg, db, "db", S), _seq(cfg, dc, "dc", S),
+                    _seq(cfg, dz, "dz"), _f32(da, "da", H, S), _f32(dskip, "dskip", H), _f32(dbias, "dbias", H),
+                    _f32(dh0, "dh0", B, H, S)))                                                    # (SsmGrads)
     _call("ssm_backward", cfg, _ssm_inputs(cfg, _seq, x, dt, b, c, z, a, skip, bias), _reset(reset, T, B),
           *_bytes_of(saved, "saved"), _seq(cfg, dy, "dy"), _f32(dh_last, "dh_last", B, H, S), grads,
           *_bytes_of(workspace, "workspace"))
