@@ -60,6 +60,8 @@ struct SsmShape {
   int cols;                 // workgroups across the channels
   int chunks, len;          // chunks of a sequence, their steps (a multiple of 16)
 };
+// Whether every workgroup goes through the chunks before its own itself.
+__host__ __device__ inline bool few_chunks(const SsmShape& s) { return s.chunks <= 64; }
 SsmShape ssm_shape(const ssm_cfg& c, bool backward);
 struct SsmArgs {
   ssm_cfg c;

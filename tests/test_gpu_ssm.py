@@ -129,7 +129,7 @@ def test_options(gated, full, resets, batch_first):
 
 
 @pytest.mark.parametrize("T,B,H,S,resets", [(700, 1, 30, 16, 0.0), (700, 2, 100, 16, 0.01), (333, 3, 50, 64, 0.01),
-                                            (1200, 1, 8, 2, 0.003)])
+                                            (1200, 1, 8, 2, 0.003), (2600, 1, 20, 16, 0.002)])
 def test_many_chunks(T, B, H, S, resets):
     run(*problem(T, T, B, H, S, "f32", True, resets), T, B, H, S, "f32", True)
 
