@@ -1,0 +1,135 @@
+"""The path that uses the operators over tokens together: a student that imitates, learns from reward, and is served."""
+import pytest
+import torch
+
+import paper_2203_04738_amd as mg
+from paper_2203_04738_amd.token_student import NAMES, TokenServed, TokenStudent, example, init
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+T, B, V, D, H, S, W = 21, 3, 30, 12, 20, 5, 4
+
+
+def small(**kw):
+    return TokenStudent(T, B, *init(V, D, H, S, W, 2, seed=1), **kw)
+
+
+def reference(student, tokens, reset):
+    """(parameters that require gradients, logits) in float64 torch on the CPU, step by step."""
+    leaf = lambda p: p.detach().double().cpu().requires_grad_(True)  # noqa: E731
+    table, head, layers = leaf(student.table), leaf(student.head), [{k: leaf(p[k]) for k in NAMES} for p in student.layers]
+    tok = tokens.cpu()
+    u = torch.where((tok >= 0)[..., None], D ** 0.5 * table[tok.clamp(min=0)], 0.0)
+    keep = (reset.cpu() == 0).double()[..., None]
+    silu = torch.nn.functional.silu
+    for p in layers:
+        xz = u @ p["W_in"].t()
+        window, h, ys = [torch.zeros(B, H, dtype=torch.float64)] * (W - 1), torch.zeros(B, H, S, dtype=torch.float64), []
+        a = -p["a_log"].exp()
+        for t in range(T):
+            window = [w * keep[t] for w in window] + [xz[t, :, :H]]
+            x = silu(p["conv_b"] + sum(p["conv_w"][:, k] * window[k] for k in range(W)))
+            window = window[1:]
+            dbc = x @ p["W_dbc"].t()
+            d = torch.nn.functional.softplus(dbc[:, :H] + p["dt_bias"])
+            h = torch.exp(d[..., None] * a) * (h * keep[t][..., None]) + (d * x)[..., None] * dbc[:, None, H:H + S]
+            ys.append(((h * dbc[:, None, H + S:]).sum(-1) + p["skip"] * x) * silu(xz[t, :, H:]))
+        u = u + torch.stack(ys) @ p["W_out"].t()
+    return [table, head] + [p[k] for p in layers for k in NAMES], u.reshape(T * B, D) @ head.t()
+
+
+def batch(seed=0):
+    g = torch.Generator().manual_seed(seed)
+    tokens = torch.randint(0, V, (T, B), generator=g)
+    tokens[0, 0] = -1
+    reset = (torch.rand(T, B, generator=g) < 0.1).to(torch.uint8)
+    return g, tokens.to(DEV), reset.to(DEV)
+
+
+def check(student, params):
+    mine = [student.table, student.head] + [p[k] for p in student.layers for k in NAMES]
+    for m, ref in zip(mine, params):
+        # (gradients are sums of some hundred products of values known to about 1e-6 each through two layers, in float)
+        err = (m.grad.double().cpu() - ref.grad).abs().max() / ref.grad.abs().max()
+        assert err <= 3e-5, (tuple(m.shape), float(err))
+
+
+def test_a_step_of_learning_has_the_gradients_of_torch():
+    g, tokens, reset = batch()
+    student = small(rule=mg.PolicyCfg(0.2, 0.3, 0.1), temperature=1.3)
+    params, logits = reference(student, tokens, reset)
+    actions = torch.randint(-1, V, (T * B,), generator=g)
+    lp = torch.log_softmax(logits / 1.3, 1).gather(1, actions.clamp(min=0)[:, None])[:, 0]
+    moved = 0.5 * torch.randn(T * B, generator=g).double()
+    old, ref = (lp.detach() - moved).float(), (lp.detach() + 0.3 * torch.randn(T * B, generator=g).double()).float()
+    A = torch.randn(T * B, generator=g)
+    ratio = torch.exp(lp - old.double())
+    assert ((ratio - 0.8).abs().min() > 1e-4) and ((ratio - 1.3).abs().min() > 1e-4)        # (clipped alike in 32 bits)
+    d = ref.double() - lp
+    each = -torch.minimum(ratio * A, ratio.clamp(0.8, 1.3) * A) + 0.1 * (torch.exp(d) - d - 1)
+    loss = each[actions >= 0].mean()
+    loss.backward()
+    got, kl, _ = student.learn(tokens, actions.to(DEV), old.to(DEV), A.to(DEV), ref.to(DEV), reset)
+    assert abs(got - float(loss.detach())) <= 1e-5 * max(1.0, abs(float(loss.detach())))
+    assert abs(kl - float((torch.exp(d) - d - 1)[actions >= 0].mean().detach())) <= 1e-5
+    check(student, params)
+
+
+def test_a_step_of_imitation_has_the_gradients_of_torch():
+    g, tokens, reset = batch(3)
+    student = small(K=3)
+    params, logits = reference(student, tokens, reset)
+    ids = torch.stack([torch.randperm(V, generator=g)[:3] for _ in range(T * B)])
+    ids[::4] = -1
+    values = torch.randn(T * B, 3, generator=g)
+    q = torch.softmax(values.double(), 1)
+    lp = torch.log_softmax(logits, 1).gather(1, ids.clamp(min=0))
+    loss = (q * (torch.log(q) - lp)).sum(1)[ids[:, 0] >= 0].mean()
+    loss.backward()
+    got = student.imitate(tokens, ids.to(DEV), values.to(DEV), reset)
+    assert abs(got - float(loss.detach())) <= 1e-5 * max(1.0, abs(float(loss.detach())))
+    check(student, params)
+
+
+def test_actions_are_as_probable_as_they_say():
+    g, tokens, _ = batch(5)
+    student = small(temperature=0.8)
+    actions, logp = student.act(tokens, torch.rand(T * B, generator=g).to(DEV))
+    p = torch.log_softmax(student.logits(tokens).double() / 0.8, 1)
+    assert ((actions >= 0) & (actions < V)).all()
+    assert (logp.double() - p.gather(1, actions[:, None])[:, 0]).abs().max() <= 1e-5
+    # what has just been sampled has a ratio of 1 and no KL to itself
+    before = [q.clone() for q in (student.table, student.head)]
+    loss, kl, beyond = student.learn(tokens, actions, logp, torch.zeros(T * B, device=DEV), logp)
+    assert abs(loss) <= 1e-6 and abs(kl) <= 1e-6 and beyond == 0
+    assert all(torch.isfinite(q).all() for q in before)
+
+
+def test_the_example_runs_and_serving_agrees():
+    first, shown, last, by_token, to_own = example(rounds=2, say=lambda *_: None)
+    assert all(0 <= r <= 1 for r in (first, shown, last))
+    # read at once or token by token: the same 8-bit products, states in another order (1e-6), which may move a value across a
+    # rounding to 8 bits (a step of 1/127 of its row's largest, one of many)
+    assert by_token <= 0.1
+    # 8-bit weights and tokens in seven products: each within 1/254 of a row's largest value
+    assert to_own <= 0.35
+
+
+def test_served_sequences_do_not_touch_each_other():
+    _, tokens, _ = batch(7)
+    tokens = tokens.clamp(min=0)
+    served = TokenServed(small(), slots=6)
+    slots = torch.tensor([4, 1, 9], dtype=torch.int32, device=DEV)
+    served.read(tokens, slots)
+    pools = served.past + served.state
+    for p in pools:
+        assert (p[[0, 2, 3, 5]] == 0).all() and (p[[1, 4]] != 0).any()
+    before = [p.clone() for p in pools]
+    logits = served.next(tokens[0, :2].contiguous(), slots[:2])
+    assert torch.isfinite(logits).all()
+    for p, b in zip(pools, before):
+        assert torch.equal(p[[0, 2, 3, 5]], b[[0, 2, 3, 5]]) and not torch.equal(p[[4, 1]], b[[4, 1]])
+    # a sequence that starts anew says what one from nothing says
+    fresh = TokenServed(small(), slots=6)
+    one = torch.ones(2, dtype=torch.uint8, device=DEV)
+    assert torch.equal(served.next(tokens[1, :2].contiguous(), slots[:2], one), fresh.next(tokens[1, :2].contiguous(), slots[:2]))
