@@ -32,7 +32,7 @@ extern "C" {
  * A negative token is padding: its row is zero.  A token >= V makes its row NaN.  Neither has a gradient.
  */
 typedef struct {
-  int32_t N, V, D;            /* tokens 1 .. 2^28, rows of the table 1 .. 2^20, width 1 .. 2^20 */
+  int32_t N, V, D;            /* tokens 1 .. 2^26, rows of the table 1 .. 2^20, width 1 .. 2^20 */
   int32_t dtype;              /* of table, out and their gradients */
   float scale;                /* finite */
   int64_t ld_table, ld_out;   /* row strides (>= D, elements) of table / dtable and out / dout */
@@ -64,12 +64,12 @@ typedef struct {
 /* Sequences are as in mgrit_ops.h ([T,B,H], any strides).  weight[H,W] float, bias[H] float or NULL (zeros).
  *   past[B,W-1,H] float or NULL (zeros): the W - 1 inputs before the first, oldest first; reset[T,B] bytes or NULL;
  *   last[B,W-1,H] float out or NULL: the same behind the last step, zeros for what was forgotten: the past of a call
- *   that goes on with the sequence.  (W = 1: neither is looked at.) */
+ *   that goes on with the sequence (not `past` itself: MGRIT_E_SIZE).  (W = 1: neither is looked at.) */
 MGRIT_API int causal_conv_forward(const conv_cfg* cfg, const glr_seq* x, const float* weight, const float* bias,
                                   const float* past, const uint8_t* reset, const glr_seq* y, float* last, void* stream);
 
 /* Backward, from the same inputs.  dlast[B,W-1,H] float or NULL (zeros).  Out: dx; dweight[H,W], dbias[H] float, each or
- * NULL; dpast[B,W-1,H] float or NULL. */
+ * NULL; dpast[B,W-1,H] float or NULL (not dlast itself: MGRIT_E_SIZE). */
 MGRIT_API int causal_conv_workspace_bytes(const conv_cfg* cfg, size_t* bytes);
 MGRIT_API int causal_conv_backward(const conv_cfg* cfg, const glr_seq* x, const float* weight, const float* bias,
                                    const float* past, const uint8_t* reset, const glr_seq* dy, const float* dlast,
@@ -127,13 +127,14 @@ MGRIT_API int ssm_workspace_bytes(const ssm_cfg* cfg, size_t* bytes);
 MGRIT_API int ssm_saved_bytes(const ssm_cfg* cfg, size_t* bytes);
 
 /* Forward.  h0[B,H,S] float or NULL (zeros); reset[T,B] bytes or NULL; y out; h_last[B,H,S] float out or NULL: h_T, the h0
- * of a call that goes on with the sequence.  saved: out or NULL: the states (float) that ssm_backward starts from,
+ * of a call that goes on with the sequence (not h0 itself: MGRIT_E_SIZE).  saved: out or NULL: the states (float) that ssm_backward starts from,
  * 16-byte aligned. */
 MGRIT_API int ssm_forward(const ssm_cfg* cfg, const ssm_inputs* in, const float* h0, const uint8_t* reset,
                           const glr_seq* y, float* h_last, void* saved, size_t saved_bytes, void* workspace,
                           size_t workspace_bytes, void* stream);
 
-/* Backward, from the same inputs and what the forward call left in `saved`.  dh_last[B,H,S] float or NULL (zeros). */
+/* Backward, from the same inputs and what the forward call left in `saved`.  dh_last[B,H,S] float or NULL (zeros);
+ * not dh0 itself: MGRIT_E_SIZE. */
 MGRIT_API int ssm_backward(const ssm_cfg* cfg, const ssm_inputs* in, const uint8_t* reset, const void* saved,
                            size_t saved_bytes, const glr_seq* dy, const float* dh_last, const ssm_grads* out,
                            void* workspace, size_t workspace_bytes, void* stream);

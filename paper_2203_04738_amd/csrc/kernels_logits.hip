@@ -923,8 +923,8 @@ struct PolicyTerm {
   float loss, logp, ratio, kl;
   float slope;               // dloss / dlogp
 };
-// exp(d) - 1 - d.  Below 1/2 by its series, whose terms from d^11 / 11! on are below 2^-24 of it.
-__device__ inline float exp_beyond_line(float d) {
+// exp(d) - 1 - d, and exp(d) - 1 in `one`.  Below 1/2 by the series, whose terms from d^11 / 11! on are below 2^-24 of it.
+__device__ inline float exp_beyond_line(float d, float& one) {
   if (fabsf(d) < 0.5f) {
     float p = fmaf(d, 1.f / 3628800, 1.f / 362880);
     p = fmaf(d, p, 1.f / 40320);
@@ -933,9 +933,12 @@ __device__ inline float exp_beyond_line(float d) {
     p = fmaf(d, p, 1.f / 120);
     p = fmaf(d, p, 1.f / 24);
     p = fmaf(d, p, 1.f / 6);
-    return d * d * fmaf(d, p, 0.5f);
+    p = d * d * fmaf(d, p, 0.5f);
+    one = d + p;
+    return p;
   }
-  return d == __builtin_inff() ? d : exp_of(d) - 1.f - d;
+  one = exp_of(d) - 1.f;
+  return d == __builtin_inff() ? d : one - d;
 }
 // x: the token's logit.  Differences of log probabilities are small beside them: those are kept in 64 bits.
 __device__ inline PolicyTerm policy_term(const PolicyRows& a, long long row, float x, float m, float s) {
@@ -953,10 +956,11 @@ __device__ inline PolicyTerm policy_term(const PolicyRows& a, long long row, flo
   p.kl = 0.f;
   if (a.ref_logp) {
     const float d = (float)((double)a.ref_logp[row] - lp);
-    p.kl = exp_beyond_line(d);
+    float one;
+    p.kl = exp_beyond_line(d, one);
     if (a.rule.kl != 0.f) {
       p.loss = fmaf(a.rule.kl, p.kl, p.loss);
-      p.slope -= a.rule.kl * (p.kl + d);
+      p.slope -= a.rule.kl * one;
     }
   }
   return p;

@@ -811,8 +811,8 @@ bool ssm_launchable(const ssm_cfg& c) {
     if (!launchable((long long)s.chunks * s.cols * c.B, SSM_THREADS)) return false;
   }
   return launchable(((long long)c.B * c.H * c.S + 255) / 256, 256) &&
-         launchable(((long long)c.T * c.B * 2 * c.S + 255) / 256, 256) &&
-         launchable(((long long)c.H * (c.S + 2) + SUM_COLS - 1) / SUM_COLS, SUM_THREADS);
+         launchable(((long long)c.T * c.B * c.S + 255) / 256, 256) &&
+         launchable(sum_groups((long long)c.H * (c.S + 2)), SUM_THREADS);
 }
 static void ssm_place(SsmArgs& a, char* ws, bool backward) {
   const SsmSpace w(a.c, backward);

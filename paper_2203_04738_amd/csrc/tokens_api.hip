@@ -10,7 +10,7 @@ namespace mg {
 // ---- embedding
 static int embed_check(const embed_cfg* c) {
   if (!c) return MGRIT_E_NULL;
-  if (c->N < 1 || c->N > (1 << 28) || c->V < 1 || c->V > (1 << 20) || c->D < 1 || c->D > (1 << 20)) return MGRIT_E_SIZE;
+  if (c->N < 1 || c->N > (1 << 26) || c->V < 1 || c->V > (1 << 20) || c->D < 1 || c->D > (1 << 20)) return MGRIT_E_SIZE;
   if (c->ld_table < c->D || c->ld_table > (1LL << 40) || c->ld_out < c->D || c->ld_out > (1LL << 40)) return MGRIT_E_SIZE;
   if (!is_dtype(c->dtype)) return MGRIT_E_ENUM;
   return std::isfinite(c->scale) ? MGRIT_OK : MGRIT_E_SIZE;
@@ -147,6 +147,7 @@ int causal_conv_forward(const conv_cfg* cfg, const glr_seq* x, const float* weig
   if ((rc = seq_check(*cfg, x, false)) || (rc = seq_check(*cfg, y, true))) return rc;
   if (!weight) return MGRIT_E_NULL;
   if (off(weight, 4) || off(bias, 4) || off(past, 4) || off(last, 4)) return MGRIT_E_ALIGN;
+  if (cfg->W > 1 && last && last == past) return MGRIT_E_SIZE;
   ConvArgs a{};
   a.c = *cfg;
   a.x = *x;
@@ -180,6 +181,7 @@ int causal_conv_backward(const conv_cfg* cfg, const glr_seq* x, const float* wei
   if (off(weight, 4) || off(bias, 4) || off(past, 4) || off(dlast, 4) || off(dweight, 4) || off(dbias, 4) ||
       off(dpast, 4) || off16(workspace))
     return MGRIT_E_ALIGN;
+  if (cfg->W > 1 && dpast && dpast == dlast) return MGRIT_E_SIZE;
   if (workspace_bytes < conv_workspace(*cfg)) return MGRIT_E_WORKSPACE;
   ConvArgs a{};
   a.c = *cfg;
@@ -242,6 +244,7 @@ int ssm_forward(const ssm_cfg* cfg, const ssm_inputs* in, const float* h0, const
   if (rc) return rc;
   if ((rc = ssm_inputs_check(*cfg, in)) || (rc = seq_check(*cfg, y, true))) return rc;
   if (off(h0, 4) || off(h_last, 4) || off16(saved)) return MGRIT_E_ALIGN;
+  if (h_last && h_last == h0) return MGRIT_E_SIZE;
   if ((rc = ssm_space(*cfg, workspace, workspace_bytes))) return rc;
   if (saved && saved_bytes < ssm_saved(*cfg)) return MGRIT_E_WORKSPACE;
   SsmArgs a = ssm_args(*cfg, *in, reset);
@@ -265,6 +268,7 @@ int ssm_backward(const ssm_cfg* cfg, const ssm_inputs* in, const uint8_t* reset,
   if (out->dz.data && (rc = seq_check(*cfg, &out->dz, true))) return rc;
   if (off16(saved) || off(dh_last, 4) || off(out->da, 4) || off(out->dskip, 4) || off(out->dbias, 4) || off(out->dh0, 4))
     return MGRIT_E_ALIGN;
+  if (out->dh0 && out->dh0 == dh_last) return MGRIT_E_SIZE;
   if ((rc = ssm_space(*cfg, workspace, workspace_bytes))) return rc;
   if (saved_bytes < ssm_saved(*cfg)) return MGRIT_E_WORKSPACE;
   SsmArgs a = ssm_args(*cfg, *in, reset);

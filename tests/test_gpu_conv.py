@@ -74,7 +74,7 @@ def run(d, dev, T, B, H, W, dtype, silu=True, with_past=True, batch_first=False)
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
 @pytest.mark.parametrize("T,B,H,W", [(1, 1, 1, 1), (1, 2, 3, 4), (2, 1, 6, 5), (16, 2, 33, 2), (17, 1, 64, 3), (61, 2, 130, 4),
-                                     (62, 1, 30, 4), (57, 3, 16, 8), (58, 1, 7, 7), (130, 2, 34, 6), (125, 1, 100, 4)])
+                                     (62, 1, 30, 4), (57, 3, 16, 8), (58, 1, 7, 7), (130, 2, 34, 6), (125, 1, 100, 4), (150, 2, 9, 1)])
 def test_shapes(dtype, T, B, H, W):
     run(*problem(T * 7 + H, T, B, H, W, dtype), T, B, H, W, dtype)
 
@@ -171,3 +171,38 @@ def test_some_gradients_only_and_by_differences():
         down[at] -= e
         num = (loss(up) - loss(down)) / (float(up[at]) - float(down[at]))
         assert abs(num - float(dw[at])) <= 5e-3 * max(1.0, float(dw.abs().max()))
+
+
+def test_the_same_bits_in_every_run_and_in_a_graph():
+    T, B, H, W = 300, 3, 70, 4
+    d, dev = problem(19, T, B, H, W, "bf16", resets=0.02)
+    cfg = mg.ConvCfg(T, B, H, W, mg.CONV_SILU, mg.MGRIT_BF16)
+    ws = torch.empty(mg.causal_conv_workspace_bytes(cfg), dtype=torch.uint8, device=DEV)
+    new = lambda *s, dtype=torch.float32: torch.zeros(*s, dtype=dtype, device=DEV)  # noqa: E731
+    bf = torch.bfloat16
+    out = [new(T, B, H, dtype=bf), new(B, W - 1, H), new(T, B, H, dtype=bf), new(H, W), new(H), new(B, W - 1, H)]
+
+    def both():
+        given = (dev["x"], dev["weight"], dev["bias"], dev["past"], dev["reset"])
+        mg.causal_conv_forward(cfg, *given, out[0], out[1])
+        mg.causal_conv_backward(cfg, *given, dev["dy"], dev["dlast"], *out[2:], ws)
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for _ in range(3):
+        dev["x"].mul_(-0.9)
+        for t in out:
+            t.zero_()
+        both()
+        eager = [t.clone() for t in out]
+        for t in out:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(eager, out):
+            assert torch.equal(a, b) and float(a.abs().max()) > 0

@@ -165,6 +165,24 @@ def test_kl_of_small_and_large_differences():
     assert (np.abs(rows[3].double().cpu().numpy() - want) <= tol).all()
 
 
+def test_slopes_of_far_reference_probabilities():
+    # exp(d) - 1 of any d, beside it d itself: 1e9, where it is 1 of 1e9; -infinity (a token that the reference leaves out)
+    diff = torch.tensor([-float("inf"), -1e9, -1e4, -30.0, -0.6, -0.4, -1e-3, 1e-3, 0.4, 0.6, 5.0, 80.0])
+    N = len(diff)
+    lp = -np.log(2.0)
+    dev = {"x": torch.zeros(N, 2, device=DEV), "tok": torch.zeros(N, dtype=torch.int64, device=DEV),
+           "old": torch.full((N,), lp, device=DEV), "ref": (diff + lp).to(DEV), "adv": torch.zeros(N, device=DEV),
+           "weight": torch.ones(N, device=DEV)}
+    rows, grad = call(dev, "f32", 1.0, 1.0)
+    d = dev["ref"].double().cpu().numpy() - lp
+    want = -np.expm1(d) / 2                                    # of the token; half of it is the other's
+    # d rounded once, an exponential to 3 units: as for k above, and 2^-24 of the 1 that is subtracted
+    tol = 2.0 ** -24 * (8 * np.abs(want) + np.where(np.isfinite(d), np.exp(np.minimum(d, 90)) * np.abs(d), 0) + 2)
+    got = grad.double().cpu().numpy()
+    assert (np.abs(got[:, 0] - want) <= tol).all() and (np.abs(got[:, 1] + want) <= tol).all()
+    assert rows[0][0] == float("inf") and torch.isfinite(rows[0][1:]).all()
+
+
 def test_captured_and_replayed():
     N, V = 40, 40000
     d, dev = problem(2, N, V, "bf16", 1.0)

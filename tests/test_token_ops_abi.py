@@ -11,14 +11,15 @@ import torch
 
 import paper_2203_04738_amd as mg
 from paper_2203_04738_amd import ops, token_ops as tk
-from test_ops_launch_limits import runtime as threads_runtime  # noqa: F401
-from test_ops_launches import runtime  # noqa: F401
+import test_ops_launch_limits as limits
+import test_ops_launches as launches
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HEADER = open(os.path.join(ROOT, "include", "mgrit_tokens.h")).read()
 NULL, SIZE, ENUM, WORKSPACE, ALIGN = -1, -2, -4, -5, -6
 P, BIG = 4096, 1 << 50                    # an aligned address that nothing reads
 ref = ctypes.byref
+runtime, threads_runtime = launches.runtime, limits.runtime
 
 
 def test_every_declared_symbol_is_exported():
@@ -61,7 +62,7 @@ def test_embedding_refusals():
         return c
 
     for cfg, code in ((mg.EmbedCfg(0, 2, 8), SIZE), (mg.EmbedCfg(4, 0, 8), SIZE), (mg.EmbedCfg(4, 2, 0), SIZE),
-                      (mg.EmbedCfg((1 << 28) + 1, 2, 8), SIZE), (mg.EmbedCfg(4, (1 << 20) + 1, 8), SIZE),
+                      (mg.EmbedCfg((1 << 26) + 1, 2, 8), SIZE), (mg.EmbedCfg(4, (1 << 20) + 1, 8), SIZE),
                       (mg.EmbedCfg(4, 2, (1 << 20) + 1), SIZE), (strided(mg.EmbedCfg(4, 2, 8), ld_table=7), SIZE),
                       (strided(mg.EmbedCfg(4, 2, 8), ld_out=7), SIZE), (strided(mg.EmbedCfg(4, 2, 8), ld_out=1 << 41), SIZE),
                       (mg.EmbedCfg(4, 2, 8, 0, float("inf")), SIZE), (mg.EmbedCfg(4, 2, 8, 0, float("nan")), SIZE),
@@ -95,10 +96,10 @@ def seq(data=P, t=16, b=8):
 def test_convolution_refusals():
     L = tk._lib()
 
-    def forward(cfg=mg.ConvCfg(5, 2, 8, 4), x=None, weight=P, bias=P, past=P, y=None, last=P):
+    def forward(cfg=mg.ConvCfg(5, 2, 8, 4), x=None, weight=P, bias=P, past=P, y=None, last=3 * P):
         return L.causal_conv_forward(ref(cfg), x or seq(), weight, bias, past, None, y or seq(), last, None)
 
-    def backward(cfg=mg.ConvCfg(5, 2, 8, 4), x=None, weight=P, dy=None, dlast=P, dx=None, dw=P, db=P, dp=P, ws=P, n=BIG):
+    def backward(cfg=mg.ConvCfg(5, 2, 8, 4), x=None, weight=P, dy=None, dlast=P, dx=None, dw=P, db=P, dp=3 * P, ws=P, n=BIG):
         return L.causal_conv_backward(ref(cfg), x or seq(), weight, P, P, None, dy or seq(), dlast, dx or seq(), dw, db, dp, ws, n,
                                       None)
 
@@ -112,6 +113,8 @@ def test_convolution_refusals():
     assert forward(x=seq(None)) == NULL and forward(y=seq(None)) == NULL and forward(weight=None) == NULL
     assert forward(x=seq(P + 2)) == ALIGN and forward(weight=P + 2) == ALIGN and forward(bias=P + 2) == ALIGN
     assert forward(past=P + 2) == ALIGN and forward(last=P + 2) == ALIGN
+    assert forward(last=P) == SIZE and forward(mg.ConvCfg(5, 2, 8, 4), past=2 * P, last=2 * P) == SIZE    # the past itself
+    assert backward(dp=P) == SIZE and backward(dlast=2 * P, dp=2 * P) == SIZE
     assert forward(x=seq(P, -16, 8)) == SIZE
     for t, b in ((0, 8), (15, 8), (8, 8), (16, 7), (7, 1 << 20)):            # outputs that would overlap themselves
         assert forward(y=seq(P, t, b)) == SIZE and backward(dx=seq(P, t, b)) == SIZE
@@ -148,10 +151,10 @@ def grads(z=True, **other):
 def test_scan_refusals():
     L, ok = tk._lib(), mg.SsmCfg(100, 2, 8, 4)
 
-    def forward(cfg=ok, i=inputs(), h0=P, y=None, saved=P, saved_n=BIG, ws=P, n=BIG):
-        return L.ssm_forward(ref(cfg), ref(i) if i else None, h0, None, y or seq(), P, saved, saved_n, ws, n, None)
+    def forward(cfg=ok, i=inputs(), h0=P, y=None, saved=P, saved_n=BIG, ws=P, n=BIG, h_last=3 * P):
+        return L.ssm_forward(ref(cfg), ref(i) if i else None, h0, None, y or seq(), h_last, saved, saved_n, ws, n, None)
 
-    def backward(cfg=ok, i=inputs(), saved=P, saved_n=BIG, dy=None, dh=P, g=grads(), ws=P, n=BIG):
+    def backward(cfg=ok, i=inputs(), saved=P, saved_n=BIG, dy=None, dh=3 * P, g=grads(), ws=P, n=BIG):
         return L.ssm_backward(ref(cfg), ref(i) if i else None, None, saved, saved_n, dy or seq(), dh, ref(g) if g else None, ws, n,
                               None)
 
@@ -173,6 +176,7 @@ def test_scan_refusals():
         assert forward(i=inputs(**{k: P + 2})) == ALIGN
     assert forward(saved=P + 8) == ALIGN and forward(saved_n=saved - 1) == WORKSPACE and forward(h0=P + 1) == ALIGN
     assert forward(n=n - 1) == WORKSPACE and forward(ws=None) == NULL and forward(ws=P + 4) == ALIGN
+    assert forward(h_last=P) == SIZE and backward(dh=P) == SIZE                          # h0, dh0 themselves
     assert backward(saved=None) == NULL and backward(g=None) == NULL and backward(g=grads(da=None)) == NULL
     assert backward(i=inputs(z=False)) == NULL and backward(g=grads(z=False)) == NULL
     assert backward(saved_n=saved - 1) == WORKSPACE and backward(n=n - 1) == WORKSPACE and backward(dy=seq(None)) == NULL
@@ -289,8 +293,8 @@ import ctypes, sys
 ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
 from ctypes import byref
 import paper_2203_04738_amd as mg
-from paper_2203_04738_amd import ops, token_ops as tk
-L, entry, n = tk._lib(), sys.argv[2], [int(a) for a in sys.argv[3:]]
+from paper_2203_04738_amd import binding, ops, token_ops as tk
+L, entry, n = tk._prototypes(ops._prototypes(binding.lib())), sys.argv[2], [int(a) for a in sys.argv[3:]]
 A, big = [(i + 1) << 44 for i in range(16)], 1 << 60
 if entry.startswith("embed"):
     c = mg.EmbedCfg(*n)
@@ -333,7 +337,7 @@ print("returned", rc)
 """
 
 
-def call(runtime, entry, *sizes, **env):  # noqa: F811
+def call(runtime, entry, *sizes, **env):
     """(what the call returned, [(workgroups, kernel)])"""
     r = subprocess.run([sys.executable, "-c", CALL, runtime, entry, *(str(v) for v in sizes)], cwd=ROOT,
                        env=dict(os.environ, **env), capture_output=True, text=True, timeout=300)
@@ -341,3 +345,66 @@ def call(runtime, entry, *sizes, **env):  # noqa: F811
     lines = [line.split(" ", 2) for line in r.stdout.splitlines()]
     (rc,) = (int(f[1]) for f in lines if f[0] == "returned")
     return rc, [(int(f[1]), f[2]) for f in lines if f[0] in ("launched", "failed")]
+
+
+@pytest.mark.parametrize("entry,sizes,kernels", [
+    ("embed_lookup", (8, 100, 64), ["embed_lookup_kernel<float, true>"]),
+    ("embed_lookup", (8, 100, 63, 1), ["embed_lookup_kernel<mg::Bf16, false>"]),
+    ("embed_backward", (32, 100, 64), ["embed_plan_kernel<128>", "embed_sum_kernel<float, true, 1>"]),
+    ("embed_backward", (33, 32769, 64, 1), ["embed_plan_kernel<512>", "embed_sum_kernel<mg::Bf16, true, 1>",
+                                            "embed_join_kernel<mg::Bf16, true>"]),
+    ("embed_backward", (33, 131073, 3, 4), ["embed_plan_kernel<2048>", "embed_sum_kernel<mg::F16, false, 2>",
+                                            "embed_join_kernel<mg::F16, false>"]),
+    ("causal_conv_forward", (100, 2, 130, 4), ["conv_forward_kernel<float, 2, 4>"]),
+    ("causal_conv_forward", (100, 2, 33, 1, 0, 1), ["conv_forward_kernel<mg::Bf16, 1, 8>"]),
+    ("causal_conv_backward", (100, 2, 130, 2, 1, 4), ["conv_backward_kernel<mg::F16, 2, 2>", "conv_params_kernel"]),
+    ("causal_conv_backward", (100, 2, 31, 3), ["conv_backward_kernel<float, 1, 3>", "conv_params_kernel"]),
+    ("causal_conv_step", (1, 4, 8, 4), ["conv_step_kernel<float>"]),
+    ("ssm_forward", (16, 2, 70, 16), ["ssm_forward_kernel<float, 4, true>"]),
+    ("ssm_forward", (128, 100, 1000, 16), ["ssm_forward_kernel<float, 4, true>"]),
+    ("ssm_forward", (777, 3, 500, 16, 1), ["ssm_forward_kernel<mg::Bf16, 4, false>", "ssm_forward_kernel<mg::Bf16, 4, true>"]),
+    ("ssm_forward", (4096, 1, 64, 3, 4), ["ssm_forward_kernel<mg::F16, 1, false>", "ssm_between_kernel",
+                                          "ssm_forward_kernel<mg::F16, 1, true>"]),
+    ("ssm_backward", (16, 2, 70, 64), ["ssm_backward_kernel<float, 16, 4>", "ssm_bc_kernel<float>", "ssm_params_kernel"]),
+    ("ssm_backward", (777, 3, 500, 17), ["ssm_adjoint_ends_kernel<float, 8>", "ssm_backward_kernel<float, 8, 8>",
+                                         "ssm_bc_kernel<float>", "ssm_params_kernel"]),
+    ("ssm_backward", (4096, 1, 64, 8, 1), ["ssm_adjoint_ends_kernel<mg::Bf16, 2>", "ssm_between_kernel",
+                                           "ssm_backward_kernel<mg::Bf16, 2, 8>", "ssm_bc_kernel<mg::Bf16>", "ssm_params_kernel"]),
+    ("ssm_step", (1, 4, 8, 16), ["ssm_step_kernel<float, 4>"]),
+    ("policy_loss", (100, 51), ["policy_kernel<float, 1>"]),
+    ("policy_loss", (8, 8192), ["policy_kernel<float, 4>"]),
+    ("policy_loss", (8, 32768, 1), ["policy_kernel<mg::Bf16, 16>"]),
+    ("policy_loss", (64, 50000), ["distill_segment_kernel<float>", "policy_join_kernel<float>", "policy_grad_kernel<float, 16>"]),
+    ("policy_loss_backward", (64, 500), ["policy_grad_kernel<float, 1>"]),
+    ("policy_loss_backward", (64, 50000, 1), ["policy_grad_kernel<mg::Bf16, 16>"])])
+def test_kernels_of_a_call_and_launches_that_fail(runtime, entry, sizes, kernels):
+    rc, got = call(runtime, entry, *sizes)
+    names = [name.replace("void mg::", "mg::") for _, name in got]
+    assert rc == 0 and len(names) == len(kernels), names
+    assert all("mg::" + k in n for k, n in zip(kernels, names)), names
+    assert all(0 < groups < 2 ** 31 for groups, _ in got)
+    for k in kernels:                                            # a failing launch ends the call and is reported
+        rc, got = call(runtime, entry, *sizes, FAKE_HIP_FAIL=k.split("<")[0])
+        assert rc == -7 and len(got) <= len(kernels)
+
+
+M = 1 << 20
+
+
+@pytest.mark.parametrize("entry,fits,more", [
+    ("embed_lookup", (4 * M - 1, 9, 4096), (4 * M, 9, 4096)),
+    ("embed_backward", (64 * M - 32, 9, 1024), (64 * M, 9, 1025)),
+    ("causal_conv_forward", (2, 256 * M - 16, 1, 4), (2, 256 * M, 1, 4)),
+    ("causal_conv_backward", (2, 256 * M - 16, 1, 4), (2, 256 * M, 1, 4)),
+    ("ssm_forward", (2, 16 * M - 1, 2, 4), (2, 16 * M, 2, 4)),
+    ("ssm_backward", (2, 16 * M - 1, 2, 4), (2, 16 * M, 2, 4)),
+    ("ssm_backward", (64, 16 * M - 1, 2, 3), (64, 16 * M - 1, 2, 5)),
+    ("causal_conv_step", (1, 64 * M, 8, 4), (1, 128 * M, 32, 4)),
+    ("ssm_step", (1, 64 * M - 4, 16, 4), (1, 64 * M, 16, 4)),
+    ("policy_loss", (4 * M - 1, 20000), (4 * M, 20000)),
+    ("policy_loss", (2 * M - 1, 50000), (2 * M, 50000)),
+    ("policy_loss_backward", (16 * M - 1, 5000), (16 * M, 5000))])
+def test_launches_of_less_than_2_to_the_32_threads(threads_runtime, entry, fits, more):
+    rc, got = call(threads_runtime, entry, *fits)
+    assert rc == 0 and got and all(0 < n < 2 ** 32 for n, _ in got), (rc, got)
+    assert call(threads_runtime, entry, *more) == (SIZE, [])
