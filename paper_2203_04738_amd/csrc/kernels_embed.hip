@@ -3,9 +3,10 @@
 // The gradient sorts: a workgroup owns a range of the vocabulary and looks through all tokens of the call twice.  The
 // first time it counts those below its range, which is where its own will stand, and, per wave, those of each of its
 // own tokens; the second time every wave puts the places of its part behind those of the waves before it.  Places are
-// therefore in order of token and place, whatever runs first.  Then a wave adds up a block of sorted places, however they
-// fall into runs of one token, so that a token that is half of all takes no longer than many, while other workgroups of the
-// launch clear the rows that no token names; sums of runs that cross blocks meet in a third launch.
+// therefore in order of token and place, whatever runs first.  Other workgroups of the launch, which waits for its loads
+// most of the time, clear the table meanwhile.  Then a wave adds up a block of sorted places, however they fall into runs of
+// one token, so that a token that is half of all takes no longer than many; sums of runs that cross blocks meet in a third
+// launch.
 #include "elem.h"
 #include "tokens.h"
 
@@ -60,10 +61,29 @@ __global__ __launch_bounds__(256) void embed_lookup_kernel(EmbedArgs a) {
   v.store((E*)a.out + row * a.c.ld_out + col, tok < 0 ? 1.f : a.c.scale);
 }
 
-// ---- gradient: places of the tokens of a range, in order, and which of them occur
+// ---- gradient: places of the tokens of a range, in order; the table cleared
 constexpr int PLAN_WAVES = 16, PLAN_THREADS = 64 * PLAN_WAVES;
-template <int RANGE>
-__global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a) {
+// Rows CLEAR_ROWS group .. of the table, a wave a row.
+constexpr int CLEAR_ROWS = 64;
+template <typename E, bool WIDE>
+__device__ inline void clear_rows(const EmbedArgs& a, int group) {
+  using P = Piece<E, WIDE>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int pieces = (a.c.D + P::n - 1) / P::n;
+  P zero;
+#pragma unroll
+  for (int k = 0; k < P::n; ++k) zero.v[k] = 0.f;
+  for (int r = CLEAR_ROWS * group + wave; r < min(CLEAR_ROWS * (group + 1), a.c.V); r += PLAN_WAVES) {
+    E* out = (E*)a.out + r * a.c.ld_table;
+    for (int i = lane; i < pieces; i += 64) zero.store(out + (long long)i * P::n, 1.f);
+  }
+}
+template <typename E, bool WIDE, int RANGE>
+__global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a, int ranges) {
+  if ((int)blockIdx.x >= ranges) {
+    clear_rows<E, WIDE>(a, (int)blockIdx.x - ranges);
+    return;
+  }
   __shared__ int count[PLAN_WAVES][RANGE];
   __shared__ int part[PLAN_WAVES], below;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -123,13 +143,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a) {
     }
     at = pos;
   }
-  if (blockIdx.x == gridDim.x - 1 && tid == PLAN_THREADS - 1) *a.total = at;
-  // (PER words for each 64 PER tokens, token i of them in word i % PER)
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const unsigned long long bits = __ballot(own[j] > 0);
-    if (lane == 0 && wave * 64 * PER < RANGE) a.occurs[(blockIdx.x * RANGE + wave * 64 * PER) / 64 + j] = bits;
-  }
+  if ((int)blockIdx.x == ranges - 1 && tid == PLAN_THREADS - 1) *a.total = at;
   __syncthreads();
   for (int i0 = begin; i0 < end; i0 += 512) {
     long long k[8];
@@ -165,33 +179,11 @@ __global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a) {
   }
 }
 
-// Clears the rows of 64 tokens that do not occur, a wave a row.
-template <typename E, bool WIDE, int PER>
-__device__ inline void clear_rows(const EmbedArgs& a, int group) {
-  using P = Piece<E, WIDE>;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int pieces = (a.c.D + P::n - 1) / P::n;
-  P zero;
-#pragma unroll
-  for (int k = 0; k < P::n; ++k) zero.v[k] = 0.f;
-  for (int r = wave; r < 64; r += 4) {
-    const int token = 64 * group + r, in = token % (64 * PER);
-    if (token >= a.c.V) break;
-    if (a.occurs[token / (64 * PER) * PER + in % PER] >> (in / PER) & 1) continue;
-    E* out = (E*)a.out + token * a.c.ld_table;
-    for (int i = lane; i < pieces; i += 64) zero.store(out + (long long)i * P::n, 1.f);
-  }
-}
-
 // ---- gradient: sums of a block of sorted places, in one wave per 64 pieces of the width
-template <typename E, bool WIDE, int PER>
-__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, unsigned sum_groups) {
+template <typename E, bool WIDE>
+__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a) {
   using P = Piece<E, WIDE>;
-  constexpr int AHEAD = 8;
-  if (blockIdx.x >= sum_groups) {
-    clear_rows<E, WIDE, PER>(a, (int)(blockIdx.x - sum_groups));
-    return;
-  }
+  constexpr int AHEAD = 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int pieces = (a.c.D + P::n - 1) / P::n, across = (pieces + 63) / 64;
   const long long item = (long long)blockIdx.x * 4 + wave;
@@ -303,11 +295,10 @@ static bool wide_rows(const void* p, long long ld, int D, int size) {
   return (uintptr_t)p % 16 == 0 && ld * size % 16 == 0 && (long long)D * size % 16 == 0;
 }
 static size_t embed_piece(size_t n) { return (n + 255) / 256 * 256; }
-// The total, the bits of the tokens that occur (of whole ranges), places, tokens, runs that cross blocks, sums.
-static size_t embed_bits(const embed_cfg& c) { return embed_piece(8 * ((size_t)c.V / 64 + 64)); }
+// The total, places, tokens, runs that cross blocks, sums.
 size_t embed_workspace(const embed_cfg& c) {
   const size_t N = (size_t)c.N, blocks = (N + EMBED_RUN - 1) / EMBED_RUN;
-  return 256 + embed_bits(c) + 2 * embed_piece(4 * N) + embed_piece(4 * blocks) + 8 * blocks * c.D;
+  return 256 + 2 * embed_piece(4 * N) + embed_piece(4 * blocks) + 8 * blocks * c.D;
 }
 template <typename E, bool WIDE>
 static hipError_t embed_lookup_start(const EmbedArgs& a, hipStream_t s) {
@@ -319,14 +310,14 @@ static hipError_t embed_lookup_start(const EmbedArgs& a, hipStream_t s) {
 // RANGE tokens of the vocabulary for a workgroup of the sort.
 template <typename E, bool WIDE, int RANGE>
 static hipError_t embed_backward_range(const EmbedArgs& a, hipStream_t s) {
-  constexpr int PER = (RANGE + PLAN_THREADS - 1) / PLAN_THREADS;
   const long long pieces = (a.c.D + Piece<E, WIDE>::n - 1) / Piece<E, WIDE>::n, across = (pieces + 63) / 64;
-  const long long items = ((a.c.N + EMBED_RUN - 1LL) / EMBED_RUN) * across, sums = (items + 3) / 4, clears = (a.c.V + 63) / 64;
-  if (!launchable(items, 64 * JOIN_WAVES) || !launchable(sums + clears, 256)) return TOO_LARGE;
-  hipLaunchKernelGGL((embed_plan_kernel<RANGE>), dim3((a.c.V + RANGE - 1) / RANGE), dim3(PLAN_THREADS), 0, s, a);
+  const long long items = ((a.c.N + EMBED_RUN - 1LL) / EMBED_RUN) * across;
+  const int ranges = (a.c.V + RANGE - 1) / RANGE, clears = (a.c.V + CLEAR_ROWS - 1) / CLEAR_ROWS;
+  if (!launchable(items, 64 * JOIN_WAVES)) return TOO_LARGE;
+  hipLaunchKernelGGL((embed_plan_kernel<E, WIDE, RANGE>), dim3(ranges + clears), dim3(PLAN_THREADS), 0, s, a, ranges);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((embed_sum_kernel<E, WIDE, PER>), dim3((unsigned)(sums + clears)), dim3(256), 0, s, a, (unsigned)sums);
+  hipLaunchKernelGGL((embed_sum_kernel<E, WIDE>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess || a.c.N <= EMBED_RUN) return e;
   hipLaunchKernelGGL((embed_join_kernel<E, WIDE>), dim3((unsigned)items), dim3(64 * JOIN_WAVES), 0, s, a);
   return hipGetLastError();
@@ -354,8 +345,6 @@ hipError_t launch_embed_lookup(const EmbedArgs& a, hipStream_t s) { return embed
 hipError_t launch_embed_backward(EmbedArgs a, char* ws, hipStream_t s) {
   a.total = (int*)ws;
   ws += 256;
-  a.occurs = (unsigned long long*)ws;
-  ws += embed_bits(a.c);
   a.place = (int*)ws;
   ws += embed_piece(4 * (size_t)a.c.N);
   a.token = (int*)ws;

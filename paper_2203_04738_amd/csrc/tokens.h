@@ -13,7 +13,6 @@ struct EmbedArgs {
   const void* in;           // table, or dout
   void* out;                // out, or dtable
   int* total;               // tokens that name a row
-  unsigned long long* occurs;   // bits of the tokens that occur
   int* place;               // [N]: places of the tokens in order of token and place
   int* token;               // [N]: their tokens
   int* crosses;             // [ceil(N / EMBED_RUN)]: the token of a run that begins in the block and goes on, or -1
