@@ -111,7 +111,7 @@ class _Group(tuple):
 
 
 _SEQS = {n: struct.Struct(f"{n}q") for n in range(1, 24)}
-_NO_SEQ = (0, 0, 0)
+_NULL, _NO_SEQ = (0,), (0, 0, 0)
 
 
 def _explain(args, device):
@@ -122,54 +122,51 @@ def _explain(args, device):
             raise ValueError(f"{a[1]}: tensor on cuda:{a[0].get_device()}, the current device is cuda:{device}")
 
 
-def _fits(a, device):
-    t, _, dtype, shape, kind = a
-    return (isinstance(t, _o._torch.Tensor) and (shape is None or t.shape == shape) and (dtype is None or t.dtype is dtype)
-            and t.get_device() == device and (t.is_contiguous() if kind == 0 else _o._unit_rows(t)))
-
-
 def _call(name, cfg, *args) -> None:
     """Checks and marshals the arguments, then calls entry point `name` on the current stream (ops._call, with
     structures of arguments, and all tensors on the current device)."""
     L, torch = _lib(), _o._torch
-    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+    tensor, device = torch.Tensor, torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
     out = []
     for a in args:
         kind = type(a)
         if kind is tuple:
-            t = a[0]
-            if t is None:
-                out.append(None)
-            elif not _fits(a, device):
-                _explain(args, device)
-                raise AssertionError(a[1])            # (not reached: _explain says what is wrong)
-            elif a[4] < 2:
-                out.append(t.data_ptr())
-            else:
-                strides = t.stride()
-                out.append(_SEQS[3].pack(t.data_ptr(), strides[0] if a[4] == _SEQ else 0, strides[-2]))
+            group = (a,)
         elif kind is _Group:
-            words = []
-            for b in a:
-                t = b[0]
-                if t is None:
-                    words += _NO_SEQ if b[4] >= 2 else (0,)
-                elif not _fits(b, device):
-                    _explain(args, device)
-                    raise AssertionError(b[1])
-                elif b[4] < 2:
-                    words.append(t.data_ptr())
-                else:
-                    strides = t.stride()
-                    words += (t.data_ptr(), strides[0] if b[4] == _SEQ else 0, strides[-2])
-            out.append(_SEQS[len(words)].pack(*words))
-        elif isinstance(a, ctypes.Structure):
-            out.append(ctypes.byref(a))
+            group = a
         else:
-            out.append(a)
+            out.append(ctypes.byref(a) if isinstance(a, ctypes.Structure) else a)
+            continue
+        words = []
+        for t, _, dtype, shape, layout in group:
+            if t is None:
+                words += _NO_SEQ if layout >= _SEQ and kind is _Group else _NULL
+                continue
+            if not (isinstance(t, tensor) and (shape is None or t.shape == shape) and (dtype is None or t.dtype is dtype)
+                    and t.get_device() == device):
+                _refuse(args, device)
+            if layout == _DENSE:
+                if not t.is_contiguous():
+                    _refuse(args, device)
+                words.append(t.data_ptr())
+                continue
+            strides = t.stride()
+            if strides[-1] != 1 and t.shape[-1] != 1:
+                _refuse(args, device)
+            if layout >= _SEQ:
+                words += (t.data_ptr(), strides[0] if layout == _SEQ else 0, strides[-2])
+            else:
+                words.append(t.data_ptr())
+        n = len(words)
+        out.append(_SEQS[n].pack(*words) if n > 1 else words[0] or None)
     rc = getattr(L, name)(ctypes.byref(cfg), *out, _o._stream())
     if rc:
         _check(rc, name)
+
+
+def _refuse(args, device):
+    _explain(args, device)
+    raise AssertionError("an argument that fits was refused")
 
 
 # ---- embedding
@@ -196,12 +193,12 @@ def causal_conv_workspace_bytes(cfg: ConvCfg) -> int:
     return _size("causal_conv_workspace_bytes", cfg)
 
 
-def _seq(cfg, t, name, width=None):
-    return t, name, _dtype(cfg), (cfg.T, cfg.B, width or cfg.H), _SEQ
+def _seq(cfg, t, name):
+    return t, name, _dtype(cfg), (cfg.T, cfg.B, cfg.H), _SEQ
 
 
-def _row(cfg, t, name, width=None):
-    return t, name, _dtype(cfg), (cfg.B, width or cfg.H), _STEP
+def _row(cfg, t, name):
+    return t, name, _dtype(cfg), (cfg.B, cfg.H), _STEP
 
 
 def _taps(cfg, weight, bias):
@@ -245,16 +242,19 @@ def ssm_saved_bytes(cfg: SsmCfg) -> int:
     return _size("ssm_saved_bytes", cfg)
 
 
-def _ssm_inputs(cfg, one, x, dt, b, c, z, a, skip, bias):
-    H, S = cfg.H, cfg.S
-    return _Group((one(cfg, x, "x"), one(cfg, dt, "dt"), one(cfg, b, "b", S), one(cfg, c, "c", S), one(cfg, z, "z"),
-                   _f32(a, "a", H, S), _f32(skip, "skip", H), _f32(bias, "bias", H)))            # (SsmInputs)
+def _ssm_inputs(cfg, rows, layout, x, dt, b, c, z, a, skip, bias):
+    """rows: what the shapes of sequences begin with."""
+    H, S, dtype = cfg.H, cfg.S, _dtype(cfg)
+    wide, narrow = rows + (H,), rows + (S,)
+    return _Group(((x, "x", dtype, wide, layout), (dt, "dt", dtype, wide, layout), (b, "b", dtype, narrow, layout),
+                   (c, "c", dtype, narrow, layout), (z, "z", dtype, wide, layout), _f32(a, "a", H, S),
+                   _f32(skip, "skip", H), _f32(bias, "bias", H)))                                  # (SsmInputs)
 
 
 def ssm_forward(cfg, x, dt, b, c, z, a, skip, bias, h0, reset, y, h_last, saved, workspace) -> None:
     """x, dt, z (or None), y: [T,B,H]; b, c: [T,B,S]; a: [H,S]; skip, bias: [H] or None; h0, h_last: [B,H,S] or None."""
     T, B, H, S = cfg.T, cfg.B, cfg.H, cfg.S
-    _call("ssm_forward", cfg, _ssm_inputs(cfg, _seq, x, dt, b, c, z, a, skip, bias), _f32(h0, "h0", B, H, S),
+    _call("ssm_forward", cfg, _ssm_inputs(cfg, (T, B), _SEQ, x, dt, b, c, z, a, skip, bias), _f32(h0, "h0", B, H, S),
           _reset(reset, T, B), _seq(cfg, y, "y"), _f32(h_last, "h_last", B, H, S), *_bytes_of(saved, "saved"),
           *_bytes_of(workspace, "workspace"))
 
@@ -262,10 +262,11 @@ def ssm_forward(cfg, x, dt, b, c, z, a, skip, bias, h0, reset, y, h_last, saved,
 def ssm_backward(cfg, x, dt, b, c, z, a, skip, bias, reset, saved, dy, dh_last, dx, ddt, db, dc, dz, da, dskip, dbias,
                  dh0, workspace) -> None:
     T, B, H, S = cfg.T, cfg.B, cfg.H, cfg.S
-    grads = _Group((_seq(cfg, dx, "dx"), _seq(cfg, ddt, "ddt"), _seq(cfg, db, "db", S), _seq(cfg, dc, "dc", S),
-                    _seq(cfg, dz, "dz"), _f32(da, "da", H, S), _f32(dskip, "dskip", H), _f32(dbias, "dbias", H),
-                    _f32(dh0, "dh0", B, H, S)))                                                    # (SsmGrads)
-    _call("ssm_backward", cfg, _ssm_inputs(cfg, _seq, x, dt, b, c, z, a, skip, bias), _reset(reset, T, B),
+    dtype, wide, narrow = _dtype(cfg), (T, B, H), (T, B, S)
+    grads = _Group(((dx, "dx", dtype, wide, _SEQ), (ddt, "ddt", dtype, wide, _SEQ), (db, "db", dtype, narrow, _SEQ),
+                    (dc, "dc", dtype, narrow, _SEQ), (dz, "dz", dtype, wide, _SEQ), _f32(da, "da", H, S),
+                    _f32(dskip, "dskip", H), _f32(dbias, "dbias", H), _f32(dh0, "dh0", B, H, S)))    # (SsmGrads)
+    _call("ssm_backward", cfg, _ssm_inputs(cfg, (T, B), _SEQ, x, dt, b, c, z, a, skip, bias), _reset(reset, T, B),
           *_bytes_of(saved, "saved"), _seq(cfg, dy, "dy"), _f32(dh_last, "dh_last", B, H, S), grads,
           *_bytes_of(workspace, "workspace"))
 
@@ -273,7 +274,7 @@ def ssm_backward(cfg, x, dt, b, c, z, a, skip, bias, reset, saved, dy, dh_last, 
 def ssm_step(cfg, x, dt, b, c, z, a, skip, bias, slots, reset, state_in, state_out, y) -> None:
     """x, dt, z (or None), y: [B,H]; b, c: [B,S]; state_in, state_out: [n_slots,H,S]."""
     B, H, S, n = cfg.B, cfg.H, cfg.S, _slots(state_in)
-    _call("ssm_step", cfg, _ssm_inputs(cfg, _row, x, dt, b, c, z, a, skip, bias),
+    _call("ssm_step", cfg, _ssm_inputs(cfg, (B,), _STEP, x, dt, b, c, z, a, skip, bias),
           (slots, "slots", _o._torch.int32, (B,), _DENSE), n, _reset(reset, B), _f32(state_in, "state_in", n, H, S),
           _f32(state_out, "state_out", n, H, S), _row(cfg, y, "y"))
 
