@@ -106,13 +106,13 @@ struct ConvPlace {
   __device__ inline unsigned resets(const ConvArgs& a, int b, int t, int n) const {
     if (!a.reset) return 0;
     auto look = [&](int i) { return i < n && t + i >= 0 && t + i < a.c.T && a.reset[(long long)(t + i) * a.c.B + b] != 0; };
-    unsigned bits = mine(__ballot(look(lane_c)));
-    if (n > lanes) bits |= mine(__ballot(look(lane_c + lanes))) << lanes;
+    unsigned bits = (unsigned)mine(__ballot(look(lane_c)));
+    if (n > lanes) bits |= (unsigned)mine(__ballot(look(lane_c + lanes))) << lanes;
     return bits;
   }
-  __device__ inline unsigned mine(unsigned long long all) const {
-    if (lanes == 64) return (unsigned)all;
-    return (unsigned)(all >> ((threadIdx.x & 63) / lanes * lanes)) & (unsigned)((1ull << lanes) - 1);
+  // What the run's lanes say of a ballot.
+  __device__ inline unsigned long long mine(unsigned long long all) const {
+    return lanes == 64 ? all : all >> ((threadIdx.x & 63) / lanes * lanes) & ((1ull << lanes) - 1);
   }
 };
 
@@ -278,17 +278,32 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, int lane
     for (int k = 0; k < WT; ++k)
 #pragma unroll
       for (int c = 0; c < VEC; ++c) v.g[k][c] = 0.f;
+    ConvRaw<E, VEC> xn[CONV_BLOCK], dn[CONV_BLOCK];
+    auto load = [&](int base) __attribute__((always_inline)) {
+#pragma unroll
+      for (int r = 0; r < CONV_BLOCK; ++r) {
+        const long long t = min(base + r, T - 1);
+        xn[r].load(x + t * a.x.stride_t);
+        dn[r].load(dy + t * a.dy.stride_t);
+      }
+    };
+    load(v.t0);
+    unsigned long long ahead = 0;
     for (int off = 0; off < a.seg + WT - 1; off += CONV_BLOCK) {
       const int base = v.t0 + off;
-      const unsigned resets = at.resets(a, b, base, CONV_BLOCK);
+      if (off % at.lanes == 0) {                     // (as many steps as a run has lanes to look at them)
+        const int t = base + at.lane_c;
+        ahead = a.reset ? at.mine(__ballot(t < T && a.reset[(long long)t * a.c.B + b] != 0)) : 0;
+      }
+      const unsigned resets = (unsigned)(ahead >> off % at.lanes) & ((1u << CONV_BLOCK) - 1);
       if (!real || base >= v.t1 + WT - 1) continue;
       ConvRaw<E, VEC> xr[CONV_BLOCK], dr[CONV_BLOCK];
 #pragma unroll
       for (int r = 0; r < CONV_BLOCK; ++r) {
-        const long long t = min(base + r, T - 1);
-        xr[r].load(x + t * a.x.stride_t);
-        dr[r].load(dy + t * a.dy.stride_t);
+        xr[r] = xn[r];
+        dr[r] = dn[r];
       }
+      load(base + CONV_BLOCK);
       if (!resets && base - (WT - 1) >= v.last_reset && base + CONV_BLOCK <= v.t1) {
 #pragma unroll
         for (int r = 0; r < CONV_BLOCK; ++r) {
