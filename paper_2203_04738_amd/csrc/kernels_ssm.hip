@@ -189,14 +189,20 @@ __device__ inline void read_bc(const float* lds, int step, int q, int which, flo
   for (int i = 0; i < SP; ++i) v[i] = p[i];
 }
 
-// Bits of the steps t0 .. t0 + n - 1 that reset.
-__device__ inline unsigned ssm_resets(const SsmArgs& a, int b, int t0, int n) {
-  if (!a.reset) return 0;
-  const int lane = threadIdx.x & 63, t = t0 + lane;
-  bool r = false;
-  if (lane < n && t < a.c.T) r = a.reset[(long long)t * a.c.B + b] != 0;
-  return (unsigned)__ballot(r);
-}
+// Which steps reset, 64 of a chunk looked at together, a lane each: a look for every tile would be a wait for every tile.
+struct Resets {
+  unsigned long long bits = 0;
+  // Bits of the n steps of the tile at t, tiles one after the other, forward or backward (n divides 64); first: the first one.
+  __device__ inline unsigned of(const SsmArgs& a, const SsmPlace& p, int t, int n, bool first, bool backward) {
+    if (!a.reset) return 0;
+    const int in = (t - p.t0) & 63;
+    if (first || in == (backward ? 64 - n : 0)) {
+      const int at = t - in + (int)(threadIdx.x & 63);
+      bits = __ballot(at < a.c.T && a.reset[(long long)at * a.c.B + p.b] != 0);
+    }
+    return (unsigned)(bits >> in) & ((1u << n) - 1);
+  }
+};
 
 __device__ inline float decay(float d, float a2) { return __builtin_amdgcn_exp2f(d * a2); }
 
@@ -277,6 +283,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
   load(p.t0);
   float sum = 0.f;
   bool forgets = false;
+  Resets looked;
   int buf = 0;
   for (int t = p.t0; t < p.t1; t += TB, buf ^= 1) {
     float x[G], d[G], z[G];
@@ -287,7 +294,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
       z[g] = gated ? elem_f32(zn[g]) : 0.f;
     }
     next.store(bc[buf]);
-    const unsigned resets = ssm_resets(a, p.b, t, TB);
+    const unsigned resets = looked.of(a, p, t, TB, t == p.t0, false);
     __syncthreads();
     if (t + TB < p.t1) load(t + TB);
     forgets |= resets != 0;
@@ -416,6 +423,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_adjoint_ends_kernel(SsmArgs a
   load(end);
   float sum = 0.f;
   bool forgets = false;
+  Resets looked;
   int buf = 0;
   for (int k = tiles - 1; k >= 0; --k, buf ^= 1) {
     const int t = p.t0 + k * TB;
@@ -429,7 +437,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_adjoint_ends_kernel(SsmArgs a
       sum += d[g];
     }
     next.store(bc[buf]);
-    const unsigned resets = ssm_resets(a, p.b, t, TB);
+    const unsigned resets = looked.of(a, p, t, TB, k == tiles - 1, true);
     __syncthreads();
     if (k > 0) load(t - TB);
     forgets |= resets != 0;
@@ -544,6 +552,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
       a.part_bc + (((long long)(blockIdx.x % (unsigned)a.s.cols) * a.c.T + end + threadIdx.x / (8 * SP)) * a.c.B + p.b) * (2 * S) + own_n;
   const long long row = 2LL * a.c.B * S;                // of a step
   float dskip = 0.f, dbias = 0.f;
+  Resets looked;
   int buf = 0;
   for (int k = tiles - 1; k >= 0; --k, buf ^= 1) {
     const int t = p.t0 + k * R;
@@ -559,7 +568,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
 #pragma unroll
     for (int i = 0; i < SP; ++i) h[i] = p.has ? hn[i] : 0.f;
     next.store(bc[buf]);
-    const unsigned resets = ssm_resets(a, p.b, t, R);
+    const unsigned resets = looked.of(a, p, t, R, k == tiles - 1, true);
     __syncthreads();                               // (and red has been read)
     if (k > 0) load(t - R);
     auto tile = [&](auto plain) SSM_INLINE {
