@@ -263,6 +263,10 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
   const float bias = a.bias ? a.bias[p.ch] : 0.f, skip = MAIN && a.skip ? a.skip[p.ch] : 0.f;
   const bool gated = MAIN && a.z.data;
   Steps<E> xs(a.x, p, p.t0), ds(a.dt, p, p.t0), zs(one_of(gated, a.z, a.x), p, p.t0), ys(one_of(MAIN, a.y, a.x), p, p.t0);
+  constexpr int SAVE = ssm_save(SP);
+  const long long states = (long long)a.c.B * a.c.H * S;
+  float* saved = a.saved + p.t0 / SAVE * states + p.at * S;
+  const bool save = a.saved && p.has;
   Tile next(a, p.b, p.t0);
   E xn[G], dn[G], zn[G];
   auto load = [&](int t) SSM_INLINE {
@@ -304,8 +308,8 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         const int ts = t + 4 * g;
-        if (MAIN && a.saved && ts % a.s.save == 0 && ts < a.c.T && p.has)
-          store_states<SP>(a.saved + (ts / a.s.save * (long long)a.c.B * a.c.H + p.at) * S, S, p.n0, h);
+        if (MAIN && 4 * g % SAVE == 0 && save && (PLAIN || ts < a.c.T))
+          store_states<SP>(saved + 4 * g / SAVE * states, S, p.n0, h);
         const bool in = PLAIN || ts + q < a.c.T;
         const float delta = in ? Softplus(d[g]).d : 0.f;
         const float xv = in ? x[g] : 0.f, dx = delta * xv;
@@ -340,7 +344,10 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
     };
     if (!resets && t + TB <= a.c.T) tile(std::true_type{});
     else tile(std::false_type{});
-    if (MAIN) ys.move(TB);
+    if (MAIN) {
+      ys.move(TB);
+      saved += TB / SAVE * states;
+    }
   }
   if (!p.has) return;
   if (MAIN) {
@@ -772,7 +779,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_step_kernel(SsmStepArgs a) {
 SsmShape ssm_shape(const ssm_cfg& c, bool backward) {
   SsmShape s;
   s.per = c.S <= 4 ? 1 : c.S <= 8 ? 2 : c.S <= 16 ? 4 : c.S <= 32 ? 8 : 16;
-  s.save = s.per <= 8 ? 8 : 4;
+  s.save = ssm_save(s.per);
   s.cols = (c.H + SSM_COLS - 1) / SSM_COLS;
   const long long across = (long long)s.cols * c.B, tiles = ((long long)c.T + SSM_TILE - 1) / SSM_TILE;
   long long chunks = 1;
@@ -859,7 +866,7 @@ static hipError_t ssm_backward_start(const SsmArgs& a, hipStream_t s) {
     if ((e = hipGetLastError()) != hipSuccess || (!few_chunks(a.s) && (e = ssm_between(a, a.dh_last, true, s)) != hipSuccess))
       return e;
   }
-  hipLaunchKernelGGL((ssm_backward_kernel<E, SP, (SP <= 8 ? 8 : 4)>), dim3((unsigned)(across * a.s.chunks)), t, 0, s, a);
+  hipLaunchKernelGGL((ssm_backward_kernel<E, SP, ssm_save(SP)>), dim3((unsigned)(across * a.s.chunks)), t, 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL((ssm_bc_kernel<E>), dim3(blocks((long long)a.c.T * a.c.B * a.c.S)), dim3(256), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;

@@ -53,9 +53,11 @@ hipError_t launch_conv_step(const ConvStepArgs& a, hipStream_t s);
 // ---- selective state space scan (kernels_ssm.hip)
 // A wave covers 16 channels, four lanes a channel, `per` states a lane; a workgroup 64 channels of one batch row and a
 // chunk of steps.
+// Steps between saved states, which are the tile of the adjoint, for lanes of `per` states.
+constexpr int ssm_save(int per) { return per <= 8 ? 8 : 4; }
 struct SsmShape {
   int per;                  // states of a lane: 1, 2, 4, 8, 16
-  int save;                 // steps between saved states, the tile of the adjoint: 8 or 4
+  int save;                 // steps between saved states
   int cols;                 // workgroups across the channels
   int chunks, len;          // chunks of a sequence, their steps (a multiple of 16)
 };
