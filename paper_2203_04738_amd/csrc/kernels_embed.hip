@@ -7,6 +7,9 @@
 // most of the time, clear the table meanwhile.  Then a wave adds up a block of sorted places, however they fall into runs of
 // one token, so that a token that is half of all takes no longer than many; sums of runs that cross blocks meet in a third
 // launch.
+//
+// 16384 tokens, most of them few, of 32768 x 1024 bf16: sort and clearing (64 MB) 19 us, sums (34 MB read) 12, join 6; lookup 67 MB
+// in 10.6 us.  The sort's time is that of the workgroup whose range holds the most frequent tokens (a quarter of all).
 #include "elem.h"
 #include "tokens.h"
 
@@ -179,7 +182,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a, i
   }
 }
 
-// ---- gradient: sums of a block of sorted places, in one wave per 64 pieces of the width
+// ---- gradient: sums of a block of sorted places, in one wave per 64 pieces of the width, 16 rows under way (8: 12.6 us)
 template <typename E, bool WIDE>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a) {
   using P = Piece<E, WIDE>;
