@@ -2,14 +2,14 @@
 //
 // The gradient sorts: a workgroup owns a range of the vocabulary and looks through all tokens of the call twice.  The
 // first time it counts those below its range, which is where its own will stand, and, per wave, those of each of its
-// own tokens; the second time every wave puts the places of its part behind those of the waves before it.  Places are
-// therefore in order of token and place, whatever runs first.  Other workgroups of the launch, which waits for its loads
-// most of the time, clear the table meanwhile.  Then a wave adds up a block of sorted places, however they fall into runs of
-// one token, so that a token that is half of all takes no longer than many; sums of runs that cross blocks meet in a third
-// launch.
+// own tokens; the second time every wave puts the places of its part behind those of the waves before it.  (Of many tokens
+// several workgroups of the range each place a part, having counted all.)  Places are therefore in order of token and place,
+// whatever runs first.  Other workgroups of the launch, which waits for its loads most of the time, clear the table meanwhile.
+// Then a wave adds up a block of sorted places, however they fall into runs of one token, so that a token that is half of all
+// takes no longer than many; sums of runs that cross blocks meet in a third launch.
 //
-// 16384 tokens, most of them few, of 32768 x 1024 bf16: sort and clearing (64 MB) 19 us, sums (34 MB read) 12, join 6; lookup 67 MB
-// in 10.6 us.  The sort's time is that of the workgroup whose range holds the most frequent tokens (a quarter of all).
+// 16384 tokens, most of them few, of 32768 x 1024 bf16: sort and clearing (64 MB) 14.5 us, sums (34 MB read) 12, join 6; lookup
+// 67 MB in 10.8 us.  The sort takes 9.6 us of it, most of them waiting for tokens that all its workgroups look at.
 #include "elem.h"
 #include "tokens.h"
 
@@ -66,6 +66,11 @@ __global__ __launch_bounds__(256) void embed_lookup_kernel(EmbedArgs a) {
 
 // ---- gradient: places of the tokens of a range, in order; the table cleared
 constexpr int PLAN_WAVES = 16, PLAN_THREADS = 64 * PLAN_WAVES;
+// Tokens that a workgroup places at least, and ranges times parts at most: a part spares its workgroup the second look, but all
+// parts count all tokens, which has to be at once.  Sort in us, one part / parts of 4096 / of 4096 with no more than 256
+// workgroups, in ranges of 128: 16384 tokens of 1000 15.1 / 8.8 / 8.7, of 32768 15.0 / 20.2 / 14.9; 65536 of 1000 48.8 / 17.5 /
+// 17.4, of 32768 45 / 141 / 45.4; 262144 of 1000 183 / 55 / 52, of 32768 158 / 494 / 158.
+constexpr int PLAN_PART = 4096, PLAN_GROUPS = 256, PLAN_PARTS = 32;
 // Rows CLEAR_ROWS group .. of the table, a wave a row.
 constexpr int CLEAR_ROWS = 64;
 template <typename E, bool WIDE>
@@ -82,36 +87,48 @@ __device__ inline void clear_rows(const EmbedArgs& a, int group) {
   }
 }
 template <typename E, bool WIDE, int RANGE>
-__global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a, int ranges) {
-  if ((int)blockIdx.x >= ranges) {
-    clear_rows<E, WIDE>(a, (int)blockIdx.x - ranges);
+__global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a, int ranges, int parts) {
+  if ((int)blockIdx.x >= ranges * parts) {
+    clear_rows<E, WIDE>(a, (int)blockIdx.x - ranges * parts);
     return;
   }
   __shared__ int count[PLAN_WAVES][RANGE];
+  __shared__ int other[2][RANGE];                    // tokens before and behind the workgroup's part
   __shared__ int part[PLAN_WAVES], below;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lo = blockIdx.x * RANGE, hi = min(lo + RANGE, a.c.V);
+  const int range = blockIdx.x / parts, lo = range * RANGE, hi = min(lo + RANGE, a.c.V);
   for (int i = tid; i < PLAN_WAVES * RANGE; i += PLAN_THREADS) (&count[0][0])[i] = 0;
+  for (int i = tid; i < 2 * RANGE; i += PLAN_THREADS) (&other[0][0])[i] = 0;
   if (tid == 0) below = 0;
   __syncthreads();
-  const int per = ((a.c.N + PLAN_THREADS - 1) / PLAN_THREADS) * 64;      // places of a wave
-  const int begin = (int)min((long long)a.c.N, (long long)wave * per), end = (int)min((long long)a.c.N, (long long)begin + per);
+  const int N = a.c.N, per = (N + parts * PLAN_THREADS - 1) / (parts * PLAN_THREADS) * 64;      // places of a wave
+  const auto place_of = [&](int i) { return (int)min((long long)N, (long long)i * per); };
+  const int first = (blockIdx.x - range * parts) * PLAN_WAVES;
+  const int begin = place_of(first + wave), end = place_of(first + wave + 1);
   // (eight tokens a lane at a time: what the loads wait for is most of the time)
-  auto load = [&](int i0, long long (&k)[8]) {
+  auto load = [&](int i0, int to, long long (&k)[8]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) k[j] = i0 + 64 * j + lane < end ? a.tokens[i0 + 64 * j + lane] : -1;
+    for (int j = 0; j < 8; ++j) k[j] = i0 + 64 * j + lane < to ? a.tokens[i0 + 64 * j + lane] : -1;
   };
   int less = 0;
-  for (int i0 = begin; i0 < end; i0 += 512) {
-    long long k[8];
-    load(i0, k);
+  auto look = [&](int from, int to, int step, int* counts) {
+    for (int i0 = from; i0 < to; i0 += step) {
+      long long k[8];
+      load(i0, to, k);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      less += k[j] >= 0 && k[j] < lo;
-      if (k[j] >= lo && k[j] < hi) atomicAdd(&count[wave][(int)k[j] - lo], 1);
+      for (int j = 0; j < 8; ++j) {
+        less += k[j] >= 0 && k[j] < lo;
+        if (k[j] >= lo && k[j] < hi) atomicAdd(&counts[(int)k[j] - lo], 1);
+      }
     }
-  }
-  atomicAdd(&below, less);
+  };
+  look(begin, end, 512, count[wave]);
+  const int before = place_of(first), behind = place_of(first + PLAN_WAVES);
+  look(wave * 512, before, 512 * PLAN_WAVES, other[0]);
+  look(behind + wave * 512, N, 512 * PLAN_WAVES, other[1]);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) less += __shfl_xor(less, o, 64);
+  if (lane == 0) atomicAdd(&below, less);
   __syncthreads();
   // where each token's places start: behind those of the smaller ones; then where each wave's do
   constexpr int PER = (RANGE + PLAN_THREADS - 1) / PLAN_THREADS;
@@ -120,8 +137,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a, i
   for (int j = 0; j < PER; ++j) {
     const int r = tid * PER + j;
     own[j] = 0;
-    if (r < RANGE)
+    if (r < RANGE) {
+      own[j] = other[0][r] + other[1][r];
       for (int w = 0; w < PLAN_WAVES; ++w) own[j] += count[w][r];
+    }
     sum += own[j];
   }
   int upto = sum;
@@ -138,19 +157,19 @@ __global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a, i
   for (int j = 0; j < PER; ++j) {
     const int r = tid * PER + j;
     if (r >= RANGE) break;
-    int pos = at;
+    int pos = at + other[0][r];
     for (int w = 0; w < PLAN_WAVES; ++w) {
       const int n = count[w][r];
       count[w][r] = pos;
       pos += n;
     }
-    at = pos;
+    at += own[j];
   }
-  if ((int)blockIdx.x == ranges - 1 && tid == PLAN_THREADS - 1) *a.total = at;
+  if (range == ranges - 1 && first == 0 && tid == PLAN_THREADS - 1) *a.total = at;
   __syncthreads();
   for (int i0 = begin; i0 < end; i0 += 512) {
     long long k[8];
-    load(i0, k);
+    load(i0, end, k);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const bool mine = k[j] >= lo && k[j] < hi;
@@ -316,8 +335,10 @@ static hipError_t embed_backward_range(const EmbedArgs& a, hipStream_t s) {
   const long long pieces = (a.c.D + Piece<E, WIDE>::n - 1) / Piece<E, WIDE>::n, across = (pieces + 63) / 64;
   const long long items = ((a.c.N + EMBED_RUN - 1LL) / EMBED_RUN) * across;
   const int ranges = (a.c.V + RANGE - 1) / RANGE, clears = (a.c.V + CLEAR_ROWS - 1) / CLEAR_ROWS;
+  const int parts = max(1, min(min((a.c.N + PLAN_PART - 1) / PLAN_PART, PLAN_GROUPS / ranges), PLAN_PARTS));
   if (!launchable(items, 64 * JOIN_WAVES)) return TOO_LARGE;
-  hipLaunchKernelGGL((embed_plan_kernel<E, WIDE, RANGE>), dim3(ranges + clears), dim3(PLAN_THREADS), 0, s, a, ranges);
+  hipLaunchKernelGGL((embed_plan_kernel<E, WIDE, RANGE>), dim3(ranges * parts + clears), dim3(PLAN_THREADS), 0, s, a, ranges,
+                     parts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((embed_sum_kernel<E, WIDE>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
@@ -327,9 +348,12 @@ static hipError_t embed_backward_range(const EmbedArgs& a, hipStream_t s) {
 }
 template <typename E, bool WIDE>
 static hipError_t embed_backward_start(const EmbedArgs& a, hipStream_t s) {
-  // ranges that leave some hundred workgroups, each of which looks through all tokens
-  if (a.c.V <= 256 * 128) return embed_backward_range<E, WIDE, 128>(a, s);
-  if (a.c.V <= 256 * 512) return embed_backward_range<E, WIDE, 512>(a, s);
+  // Small ranges leave more workgroups, large ones more parts of many tokens.  Sort in us for ranges of 128 / 512 / 2048:
+  // 1000 tokens of 32768 8.0 / 8.1 / 10.2, of 131072 23.5 / 11.5 / 12.0; 16384 of 1000 8.7 / 9.3 / -, of 32768 14.9 / 9.6 / -, of
+  // 10^6 206 / 80 / 72; 65536 of 8192 21.3 / 16.3 / 17.7, of 32768 45 / 23.5 / 20.4, of 131072 - / 51 / 29.5; 262144 of 1000
+  // 52 / 53 / 59, of 8192 67 / 47 / 45, of 32768 158 / 72 / 51, of 131072 - / 180 / 79.
+  if (a.c.N <= 8192 && a.c.V <= 256 * 128) return embed_backward_range<E, WIDE, 128>(a, s);
+  if (a.c.V <= 16 * 512 || (a.c.N <= 32768 && a.c.V <= 256 * 512)) return embed_backward_range<E, WIDE, 512>(a, s);
   return embed_backward_range<E, WIDE, 2048>(a, s);
 }
 template <typename E>

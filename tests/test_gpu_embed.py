@@ -61,6 +61,15 @@ def test_lookup_and_gradient(dtype, N, V, D, pad):
     run(tokens, V, D, dtype, 2.5, pad)
 
 
+@pytest.mark.parametrize("N,V", [(8193, 1000), (30000, 20000), (40000, 129), (40000, 70000), (140001, 3000), (70000, 600000)])
+def test_parts_of_many_tokens(N, V):
+    """Several workgroups place the tokens of a range; the last part is short, or has waves with nothing."""
+    rng = np.random.default_rng(N)
+    tokens = np.minimum((V * rng.random(N) ** 3).astype(np.int64), V - 1)
+    tokens[rng.random(N) < 0.1] = -1
+    run(tokens, V, 3, "f32", 1.0, seed=N)
+
+
 @pytest.mark.parametrize("kind", ["same", "padding", "beyond", "last", "two", "rising", "falling"])
 @pytest.mark.parametrize("N", [1, 32, 33, 700, 9000])
 def test_tokens_of_every_kind(kind, N):
