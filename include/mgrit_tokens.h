@@ -127,8 +127,8 @@ MGRIT_API int ssm_workspace_bytes(const ssm_cfg* cfg, size_t* bytes);
 MGRIT_API int ssm_saved_bytes(const ssm_cfg* cfg, size_t* bytes);
 
 /* Forward.  h0[B,H,S] float or NULL (zeros); reset[T,B] bytes or NULL; y out; h_last[B,H,S] float out or NULL: h_T, the h0
- * of a call that goes on with the sequence (not h0 itself: MGRIT_E_SIZE).  saved: out or NULL: the states (float) that ssm_backward starts from,
- * 16-byte aligned. */
+ * of a call that goes on with the sequence (not h0 itself: MGRIT_E_SIZE).  saved: out or NULL: the states (float) that
+ * ssm_backward starts from, 16-byte aligned. */
 MGRIT_API int ssm_forward(const ssm_cfg* cfg, const ssm_inputs* in, const float* h0, const uint8_t* reset,
                           const glr_seq* y, float* h_last, void* saved, size_t saved_bytes, void* workspace,
                           size_t workspace_bytes, void* stream);

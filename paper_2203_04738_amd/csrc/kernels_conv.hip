@@ -146,7 +146,8 @@ __global__ __launch_bounds__(256) void conv_forward_kernel(ConvArgs a, int lanes
   const unsigned group = blockIdx.x / (unsigned)cols;
   const ConvPlace at(lanes, (int)(blockIdx.x - group * cols), a.c.H, VEC);
   const long long item = (long long)group * at.rows + at.row;
-  const bool run_exists = item < (long long)runs * a.c.B, has = at.has && run_exists;     // (all lanes of a run look at its resets)
+  // (all lanes of a run look at its resets)
+  const bool run_exists = item < (long long)runs * a.c.B, has = at.has && run_exists;
   const int b = run_exists ? (int)(item / runs) : 0, t0 = run_exists ? (int)(item - (long long)b * runs) * CONV_RUN : 0;
   const int ch = at.ch;
   ConvRaw<E, VEC> raw[CONV_RUN];

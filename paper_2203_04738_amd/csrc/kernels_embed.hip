@@ -349,8 +349,8 @@ static hipError_t embed_backward_range(const EmbedArgs& a, hipStream_t s) {
 template <typename E, bool WIDE>
 static hipError_t embed_backward_start(const EmbedArgs& a, hipStream_t s) {
   // Small ranges leave more workgroups, large ones more parts of many tokens.  Sort in us for ranges of 128 / 512 / 2048:
-  // 1000 tokens of 32768 8.0 / 8.1 / 10.2, of 131072 23.5 / 11.5 / 12.0; 16384 of 1000 8.7 / 9.3 / -, of 32768 14.9 / 9.6 / -, of
-  // 10^6 206 / 80 / 72; 65536 of 8192 21.3 / 16.3 / 17.7, of 32768 45 / 23.5 / 20.4, of 131072 - / 51 / 29.5; 262144 of 1000
+  // 1000 tokens of 32768 8.0 / 8.1 / 10.2, of 131072 23.5 / 11.5 / 12.0; 16384 of 1000 8.7 / 9.3 / -, of 32768 14.9 / 9.6 / -,
+  // of 10^6 206 / 80 / 72; 65536 of 8192 21.3 / 16.3 / 17.7, of 32768 45 / 23.5 / 20.4, of 131072 - / 51 / 29.5; 262144 of 1000
   // 52 / 53 / 59, of 8192 67 / 47 / 45, of 32768 158 / 72 / 51, of 131072 - / 180 / 79.
   if (a.c.N <= 8192 && a.c.V <= 256 * 128) return embed_backward_range<E, WIDE, 128>(a, s);
   if (a.c.V <= 16 * 512 || (a.c.N <= 32768 && a.c.V <= 256 * 512)) return embed_backward_range<E, WIDE, 512>(a, s);

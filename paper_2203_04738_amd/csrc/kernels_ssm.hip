@@ -509,8 +509,8 @@ __device__ inline void channel_sums(const float (&v)[2 * SP], float* out, int la
 
 // A tile of R steps goes forward again from its saved state, keeping the decays and the states before each step in registers,
 // and then back.  Instructions bound it (107 a wave and step, two waves a SIMD, a vector instruction in execution 94 % of
-// the time): 8192 x 4 x 1024 bf16, 16 states, 516 us as traced, 128 x 100 x 1000 floats 245.  Tiles of 8 steps: 16 leave room for
-// one wave a SIMD (755 us).  Of a step's instructions the states take 60 %, the sums over the channels 15 %: through LDS
+// the time): 8192 x 4 x 1024 bf16, 16 states, 500 us as traced, 128 x 100 x 1000 floats 240 to 260.  Tiles of 8 steps: 16 leave
+// room for one wave a SIMD (755 us).  Of a step's instructions the states take 60 %, the sums over the channels 15 %: through LDS
 // those took 576 against 549 us, on the matrix pipe (products with ones) the registers of the second wave (840).
 template <typename E, int SP, int R>
 __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
@@ -565,8 +565,8 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
   load(end);
   // the thread's place in the tile's sums (those i * SSM_THREADS behind it are of the same state): [col][T,B,2S]
   const int own = threadIdx.x % (8 * SP), own_n = own % (4 * SP) < S ? own / (4 * SP) * S + own % (4 * SP) : -1;
-  float* part_bc =
-      a.part_bc + (((long long)(blockIdx.x % (unsigned)a.s.cols) * a.c.T + end + threadIdx.x / (8 * SP)) * a.c.B + p.b) * (2 * S) + own_n;
+  const long long own_row = (long long)(blockIdx.x % (unsigned)a.s.cols) * a.c.T + end + threadIdx.x / (8 * SP);
+  float* part_bc = a.part_bc + (own_row * a.c.B + p.b) * (2 * S) + own_n;
   const long long row = 2LL * a.c.B * S;                // of a step
   float dskip = 0.f, dbias = 0.f;
   Resets looked;
@@ -793,7 +793,7 @@ SsmShape ssm_shape(const ssm_cfg& c, bool backward) {
   s.cols = (c.H + SSM_COLS - 1) / SSM_COLS;
   const long long across = (long long)s.cols * c.B, tiles = ((long long)c.T + SSM_TILE - 1) / SSM_TILE;
   long long chunks = 1;
-  // Chunks cost a second sweep and fill the card: with chunks : without, us, 1024 steps of bf16, 16 states, by workgroups across
+  // Chunks cost a second sweep and fill the card: with : without, us, 1024 steps of bf16, 16 states, by workgroups across
   // - forward: 130 88 : 135, 250 135 : 135, 320 168 : 187, 380 206 : 190, 510 252 : 193, 640 307 : 272, 770 400 : 332;
   // - backward: 130 194 : 327, 250 295 : 327, 320 363 : 466, 380 452 : 471, 510 548 : 471, 640 683 : 722, 770 914 : 899.
   // Then about four a CU (8192 x 4 x 1024: 768 to 2048 workgroups within 3 % of each other), of two tiles at least.
