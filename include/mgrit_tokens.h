@@ -16,7 +16,8 @@
  * overlap no other buffer of the call unless its comment says so, nothing kept in a workspace from call to call, a
  * workspace of 0 bytes may be NULL, others are 16-byte aligned, calls that share one are ordered on one stream.
  * Sums, states and statistics are float (a row's loss double); a result is rounded once, to nearest, when it is stored.
- * A call whose launches would take 2^32 threads or more is refused with MGRIT_E_SIZE.
+ * A call whose launches would take 2^32 threads or more is refused with MGRIT_E_SIZE, and so is one over sequences or rows
+ * of which one that is written begins where another begins.
  */
 #ifndef MGRIT_TOKENS_H
 #define MGRIT_TOKENS_H

@@ -1,11 +1,19 @@
 // C ABI of the operators of a recurrent student over tokens (include/mgrit_tokens.h): arguments are checked on the host
 // before anything is launched.
 #include <cmath>
+#include <initializer_list>
 
 #include "checks.h"
 #include "tokens.h"
 
 namespace mg {
+
+// Whether a buffer that is written begins where another of the call does.
+static bool begins_as(const void* out, std::initializer_list<const void*> others) {
+  for (const void* p : others)
+    if (out && out == p) return true;
+  return false;
+}
 
 // ---- embedding
 static int embed_check(const embed_cfg* c) {
@@ -106,6 +114,7 @@ int embed_lookup(const embed_cfg* cfg, const int64_t* tokens, const void* table,
   if (rc) return rc;
   if (!tokens || !table || !out) return MGRIT_E_NULL;
   if (off(tokens, 8) || off(table, elem_bytes(cfg->dtype)) || off(out, elem_bytes(cfg->dtype))) return MGRIT_E_ALIGN;
+  if (begins_as(out, {table, tokens})) return MGRIT_E_SIZE;
   EmbedArgs a{};
   a.c = *cfg;
   a.tokens = tokens;
@@ -131,6 +140,7 @@ int embed_backward(const embed_cfg* cfg, const int64_t* tokens, const void* dout
   if (off(tokens, 8) || off(dout, elem_bytes(cfg->dtype)) || off(dtable, elem_bytes(cfg->dtype)) || off16(workspace))
     return MGRIT_E_ALIGN;
   if (workspace_bytes < embed_workspace(*cfg)) return MGRIT_E_WORKSPACE;
+  if (begins_as(dtable, {dout, tokens, workspace})) return MGRIT_E_SIZE;
   EmbedArgs a{};
   a.c = *cfg;
   a.tokens = tokens;
@@ -147,7 +157,7 @@ int causal_conv_forward(const conv_cfg* cfg, const glr_seq* x, const float* weig
   if ((rc = seq_check(*cfg, x, false)) || (rc = seq_check(*cfg, y, true))) return rc;
   if (!weight) return MGRIT_E_NULL;
   if (off(weight, 4) || off(bias, 4) || off(past, 4) || off(last, 4)) return MGRIT_E_ALIGN;
-  if (cfg->W > 1 && last && last == past) return MGRIT_E_SIZE;
+  if (begins_as(y->data, {x->data}) || (cfg->W > 1 && begins_as(last, {past}))) return MGRIT_E_SIZE;
   ConvArgs a{};
   a.c = *cfg;
   a.x = *x;
@@ -181,8 +191,8 @@ int causal_conv_backward(const conv_cfg* cfg, const glr_seq* x, const float* wei
   if (off(weight, 4) || off(bias, 4) || off(past, 4) || off(dlast, 4) || off(dweight, 4) || off(dbias, 4) ||
       off(dpast, 4) || off16(workspace))
     return MGRIT_E_ALIGN;
-  if (cfg->W > 1 && dpast && dpast == dlast) return MGRIT_E_SIZE;
   if (workspace_bytes < conv_workspace(*cfg)) return MGRIT_E_WORKSPACE;
+  if (begins_as(dx->data, {x->data, dy->data}) || (cfg->W > 1 && begins_as(dpast, {dlast, past}))) return MGRIT_E_SIZE;
   ConvArgs a{};
   a.c = *cfg;
   a.x = *x;
@@ -244,9 +254,10 @@ int ssm_forward(const ssm_cfg* cfg, const ssm_inputs* in, const float* h0, const
   if (rc) return rc;
   if ((rc = ssm_inputs_check(*cfg, in)) || (rc = seq_check(*cfg, y, true))) return rc;
   if (off(h0, 4) || off(h_last, 4) || off16(saved)) return MGRIT_E_ALIGN;
-  if (h_last && h_last == h0) return MGRIT_E_SIZE;
   if ((rc = ssm_space(*cfg, workspace, workspace_bytes))) return rc;
   if (saved && saved_bytes < ssm_saved(*cfg)) return MGRIT_E_WORKSPACE;
+  if (begins_as(y->data, {in->x.data, in->dt.data, in->b.data, in->c.data, in->z.data}) || begins_as(h_last, {h0}))
+    return MGRIT_E_SIZE;
   SsmArgs a = ssm_args(*cfg, *in, reset);
   a.h0 = h0;
   a.y = *y;
@@ -268,9 +279,17 @@ int ssm_backward(const ssm_cfg* cfg, const ssm_inputs* in, const uint8_t* reset,
   if (out->dz.data && (rc = seq_check(*cfg, &out->dz, true))) return rc;
   if (off16(saved) || off(dh_last, 4) || off(out->da, 4) || off(out->dskip, 4) || off(out->dbias, 4) || off(out->dh0, 4))
     return MGRIT_E_ALIGN;
-  if (out->dh0 && out->dh0 == dh_last) return MGRIT_E_SIZE;
   if ((rc = ssm_space(*cfg, workspace, workspace_bytes))) return rc;
   if (saved_bytes < ssm_saved(*cfg)) return MGRIT_E_WORKSPACE;
+  const void* read[] = {in->x.data, in->dt.data, in->b.data, in->c.data, in->z.data, dy->data};
+  const void* written[] = {out->dx.data, out->ddt.data, out->db.data, out->dc.data, out->dz.data};
+  for (int i = 0; i < 5; ++i) {
+    for (const void* p : read)
+      if (begins_as(written[i], {p})) return MGRIT_E_SIZE;
+    for (int j = 0; j < i; ++j)
+      if (begins_as(written[i], {written[j]})) return MGRIT_E_SIZE;
+  }
+  if (begins_as(out->dh0, {dh_last})) return MGRIT_E_SIZE;
   SsmArgs a = ssm_args(*cfg, *in, reset);
   a.saved = (float*)const_cast<void*>(saved);
   a.dy = *dy;

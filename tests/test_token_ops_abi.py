@@ -193,6 +193,46 @@ def test_scan_refusals():
     assert step(state=P + 2) == ALIGN and step(slots=P + 2) == ALIGN and step(y=seq(P, 0, 7)) == SIZE
 
 
+def test_a_result_that_begins_where_another_array_does_is_refused():
+    """All other arguments are right: without the refusal the call would try to launch."""
+    L, at = tk._lib(), [1 << 20]
+
+    def new():
+        at[0] += 1 << 20
+        return at[0]
+
+    cfg = mg.EmbedCfg(4, 5, 8)
+    p = new()
+    assert L.embed_lookup(ref(cfg), new(), p, p, None) == SIZE
+    assert L.embed_backward(ref(cfg), new(), p, p, new(), BIG, None) == SIZE
+    assert L.embed_backward(ref(cfg), new(), new(), p, p, BIG, None) == SIZE
+    cfg = mg.ConvCfg(5, 2, 8, 4)
+    assert L.causal_conv_forward(ref(cfg), seq(p), new(), None, None, None, seq(p), None, None) == SIZE
+    for x, dy in ((p, new()), (new(), p)):
+        assert L.causal_conv_backward(ref(cfg), seq(x), new(), None, None, None, seq(dy), None, seq(p), new(), None, None, new(),
+                                      BIG, None) == SIZE
+    assert L.causal_conv_backward(ref(cfg), seq(new()), new(), None, p, None, seq(new()), None, seq(new()), new(), None, p, new(),
+                                  BIG, None) == SIZE
+    cfg, names = mg.SsmCfg(100, 2, 8, 8), ("x", "dt", "b", "c", "z")
+
+    def group(cls, **other):
+        g = cls()
+        for n in names:
+            name = "d" + n if cls is tk.SsmGrads else n
+            setattr(g, name, ops.GlrSeq(other.get(n) or new(), 16, 8))
+        if cls is tk.SsmGrads:
+            g.da = new()
+        else:
+            g.a = new()
+        return g
+
+    for n in names:
+        assert L.ssm_forward(ref(cfg), ref(group(tk.SsmInputs, **{n: p})), None, None, seq(p), None, None, 0, new(), BIG, None) == SIZE
+        for inputs_, dy, out in ((dict(x=p), new(), {n: p}), ({}, p, {n: p}), ({}, new(), {n: p, "x" if n != "x" else "z": p})):
+            assert L.ssm_backward(ref(cfg), ref(group(tk.SsmInputs, **inputs_)), None, new(), BIG, seq(dy), None,
+                                  ref(group(tk.SsmGrads, **out)), new(), BIG, None) == SIZE
+
+
 def test_policy_refusals():
     L = tk._lib()
 
