@@ -93,6 +93,7 @@ MGRIT_API int causal_conv_step(const conv_cfg* cfg, const glr_seq* x, const floa
  * b_t and c_t the same for all channels of a batch row, a, bias and skip of each channel.
  * a <= 0 is a decay; it is not enforced.  a > 0 can carry exp(d a), or its product over some steps, beyond the floats,
  * where a state that is not zero becomes infinite or NaN.  An infinite state may be NaN later.
+ * a = -infinity forgets at every step; ssm_backward needs finite ones (others leave NaN).
  * A step whose `reset` byte is not zero forgets the past: h_t = d_t b_t x_t, whatever h_{t-1} was, and no gradient
  * passes to the steps before it.
  */

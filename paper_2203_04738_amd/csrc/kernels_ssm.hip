@@ -322,6 +322,8 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
         float part[4];
         auto step = [&](auto j_) SSM_INLINE {
           constexpr int j = decltype(j_)::value;
+          part[j] = 0.f;
+          if (!PLAIN && ts + j >= a.c.T) return;      // (an infinite a would leave no number of d = 0)
           const float dj = quad_of<j>(delta), xj = quad_of<j>(dx);
           const bool cut = !PLAIN && (resets >> (4 * g + j) & 1);
           float b[SP], c[SP];

@@ -164,6 +164,17 @@ def test_infinities_before_a_reset_stay_there():
         close(got[45:], w[k], 2.0 ** -24, GRAD_TOL, k)
 
 
+@pytest.mark.parametrize("T", [1, 15, 16, 17, 700])
+def test_an_infinite_decay_forgets_at_every_step(T):
+    d, dev = problem(21, T, 2, 20, 5)
+    dev["a"][::2, ::2] = float("-inf")
+    d["a"][::2, ::2] = -np.inf
+    _, _, _, y, h_last = forward(dev, T, 2, 20, 5)
+    want, states, _ = orc.ssm_forward(*(d[k] for k in INPUTS[:6]), skip=d["skip"], bias=d["bias"], h0=d["h0"])
+    close(y, want, 2.0 ** -24, TOL, "y")
+    close(h_last, states[-1], 0, TOL, "h_last")
+
+
 def test_steps_so_large_or_small_that_exponentials_leave_the_floats():
     # d a down to -1e4 (a state that is forgotten at once) and to -1e-9 (one that stays), d down to e^-60
     T, B, H, S = 40, 1, 12, 16
