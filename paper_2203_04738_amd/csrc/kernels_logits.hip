@@ -1038,30 +1038,40 @@ __global__ __launch_bounds__(64) void policy_join_kernel(PolicyRows a) {
   if (threadIdx.x == 0)
     put_policy(a, row, policy_row<E>(a, row, (const E*)a.d.logits + row * a.d.ld, st.m, st.s, t), st.m, st.s);
 }
-// Gradient of a row, or of a segment of one, from its statistics.
-template <typename E, int NW>
+// Gradient of a row, or of a segment of one, from its statistics.  In place (WHOLE) a team goes through all segments of its row:
+// the slope needs the token's logit, which another team would have overwritten.
+template <typename E, int NW, bool WHOLE = false>
 __global__ __launch_bounds__((TeamOf<E, NW>::block)) void policy_grad_kernel(PolicyRows a) {
   using T = TeamOf<E, NW>;
   __shared__ Teacher teachers[T::teams];
   __shared__ float weights[T::teams];
   const int team = NW == 1 ? threadIdx.x >> 6 : 0, tid = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
   const long long item = (long long)blockIdx.x * T::teams + team;
-  const long long row = item / a.d.shape.segs;
-  const int seg = (int)(item - row * a.d.shape.segs);
+  const int segs = a.d.shape.segs;
+  const long long row = WHOLE ? item : item / segs;
   if (row >= a.d.N) return;
   Teacher& t = teachers[team];
   const E* x = (const E*)a.d.logits + row * a.d.ld;
-  const int begin = seg * a.d.shape.seg * T::per_load - row_shift(x);
-  const int lo = max(begin, 0), hi = (int)min((long long)a.d.V, begin + (long long)a.d.shape.seg * T::per_load);
-  Held<E, NW> held;
-  held.load(x, lo, hi, lo - begin, tid);
   const float m = a.d.stats_in[2 * row], s = a.d.stats_in[2 * row + 1];
-  if (tid == 0) weights[team] = policy_weight(a, row, policy_row<E>(a, row, x, m, s, t).slope);
-  team_sync<NW>();
   E* out = (E*)a.d.dlogits + row * a.d.ld_grad;
-  const float w = weights[team];
-  if (t.total == 0.f || w == 0.f) put_zeros(out, lo, hi, tid, T::threads);
-  else put_gradient<E, NW>(a.d, held, out, lo, hi, m, s, w, t, tid);
+  auto segment = [&](int seg, bool first) __attribute__((always_inline)) {
+    const int begin = seg * a.d.shape.seg * T::per_load - row_shift(x);
+    const int lo = max(begin, 0), hi = (int)min((long long)a.d.V, begin + (long long)a.d.shape.seg * T::per_load);
+    Held<E, NW> held;
+    held.load(x, lo, hi, lo - begin, tid);
+    if (first) {
+      if (tid == 0) weights[team] = policy_weight(a, row, policy_row<E>(a, row, x, m, s, t).slope);
+      team_sync<NW>();
+    }
+    const float w = weights[team];
+    if (t.total == 0.f || w == 0.f) put_zeros(out, lo, hi, tid, T::threads);
+    else put_gradient<E, NW>(a.d, held, out, lo, hi, m, s, w, t, tid);
+  };
+  if constexpr (WHOLE) {
+    for (int seg = 0; seg < segs; ++seg) segment(seg, seg == 0);
+  } else {
+    segment((int)(item - row * segs), true);
+  }
 }
 
 // ---- launches
@@ -1289,9 +1299,13 @@ static hipError_t policy_grad_start(const PolicyArgs& a, const float* stats, hip
       p.d.shape = {1, TeamOf<E, 16>::chunks};
       hipLaunchKernelGGL((policy_grad_kernel<E, 16>), dim3(N), dim3(1024), 0, s, p);
       break;
-    default:
+    default: {
       p.d.shape = segments(a.c.V, sizeof(E), aligned);
-      hipLaunchKernelGGL((policy_grad_kernel<E, 16>), dim3(N * (unsigned)p.d.shape.segs), dim3(1024), 0, s, p);
+      if (a.dlogits == a.logits)
+        hipLaunchKernelGGL((policy_grad_kernel<E, 16, true>), dim3(N), dim3(1024), 0, s, p);
+      else
+        hipLaunchKernelGGL((policy_grad_kernel<E, 16>), dim3(N * (unsigned)p.d.shape.segs), dim3(1024), 0, s, p);
+    }
   }
   return hipGetLastError();
 }

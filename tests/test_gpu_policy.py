@@ -99,6 +99,19 @@ def test_in_place_padded_and_without_weights(V):
     compare(d, rows, grad, "bf16", 1.0, 0.05)
 
 
+@pytest.mark.parametrize("dtype,V", [("f32", 70001), ("bf16", 70000), ("f32", 3000)])
+@pytest.mark.parametrize("apart", [False, True])
+def test_many_long_rows_in_place_are_those_of_a_place_of_their_own(dtype, V, apart):
+    """The slope of a row needs its token's logit, which is overwritten: it has to be read before, also where a row is cut up."""
+    d, dev = problem(3, 200, V, dtype, 1.0)
+    dev["tok"] %= 4000
+    dev["old"].zero_().add_(-11)
+    rows, grad = call(dev, dtype, 1.0, 0.05, apart)
+    again, place = call(dev, dtype, 1.0, 0.05, apart, inplace=True)
+    for a, b in zip(rows + [grad], again + [place]):
+        assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(nan=0.0), b.nan_to_num(nan=0.0))
+
+
 @pytest.mark.parametrize("V", [30, 3000, 50000])
 @pytest.mark.parametrize("beta", [0.0, 0.1])
 def test_rows_that_masks_tokens_and_values_leave_empty(V, beta):

@@ -414,9 +414,10 @@ def call(runtime, entry, *sizes, **env):
     ("policy_loss", (100, 51), ["policy_kernel<float, 1>"]),
     ("policy_loss", (8, 8192), ["policy_kernel<float, 4>"]),
     ("policy_loss", (8, 32768, 1), ["policy_kernel<mg::Bf16, 16>"]),
-    ("policy_loss", (64, 50000), ["distill_segment_kernel<float>", "policy_join_kernel<float>", "policy_grad_kernel<float, 16>"]),
-    ("policy_loss_backward", (64, 500), ["policy_grad_kernel<float, 1>"]),
-    ("policy_loss_backward", (64, 50000, 1), ["policy_grad_kernel<mg::Bf16, 16>"])])
+    ("policy_loss", (64, 50000), ["distill_segment_kernel<float>", "policy_join_kernel<float>",
+                                  "policy_grad_kernel<float, 16, false>"]),
+    ("policy_loss_backward", (64, 500), ["policy_grad_kernel<float, 1, false>"]),
+    ("policy_loss_backward", (64, 50000, 1), ["policy_grad_kernel<mg::Bf16, 16, false>"])])
 def test_kernels_of_a_call_and_launches_that_fail(runtime, entry, sizes, kernels):
     rc, got = call(runtime, entry, *sizes)
     names = [name.replace("void mg::", "mg::") for _, name in got]
