@@ -173,7 +173,7 @@ MGRIT_API int policy_loss(const logits_cfg* cfg, const policy_cfg* rule, const v
                           const float* old_logp, const float* ref_logp, const float* advantage, const float* weight,
                           float* loss, float* logp, float* ratio, float* kl, float* stats, void* dlogits,
                           void* workspace, size_t workspace_bytes, void* stream);
-/* The gradient alone, where dL/dloss (dloss[N], or NULL: ones) is known later; stats from policy_loss. */
+/* The gradient alone, where dL/dloss (dloss[N], or NULL: ones) is known later; stats from policy_loss, dlogits as there. */
 MGRIT_API int policy_loss_backward(const logits_cfg* cfg, const policy_cfg* rule, const void* logits,
                                    const int64_t* tokens, const float* old_logp, const float* ref_logp,
                                    const float* advantage, const float* stats, const float* dloss, void* dlogits,

@@ -341,6 +341,12 @@ int policy_loss(const logits_cfg* cfg, const policy_cfg* rule, const void* logit
   if (!loss) return MGRIT_E_NULL;
   if (off(loss, 4) || off(logp, 4) || off(ratio, 4) || off(kl, 4) || off(stats, 4)) return MGRIT_E_ALIGN;
   if ((rc = logits_space(policy_space_cfg(*cfg), workspace, workspace_bytes))) return rc;
+  const void* rows[] = {loss, logp, ratio, kl, stats};
+  for (int i = 0; i < 5; ++i) {
+    if (begins_as(rows[i], {logits, tokens, old_logp, ref_logp, advantage, weight, dlogits})) return MGRIT_E_SIZE;
+    for (int j = 0; j < i; ++j)
+      if (begins_as(rows[i], {rows[j]})) return MGRIT_E_SIZE;
+  }
   PolicyArgs a{*cfg, *rule, logits, tokens, old_logp, ref_logp, advantage, weight, loss, logp, ratio, kl, stats, nullptr,
                dlogits, (char*)workspace};
   (void)hipGetLastError();

@@ -231,6 +231,14 @@ def test_a_result_that_begins_where_another_array_does_is_refused():
         for inputs_, dy, out in ((dict(x=p), new(), {n: p}), ({}, p, {n: p}), ({}, new(), {n: p, "x" if n != "x" else "z": p})):
             assert L.ssm_backward(ref(cfg), ref(group(tk.SsmInputs, **inputs_)), None, new(), BIG, seq(dy), None,
                                   ref(group(tk.SsmGrads, **out)), new(), BIG, None) == SIZE
+    cfg, rule = mg.LogitsCfg(4, 100, 0), mg.PolicyCfg()
+    names = ("logits", "tok", "old", "ref", "adv", "w", "loss", "logp", "ratio", "kl", "stats", "grad")
+    for k in names[6:11]:
+        for other in names:
+            a = {n: new() for n in names}
+            a[k] = a[other]
+            if k != other:
+                assert L.policy_loss(ref(cfg), ref(rule), *(a[n] for n in names), None, 0, None) == SIZE, (k, other)
 
 
 def test_policy_refusals():
