@@ -216,7 +216,7 @@ struct ConvBack {
       if (a.c.act == CONV_SILU) {
         const float p = taps.apply(win, xv, c);
         const Sigmoid s(p);
-        dp *= s.s * fmaf(p, s.n, 1.f);
+        dp *= s.s * fmaf(gate_factor(p), s.n, 1.f);
       }
 #pragma unroll
       for (int k = 0; k < WT; ++k) {

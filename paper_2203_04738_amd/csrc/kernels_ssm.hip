@@ -603,7 +603,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
         delta[g] = in ? sp.d : 0.f;
         slope[g] = sp.slope(v);
         dy[g] = in && p.has ? elem_f32(yr[g]) : 0.f;
-        z[g] = in && gated ? elem_f32(zr[g]) : 1.f;
+        z[g] = in && gated ? gate_factor(elem_f32(zr[g])) : 1.f;
         sz[g] = gated ? Sigmoid(z[g]).s : 1.f;
       }
       float keep[R][SP], past[R][SP], sum[G];

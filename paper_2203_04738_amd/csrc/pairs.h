@@ -87,5 +87,7 @@ struct Sigmoid {
     n = e * s;
   }
 };
-__device__ inline float silu(float z) { return z * Sigmoid(z).s; }
+// z as a factor of sigmoid(z), which is not quite 0 below -88: the lowest value of a type times that would be far from 0.
+__device__ inline float gate_factor(float z) { return z < -104.f ? -104.f : z; }
+__device__ inline float silu(float z) { return gate_factor(z) * Sigmoid(z).s; }
 }  // namespace mg

@@ -94,6 +94,16 @@ def test_long_and_many_rows():
     run(*problem(5, 400, 40, 6, 4, "bf16", resets=0.02), 400, 40, 6, 4, "bf16")
 
 
+@pytest.mark.parametrize("low", [-3e38, -1e30, -200.0])
+def test_the_activation_of_the_lowest_values_is_0(low):
+    """p sigmoid(p) and its slope are 0 to within 1e-36 from p = -89 on, whatever p."""
+    d, dev = problem(31, 50, 2, 24, 4, "f32")
+    dev["bias"][::3] = low
+    d["bias"] = dev["bias"].double().cpu().numpy()
+    y, _, dx, dw, db, _ = run(d, dev, 50, 2, 24, 4, "f32")
+    assert (y[..., ::3].abs() <= 1e-30).all() and (dw[::3].abs() <= 1e-30).all() and (db[::3].abs() <= 1e-30).all()
+
+
 def test_what_a_reset_forgets_may_be_anything():
     T, B, H, W = 40, 2, 10, 4
     d, dev = problem(9, T, B, H, W, "f32")

@@ -164,6 +164,21 @@ def test_infinities_before_a_reset_stay_there():
         close(got[45:], w[k], 2.0 ** -24, GRAD_TOL, k)
 
 
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_gates_of_the_lowest_value_are_closed(dtype):
+    """z sigmoid(z) is 0 to within 1e-36 from z = -89 on, down to the type's lowest value, and so is its slope."""
+    T, B, H, S = 40, 2, 20, 8
+    d, dev = problem(22, T, B, H, S, dtype)
+    low = torch.finfo(TYPES[dtype][1]).min
+    for t, v in ((3, low), (4, low / 2), (11, -1000.0), (12, -120.0), (39, low)):
+        dev["z"][t] = v
+        d["z"][t] = dev["z"][t].double().cpu().numpy()
+    with np.errstate(over="ignore"):
+        y, _, g = run(d, dev, T, B, H, S, dtype)
+    for t in (3, 4, 11, 12, 39):
+        assert (y[t].abs() <= 1e-30).all() and (g["dz"][t].abs() <= 1e-30).all()
+
+
 @pytest.mark.parametrize("T", [1, 15, 16, 17, 700])
 def test_an_infinite_decay_forgets_at_every_step(T):
     d, dev = problem(21, T, 2, 20, 5)
