@@ -1,12 +1,12 @@
 // Embedding of tokens and the gradient of its table (include/mgrit_tokens.h).
 //
-// The gradient sorts: a workgroup owns a range of the vocabulary and looks through all tokens of the call twice.  The
-// first time it counts those below its range, which is where its own will stand, and, per wave, those of each of its
-// own tokens; the second time every wave puts the places of its part behind those of the waves before it.  (Of many tokens
-// several workgroups of the range each place a part, having counted all.)  Places are therefore in order of token and place,
-// whatever runs first.  Other workgroups of the launch, which waits for its loads most of the time, clear the table meanwhile.
-// Then a wave adds up a block of sorted places, however they fall into runs of one token, so that a token that is half of all
-// takes no longer than many; sums of runs that cross blocks meet in a third launch.
+// The gradient sorts: a workgroup owns a range of the vocabulary and looks through all tokens of the call twice.  The first
+// time it counts those below its range, which is where its own will stand, and, per wave, those of each of its own tokens;
+// the second time every wave puts the places of its part behind those of the waves before it.  (Of many tokens several
+// workgroups of the range each place a part, having counted all.)  Places are therefore in order of token and place,
+// whatever runs first.  Other workgroups of the launch, which waits for its loads most of the time, clear the table
+// meanwhile. Then a wave adds up a block of 8 or 32 sorted places, however they fall into runs of one token, so that a token
+// that is half of all takes no longer than many; sums of runs that cross blocks meet in a third launch.
 //
 // 16384 tokens, most of them few, of 32768 x 1024 bf16: sort and clearing (64 MB) 14.5 us, sums (34 MB read) 12, join 6; lookup
 // 67 MB in 10.8 us.  The sort takes 9.6 us of it, most of them waiting for tokens that all its workgroups look at.
@@ -201,19 +201,20 @@ __global__ __launch_bounds__(PLAN_THREADS) void embed_plan_kernel(EmbedArgs a, i
   }
 }
 
-// ---- gradient: sums of a block of sorted places, in one wave per 64 pieces of the width, 16 rows under way (8: 12.6 us)
-template <typename E, bool WIDE>
+// ---- gradient: sums of a block of RUN sorted places, in one wave per 64 pieces of the width, up to 16 rows under way (8 of 32:
+// 12.6 us)
+template <typename E, bool WIDE, int RUN>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a) {
   using P = Piece<E, WIDE>;
-  constexpr int AHEAD = 16;
+  constexpr int AHEAD = RUN < 16 ? RUN : 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int pieces = (a.c.D + P::n - 1) / P::n, across = (pieces + 63) / 64;
   const long long item = (long long)blockIdx.x * 4 + wave;
   const int block = (int)(item / across), piece = (int)(item - (long long)block * across) * 64 + lane;
   const int M = *a.total;
-  const int first = block * EMBED_RUN;
+  const int first = block * RUN;
   if (first >= M) return;
-  const int n = min(EMBED_RUN, M - first), col = min(piece, pieces - 1) * P::n;
+  const int n = min(RUN, M - first), col = min(piece, pieces - 1) * P::n;
   const bool has = piece < pieces;
   // a lane for each place: its token, and whether its run ends there
   const int i = first + min(lane, n - 1);
@@ -270,17 +271,17 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void embed_join_kernel(EmbedArgs a
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int pieces = (a.c.D + P::n - 1) / P::n, across = (pieces + 63) / 64;
   const int block = blockIdx.x / across, piece = (blockIdx.x - block * across) * 64 + lane;
-  const int M = *a.total;
+  const int M = *a.total, run = a.run;
   const int tok = a.crosses[block];                  // (anything, where no place of the block is used)
-  if ((block + 1LL) * EMBED_RUN >= M || tok < 0) return;
+  if ((block + 1LL) * run >= M || tok < 0) return;
   // blocks behind this one that begin with the token
-  const int blocks = (int)((M + EMBED_RUN - 1LL) / EMBED_RUN);
+  const int blocks = (int)((M + run - 1LL) / run);
   int end = blocks;
   for (int b0 = block + 1; b0 < blocks; b0 += 64 * JOIN_WAVES) {
     if (threadIdx.x == 0) found = blocks;
     __syncthreads();
     const int b = b0 + threadIdx.x;
-    if (b < blocks && a.token[(long long)b * EMBED_RUN] != tok) atomicMin(&found, b);
+    if (b < blocks && a.token[(long long)b * run] != tok) atomicMin(&found, b);
     __syncthreads();
     end = found;
     __syncthreads();
@@ -317,9 +318,13 @@ static bool wide_rows(const void* p, long long ld, int D, int size) {
   return (uintptr_t)p % 16 == 0 && ld * size % 16 == 0 && (long long)D * size % 16 == 0;
 }
 static size_t embed_piece(size_t n) { return (n + 255) / 256 * 256; }
+// Sorted places that a wave adds up: few make the sums of few tokens short, but leave more to join.  Both directions, us,
+// runs of 8 / 16 / 32: 1003 tokens of 32768 x 1024 bf16 24.1 / 25.4 / 26.8, of 50021 x 500 floats 26.9 / 27.8 / 29.0; 4096
+// 28.7 / 29.5 / 30.9, 30.1 / 31.2 / 32.7; 16384 45.4 / 42.9 / 42.8, 47.2 / 46.1 / 46.3.
+static int embed_run(int N) { return N <= 4096 ? 8 : 32; }
 // The total, places, tokens, runs that cross blocks, sums.
 size_t embed_workspace(const embed_cfg& c) {
-  const size_t N = (size_t)c.N, blocks = (N + EMBED_RUN - 1) / EMBED_RUN;
+  const size_t N = (size_t)c.N, blocks = (N + embed_run(c.N) - 1) / embed_run(c.N);
   return 256 + 2 * embed_piece(4 * N) + embed_piece(4 * blocks) + 8 * blocks * c.D;
 }
 template <typename E, bool WIDE>
@@ -333,7 +338,7 @@ static hipError_t embed_lookup_start(const EmbedArgs& a, hipStream_t s) {
 template <typename E, bool WIDE, int RANGE>
 static hipError_t embed_backward_range(const EmbedArgs& a, hipStream_t s) {
   const long long pieces = (a.c.D + Piece<E, WIDE>::n - 1) / Piece<E, WIDE>::n, across = (pieces + 63) / 64;
-  const long long items = ((a.c.N + EMBED_RUN - 1LL) / EMBED_RUN) * across;
+  const long long items = ((a.c.N + a.run - 1LL) / a.run) * across;
   const int ranges = (a.c.V + RANGE - 1) / RANGE, clears = (a.c.V + CLEAR_ROWS - 1) / CLEAR_ROWS;
   const int parts = max(1, min(min((a.c.N + PLAN_PART - 1) / PLAN_PART, PLAN_GROUPS / ranges), PLAN_PARTS));
   if (!launchable(items, 64 * JOIN_WAVES)) return TOO_LARGE;
@@ -341,8 +346,10 @@ static hipError_t embed_backward_range(const EmbedArgs& a, hipStream_t s) {
                      parts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((embed_sum_kernel<E, WIDE>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
-  if ((e = hipGetLastError()) != hipSuccess || a.c.N <= EMBED_RUN) return e;
+  const dim3 groups((unsigned)((items + 3) / 4));
+  if (a.run == 8) hipLaunchKernelGGL((embed_sum_kernel<E, WIDE, 8>), groups, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((embed_sum_kernel<E, WIDE, 32>), groups, dim3(256), 0, s, a);
+  if ((e = hipGetLastError()) != hipSuccess || a.c.N <= a.run) return e;
   hipLaunchKernelGGL((embed_join_kernel<E, WIDE>), dim3((unsigned)items), dim3(64 * JOIN_WAVES), 0, s, a);
   return hipGetLastError();
 }
@@ -370,6 +377,7 @@ static hipError_t embed_typed(const EmbedArgs& a, bool backward, hipStream_t s) 
 }
 hipError_t launch_embed_lookup(const EmbedArgs& a, hipStream_t s) { return embed_typed(a, false, s); }
 hipError_t launch_embed_backward(EmbedArgs a, char* ws, hipStream_t s) {
+  a.run = embed_run(a.c.N);
   a.total = (int*)ws;
   ws += 256;
   a.place = (int*)ws;
@@ -377,7 +385,7 @@ hipError_t launch_embed_backward(EmbedArgs a, char* ws, hipStream_t s) {
   a.token = (int*)ws;
   ws += embed_piece(4 * (size_t)a.c.N);
   a.crosses = (int*)ws;
-  ws += embed_piece(4 * (((size_t)a.c.N + EMBED_RUN - 1) / EMBED_RUN));
+  ws += embed_piece(4 * (((size_t)a.c.N + a.run - 1) / a.run));
   a.part = (float*)ws;
   return embed_typed(a, true, s);
 }

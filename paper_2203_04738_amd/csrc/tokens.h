@@ -6,17 +6,17 @@
 namespace mg {
 
 // ---- embedding (kernels_embed.hip)
-constexpr int EMBED_RUN = 32;                        // sorted places that a wave adds up
 struct EmbedArgs {
   embed_cfg c;
   const int64_t* tokens;
   const void* in;           // table, or dout
   void* out;                // out, or dtable
+  int run;                  // sorted places that a wave adds up: a block
   int* total;               // tokens that name a row
   int* place;               // [N]: places of the tokens in order of token and place
   int* token;               // [N]: their tokens
-  int* crosses;             // [ceil(N / EMBED_RUN)]: the token of a run that begins in the block and goes on, or -1
-  float* part;              // [ceil(N / EMBED_RUN)][2][D]: sums of runs that go on beyond their block
+  int* crosses;             // [ceil(N / run)]: the token of a run that begins in the block and goes on, or -1
+  float* part;              // [ceil(N / run)][2][D]: sums of runs that go on beyond their block
 };
 size_t embed_workspace(const embed_cfg& c);
 hipError_t launch_embed_lookup(const EmbedArgs& a, hipStream_t s);

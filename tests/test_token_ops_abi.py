@@ -398,10 +398,12 @@ def call(runtime, entry, *sizes, **env):
 @pytest.mark.parametrize("entry,sizes,kernels", [
     ("embed_lookup", (8, 100, 64), ["embed_lookup_kernel<float, true>"]),
     ("embed_lookup", (8, 100, 63, 1), ["embed_lookup_kernel<mg::Bf16, false>"]),
-    ("embed_backward", (32, 100, 64), ["embed_plan_kernel<float, true, 128>", "embed_sum_kernel<float, true>"]),
-    ("embed_backward", (33, 32769, 64, 1), ["embed_plan_kernel<mg::Bf16, true, 512>", "embed_sum_kernel<mg::Bf16, true>",
+    ("embed_backward", (8, 100, 64), ["embed_plan_kernel<float, true, 128>", "embed_sum_kernel<float, true, 8>"]),
+    ("embed_backward", (8193, 100, 64), ["embed_plan_kernel<float, true, 512>", "embed_sum_kernel<float, true, 32>",
+                                         "embed_join_kernel<float, true>"]),
+    ("embed_backward", (33, 32769, 64, 1), ["embed_plan_kernel<mg::Bf16, true, 512>", "embed_sum_kernel<mg::Bf16, true, 8>",
                                             "embed_join_kernel<mg::Bf16, true>"]),
-    ("embed_backward", (33, 131073, 3, 4), ["embed_plan_kernel<mg::F16, false, 2048>", "embed_sum_kernel<mg::F16, false>",
+    ("embed_backward", (33, 131073, 3, 4), ["embed_plan_kernel<mg::F16, false, 2048>", "embed_sum_kernel<mg::F16, false, 8>",
                                             "embed_join_kernel<mg::F16, false>"]),
     ("causal_conv_forward", (100, 2, 130, 4), ["conv_forward_kernel<float, 2, 4>"]),
     ("causal_conv_forward", (100, 2, 33, 1, 0, 1), ["conv_forward_kernel<mg::Bf16, 1, 8>"]),
