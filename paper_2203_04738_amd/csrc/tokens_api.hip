@@ -228,6 +228,7 @@ int causal_conv_step(const conv_cfg* cfg, const glr_seq* x, const float* weight,
   if (!weight || (cfg->W > 1 && (!past_in || !past_out))) return MGRIT_E_NULL;
   if (off(weight, 4) || off(bias, 4) || off(slots, 4)) return MGRIT_E_ALIGN;
   if (cfg->W > 1 && (off(past_in, 4) || off(past_out, 4))) return MGRIT_E_ALIGN;
+  if (begins_as(y->data, {x->data})) return MGRIT_E_SIZE;
   ConvStepArgs a{*cfg, rows[0], rows[1], weight, bias, slots, n_slots, reset, past_in, past_out};
   (void)hipGetLastError();
   return code_of(launch_conv_step(a, (hipStream_t)stream));
@@ -319,6 +320,7 @@ int ssm_step(const ssm_cfg* cfg, const ssm_inputs* in, const int32_t* slots, int
   if ((rc = ssm_inputs_check(*cfg, &i)) || (rc = seq_check(*cfg, &out, true))) return rc;
   if (!state_in || !state_out) return MGRIT_E_NULL;
   if (off(state_in, 4) || off(state_out, 4) || off(slots, 4)) return MGRIT_E_ALIGN;
+  if (begins_as(y->data, {i.x.data, i.dt.data, i.b.data, i.c.data, i.z.data})) return MGRIT_E_SIZE;
   SsmStepArgs a{*cfg, i.x, i.dt, i.b, i.c, i.z, out, i.a, i.skip, i.bias, slots, n_slots, reset, state_in, state_out};
   (void)hipGetLastError();
   return code_of(launch_ssm_step(a, (hipStream_t)stream));

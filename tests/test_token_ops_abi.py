@@ -213,6 +213,7 @@ def test_a_result_that_begins_where_another_array_does_is_refused():
                                       BIG, None) == SIZE
     assert L.causal_conv_backward(ref(cfg), seq(new()), new(), None, p, None, seq(new()), None, seq(new()), new(), None, p, new(),
                                   BIG, None) == SIZE
+    assert L.causal_conv_step(ref(mg.ConvCfg(1, 2, 8, 4)), seq(p), new(), None, None, 2, None, new(), new(), seq(p), None) == SIZE
     cfg, names = mg.SsmCfg(100, 2, 8, 8), ("x", "dt", "b", "c", "z")
 
     def group(cls, **other):
@@ -227,6 +228,8 @@ def test_a_result_that_begins_where_another_array_does_is_refused():
         return g
 
     for n in names:
+        assert L.ssm_step(ref(mg.SsmCfg(1, 2, 8, 8)), ref(group(tk.SsmInputs, **{n: p})), None, 2, None, new(), new(), seq(p),
+                          None) == SIZE
         assert L.ssm_forward(ref(cfg), ref(group(tk.SsmInputs, **{n: p})), None, None, seq(p), None, None, 0, new(), BIG, None) == SIZE
         for inputs_, dy, out in ((dict(x=p), new(), {n: p}), ({}, p, {n: p}), ({}, new(), {n: p, "x" if n != "x" else "z": p})):
             assert L.ssm_backward(ref(cfg), ref(group(tk.SsmInputs, **inputs_)), None, new(), BIG, seq(dy), None,
