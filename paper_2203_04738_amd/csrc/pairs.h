@@ -70,11 +70,12 @@ inline bool pairs(const glr_seq& q, int H) {
 }
 
 // exp(x), x of any size: 2^p with p = x log2(e) as rounded, and e^r for what the rounding left, r = x - p ln 2 (at
-// most 2^-17 where 2^p is a number other than 0; where x is infinite, NaN, for which fminf takes the bound).  Without
-// the second factor the result is off by 7 units of 2^-24 at x = -6, 16 at -20, 62 at -80.
+// most 2^-17 where 2^p is a number other than 0 and infinity).  Without the second factor the result is off by 7 units of
+// 2^-24 at x = -6, 16 at -20, 62 at -80.  Where 2^p is 0 or infinity, it is the result, and r may be anything: the product is
+// NaN there or the result, and the maximum with 2^p / 2, which is below any other result, takes the number (of NaN alone, NaN).
 __device__ inline float exp_of(float x) {
   const float p = LOG2E * x, e = __builtin_amdgcn_exp2f(p);
-  return fmaf(e, fminf(fmaf(-p, LN2, x), 0x1p-16f), e);
+  return fmaxf(fmaf(e, fmaf(-p, LN2, x), e), 0.5f * e);
 }
 // s = sigmoid(z), n = sigmoid(-z).  (Of a NaN they are numbers: each use multiplies by z.)
 struct Sigmoid {

@@ -284,3 +284,19 @@ def test_offsets_beyond_32_bits(T, stride):
     torch.cuda.synchronize()
     close({"h": wide[..., :H].double().cpu().numpy()}, expected(d, "mix"), "f32")
     assert torch.all(wide[..., H:] == 7)
+
+
+@pytest.mark.parametrize("gate", [88.0, 89.0, 95.0, 99.0, 100.0, 101.0, 200.0, 1e4, 3e38])
+def test_a_factor_beyond_the_floats_is_infinite(gate):
+    """One step from a state of 1, exp(gate) + 1: within the floats to some units, beyond them infinite."""
+    B, H = 2, 40
+    given = torch.full((B, H), gate, device=DEV)
+    step, pool = torch.full((B, H), float("nan"), device=DEV), torch.ones(B, H, device=DEV)
+    mg.glr_step(mg.GlrCfg(1, B, H, mg.GLR_DECAY), given, torch.ones(B, H, device=DEV), None, None, pool, pool, step)
+    with np.errstate(over="ignore"):
+        want = np.float64(np.float32(np.exp(np.float64(np.float32(gate)))))
+    for got in (step.double().cpu().numpy(), pool.double().cpu().numpy()):
+        if np.isinf(want):
+            assert np.isposinf(got).all(), got.flat[0]
+        else:
+            assert (np.abs(got - want) <= 2.0 ** -24 * 100 * want).all()

@@ -222,3 +222,77 @@ def test_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(loss, l2) and torch.equal(grad, g2) and float(loss.abs().max()) > 0
+
+
+# differences of log probabilities whose exponential is the largest that a float holds, and beyond
+FAR = [80.0, 88.0, 88.7, 88.8, 89.0, 95.0, 99.0, 100.0, 101.0, 200.0, 1e3, 1e9, 3e38]
+
+
+def far_rows():
+    """(differences, their exponentials as floats, relative errors of those) of tokens of probability 1/2."""
+    lp = np.log(0.5)
+    given = (lp - np.array(FAR)).astype(np.float32)
+    d = lp - given.astype(float)
+    with np.errstate(over="ignore"):
+        e = np.exp(d)
+        # d rounded once, an exponential to some units; 88.73 is where floats end
+        return given, d, np.where(e > np.finfo(np.float32).max, np.inf, e), 2.0 ** -24 * (np.minimum(d, 90) + 20)
+
+
+@pytest.mark.parametrize("A", [1.5, -1.0])
+@pytest.mark.parametrize("V", [2, 40000])
+@pytest.mark.parametrize("apart", [False, True])
+def test_ratios_beyond_the_floats_are_infinite_and_clipped(A, V, apart):
+    """-min(r A, 1.28 A) is -1.28 A for A > 0 whatever r, r |A| for A < 0."""
+    old, d, r, rel = far_rows()
+    N = len(d)
+    x = torch.full((N, V), -float("inf"), device=DEV)
+    x[:, :2] = 0
+    dev = {"x": x, "tok": torch.zeros(N, dtype=torch.int64, device=DEV), "old": torch.from_numpy(old).to(DEV),
+           "adv": torch.full((N,), A, device=DEV), "weight": torch.ones(N, device=DEV)}
+    rows, grad = call(dev, "f32", 1.0, 0.0, apart)
+    loss, logp, ratio, kl = (t.double().cpu().numpy() for t in rows)
+    fin = np.isfinite(r)
+    assert fin.any() and (~fin).any()
+    assert np.array_equal(ratio[~fin], r[~fin]) and (np.abs(ratio[fin] - r[fin]) <= (rel * r)[fin]).all()
+    grad = grad.double().cpu().numpy()
+    if A > 0:
+        assert (np.abs(loss + 1.28 * A) <= 2.0 ** -23 * 1.28 * A).all() and (grad == 0).all()
+        return
+    assert np.array_equal(loss[~fin], -A * r[~fin]) and (np.abs(loss[fin] + A * r[fin]) <= -A * (rel * r)[fin]).all()
+    # dloss / dlp = r |A|, times 1 - 1/2 for the token and -1/2 for the other
+    assert not np.isfinite(grad[~fin, :2]).any()
+    want = -A * r[fin, None] * np.array([0.5, -0.5])
+    assert (np.abs(grad[fin, :2] - want) <= 2 * rel[fin, None] * np.abs(want)).all() and (grad[fin, 2:] == 0).all()
+
+
+@pytest.mark.parametrize("V", [2, 40000])
+@pytest.mark.parametrize("beta", [0.0, 0.1])
+def test_kl_terms_beyond_the_floats_are_infinite(V, beta):
+    """k = e^d - d - 1 of a token that the reference finds far more probable; with a factor of 0 it is not in the loss."""
+    lp = np.log(0.5)
+    d = np.array(FAR)
+    ref = (lp + d).astype(np.float32)
+    d = ref.astype(float) - lp
+    with np.errstate(over="ignore"):
+        want = np.expm1(d) - d
+    N, fin = len(d), want <= np.finfo(np.float32).max
+    want[~fin] = np.inf
+    x = torch.full((N, V), -float("inf"), device=DEV)
+    x[:, :2] = 0
+    one = torch.ones(N, device=DEV)
+    cfg, rule = mg.LogitsCfg(N, V, 0), mg.PolicyCfg(LOW, HIGH, beta)
+    ws = torch.empty(mg.policy_workspace_bytes(cfg), dtype=torch.uint8, device=DEV)
+    loss, kl, grad = torch.empty(N, device=DEV), torch.empty(N, device=DEV), torch.empty(N, V, device=DEV)
+    mg.policy_loss(cfg, rule, x, torch.zeros(N, dtype=torch.int64, device=DEV), torch.full((N,), lp, device=DEV),
+                   torch.from_numpy(ref).to(DEV), one, None, loss, None, None, kl, None, grad, ws)
+    kl, loss = kl.double().cpu().numpy(), loss.double().cpu().numpy()
+    rel = 2.0 ** -24 * (np.minimum(d, 90) + 20)
+    assert np.array_equal(kl[~fin], want[~fin]) and (np.abs(kl[fin] - want[fin]) <= (rel * want)[fin]).all()
+    # a ratio of 1, as near as log(1/2) is a float, and A = 1
+    total = beta * want if beta else np.zeros(N)
+    near = np.isfinite(total)
+    assert np.array_equal(loss[~near], total[~near])
+    assert (np.abs(loss[near] + 1 - total[near]) <= 1e-6 + (2 * rel * total)[near]).all()
+    finite = torch.isfinite(grad[:, :2]).all(1).cpu().numpy()
+    assert np.array_equal(finite, fin if beta else np.ones(N, bool))
