@@ -949,7 +949,8 @@ __device__ inline PolicyTerm policy_term(const PolicyRows& a, long long row, flo
   p.logp = (float)lp;
   const float A = a.advantage[row], r = exp_of((float)(lp - (double)a.old_logp[row]));
   const float in = fminf(fmaxf(r, 1.f - a.rule.clip_low), 1.f + a.rule.clip_high);
-  const float gain = r * A, clipped = (r != r ? r : in) * A;
+  // (an advantage of 0 is no gain, also where the ratio is beyond the floats)
+  const float gain = A == 0.f && r == __builtin_inff() ? 0.f : r * A, clipped = (r != r ? r : in) * A;
   p.ratio = r;
   p.loss = gain > clipped ? -clipped : -gain;
   p.slope = gain > clipped ? 0.f : -gain;

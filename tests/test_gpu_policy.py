@@ -239,11 +239,11 @@ def far_rows():
         return given, d, np.where(e > np.finfo(np.float32).max, np.inf, e), 2.0 ** -24 * (np.minimum(d, 90) + 20)
 
 
-@pytest.mark.parametrize("A", [1.5, -1.0])
+@pytest.mark.parametrize("A", [1.5, 0.0, -1.0])
 @pytest.mark.parametrize("V", [2, 40000])
 @pytest.mark.parametrize("apart", [False, True])
 def test_ratios_beyond_the_floats_are_infinite_and_clipped(A, V, apart):
-    """-min(r A, 1.28 A) is -1.28 A for A > 0 whatever r, r |A| for A < 0."""
+    """-min(r A, 1.28 A) is -1.28 A for A > 0 whatever r, 0 for A = 0, r |A| for A < 0."""
     old, d, r, rel = far_rows()
     N = len(d)
     x = torch.full((N, V), -float("inf"), device=DEV)
@@ -256,7 +256,7 @@ def test_ratios_beyond_the_floats_are_infinite_and_clipped(A, V, apart):
     assert fin.any() and (~fin).any()
     assert np.array_equal(ratio[~fin], r[~fin]) and (np.abs(ratio[fin] - r[fin]) <= (rel * r)[fin]).all()
     grad = grad.double().cpu().numpy()
-    if A > 0:
+    if A >= 0:
         assert (np.abs(loss + 1.28 * A) <= 2.0 ** -23 * 1.28 * A).all() and (grad == 0).all()
         return
     assert np.array_equal(loss[~fin], -A * r[~fin]) and (np.abs(loss[fin] + A * r[fin]) <= -A * (rel * r)[fin]).all()
