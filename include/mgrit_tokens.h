@@ -160,8 +160,9 @@ MGRIT_API int ssm_step(const ssm_cfg* cfg, const ssm_inputs* in, const int32_t* 
  *   stats[N,2] float out or NULL: max_j x_j and sum_j exp((x_j - max) / t), for policy_loss_backward.
  *   dlogits[N,V] of the dtype, row stride ld_grad, or NULL: the gradient in the same pass; it may be
  *   logits itself (then ld_grad == ld).
- * A token that the mask (-inf) leaves out has lp = -inf: r = 0, and with a KL term an infinite loss.  A ratio or KL term
- * beyond the floats is infinite.  The row of dlogits of an infinite loss is not finite.
+ * A token that the mask (-inf) leaves out has lp = -inf: r = 0, and with a KL term an infinite loss, also where
+ * old or ref is -inf.  A ratio or KL term beyond the floats is infinite.  The row of dlogits of an infinite loss is not
+ * finite.
  */
 typedef struct {
   float clip_low, clip_high;   /* 0 <= clip_low <= 1, 0 <= clip_high, finite */

@@ -947,7 +947,10 @@ __device__ inline PolicyTerm policy_term(const PolicyRows& a, long long row, flo
   if (x != x || m != m || s != s) lp = (double)__uint_as_float(0x7fc00000u);
   else if (s != 0.f && x != -__builtin_inff()) lp = ((double)x - (double)m) / (double)a.t - log((double)s);
   p.logp = (float)lp;
-  const float A = a.advantage[row], r = exp_of((float)(lp - (double)a.old_logp[row]));
+  // (a token that is left out now has a ratio of 0 and an infinite KL term, also where it was left out before)
+  const float lowest = -__builtin_inff(), old = a.old_logp[row], A = a.advantage[row];
+  const bool out = lp == (double)lowest;
+  const float r = out && old == lowest ? 0.f : exp_of((float)(lp - (double)old));
   const float in = fminf(fmaxf(r, 1.f - a.rule.clip_low), 1.f + a.rule.clip_high);
   // (an advantage of 0 is no gain, also where the ratio is beyond the floats)
   const float gain = A == 0.f && r == __builtin_inff() ? 0.f : r * A, clipped = (r != r ? r : in) * A;
@@ -956,7 +959,7 @@ __device__ inline PolicyTerm policy_term(const PolicyRows& a, long long row, flo
   p.slope = gain > clipped ? 0.f : -gain;
   p.kl = 0.f;
   if (a.ref_logp) {
-    const float d = (float)((double)a.ref_logp[row] - lp);
+    const float ref = a.ref_logp[row], d = out && ref == lowest ? -lowest : (float)((double)ref - lp);
     float one;
     p.kl = exp_beyond_line(d, one);
     if (a.rule.kl != 0.f) {

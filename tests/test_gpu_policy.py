@@ -296,3 +296,22 @@ def test_kl_terms_beyond_the_floats_are_infinite(V, beta):
     assert (np.abs(loss[near] + 1 - total[near]) <= 1e-6 + (2 * rel * total)[near]).all()
     finite = torch.isfinite(grad[:, :2]).all(1).cpu().numpy()
     assert np.array_equal(finite, fin if beta else np.ones(N, bool))
+
+
+@pytest.mark.parametrize("V", [6, 40000])
+def test_tokens_that_both_policies_leave_out(V):
+    """lp = -inf is a ratio of 0 and an infinite KL term, whatever the old and the reference log probability: no NaN."""
+    inf = float("inf")
+    x = torch.zeros(4, V, device=DEV)
+    x[:, 3] = -inf
+    dev = {"x": x, "tok": torch.full((4,), 3, dtype=torch.int64, device=DEV), "old": torch.tensor([-inf, -inf, -2.0, -2.0], device=DEV),
+           "ref": torch.tensor([-inf, -1.0, -inf, -1.0], device=DEV), "adv": torch.tensor([1.0, -2.0, 1.0, -2.0], device=DEV),
+           "weight": torch.ones(4, device=DEV)}
+    for apart in (False, True):
+        rows, grad = call(dev, "f32", 1.0, 0.0, apart)
+        # -min(0 A, (1 - 0.2) A): nothing for A > 0, 0.8 |A| for A < 0, with no slope either way
+        assert torch.allclose(rows[0], torch.tensor([0.0, 1.6, 0.0, 1.6], device=DEV), rtol=2.0 ** -22, atol=0)
+        assert (rows[1] == -inf).all() and (rows[2] == 0).all() and (grad == 0).all()
+        rows, grad = call(dev, "f32", 1.0, 0.1, apart)
+        assert (rows[0] == inf).all() and (rows[2] == 0).all() and (rows[3] == inf).all()
+        assert (~torch.isfinite(grad)).any(1).all()
