@@ -95,7 +95,7 @@ static int policy_check(const logits_cfg* c, const policy_cfg* rule, const void*
   if (off(logits, e) || off(dlogits, e) || off(tokens, 8) || off(old_logp, 4) || off(ref_logp, 4) || off(advantage, 4) ||
       off(weight, 4))
     return MGRIT_E_ALIGN;
-  return MGRIT_OK;
+  return begins_as(dlogits, {tokens, old_logp, ref_logp, advantage, weight}) ? MGRIT_E_SIZE : MGRIT_OK;
 }
 static logits_cfg policy_space_cfg(const logits_cfg& c) {
   logits_cfg one = c;
@@ -362,6 +362,7 @@ int policy_loss_backward(const logits_cfg* cfg, const policy_cfg* rule, const vo
   if (rc) return rc;
   if (!stats || !dlogits) return MGRIT_E_NULL;
   if (off(stats, 4)) return MGRIT_E_ALIGN;
+  if (begins_as(dlogits, {stats})) return MGRIT_E_SIZE;
   PolicyArgs a{};
   a.c = *cfg;
   a.rule = *rule;

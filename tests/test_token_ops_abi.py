@@ -244,6 +244,20 @@ def test_a_result_that_begins_where_another_array_does_is_refused():
                 assert L.policy_loss(ref(cfg), ref(rule), *(a[n] for n in names), None, 0, None) == SIZE, (k, other)
 
 
+def test_a_gradient_that_begins_where_another_array_of_its_rows_does_is_refused():
+    """Workgroups of other rows read those arrays while gradients are written; the logits alone may be the gradient."""
+    L, cfg, rule = tk._lib(), mg.LogitsCfg(4, 100, 0), mg.PolicyCfg()
+    names = ("logits", "tok", "old", "ref", "adv", "w", "loss", "logp", "ratio", "kl", "stats", "grad")
+    for k in names[1:11]:
+        a = {n: (i + 1) << 20 for i, n in enumerate(names)}
+        a["grad"] = a[k]
+        assert L.policy_loss(ref(cfg), ref(rule), *(a[n] for n in names), None, 0, None) == SIZE, k
+        if k in ("loss", "logp", "ratio", "kl"):
+            continue
+        given = [a[n] for n in ("logits", "tok", "old", "ref", "adv", "stats", "w", "grad")]
+        assert L.policy_loss_backward(ref(cfg), ref(rule), *given, None) == SIZE, k
+
+
 def test_policy_refusals():
     L = tk._lib()
 
