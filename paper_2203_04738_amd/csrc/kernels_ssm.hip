@@ -615,6 +615,8 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
         auto step = [&](auto j_) SSM_INLINE {
           constexpr int j = decltype(j_)::value;
           const int r = 4 * g + j;
+          part[j] = 0.f;
+          if (!PLAIN && t + r >= a.c.T) return;       // (0 times an infinite state or b would be NaN)
           const float dj = quad_of<j>(delta[g]), xj = quad_of<j>(dx);
           const bool cut = !PLAIN && (resets >> r & 1);
           float b[SP], c[SP];
@@ -645,6 +647,8 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_backward_kernel(SsmArgs a) {
         auto step = [&](auto j_) SSM_INLINE {
           constexpr int j = decltype(j_)::value;
           const int r = 4 * g + j;
+          of_x[j] = of_d[j] = 0.f;
+          if (!PLAIN && t + r >= a.c.T) return;
           const float dj = quad_of<j>(delta[g]), xj = quad_of<j>(dx), oj = quad_of<j>(out);
           const bool cut = !PLAIN && (resets >> r & 1);
           float b[SP], c[SP], v[2 * SP];

@@ -319,3 +319,32 @@ def test_the_same_bits_in_every_run_and_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(eager, [y, h_last] + g):
             assert torch.equal(a, b) and float(a.abs().max()) > 0
+
+
+@pytest.mark.parametrize("T", [1, 8, 15, 16, 17, 21, 33, 700])
+@pytest.mark.parametrize("S", [5, 16, 64])
+@pytest.mark.parametrize("full", [False, True])
+def test_an_infinite_last_state_is_in_no_gradient_that_it_is_not_read_for(T, S, full):
+    """The last input is infinite, and so is h_T.  da, dh0 and the gradients of the steps before do not read it, whether T is a
+    multiple of a tile or not."""
+    B, H, ch = 2, 20, 7
+    d, dev = problem(23, T, B, H, S)
+    dev["x"][T - 1, 1, ch] = float("inf")
+    d["x"] = dev["x"].double().cpu().numpy()
+    cfg, ws, saved, y, h_last = forward(dev, T, B, H, S, h0=full)
+    new = lambda *s: torch.full(s, float("nan"), device=DEV)  # noqa: E731
+    g = {"dx": new(T, B, H), "ddt": new(T, B, H), "db": new(T, B, S), "dc": new(T, B, S), "dz": new(T, B, H), "da": new(H, S),
+         "dskip": new(H), "dbias": new(H), "dh0": new(B, H, S)}
+    mg.ssm_backward(cfg, *(dev[k] for k in INPUTS), None, saved, dev["dy"], dev["dh_last"] if full else None, *g.values(), ws)
+    with np.errstate(invalid="ignore"):
+        want = orc.ssm_backward(*(d[k] for k in INPUTS[:6]), d["dy"], skip=d["skip"], bias=d["bias"], h0=d["h0"] if full else None,
+                                dh_last=d["dh_last"] if full else None)
+    assert torch.isinf(h_last[1, ch]).all() and torch.isfinite(h_last[0]).all()
+    for k in ("da", "dh0", "dx"):
+        assert np.isfinite(want[k]).all()
+        close(g[k], want[k], 2.0 ** -24, GRAD_TOL, k)
+    for k in ("ddt", "db", "dc", "dz"):
+        close(g[k][:T - 1], want[k][:T - 1], 2.0 ** -24, GRAD_TOL, k) if T > 1 else None
+    others = [i for i in range(H) if i != ch]
+    for k in ("dskip", "dbias"):
+        close(g[k][others], want[k][others], 0, GRAD_TOL, k)
