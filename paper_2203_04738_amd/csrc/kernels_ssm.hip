@@ -204,6 +204,9 @@ struct Resets {
   }
 };
 
+// d as the decays take it.  A softplus is above 0: where it is below the floats, an infinite a still forgets, and for any other
+// the smallest float is as little of a decay as 0 is (to 2^-20 for the lowest float).  (A NaN reaches the state through d b x.)
+__device__ inline float above_zero(float d) { return fmaxf(d, 0x1p-149f); }
 __device__ inline float decay(float d, float a2) { return __builtin_amdgcn_exp2f(d * a2); }
 
 // The state behind a chunk from the one before it: S + P v, P = exp(a sum d); a sum below 0: the chunk forgets.
@@ -317,14 +320,14 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_forward_kernel(SsmArgs a) {
           store_states<SP>(saved + 4 * g / SAVE * states, S, p.n0, h);
         const bool in = PLAIN || ts + q < a.c.T;
         const float delta = in ? Softplus(d[g]).d : 0.f;
-        const float xv = in ? x[g] : 0.f, dx = delta * xv;
-        if (!MAIN) sum += delta;
+        const float xv = in ? x[g] : 0.f, dx = delta * xv, dd = above_zero(delta);
+        if (!MAIN) sum += dd;
         float part[4];
         auto step = [&](auto j_) SSM_INLINE {
           constexpr int j = decltype(j_)::value;
           part[j] = 0.f;
-          if (!PLAIN && ts + j >= a.c.T) return;      // (an infinite a would leave no number of d = 0)
-          const float dj = quad_of<j>(delta), xj = quad_of<j>(dx);
+          if (!PLAIN && ts + j >= a.c.T) return;
+          const float dj = quad_of<j>(dd), xj = quad_of<j>(dx);
           const bool cut = !PLAIN && (resets >> (4 * g + j) & 1);
           float b[SP], c[SP];
           read_bc<SP>(bc[buf], 4 * g + j, q, 0, b);
@@ -776,7 +779,7 @@ __global__ __launch_bounds__(SSM_THREADS) void ssm_step_kernel(SsmStepArgs a) {
 #pragma unroll
   for (int k = 0; k < SP; ++k) {
     const int n = min(q * SP + k, S - 1);
-    const float keep = decay(d, A[k] * LOG2E), in = d * x * elem_f32(bs[n]);
+    const float keep = decay(above_zero(d), A[k] * LOG2E), in = d * x * elem_f32(bs[n]);
     h[k] = cut ? in : fmaf(keep, h[k], in);
     if (q * SP + k < S) sum = fmaf(h[k], elem_f32(cs[n]), sum);
   }

@@ -348,3 +348,27 @@ def test_an_infinite_last_state_is_in_no_gradient_that_it_is_not_read_for(T, S, 
     others = [i for i in range(H) if i != ch]
     for k in ("dskip", "dbias"):
         close(g[k][others], want[k][others], 0, GRAD_TOL, k)
+
+
+@pytest.mark.parametrize("T", [1, 15, 16, 17, 90, 700])
+@pytest.mark.parametrize("low", [-90.0, -110.0, -500.0])
+def test_an_infinite_decay_forgets_where_the_step_is_too_small_for_a_float(T, low):
+    """softplus(low) is above 0, if only by e^low: exp(d a) is 0 for a = -infinity, in sequences and single steps."""
+    B, H, S = 2, 20, 5
+    d, dev = problem(24, T, B, H, S)
+    dev["a"][::2, ::2] = float("-inf")
+    d["a"][::2, ::2] = -np.inf
+    dev["dt"][::3] = low
+    dev["dt"][:, 1] = low                                      # and nothing but such steps
+    d["dt"] = dev["dt"].double().cpu().numpy()
+    cfg, _, _, y, h_last = forward(dev, T, B, H, S)
+    want, states, _ = orc.ssm_forward(*(d[k] for k in INPUTS[:6]), skip=d["skip"], bias=d["bias"], h0=d["h0"])
+    close(y, want, 2.0 ** -24, TOL, "y")
+    close(h_last, states[-1], 0, TOL, "h_last")
+    pool, out = dev["h0"].clone(), []
+    one = mg.SsmCfg(1, B, H, S)
+    for t in range(min(T, 20)):
+        out.append(torch.full((B, H), float("nan"), device=DEV))
+        mg.ssm_step(one, *(dev[k][t] if k in ("x", "dt", "b", "c", "z") else dev[k] for k in INPUTS), None, None, pool, pool, out[-1])
+    close(torch.stack(out), want[:20], 2.0 ** -24, TOL, "step")
+    close(pool, states[len(out) - 1], 0, TOL, "pool")
