@@ -226,8 +226,10 @@ def _slots(t):
 
 
 def causal_conv_step(cfg, x, weight, bias, slots, reset, past_in, past_out, y) -> None:
-    """x, y: [B,H]; past_in, past_out: [n_slots,W-1,H]."""
+    """x, y: [B,H]; past_in, past_out: [n_slots,W-1,H].  (W = 1: or None, then any slot that is not negative is one.)"""
     B, H, W, n = cfg.B, cfg.H, cfg.W, _slots(past_in)
+    if W == 1 and past_in is None:
+        n = 2 ** 31 - 1 if past_out is None else _slots(past_out)
     _call("causal_conv_step", cfg, _row(cfg, x, "x"), *_taps(cfg, weight, bias),
           (slots, "slots", _o._torch.int32, (B,), _DENSE), n, _reset(reset, B), _f32(past_in, "past_in", n, W - 1, H),
           _f32(past_out, "past_out", n, W - 1, H), _row(cfg, y, "y"))

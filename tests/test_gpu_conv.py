@@ -216,3 +216,26 @@ def test_the_same_bits_in_every_run_and_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(eager, out):
             assert torch.equal(a, b) and float(a.abs().max()) > 0
+
+
+@pytest.mark.parametrize("slots", [None, [2, -1, 0, 70000]])
+def test_steps_of_one_tap_have_no_pool(slots):
+    """W = 1: no past is looked at, so that none has to be there; without a pool only a negative slot is outside of it."""
+    B, H = 4, 50
+    d, dev = problem(14, 1, B, H, 1, "f32")
+    cfg = mg.ConvCfg(1, B, H, 1)
+    s = None if slots is None else torch.tensor(slots, dtype=torch.int32, device=DEV)
+    want = orc.conv_forward(d["x"], d["weight"], d["bias"])[0][0]
+    live = [b for b in range(B) if slots is None or slots[b] >= 0]
+    y = torch.full((B, H), float("nan"), device=DEV)
+    mg.causal_conv_step(cfg, dev["x"][0], dev["weight"], dev["bias"], s, None, None, None, y)
+    close(y[live], want[live], 2.0 ** -24, TOL)
+    assert (y[[b for b in range(B) if b not in live]] == 0).all()
+    # with a pool its rows count as before
+    pool = torch.empty(3 if slots else B, 0, H, device=DEV)
+    live = [b for b in live if slots is None or slots[b] < 3]
+    for pools in ((pool, pool), (None, pool), (pool, None)):
+        again = torch.full((B, H), float("nan"), device=DEV)
+        mg.causal_conv_step(cfg, dev["x"][0], dev["weight"], dev["bias"], s, None, *pools, again)
+        close(again[live], want[live], 2.0 ** -24, TOL)
+        assert (again[[b for b in range(B) if b not in live]] == 0).all()
