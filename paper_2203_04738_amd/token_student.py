@@ -141,8 +141,12 @@ class TokenStudent:
         uniform[T*B] in [0, 1)."""
         import torch
         out = self.logits(tokens, reset)
-        p = torch.softmax(out / self.rows.temperature, 1).cumsum(1)
-        actions = torch.searchsorted(p, uniform[:, None] * p[:, -1:]).clamp(max=self.V - 1)[:, 0]
+        p = torch.softmax(out / self.rows.temperature, 1)
+        upto = p.cumsum(1)
+        # the first token whose sum exceeds the number; a token of no probability, which only sums that rounding leaves out of
+        # order could name, gives way to the likeliest
+        actions = torch.searchsorted(upto, uniform[:, None] * upto[:, -1:], right=True).clamp(max=self.V - 1)
+        actions = torch.where(p.gather(1, actions) > 0, actions, p.argmax(1, keepdim=True))[:, 0]
         return actions, self.log_probs(out, actions)
 
     def log_probs(self, logits, actions):

@@ -133,3 +133,15 @@ def test_served_sequences_do_not_touch_each_other():
     fresh = TokenServed(small(), slots=6)
     one = torch.ones(2, dtype=torch.uint8, device=DEV)
     assert torch.equal(served.next(tokens[1, :2].contiguous(), slots[:2], one), fresh.next(tokens[1, :2].contiguous(), slots[:2]))
+
+
+def test_a_sampled_token_is_one_that_can_be():
+    """The numbers 0 and the largest below 1, where the head leaves the first and the last tokens a probability of 0."""
+    _, tokens, _ = batch(11)
+    student = small()
+    logits = student.logits(tokens)
+    logits[:, :4] = logits[:, V - 3:] = -1e30
+    student.logits = lambda tokens, reset=None: logits.clone()
+    for number in (0.0, 1.0 - 2.0 ** -24):
+        actions, logp = student.act(tokens, torch.full((T * B,), number, device=DEV))
+        assert ((actions >= 4) & (actions < V - 3)).all() and torch.isfinite(logp).all()
