@@ -145,3 +145,14 @@ def test_a_sampled_token_is_one_that_can_be():
     for number in (0.0, 1.0 - 2.0 ** -24):
         actions, logp = student.act(tokens, torch.full((T * B,), number, device=DEV))
         assert ((actions >= 4) & (actions < V - 3)).all() and torch.isfinite(logp).all()
+
+
+def test_learning_leaves_finite_weights_and_moves_them():
+    g, tokens, reset = batch(9)
+    student = small(rule=mg.PolicyCfg(0.2, 0.3, 0.1))
+    actions, logp = student.act(tokens, torch.rand(T * B, generator=g).to(DEV), reset)
+    mine = [student.table, student.head] + [p[k] for p in student.layers for k in NAMES]
+    before = [q.clone() for q in mine]
+    student.learn(tokens, actions, logp, torch.randn(T * B, generator=g).to(DEV), logp, reset)
+    for q, b in zip(mine, before):
+        assert torch.isfinite(q).all() and torch.isfinite(q.grad).all() and not torch.equal(q, b)
