@@ -17,7 +17,7 @@
  * workspace of 0 bytes may be NULL, others are 16-byte aligned, calls that share one are ordered on one stream.
  * Sums, states and statistics are float (a row's loss double); a result is rounded once, to nearest, when it is stored.
  * A call whose launches would take 2^32 threads or more is refused with MGRIT_E_SIZE, and so is one over sequences or rows
- * of which one that is written begins where another begins.
+ * of which one that is written begins where another begins (but for a gradient of logits in their place).
  */
 #ifndef MGRIT_TOKENS_H
 #define MGRIT_TOKENS_H
@@ -91,8 +91,8 @@ MGRIT_API int causal_conv_step(const conv_cfg* cfg, const glr_seq* x, const floa
  *     d_t = softplus(dt_t + bias),   h_t[n] = exp(d_t a[n]) h_{t-1}[n] + d_t b_t[n] x_t,
  *     y_t = (sum_n c_t[n] h_t[n] + skip x_t) z_t sigmoid(z_t),
  * b_t and c_t the same for all channels of a batch row, a, bias and skip of each channel.
- * a <= 0 is a decay; it is not enforced.  a > 0 can carry exp(d a), or its product over some steps, beyond the floats,
- * where a state that is not zero becomes infinite or NaN.  An infinite state may be NaN later.
+ * a <= 0 is a decay; it is not enforced.  a > 0 can carry exp(d a) beyond the floats, where a state becomes infinite or
+ * NaN (one of zero too), or its product over some steps, where one that is not zero does.  An infinite state may be NaN later.
  * a = -infinity forgets at every step; ssm_backward needs finite ones (others leave NaN).
  * A step whose `reset` byte is not zero forgets the past: h_t = d_t b_t x_t, whatever h_{t-1} was, and no gradient
  * passes to the steps before it.

@@ -1043,7 +1043,9 @@ __global__ __launch_bounds__(64) void policy_join_kernel(PolicyRows a) {
     put_policy(a, row, policy_row<E>(a, row, (const E*)a.d.logits + row * a.d.ld, st.m, st.s, t), st.m, st.s);
 }
 // Gradient of a row, or of a segment of one, from its statistics.  In place (WHOLE) a team goes through all segments of its row:
-// the slope needs the token's logit, which another team would have overwritten.
+// the slope needs the token's logit, which another team would have overwritten.  Loss and gradient, us, in a place of its own
+// / in place: 131072 bf16 of 1 row 18.8 / 19.6, 64 18.9 / 26.6, 256 40.8 / 40.6, 1024 145 / 123, 2048 308 / 318; 50021 floats of
+// 64 19.6 / 24.3, 256 35.0 / 34.9, 2048 237 / 249.
 template <typename E, int NW, bool WHOLE = false>
 __global__ __launch_bounds__((TeamOf<E, NW>::block)) void policy_grad_kernel(PolicyRows a) {
   using T = TeamOf<E, NW>;

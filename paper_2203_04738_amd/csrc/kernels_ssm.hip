@@ -243,7 +243,7 @@ __device__ inline void through_chunks(const SsmArgs& a, const SsmPlace& p, const
 // ---- forward
 // MAIN: results of a chunk from its state; otherwise its end state from zero and the sum of its d.
 // Per step and state: d a, an exponential, b d x and two multiply-adds; around them, for every 16 states, softplus, the gate
-// and the loads of a channel's step.  Instructions bound it: 8192 x 4 x 1024 bf16, 16 states, takes 193 us as traced (163
+// and the loads of a channel's step.  Instructions bound it: 8192 x 4 x 1024 bf16, 16 states, takes 191 us as traced (163
 // without states to save, which are 268 of its 600 MB), 120 for the chunks' ends; four waves a SIMD hold 80 to 90 % of its
 // issue.  128 x 100 x 1000 floats, one chunk: 94 us.  Four lanes a channel rather than one: a quarter of the chunks' second
 // sweep for as many waves, and softplus and gate still once for each step.
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(256) void ssm_between_kernel(SsmArgs a, const float
 
 // ---- backward
 // mu_t = exp(d_t a) lambda_t is what step t hands on to step t - 1.  What a chunk hands on from nothing, and the sum of
-// its d.  (Chunk 0 hands on to nobody.)  144 us at the sizes above.
+// its d.  (Chunk 0 hands on to nobody.)  142 us at the sizes above.
 template <typename E, int SP>
 __global__ __launch_bounds__(SSM_THREADS) void ssm_adjoint_ends_kernel(SsmArgs a) {
   constexpr int TB = SSM_TILE, G = TB / 4;
@@ -513,8 +513,8 @@ __device__ inline void channel_sums(const float (&v)[2 * SP], float* out, int la
 }
 
 // A tile of R steps goes forward again from its saved state, keeping the decays and the states before each step in registers,
-// and then back.  Instructions bound it (107 a wave and step, two waves a SIMD, a vector instruction in execution 94 % of
-// the time): 8192 x 4 x 1024 bf16, 16 states, 500 us as traced, 128 x 100 x 1000 floats 240 to 260.  Tiles of 8 steps: 16 leave
+// and then back.  Instructions bound it (105 a wave and step, two waves a SIMD, a vector instruction in execution 94 % of
+// the time): 8192 x 4 x 1024 bf16, 16 states, 504 us as traced, 128 x 100 x 1000 floats 240 to 260.  Tiles of 8 steps: 16 leave
 // room for one wave a SIMD (755 us).  Of a step's instructions the states take 60 %, the sums over the channels 15 %: through LDS
 // those took 576 against 549 us, on the matrix pipe (products with ones) the registers of the second wave (840).
 template <typename E, int SP, int R>

@@ -304,7 +304,8 @@ def test_tokens_that_both_policies_leave_out(V):
     inf = float("inf")
     x = torch.zeros(4, V, device=DEV)
     x[:, 3] = -inf
-    dev = {"x": x, "tok": torch.full((4,), 3, dtype=torch.int64, device=DEV), "old": torch.tensor([-inf, -inf, -2.0, -2.0], device=DEV),
+    dev = {"x": x, "tok": torch.full((4,), 3, dtype=torch.int64, device=DEV),
+           "old": torch.tensor([-inf, -inf, -2.0, -2.0], device=DEV),
            "ref": torch.tensor([-inf, -1.0, -inf, -1.0], device=DEV), "adv": torch.tensor([1.0, -2.0, 1.0, -2.0], device=DEV),
            "weight": torch.ones(4, device=DEV)}
     for apart in (False, True):
